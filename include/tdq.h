@@ -38,7 +38,8 @@ extern "C" {
 
 #define TDQ_VERSION 110
 
-typedef enum { TDQ_F16 = 0, TDQ_F32 = 1 } tdq_dtype;
+/* TDQ_BF16 (bfloat16): the entry points from tdq_quantize_act_f8 on. */
+typedef enum { TDQ_F16 = 0, TDQ_F32 = 1, TDQ_BF16 = 2 } tdq_dtype;
 
 typedef enum {
   TDQ_OK = 0,
@@ -403,6 +404,101 @@ int tdq_probe(int32_t kind, void* buf, size_t bytes, int32_t iters, int32_t grid
  */
 int tdq_quantize_weight(const float* W, int32_t N, int32_t K, int64_t ld_w_in, uint8_t* Qw,
                         int64_t ld_w, float* w_scale, void* stream);
+
+/*
+ * A transformer layer's other operators, for layers that the W4A4 path leaves in wider types:
+ * a linear in 8-bit floating point with one step for each block of 128, the norm of query and
+ * key heads with the rotation by position, and softmax attention over packed sequences.
+ */
+#define TDQ_BLOCK_F8 128 /* channels (and, of a weight, outputs) that share one step */
+
+/*
+ * e4m3 codes (OCP: 448 the largest value) with a step for each (row, block of 128 channels):
+ *   step[m, b] = max(max_i |X[m, i]|, 1e-8) / 448,   code = e4m3(X[m, i] / step[m, b])
+ * quotients correctly rounded, codes to nearest, ties to even.  A block that holds an Inf or
+ * NaN gets a step or codes that make every output of its row NaN or Inf.
+ *
+ * X [M, ld_x] of dt (binary16, bfloat16 or binary32), ld_x >= K.  Q [M, ld_q] bytes out, 16-byte
+ * aligned, ld_q a multiple of 16, at least K; bytes from K to the next multiple of 16 are
+ * zeroed, those past it not written.  step [M, ld_s] floats out, ld_s >= ceil(K / 128).
+ * M <= 2^30, K <= 131072, M * ceil(K / 128) < 2^31, else TDQ_ERR_SHAPE.
+ */
+int tdq_quantize_act_f8(const void* X, tdq_dtype dt, int64_t M, int32_t K, int64_t ld_x, uint8_t* Q,
+                        int64_t ld_q, float* step, int64_t ld_s, void* stream);
+/* The same for a weight W [N, ld_w_in], one step for each block of 128 outputs x 128 channels:
+ * step [ceil(N / 128), ld_s].  N <= 2^22. */
+int tdq_quantize_weight_f8(const void* W, tdq_dtype dt, int32_t N, int32_t K, int64_t ld_w_in, uint8_t* Qw,
+                           int64_t ld_w, float* step, int64_t ld_s, void* stream);
+
+/*
+ * Linear on such codes:
+ *   Y[m, n] = sum_b x_step[m, b] * w_step[n / 128, b] * sum_{i in block b} Qx[m, i] Qw[n, i] (+ bias[n])
+ * Blocks are added in binary32, b ascending, and the result is rounded once.  Binary16 and
+ * bfloat16 results take the 8-bit matrix instruction, which adds the products of a few
+ * neighbouring channels with about 16 bits below the largest (some 2e-5 of the result's norm,
+ * below a tenth of what the result's own rounding costs); binary32 results take the codes as
+ * binary16, at half the rate, and are as exact as a binary32 sum.
+ *
+ * Qx [M, ld_q], Qw [N, ld_w]: 16-byte aligned, ld a multiple of 16, at least K and at most 2^22;
+ * bytes past K of a row are ignored.  x_step [M, ld_xs], w_step [ceil(N / 128), ld_ws] floats,
+ * ld >= ceil(K / 128), ld_xs <= 2^20.  bias [N] floats or NULL.  Y [M, ld_y] of y_dt.
+ * M <= 2^30, K <= 131072, N <= 2^22.
+ */
+int tdq_linear_f8(const uint8_t* Qx, int64_t ld_q, const float* x_step, int64_t ld_xs, int64_t M, int32_t K,
+                  int32_t N, const uint8_t* Qw, int64_t ld_w, const float* w_step, int64_t ld_ws,
+                  const float* bias, void* Y, tdq_dtype y_dt, int64_t ld_y, void* stream);
+
+/* Heads of a token-major tensor: element d of head h of token t is data[t token + h head + d],
+ * strides in elements, so that the parts of a fused projection are named in place. */
+typedef struct tdq_heads {
+  void* data;
+  int64_t token, head;
+} tdq_heads;
+
+#define TDQ_MAX_HEAD 256 /* largest D of tdq_norm_rotate and tdq_attention */
+
+/*
+ * Norm of every query and key head and the rotation by position, in one pass:
+ *   y[d] = x[d] / sqrt(mean_d x[d]^2 + eps) * weight[d]        (weight NULL: y = x)
+ * then pair p < R / 2 of the first R elements by the angle w = pos[axis[p], t] * freq[p]:
+ *   (a, b) -> (a cos w - b sin w, b cos w + a sin w)
+ * where (a, b) are elements (2 p, 2 p + 1) if interleaved, else (p, p + R / 2); elements from R
+ * on are not turned.  Several position axes (time, height, width): axis [R / 2] says which axis
+ * turns a pair (values outside 0 .. axes - 1 are taken as the nearest), NULL = the first.
+ * Angles are reduced in binary64.
+ *
+ * Q, K: T tokens of Hq and Hk heads of D elements of dt (any of the three); K may be NULL with
+ * Hk = 0.  D and R multiples of 8, R <= D <= TDQ_MAX_HEAD.  q_weight, k_weight [D] floats or
+ * NULL.  pos [axes, ld_pos] int32, ld_pos >= T.  freq [R / 2] floats; R = 0 turns nothing (pos
+ * and freq may be NULL then).  Qo, Ko as Q, K; they may be the same tensors as Q and K.
+ * T <= 2^30, Hq + Hk <= 4096.
+ */
+int tdq_norm_rotate(const tdq_heads* Q, const tdq_heads* K, tdq_dtype dt, int64_t T, int32_t Hq, int32_t Hk,
+                    int32_t D, const float* q_weight, const float* k_weight, float eps, int32_t R,
+                    int32_t interleaved, const int32_t* pos, int64_t ld_pos, int32_t axes, const int32_t* axis,
+                    const float* freq, const tdq_heads* Qo, const tdq_heads* Ko, void* stream);
+
+/*
+ * Softmax attention over packed sequences with grouped heads:
+ *   O[t, h] = sum_j p_j V[j, h / g],  p = softmax_j(scale * Q[t, h] . K[j, h / g]),  g = Hq / Hk
+ * over the keys j of t's sequence; sequence s has the queries cu_q[s] .. cu_q[s + 1] - 1 and the
+ * keys cu_k[s] .. cu_k[s + 1] - 1 (device arrays of S + 1, ascending, within 0 .. Tq and 0 .. Tk;
+ * what lies outside is cut off).  causal: the last query of a sequence sees all of its keys, the
+ * one before it all but the last, and so on.  A query that sees no key gets O = 0 and lse = -inf.
+ * lse [Tq, Hq] floats or NULL: log of the sum of exp(scale * score).
+ * Scores, maxima, sums and O are held in binary32; the probabilities are rounded to the type of
+ * V for the product with it.
+ *
+ * Q [Tq, Hq, D], K, V [Tk, Hk, D], O [Tq, Hq, D] of dt = TDQ_F16 or TDQ_BF16, all 16-byte aligned
+ * with strides that are multiples of 8.  D a multiple of 8 up to TDQ_MAX_HEAD, Hk divides Hq,
+ * Hq <= 4096, 1 <= Tq <= 2^30, 0 <= Tk <= 2^30, S <= 2^20.  workspace: device scratch of
+ * tdq_attention_workspace_bytes(Tq, Tk, S, Hq, Hk, D), 256-byte aligned (NULL if that is 0).
+ */
+size_t tdq_attention_workspace_bytes(int64_t Tq, int64_t Tk, int32_t S, int32_t Hq, int32_t Hk, int32_t D);
+int tdq_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, tdq_dtype dt, int64_t Tq, int64_t Tk,
+                  int32_t S, const int32_t* cu_q, const int32_t* cu_k, int32_t Hq, int32_t Hk, int32_t D, float scale,
+                  int32_t causal, const tdq_heads* O, float* lse, void* workspace, size_t workspace_bytes,
+                  void* stream);
 
 #ifdef __cplusplus
 }

@@ -881,4 +881,115 @@ int tdq_quantize_weight(const float* W, int32_t N, int32_t K, int64_t ld_w_in, u
   return TDQ_OK;
 }
 
+// ---- 8-bit floating point, head norm and attention -----------------------------
+
+static bool any_type(tdq_dtype dt) { return dt == TDQ_F16 || dt == TDQ_F32 || dt == TDQ_BF16; }
+static size_t type_bytes(tdq_dtype dt) { return dt == TDQ_F32 ? 4 : 2; }
+static bool misaligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
+
+static int check_quantize_f8(const void* X, tdq_dtype dt, int64_t rows, int32_t K, int64_t ld_x, const uint8_t* Q,
+                             int64_t ld_q, const float* step, int64_t ld_s) {
+  if (!X || !Q || !step) return TDQ_ERR_NULL;
+  if (!any_type(dt)) return TDQ_ERR_DTYPE;
+  if (rows < 1 || rows > (int64_t)1 << 30 || K < 1 || K > 131072) return TDQ_ERR_SHAPE;
+  const int64_t KB = ((int64_t)K + TDQ_BLOCK_F8 - 1) / TDQ_BLOCK_F8;
+  if (ld_x < K || ld_q < K || ld_s < KB || rows * KB >= (int64_t)1 << 31) return TDQ_ERR_SHAPE;
+  if (misaligned(X, type_bytes(dt)) || misaligned(Q, 16) || ld_q % 16 || misaligned(step, 4)) return TDQ_ERR_ALIGN;
+  return TDQ_OK;
+}
+
+int tdq_quantize_act_f8(const void* X, tdq_dtype dt, int64_t M, int32_t K, int64_t ld_x, uint8_t* Q, int64_t ld_q,
+                        float* step, int64_t ld_s, void* stream) {
+  const int rc = check_quantize_f8(X, dt, M, K, ld_x, Q, ld_q, step, ld_s);
+  if (rc != TDQ_OK) return rc;
+  if (launch_quantize_f8_rows(X, dt, M, K, ld_x, Q, ld_q, step, ld_s, static_cast<hipStream_t>(stream)) != hipSuccess)
+    return TDQ_ERR_HIP;
+  return TDQ_OK;
+}
+
+int tdq_quantize_weight_f8(const void* W, tdq_dtype dt, int32_t N, int32_t K, int64_t ld_w_in, uint8_t* Qw,
+                           int64_t ld_w, float* step, int64_t ld_s, void* stream) {
+  const int rc = check_quantize_f8(W, dt, N, K, ld_w_in, Qw, ld_w, step, ld_s);
+  if (rc != TDQ_OK) return rc;
+  if (N > 1 << 22) return TDQ_ERR_SHAPE;               // (its blocks are an axis of a grid)
+  if (launch_quantize_f8_tiles(W, dt, N, K, ld_w_in, Qw, ld_w, step, ld_s, static_cast<hipStream_t>(stream)) !=
+      hipSuccess)
+    return TDQ_ERR_HIP;
+  return TDQ_OK;
+}
+
+int tdq_linear_f8(const uint8_t* Qx, int64_t ld_q, const float* x_step, int64_t ld_xs, int64_t M, int32_t K, int32_t N,
+                  const uint8_t* Qw, int64_t ld_w, const float* w_step, int64_t ld_ws, const float* bias, void* Y,
+                  tdq_dtype y_dt, int64_t ld_y, void* stream) {
+  if (!Qx || !x_step || !Qw || !w_step || !Y) return TDQ_ERR_NULL;
+  if (!any_type(y_dt)) return TDQ_ERR_DTYPE;
+  if (M < 1 || M > (int64_t)1 << 30 || K < 1 || K > 131072 || N < 1 || N > 1 << 22) return TDQ_ERR_SHAPE;
+  const int64_t KB = ((int64_t)K + TDQ_BLOCK_F8 - 1) / TDQ_BLOCK_F8;
+  if (ld_q < K || ld_w < K || ld_xs < KB || ld_ws < KB || ld_y < N) return TDQ_ERR_SHAPE;
+  // the rows of a tile are within 32-bit offsets
+  if (ld_q > (int64_t)1 << 22 || ld_w > (int64_t)1 << 22 || ld_xs > (int64_t)1 << 20) return TDQ_ERR_SHAPE;
+  if (misaligned(Qx, 16) || misaligned(Qw, 16) || ld_q % 16 || ld_w % 16) return TDQ_ERR_ALIGN;
+  if (misaligned(x_step, 4) || misaligned(w_step, 4) || misaligned(bias, 4) || misaligned(Y, type_bytes(y_dt)))
+    return TDQ_ERR_ALIGN;
+  if (launch_linear_f8(Qx, ld_q, x_step, ld_xs, (int)M, K, N, Qw, ld_w, w_step, ld_ws, bias, Y, y_dt, ld_y,
+                       static_cast<hipStream_t>(stream)) != hipSuccess)
+    return TDQ_ERR_HIP;
+  return TDQ_OK;
+}
+
+int tdq_norm_rotate(const tdq_heads* Q, const tdq_heads* K, tdq_dtype dt, int64_t T, int32_t Hq, int32_t Hk, int32_t D,
+                    const float* q_weight, const float* k_weight, float eps, int32_t R, int32_t interleaved,
+                    const int32_t* pos, int64_t ld_pos, int32_t axes, const int32_t* axis, const float* freq,
+                    const tdq_heads* Qo, const tdq_heads* Ko, void* stream) {
+  if (!Q || !Qo || !Q->data || !Qo->data) return TDQ_ERR_NULL;
+  if (Hk > 0 && (!K || !Ko || !K->data || !Ko->data)) return TDQ_ERR_NULL;
+  if (R > 0 && (!pos || !freq)) return TDQ_ERR_NULL;
+  if (!any_type(dt)) return TDQ_ERR_DTYPE;
+  if (T < 1 || T > (int64_t)1 << 30 || Hq < 1 || Hk < 0 || Hq > 4096 || Hk > 4096 || Hq + Hk > 4096)
+    return TDQ_ERR_SHAPE;
+  if (D < 8 || D > TDQ_MAX_HEAD || D % 8 || R < 0 || R > D || R % 8) return TDQ_ERR_SHAPE;
+  if (R > 0 && (axes < 1 || ld_pos < T)) return TDQ_ERR_SHAPE;
+  if (!(eps >= 0.f) || !isfinite(eps)) return TDQ_ERR_PARAM;
+  const size_t z = type_bytes(dt);
+  if (misaligned(Q->data, z) || misaligned(Qo->data, z)) return TDQ_ERR_ALIGN;
+  if (Hk > 0 && (misaligned(K->data, z) || misaligned(Ko->data, z))) return TDQ_ERR_ALIGN;
+  if (misaligned(q_weight, 4) || misaligned(k_weight, 4) || misaligned(pos, 4) || misaligned(axis, 4) ||
+      misaligned(freq, 4))
+    return TDQ_ERR_ALIGN;
+  if (launch_norm_rotate(Q, Hk > 0 ? K : nullptr, dt, T, Hq, Hk, D, q_weight, k_weight, eps, R, interleaved != 0, pos,
+                         ld_pos, axes, axis, freq, Qo, Hk > 0 ? Ko : nullptr,
+                         static_cast<hipStream_t>(stream)) != hipSuccess)
+    return TDQ_ERR_HIP;
+  return TDQ_OK;
+}
+
+static bool attention_shape(int64_t Tq, int64_t Tk, int32_t S, int32_t Hq, int32_t Hk, int32_t D) {
+  return Tq >= 1 && Tq <= (int64_t)1 << 30 && Tk >= 0 && Tk <= (int64_t)1 << 30 && S >= 1 && S <= 1 << 20 && Hq >= 1 &&
+         Hq <= 4096 && Hk >= 1 && Hq % Hk == 0 && D >= 8 && D <= TDQ_MAX_HEAD && D % 8 == 0;
+}
+
+size_t tdq_attention_workspace_bytes(int64_t Tq, int64_t Tk, int32_t S, int32_t Hq, int32_t Hk, int32_t D) {
+  return attention_shape(Tq, Tk, S, Hq, Hk, D) ? attention_workspace(Tq, Tk, S, Hq, Hk, D) : 0;
+}
+
+int tdq_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, tdq_dtype dt, int64_t Tq, int64_t Tk,
+                  int32_t S, const int32_t* cu_q, const int32_t* cu_k, int32_t Hq, int32_t Hk, int32_t D, float scale,
+                  int32_t causal, const tdq_heads* O, float* lse, void* workspace, size_t workspace_bytes,
+                  void* stream) {
+  if (!Q || !K || !V || !O || !cu_q || !cu_k || !Q->data || !O->data) return TDQ_ERR_NULL;
+  if (Tk > 0 && (!K->data || !V->data)) return TDQ_ERR_NULL;
+  if (dt != TDQ_F16 && dt != TDQ_BF16) return TDQ_ERR_DTYPE;
+  if (!attention_shape(Tq, Tk, S, Hq, Hk, D)) return TDQ_ERR_SHAPE;
+  if (!isfinite(scale)) return TDQ_ERR_PARAM;
+  for (const tdq_heads* t : {Q, K, V, O})
+    if (misaligned(t->data, 16) || t->token % 8 || t->head % 8) return TDQ_ERR_ALIGN;
+  if (misaligned(cu_q, 4) || misaligned(cu_k, 4) || misaligned(lse, 4)) return TDQ_ERR_ALIGN;
+  const size_t need = attention_workspace(Tq, Tk, S, Hq, Hk, D);
+  if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 256))) return TDQ_ERR_WORKSPACE;
+  if (launch_attention(Q, K, V, dt, Tq, Tk, S, cu_q, cu_k, Hq, Hk, D, scale, causal != 0, O, lse, workspace,
+                       static_cast<hipStream_t>(stream)) != hipSuccess)
+    return TDQ_ERR_HIP;
+  return TDQ_OK;
+}
+
 }  // extern "C"

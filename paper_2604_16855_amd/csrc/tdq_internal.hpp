@@ -233,4 +233,21 @@ hipError_t launch_w4a4_gemm(const uint8_t* Qx, long long ld_q, const int* gid, c
                             const float* w_scale, const float* bias, void* Y, tdq_dtype y_dt,
                             long long ld_y, int* acc_dump, hipStream_t st);
 
+// ---- 8-bit floating point, head norm and attention -----------------------------
+hipError_t launch_quantize_f8_rows(const void* X, tdq_dtype dt, long long M, int K, long long ld_x, uint8_t* Q,
+                                   long long ld_q, float* step, long long ld_s, hipStream_t st);
+hipError_t launch_quantize_f8_tiles(const void* W, tdq_dtype dt, int N, int K, long long ld_in, uint8_t* Q,
+                                    long long ld_q, float* step, long long ld_s, hipStream_t st);
+hipError_t launch_linear_f8(const uint8_t* Qx, long long ld_q, const float* xs, long long ld_xs, int M, int K, int N,
+                            const uint8_t* Qw, long long ld_w, const float* ws, long long ld_ws, const float* bias,
+                            void* Y, tdq_dtype y_dt, long long ld_y, hipStream_t st);
+hipError_t launch_norm_rotate(const tdq_heads* Q, const tdq_heads* K, tdq_dtype dt, long long T, int Hq, int Hk, int D,
+                              const float* q_weight, const float* k_weight, float eps, int R, bool interleaved,
+                              const int* pos, long long ld_pos, int axes, const int* axis, const float* freq,
+                              const tdq_heads* Qo, const tdq_heads* Ko, hipStream_t st);
+size_t attention_workspace(long long Tq, long long Tk, int S, int Hq, int Hk, int D);
+hipError_t launch_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, tdq_dtype dt, long long Tq,
+                            long long Tk, int S, const int* cu_q, const int* cu_k, int Hq, int Hk, int D, float scale,
+                            bool causal, const tdq_heads* O, float* lse, void* workspace, hipStream_t st);
+
 }  // namespace tdq

@@ -8,6 +8,7 @@ library is missing — there is no fallback.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from typing import Optional, Tuple
 
@@ -16,7 +17,7 @@ import torch  # first: the library resolves libamdhip64 against the copy torch l
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libtdq.so")
 
-TDQ_F16, TDQ_F32 = 0, 1
+TDQ_F16, TDQ_F32, TDQ_BF16 = 0, 1, 2
 FLAG_C1, FLAG_C2 = 1, 2
 FLAG_EXACT_SELECT = 256     # validation switch: rank select without the sampled interval
 DEV_NONFINITE = 1
@@ -40,6 +41,12 @@ class GroupStats(C.Structure):
     _fields_ = [("n", C.c_int64), ("k", C.c_int64), ("c_base", C.c_float), ("sigma", C.c_float),
                 ("thr", C.c_float), ("c_tau", C.c_float), ("c_zr", C.c_float), ("clip", C.c_float),
                 ("scale", C.c_float), ("bind", C.c_uint32)]
+
+
+class Heads(C.Structure):
+    """Mirror of tdq_heads: a tensor [tokens, heads, D] with contiguous heads of D elements."""
+
+    _fields_ = [("data", C.c_void_p), ("token", C.c_int64), ("head", C.c_int64)]
 
 
 class TdqError(RuntimeError):
@@ -121,6 +128,21 @@ def lib() -> C.CDLL:
                                         vp, vp, vp, vp]
     L.tdq_probe.restype = C.c_int
     L.tdq_probe.argtypes = [C.c_int32, vp, sz, C.c_int32, C.c_int32, vp]
+    hp, f32 = C.POINTER(Heads), C.c_float
+    L.tdq_quantize_act_f8.restype = C.c_int
+    L.tdq_quantize_act_f8.argtypes = [vp, C.c_int, i64, i32, i64, vp, i64, vp, i64, vp]
+    L.tdq_quantize_weight_f8.restype = C.c_int
+    L.tdq_quantize_weight_f8.argtypes = [vp, C.c_int, i32, i32, i64, vp, i64, vp, i64, vp]
+    L.tdq_linear_f8.restype = C.c_int
+    L.tdq_linear_f8.argtypes = [vp, i64, vp, i64, i64, i32, i32, vp, i64, vp, i64, vp, vp, C.c_int, i64, vp]
+    L.tdq_norm_rotate.restype = C.c_int
+    L.tdq_norm_rotate.argtypes = [hp, hp, C.c_int, i64, i32, i32, i32, vp, vp, f32, i32, i32, vp, i64, i32, vp,
+                                  vp, hp, hp, vp]
+    L.tdq_attention_workspace_bytes.restype = sz
+    L.tdq_attention_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32]
+    L.tdq_attention.restype = C.c_int
+    L.tdq_attention.argtypes = [hp, hp, hp, C.c_int, i64, i64, i32, vp, vp, i32, i32, i32, f32, i32, hp, vp, vp,
+                                sz, vp]
     L.tdq_quantize_weight.restype = C.c_int
     L.tdq_quantize_weight.argtypes = [vp, i32, i32, i64, vp, i64, vp, vp]
     _lib = L
@@ -580,6 +602,186 @@ def tdq_w4a4_linear(Qx: torch.Tensor, gid: Optional[torch.Tensor], scale: torch.
                                out.data_ptr(), _dt(out), out.stride(0), _ptr(acc_dump), _stream())
     _check(rc, "tdq_w4a4_linear")
     return out
+
+
+# --------------------------------------------------------------------------------------
+# 8-bit floating point, head norm and attention
+# --------------------------------------------------------------------------------------
+BLOCK_F8 = 128              # TDQ_BLOCK_F8
+MAX_HEAD = 256              # TDQ_MAX_HEAD
+
+_WIDE_DTYPES = {torch.float16: TDQ_F16, torch.float32: TDQ_F32, torch.bfloat16: TDQ_BF16}
+
+
+def _wdt(t: torch.Tensor) -> int:
+    dt = _WIDE_DTYPES.get(t.dtype)
+    if dt is None:
+        raise TypeError(f"unsupported dtype {t.dtype}")
+    return dt
+
+
+def _expect(t: Optional[torch.Tensor], dtype, name: str) -> None:
+    if t is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+
+
+def _matrix(X: torch.Tensor, name: str) -> Tuple[int, int, int]:
+    """(rows, columns, leading dimension) of [R, C], or of [B, T, C] with a uniform row stride."""
+    if X.dim() == 3:
+        B, T, Cc, ld = _btc(X)
+        return B * T, Cc, ld
+    if X.dim() != 2 or (X.shape[1] > 1 and X.stride(1) != 1):
+        raise ValueError(f"{name} must be a matrix with contiguous rows")
+    # the stride of an axis of extent 1 addresses nothing
+    return X.shape[0], X.shape[1], X.stride(0) if X.shape[0] > 1 else max(X.shape[1], 1)
+
+
+def _rows_of(t: torch.Tensor, rows: int, cols: int, dtype, name: str) -> int:
+    """Leading dimension of a matrix of `dtype` with at least rows x cols elements."""
+    _expect(t, dtype, name)
+    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] < cols or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be [{rows}, {cols}] or larger, with contiguous rows")
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+
+
+def f8_row_bytes(K: int) -> int:
+    """Leading dimension of the e4m3 codes of K channels."""
+    return 16 * ((K + 15) // 16)
+
+
+def _f8_out(rows: int, step_rows: int, K: int, device, out):
+    KB = (K + BLOCK_F8 - 1) // BLOCK_F8
+    if out is None:
+        out = (torch.empty((rows, f8_row_bytes(K)), dtype=torch.uint8, device=device),
+               torch.empty((step_rows, KB), dtype=torch.float32, device=device))
+    Q, step = out
+    return Q, step, _rows_of(Q, rows, f8_row_bytes(K), torch.uint8, "codes"), _rows_of(step, step_rows, KB,
+                                                                                   torch.float32, "step")
+
+
+def tdq_quantize_act_f8(X: torch.Tensor, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
+    """X[M, K] or [B, T, K] -> (codes[M, 16 ceil(K/16)] uint8 (e4m3), step[M, ceil(K/128)] f32)."""
+    M, K, ld = _matrix(X, "X")
+    Q, step, ld_q, ld_s = _f8_out(M, M, K, X.device, out)
+    rc = lib().tdq_quantize_act_f8(X.data_ptr(), _wdt(X), M, K, ld, Q.data_ptr(), ld_q, step.data_ptr(), ld_s,
+                                   _stream())
+    _check(rc, "tdq_quantize_act_f8")
+    return Q, step
+
+
+def tdq_quantize_weight_f8(W: torch.Tensor, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
+    """W[N, K] -> (codes[N, 16 ceil(K/16)] uint8 (e4m3), step[ceil(N/128), ceil(K/128)] f32)."""
+    N, K, ld = _matrix(W, "W")
+    Q, step, ld_q, ld_s = _f8_out(N, (N + BLOCK_F8 - 1) // BLOCK_F8, K, W.device, out)
+    rc = lib().tdq_quantize_weight_f8(W.data_ptr(), _wdt(W), N, K, ld, Q.data_ptr(), ld_q, step.data_ptr(), ld_s,
+                                      _stream())
+    _check(rc, "tdq_quantize_weight_f8")
+    return Q, step
+
+
+def tdq_linear_f8(Qx: torch.Tensor, x_step: torch.Tensor, K: int, Qw: torch.Tensor, w_step: torch.Tensor,
+                  bias: Optional[torch.Tensor] = None, out_dtype=torch.float32,
+                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """-> Y[M, N] from e4m3 codes with a step per block of 128, M = Qx.shape[0], N = Qw.shape[0]."""
+    M, N, KB = Qx.shape[0], Qw.shape[0], (K + BLOCK_F8 - 1) // BLOCK_F8
+    if out is None:
+        out = torch.empty((M, N), dtype=out_dtype, device=Qx.device)
+    if bias is not None and (bias.dtype != torch.float32 or bias.shape != (N,) or not bias.is_contiguous()):
+        raise ValueError("bias must be contiguous float32 [N]")
+    rc = lib().tdq_linear_f8(Qx.data_ptr(), _rows_of(Qx, M, K, torch.uint8, "Qx"), x_step.data_ptr(),
+                             _rows_of(x_step, M, KB, torch.float32, "x_step"), M, K, N, Qw.data_ptr(),
+                             _rows_of(Qw, N, K, torch.uint8, "Qw"), w_step.data_ptr(),
+                             _rows_of(w_step, (N + BLOCK_F8 - 1) // BLOCK_F8, KB, torch.float32, "w_step"), _ptr(bias),
+                             out.data_ptr(), _wdt(out), _rows_of(out, M, N, out.dtype, "out"), _stream())
+    _check(rc, "tdq_linear_f8")
+    return out
+
+
+def _heads(X: torch.Tensor, name: str) -> Heads:
+    if X.dim() != 3 or (X.shape[2] > 1 and X.stride(2) != 1):
+        raise ValueError(f"{name} must be [tokens, heads, D] with contiguous heads")
+    # (the stride of an axis of extent 1 addresses nothing; torch may report any value for it)
+    return Heads(X.data_ptr(), X.stride(0) if X.shape[0] > 1 else 0, X.stride(1) if X.shape[1] > 1 else 0)
+
+
+def tdq_norm_rotate(Q: torch.Tensor, K: Optional[torch.Tensor], pos: Optional[torch.Tensor],
+                    freq: Optional[torch.Tensor], q_weight: Optional[torch.Tensor] = None,
+                    k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                    axis: Optional[torch.Tensor] = None, interleaved: bool = False, out=None):
+    """Q[T, Hq, D], K[T, Hk, D] or None -> (Qo, Ko): heads normed (where a weight is given) and turned by
+    pos[axes, T] (or [T]) * freq[R/2].  out = (Q, K) works in place."""
+    T, Hq, D = Q.shape
+    Hk = 0 if K is None else K.shape[1]
+    if K is not None and (K.shape[0] != T or K.shape[2] != D or K.dtype != Q.dtype):
+        raise ValueError("K must have Q's tokens, head size and type")
+    R, axes, ld_pos = 0, 1, 0
+    if freq is not None and freq.numel() > 0:
+        _expect(freq, torch.float32, "freq")
+        _expect(pos, torch.int32, "pos")
+        _expect(axis, torch.int32, "axis")
+        R = 2 * freq.numel()
+        if pos is None or pos.shape[-1] != T or pos.dim() not in (1, 2) or (T > 1 and pos.stride(-1) != 1):
+            raise ValueError("pos must be [T] or [axes, T] with contiguous rows")
+        axes = pos.shape[0] if pos.dim() == 2 else 1
+        ld_pos = pos.stride(0) if axes > 1 else T
+        if axis is not None and axis.numel() != freq.numel():
+            raise ValueError("axis must name an axis for each of freq")
+        if not freq.is_contiguous() or (axis is not None and not axis.is_contiguous()):
+            raise ValueError("freq and axis must be contiguous")
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None and (w.dtype != torch.float32 or w.numel() != D or not w.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous float32 [D]")
+    if out is None:
+        out = (torch.empty((T, Hq, D), dtype=Q.dtype, device=Q.device),
+               None if K is None else torch.empty((T, Hk, D), dtype=K.dtype, device=K.device))
+    Qo, Ko = out
+    if Qo.shape != Q.shape or Qo.dtype != Q.dtype or (K is not None and (Ko.shape != K.shape or Ko.dtype != K.dtype)):
+        raise ValueError("out must have the shapes and types of Q and K")
+    kin, kout = (None, None) if K is None else (C.byref(_heads(K, "K")), C.byref(_heads(Ko, "out K")))
+    rc = lib().tdq_norm_rotate(C.byref(_heads(Q, "Q")), kin, _wdt(Q), T, Hq, Hk, D, _ptr(q_weight), _ptr(k_weight),
+                               eps, R, int(interleaved), _ptr(pos), ld_pos, axes, _ptr(axis), _ptr(freq),
+                               C.byref(_heads(Qo, "out Q")), kout, _stream())
+    _check(rc, "tdq_norm_rotate")
+    return Qo, Ko
+
+
+def tdq_attention_workspace_bytes(Tq: int, Tk: int, S: int, Hq: int, Hk: int, D: int) -> int:
+    return int(lib().tdq_attention_workspace_bytes(Tq, Tk, S, Hq, Hk, D))
+
+
+def tdq_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, cu_q: torch.Tensor, cu_k: torch.Tensor,
+                  scale: Optional[float] = None, causal: bool = True, out: Optional[torch.Tensor] = None,
+                  lse: Optional[torch.Tensor] = None, want_lse: bool = False,
+                  workspace: Optional[torch.Tensor] = None):
+    """Q[Tq, Hq, D], K and V[Tk, Hk, D], cu_q and cu_k[S + 1] int32 -> (O[Tq, Hq, D], lse[Tq, Hq] f32 or None).
+    scale: 1 / sqrt(D) if None."""
+    Tq, Hq, D = Q.shape
+    Tk, Hk = K.shape[0], K.shape[1]
+    if K.shape != V.shape or K.shape[2] != D or K.dtype != Q.dtype or V.dtype != Q.dtype:
+        raise ValueError("K and V must have the same shape, and Q's head size and type")
+    _expect(cu_q, torch.int32, "cu_q")
+    _expect(cu_k, torch.int32, "cu_k")
+    S = cu_q.numel() - 1
+    if cu_k.numel() != S + 1 or not cu_q.is_contiguous() or not cu_k.is_contiguous():
+        raise ValueError("cu_q and cu_k must be contiguous, one longer than the number of sequences")
+    if out is None:
+        out = torch.empty((Tq, Hq, D), dtype=Q.dtype, device=Q.device)
+    if out.shape != Q.shape or out.dtype != Q.dtype:
+        raise ValueError("out must have the shape and type of Q")
+    if lse is None and want_lse:
+        lse = torch.empty((Tq, Hq), dtype=torch.float32, device=Q.device)
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (Tq, Hq) or not lse.is_contiguous()):
+        raise ValueError("lse must be contiguous float32 [Tq, Hq]")
+    if workspace is None:
+        n = tdq_attention_workspace_bytes(Tq, Tk, S, Hq, Hk, D)
+        workspace = torch.empty(n, dtype=torch.uint8, device=Q.device) if n else None
+    rc = lib().tdq_attention(C.byref(_heads(Q, "Q")), C.byref(_heads(K, "K")), C.byref(_heads(V, "V")), _wdt(Q), Tq,
+                             Tk, S, cu_q.data_ptr(), cu_k.data_ptr(), Hq, Hk, D,
+                             1.0 / math.sqrt(D) if scale is None else scale, int(causal),
+                             C.byref(_heads(out, "out")), _ptr(lse), _ptr(workspace),
+                             0 if workspace is None else workspace.numel(), _stream())
+    _check(rc, "tdq_attention")
+    return out, lse
 
 
 # the helper entry points under their C names as well
