@@ -1,5 +1,7 @@
 // Norm of query and key heads with the rotation by position, and softmax attention with grouped
 // heads over packed sequences.
+#include <math.h>
+
 #include "tdq_half.hpp"
 
 namespace tdq {
@@ -179,12 +181,14 @@ hipError_t launch_norm_rotate(const tdq_heads* Q, const tdq_heads* K, tdq_dtype 
 // The query heads of a key head are rows of one tile: row r of a sequence is token r / g, head
 // r % g of the group of g, so keys and values are read once for all of them, and one token
 // (g rows) goes the same way as a prompt.  One pass over the keys with the running maximum and
-// sum of the softmax (binary32):
+// sum of the softmax (binary32); a wavefront has 32 rows:
 //   S^T = K Q^T       keys x rows: a lane holds 16 of every 32 keys of ONE row, so that a row's
 //                     maximum is 15 steps in the lane and one exchange of the two halves
 //   P^T = 2^(c S^T - c m), rounded to the type of V as the matrix instruction's operand
 //   O^T += V^T P^T    a lane's probabilities are its operand as they lie: the order of the keys
 //                     within an instruction is free as long as V^T is read in the same order
+// The maximum m that P refers to is raised, and O rescaled, only when a score exceeds it by 8
+// octaves: the quotient O / sum is the same for any m, and 2^8 leaves every type its precision.
 // The sum of the probabilities is taken before their rounding.
 struct AttendArgs {
   const void *Q, *K, *V;
@@ -194,7 +198,10 @@ struct AttendArgs {
   long long q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;
   long long Tq, Tk;
   int S, Hq, Hk, group, D, causal;
-  float scale_log2;                    // scale * log2(e)
+  float scale_log2;                    // |scale| log2(e), at least 1e-30 (a masked score stays -inf)
+  u32 flip;                            // sign bits of two elements if the scale is negative: Q is negated
+  int splits;                          // parts that the keys of a sequence are cut into
+  float *part_o, *part_ml;             // [Tq Hq][splits][D], and maximum and sum [Tq Hq][splits][2]
 };
 
 // What keys and values past the end of a sequence, or past D, are copied from.
@@ -221,6 +228,10 @@ __device__ __forceinline__ float other_half(float x) {   // the value of lane ^ 
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
 }
+__device__ __forceinline__ float max_of_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 // Four elements down a column: 16 lanes give the addresses of 4 rows x 16 columns (a lane 4
@@ -229,6 +240,118 @@ __device__ __forceinline__ u32x2 read_column(u32 lds) {
   const s16x4 r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)lds);
   return __builtin_bit_cast(u32x2, r);
 }
+__device__ __forceinline__ u32x4 read_lds16(u32 lds) {
+  return *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)lds;
+}
+
+// Where the 16-byte piece c of row r lies in a row of LDS (c ^ place), so that what an
+// instruction reads at a time spreads over the banks: K by 16 rows of one piece, V by 4 rows of
+// 64 bytes.
+template <int DP>
+__device__ __forceinline__ int place_k(int r) {
+  return DP >= 128 ? r & 15 : DP == 64 ? (r >> 1) & 7 : (r >> 2) & 3;
+}
+template <int DP>
+__device__ __forceinline__ int place_v(int r) {
+  return DP >= 128 ? 4 * (r & 3) : DP == 64 ? 4 * ((r >> 1) & 1) : 0;
+}
+
+// A wavefront's 32 rows: their queries, and the softmax and output so far.
+template <typename T, int DP>
+struct Rows {
+  u32x4 q[DP / 16];                    // operand columns: row lane % 32, elements 16 i + 8 (lane / 32) ..
+  f32x16 o[DP / 32];                   // element j of o[i]: row lane % 32, output 32 i + 8 (j / 4) + 4 (lane / 32) + j % 4
+  float m, l;                          // reference of the exponents (of the row), sum (of this lane's keys)
+
+  __device__ __forceinline__ void start(const T* qp, int D, u32 flip) {
+    const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) {
+      const int c = 16 * i + 8 * half;
+      q[i] = u32x4{0, 0, 0, 0};
+      if (c < D) q[i] = *reinterpret_cast<const u32x4*>(qp + c) ^ flip;
+    }
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+  }
+
+  // Products of 32 keys from row r of a tile on: element j is key 8 (j / 4) + 4 (lane / 32) + j % 4.
+  __device__ __forceinline__ f32x16 scores(u32 lk, int r) const {
+    const int lane = threadIdx.x & 63, row = r + (lane & 31);
+    f32x16 s;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) s[j] = 0.f;
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i)
+      s = Mfma<T>::mul(read_lds16(lk + row * (2 * DP) + 16 * ((2 * i + (lane >> 5)) ^ place_k<DP>(row))), q[i], s);
+    return s;
+  }
+
+  // Scores -> probabilities, of N times 32 keys from key j0 on; `sees`: how many keys the row
+  // sees (looked at only where `masked`).
+  template <int N>
+  __device__ __forceinline__ void softmax(f32x16 (&s)[N], u32 (&p)[N][8], float c, int j0, int sees, bool masked) {
+    const int half = (threadIdx.x >> 5) & 1;
+    if (masked) {
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          s[n][j] = j0 + 32 * n + 8 * (j / 4) + 4 * half + j % 4 < sees ? s[n][j] : -INFINITY;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) top = fmaxf(top, s[n][j]);
+    top = max_of_halves(top);
+    if (__ballot((top - m) * c > 8.0f || (m == -INFINITY && top > m))) {
+      const float m_new = fmaxf(m, top);
+      // (rows that have seen no key yet keep their zeros)
+      const float keep = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - m_new) * c);
+      m = m_new;
+      l *= keep;
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[i][j] *= keep;
+    }
+    const float base = m == -INFINITY ? 0.f : -m * c;
+    float sum = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int j = 0; j < 16; j += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[n][j], c, base));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(s[n][j + 1], c, base));
+        sum += p0 + p1;
+        p[n][j / 2] = two_rounded<T>(p0, p1);
+      }
+    l += sum;
+  }
+
+  // O^T += V^T P^T for 32 keys from row r of a tile on: an operand has 16 keys, a lane's 8 of
+  // them 4 half .. + 3 and 8 + 4 half .. + 3, as its probabilities lie.
+  __device__ __forceinline__ void values(u32 lv, int r, const u32 (&p)[8]) {
+    const int lane = threadIdx.x & 63, half = lane >> 5, tr = lane & 15;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const u32x4 pb = {p[4 * n], p[4 * n + 1], p[4 * n + 2], p[4 * n + 3]};
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i) {
+        const int c = 4 * i + 2 * ((lane >> 4) & 1) + ((tr & 3) >> 1);      // 16-byte piece of this lane's four columns
+        const int ra = r + 16 * n + 4 * half + (tr >> 2), rb = ra + 8;
+        const u32x2 va = read_column(lv + ra * (2 * DP) + 16 * (c ^ place_v<DP>(ra)) + 8 * (tr & 1));
+        const u32x2 vb = read_column(lv + rb * (2 * DP) + 16 * (c ^ place_v<DP>(rb)) + 8 * (tr & 1));
+        o[i] = Mfma<T>::mul(u32x4{va[0], va[1], vb[0], vb[1]}, pb, o[i]);
+      }
+    }
+  }
+};
 
 // The sequence and the tile of a slot: sequence s has the slots from floor(first row / BM) + s
 // on, which leaves it at least as many as it has tiles of BM rows.
@@ -263,172 +386,346 @@ __device__ __forceinline__ Slot find_slot(const AttendArgs& a, long long slot) {
   return r;
 }
 
+// A tile of rows of a sequence.
+struct Tile {
+  int q0, nq, k0, nk;                  // first query and key of the sequence, and how many
+  long long r0, rows;                  // first row of the tile, rows of the sequence
+  int ahead;                           // a causal token t sees the keys up to t + ahead
+  __device__ __forceinline__ bool none() const { return r0 < 0 || r0 >= rows; }
+  // Keys that row r sees.
+  __device__ __forceinline__ int sees(const AttendArgs& a, long long r) const {
+    if (!a.causal) return nk;
+    const long long e = r / a.group + ahead + 1;
+    return e < 0 ? 0 : e < nk ? (int)e : nk;
+  }
+};
+template <int BM>
+__device__ __forceinline__ Tile find_tile(const AttendArgs& a, long long slot) {
+  const Slot s = find_slot<BM>(a, slot);
+  Tile t;
+  t.q0 = clamp_start(a.cu_q, s.seq, a.Tq);
+  t.nq = clamp_start(a.cu_q, s.seq + 1, a.Tq) - t.q0;
+  t.k0 = clamp_start(a.cu_k, s.seq, a.Tk);
+  t.nk = clamp_start(a.cu_k, s.seq + 1, a.Tk) - t.k0;
+  t.nk = t.nk > 0 ? t.nk : 0;
+  t.rows = t.nq > 0 ? (long long)t.nq * a.group : 0;
+  t.r0 = (long long)s.tile * BM;
+  t.ahead = t.nk - t.nq;
+  return t;
+}
+
+// One copy instruction: ROWS_PER_COPY rows of keys or values to LDS, zeros past the sequence's
+// end and past D.
+template <typename T, int DP, int PLACE(int)>
+__device__ __forceinline__ void copy_rows(const T* first, long long token, int r, int left, int D, u32 lds) {
+  constexpr int PIECES = DP / 8;
+  const int lane = threadIdx.x & 63, row = r + lane / PIECES, piece = (lane % PIECES) ^ PLACE(row);
+  const T* p = first + row * token + 8 * piece;
+  copy_to_lds(row < left && 8 * piece < D ? (const void*)p : (const void*)kZeros, lds);
+}
+
 constexpr int kKeys = 64;              // keys of a tile
 
+// Many rows: 128 of them by four wavefronts that share tiles of 64 keys, the next tile on its way
+// while one is worked on.
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void k_attend(AttendArgs a, long long slots) {
-  constexpr int BM = 128, PIECES = DP / 8, ROW = DP * 2;     // 16-byte pieces and bytes of a row in LDS
-  constexpr int ROWS_PER_COPY = 64 / PIECES, COPIES = kKeys / ROWS_PER_COPY / 4;   // per wavefront
-  // Where piece c of row r lies, so that what is read at a time spreads over the banks: K by 16
-  // rows of one piece, V by 4 rows of 64 bytes.
-  auto place_k = [](int r) { return DP >= 128 ? r & 15 : DP == 64 ? (r >> 1) & 7 : (r >> 2) & 3; };
-  auto place_v = [](int r) { return DP >= 128 ? 4 * (r & 3) : DP == 64 ? 4 * ((r >> 1) & 1) : 0; };
-  __shared__ __attribute__((aligned(1024))) uint8_t sk[kKeys * ROW], sv[kKeys * ROW];
+  constexpr int BM = 128, ROW = DP * 2;                // bytes of a row in LDS
+  constexpr int ROWS_PER_COPY = 512 / DP, COPIES = kKeys / ROWS_PER_COPY / 4;   // per wavefront
+  constexpr int STAGES = DP <= 128 ? 2 : 1;
+  __shared__ __attribute__((aligned(1024))) uint8_t sk[STAGES][kKeys * ROW], sv[STAGES][kKeys * ROW];
 
   const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
   if (id >= slots * a.Hk) return;
   const int hk = (int)(id % a.Hk);
-  const Slot slot = find_slot<BM>(a, slots - 1 - id / a.Hk);
-  const int q0 = clamp_start(a.cu_q, slot.seq, a.Tq), nq = clamp_start(a.cu_q, slot.seq + 1, a.Tq) - q0;
-  const int k0 = clamp_start(a.cu_k, slot.seq, a.Tk);
-  int nk = clamp_start(a.cu_k, slot.seq + 1, a.Tk) - k0;
-  nk = nk > 0 ? nk : 0;
-  const long long rows = nq > 0 ? (long long)nq * a.group : 0;
-  const long long r0 = (long long)slot.tile * BM;
-  if (r0 >= rows) return;
+  const Tile t = find_tile<BM>(a, slots - 1 - id / a.Hk);
+  if (t.none()) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, D = a.D;
-  const int ahead = nk - nq;                           // a causal token t sees the keys up to t + ahead
 
-  // this lane's row
-  const long long row = r0 + wave * 32 + (lane & 31);
-  const bool real = row < rows;
-  const long long row_c = real ? row : rows - 1;
+  const long long first = t.r0 + wave * 32, row = first + (lane & 31);
+  const bool real = row < t.rows;
+  const long long row_c = real ? row : t.rows - 1;
   const int token = (int)(row_c / a.group), head = hk * a.group + (int)(row_c - (long long)token * a.group);
-  const int sees = a.causal ? (token + ahead + 1 < nk ? token + ahead + 1 : nk) : nk;   // keys that the row sees
-  // and how many of the tile's keys the workgroup, and this wavefront, need
-  long long last = r0 + BM - 1;
-  if (last > rows - 1) last = rows - 1;
-  int end = a.causal ? (int)(last / a.group) + ahead + 1 : nk;
-  end = end < nk ? end : nk;
-  end = __builtin_amdgcn_readfirstlane(end);
+  const int sees = t.sees(a, row_c);
+  // how many keys the workgroup needs, and all rows of this wavefront see
+  const int end = __builtin_amdgcn_readfirstlane(t.sees(a, t.r0 + BM < t.rows ? t.r0 + BM - 1 : t.rows - 1));
+  const int last = __builtin_amdgcn_readfirstlane(t.sees(a, first + 32 < t.rows ? first + 31 : t.rows - 1));
+  const int all = __builtin_amdgcn_readfirstlane(t.sees(a, first < t.rows ? first : t.rows - 1));
 
-  u32x4 q[DP / 16];
-  {
-    const T* qp = static_cast<const T*>(a.Q) + (q0 + token) * a.q_token + head * a.q_head;
-#pragma unroll
-    for (int i = 0; i < DP / 16; ++i) {
-      const int c = 16 * i + 8 * half;
-      q[i] = u32x4{0, 0, 0, 0};
-      if (c < D) q[i] = *reinterpret_cast<const u32x4*>(qp + c);
-    }
-  }
-  f32x16 o[DP / 32];
-#pragma unroll
-  for (int i = 0; i < DP / 32; ++i)
-#pragma unroll
-    for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
-  float m = -INFINITY, l = 0.f;                        // running maximum (of the row), sum (of this lane's keys)
-
-  const T* kp = static_cast<const T*>(a.K) + k0 * a.k_token + hk * a.k_head;
-  const T* vp = static_cast<const T*>(a.V) + k0 * a.v_token + hk * a.v_head;
-  const u32 lk = lds_address(sk), lv = lds_address(sv);
-  const int crow = lane / PIECES, cpos = lane % PIECES;
-  for (int j0 = 0; j0 < end; j0 += kKeys) {
-    __syncthreads();                                   // the last tile has been read
+  Rows<T, DP> w;
+  w.start(static_cast<const T*>(a.Q) + (t.q0 + token) * a.q_token + head * a.q_head, D, a.flip);
+  const T* kp = static_cast<const T*>(a.K) + t.k0 * a.k_token + hk * a.k_head;
+  const T* vp = static_cast<const T*>(a.V) + t.k0 * a.v_token + hk * a.v_head;
+  auto copy_tile = [&](int j0, int stage) {
+    const u32 lk = lds_address(sk[stage]), lv = lds_address(sv[stage]);
+    const T *kt = kp + j0 * a.k_token, *vt = vp + j0 * a.v_token;
 #pragma unroll
     for (int i = 0; i < COPIES; ++i) {
-      const int c = wave * COPIES + i, r = c * ROWS_PER_COPY + crow;
-      const int pk = cpos ^ place_k(r), pv = cpos ^ place_v(r);
-      const T* sk_ = kp + (j0 + r) * a.k_token + 8 * pk;
-      const T* sv_ = vp + (j0 + r) * a.v_token + 8 * pv;
-      copy_to_lds(j0 + r < nk && 8 * pk < D ? (const void*)sk_ : (const void*)kZeros, lk + c * 1024);
-      copy_to_lds(j0 + r < nk && 8 * pv < D ? (const void*)sv_ : (const void*)kZeros, lv + c * 1024);
+      const int c = wave * COPIES + i, r = c * ROWS_PER_COPY;
+      copy_rows<T, DP, place_k<DP>>(kt, a.k_token, r, t.nk - j0, D, lk + c * 1024);
+      copy_rows<T, DP, place_v<DP>>(vt, a.v_token, r, t.nk - j0, D, lv + c * 1024);
+    }
+  };
+  if (STAGES == 2 && end > 0) copy_tile(0, 0);
+  for (int j0 = 0; j0 < end; j0 += kKeys) {
+    const int stage = STAGES == 2 ? (j0 / kKeys) & 1 : 0;
+    if (STAGES == 1) {
+      __syncthreads();                                 // the last tile has been read
+      copy_tile(j0, 0);
     }
     wait_copies();
     __syncthreads();
-
-    // scores: element i of s[n] is key 32 n + 8 (i / 4) + 4 half + i % 4
-    f32x16 s[2];
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-#pragma unroll
-      for (int j = 0; j < 16; ++j) s[n][j] = 0.f;
-      const int r = 32 * n + (lane & 31);
-#pragma unroll
-      for (int i = 0; i < DP / 16; ++i) {
-        const u32x4 k = *reinterpret_cast<const u32x4*>(&sk[r * ROW + 16 * ((2 * i + half) ^ place_k(r))]);
-        s[n] = Mfma<T>::mul(k, q[i], s[n]);
-      }
-    }
-    float top = -INFINITY;
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const int key = j0 + 32 * n + 8 * (j / 4) + 4 * half + j % 4;
-        s[n][j] = key < sees ? s[n][j] * a.scale_log2 : -INFINITY;
-        top = fmaxf(top, s[n][j]);
-      }
-    top = fmaxf(top, other_half(top));
-    const float m_new = fmaxf(m, top);
-    const float base = m_new == -INFINITY ? 0.f : m_new;       // (a row that has seen no key yet)
-    const float keep = __builtin_amdgcn_exp2f(m - base);
-    m = m_new;
-    float sum = 0.f;
-    u32 p[2][8];
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int j = 0; j < 16; j += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(s[n][j] - base), p1 = __builtin_amdgcn_exp2f(s[n][j + 1] - base);
-        sum += p0 + p1;
-        p[n][j / 2] = two_rounded<T>(p0, p1);
-      }
-    l = fmaf(l, keep, sum);
-#pragma unroll
-    for (int i = 0; i < DP / 32; ++i)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) o[i][j] *= keep;
-    // values: 16 keys at a time, a lane's 8 of them 4 half .. + 3 and 8 + 4 half .. + 3
-    const int tr = lane & 15;
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const u32x4 pb = {p[n / 2][4 * (n & 1)], p[n / 2][4 * (n & 1) + 1], p[n / 2][4 * (n & 1) + 2],
-                        p[n / 2][4 * (n & 1) + 3]};
-#pragma unroll
-      for (int i = 0; i < DP / 32; ++i) {
-        const int c = 4 * i + 2 * ((lane >> 4) & 1) + ((tr & 3) >> 1);      // 16-byte piece of this lane's four columns
-        const int ra = 16 * n + 4 * half + (tr >> 2), rb = ra + 8;
-        const u32x2 va = read_column(lv + ra * ROW + 16 * (c ^ place_v(ra)) + 8 * (tr & 1));
-        const u32x2 vb = read_column(lv + rb * ROW + 16 * (c ^ place_v(rb)) + 8 * (tr & 1));
-        o[i] = Mfma<T>::mul(u32x4{va[0], va[1], vb[0], vb[1]}, pb, o[i]);
-      }
+    if (STAGES == 2 && j0 + kKeys < end) copy_tile(j0 + kKeys, stage ^ 1);
+    if (j0 < last) {
+      const u32 lk = lds_address(sk[stage]), lv = lds_address(sv[stage]);
+      f32x16 s[2];
+      u32 p[2][8];
+      s[0] = w.scores(lk, 0);
+      s[1] = w.scores(lk, 32);
+      w.softmax(s, p, a.scale_log2, j0, sees, j0 + kKeys > all);
+      w.values(lv, 0, p[0]);
+      w.values(lv, 32, p[1]);
     }
   }
 
-  l += other_half(l);
+  const float l = w.l + other_half(w.l);
   if (!real) return;
-  const float inv = m == -INFINITY ? 0.f : 1.0f / l;   // a row that sees no key: zeros, and -inf
-  T* op = static_cast<T*>(a.O) + (q0 + token) * a.o_token + head * a.o_head;
+  const float inv = w.m == -INFINITY ? 0.f : 1.0f / l;   // a row that sees no key: zeros, and -inf
+  T* op = static_cast<T*>(a.O) + (t.q0 + token) * a.o_token + head * a.o_head;
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
     for (int j = 0; j < 16; j += 4) {
       const int c = 32 * i + 2 * j + 4 * half;
       if (c < D) {
-        const float y[4] = {o[i][j] * inv, o[i][j + 1] * inv, o[i][j + 2] * inv, o[i][j + 3] * inv};
+        const float y[4] = {w.o[i][j] * inv, w.o[i][j + 1] * inv, w.o[i][j + 2] * inv, w.o[i][j + 3] * inv};
         store_floats<T, 4>(op + c, y);
       }
     }
   if (a.lse && half == 0)
-    a.lse[(q0 + (long long)token) * a.Hq + head] =
-        m == -INFINITY ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+    a.lse[(t.q0 + (long long)token) * a.Hq + head] =
+        w.m == -INFINITY ? -INFINITY : fmaf(w.m, a.scale_log2, __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+}
+
+// Few rows (single tokens over a cache): 32 of them, and it is the keys that are shared out, to
+// `splits` workgroups and in each to four wavefronts.  Bound by reading K and V once: a wavefront
+// copies its own tiles of 32 keys, K of the next while it works on V of this and the other way
+// round, and waits for nobody until the end, where the wavefronts' parts are joined in LDS.
+constexpr int kFewRows = 32, kFewKeys = 32;
+template <int DP>
+struct FewShared {
+  union {
+    uint8_t kv[4][2][kFewKeys * 2 * DP];               // [wavefront][K, V]
+    float o[4][32][DP + 4];                            // parts of the output, rows 16 bytes apart in the banks
+  };
+  float ml[4][32][2];
+};
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void k_attend_few(AttendArgs a, long long slots) {
+  constexpr int ROWS_PER_COPY = 512 / DP, COPIES = kFewKeys / ROWS_PER_COPY;
+  __shared__ __attribute__((aligned(1024))) FewShared<DP> sh;
+
+  const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
+  const int hk = (int)(id % a.Hk), split = (int)(id / a.Hk % a.splits);
+  const long long slot = id / a.Hk / a.splits;
+  if (slot >= slots) return;
+  const Tile t = find_tile<kFewRows>(a, slots - 1 - slot);
+  if (t.none()) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int D = a.D;
+  const long long row = t.r0 + (lane & 31);
+  const long long row_c = row < t.rows ? row : t.rows - 1;
+  const int token = (int)(row_c / a.group), head = hk * a.group + (int)(row_c - (long long)token * a.group);
+  const int sees = t.sees(a, row_c);
+  const int here = (int)(t.rows - t.r0 < kFewRows ? t.rows - t.r0 : kFewRows);       // rows of the tile
+  const int end = __builtin_amdgcn_readfirstlane(t.sees(a, t.r0 + here - 1));
+  const int all = __builtin_amdgcn_readfirstlane(t.sees(a, t.r0));
+  const int tiles = (end + kFewKeys - 1) / kFewKeys, share = (tiles + a.splits - 1) / a.splits;
+  const int stop = (split + 1) * share < tiles ? (split + 1) * share : tiles;
+
+  Rows<T, DP> w;
+  w.start(static_cast<const T*>(a.Q) + (t.q0 + token) * a.q_token + head * a.q_head, D, a.flip);
+  const T* kp = static_cast<const T*>(a.K) + t.k0 * a.k_token + hk * a.k_head;
+  const T* vp = static_cast<const T*>(a.V) + t.k0 * a.v_token + hk * a.v_head;
+  const u32 lk = lds_address(sh.kv[wave][0]), lv = lds_address(sh.kv[wave][1]);
+  auto copy_k = [&](int i) {
+    const T* kt = kp + (long long)i * kFewKeys * a.k_token;
+#pragma unroll
+    for (int c = 0; c < COPIES; ++c)
+      copy_rows<T, DP, place_k<DP>>(kt, a.k_token, c * ROWS_PER_COPY, t.nk - i * kFewKeys, D, lk + c * 1024);
+  };
+  auto copy_v = [&](int i) {
+    const T* vt = vp + (long long)i * kFewKeys * a.v_token;
+#pragma unroll
+    for (int c = 0; c < COPIES; ++c)
+      copy_rows<T, DP, place_v<DP>>(vt, a.v_token, c * ROWS_PER_COPY, t.nk - i * kFewKeys, D, lv + c * 1024);
+  };
+  int i = split * share + wave;
+  if (i < stop) {
+    copy_k(i);
+    copy_v(i);
+  }
+  for (; i < stop; i += 4) {
+    const bool more = i + 4 < stop;
+    // (copies arrive in order: all but the last COPIES, those of V, are there)
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
+    f32x16 s[1];
+    u32 p[1][8];
+    s[0] = w.scores(lk, 0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // K has been read
+    if (more) copy_k(i + 4);
+    w.softmax(s, p, a.scale_log2, i * kFewKeys, sees, (i + 1) * kFewKeys > all);
+    if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
+    else wait_copies();
+    w.values(lv, 0, p[0]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // V has been read
+    if (more) copy_v(i + 4);
+  }
+
+  // join the wavefronts' parts: they refer to different maxima
+  const float l = w.l + other_half(w.l);
+  if (lane < 32) {
+    sh.ml[wave][lane][0] = w.m;
+    sh.ml[wave][lane][1] = l;
+  }
+  __syncthreads();                                       // (nobody reads K and V any more)
+  float m = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int v = 0; v < 4; ++v) m = fmaxf(m, sh.ml[v][lane & 31][0]);
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    const float mv = sh.ml[v][lane & 31][0];
+    if (mv != -INFINITY) sum += sh.ml[v][lane & 31][1] * __builtin_amdgcn_exp2f((mv - m) * a.scale_log2);
+  }
+  const float keep = w.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((w.m - m) * a.scale_log2);
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int j = 0; j < 16; j += 4)
+      *reinterpret_cast<f32x4*>(&sh.o[wave][lane & 31][32 * d + 2 * j + 4 * (lane >> 5)]) =
+          f32x4{w.o[d][j] * keep, w.o[d][j + 1] * keep, w.o[d][j + 2] * keep, w.o[d][j + 3] * keep};
+  __syncthreads();
+  if (wave == 0 && lane < 32) {                          // for the threads that store a row
+    sh.ml[0][lane][0] = m;
+    sh.ml[0][lane][1] = sum;
+  }
+  __syncthreads();
+  constexpr int QUADS = DP / 4;
+  for (int e = threadIdx.x; e < here * QUADS; e += 256) {
+    const int r = e / QUADS, c = 4 * (e % QUADS);
+    if (c >= D) continue;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int v = 0; v < 4; ++v) y += *reinterpret_cast<const f32x4*>(&sh.o[v][r][c]);
+    const float mr = sh.ml[0][r][0], lr = sh.ml[0][r][1];
+    const long long rr = t.r0 + r;
+    const int tok = (int)(rr / a.group), h = hk * a.group + (int)(rr - (long long)tok * a.group);
+    const long long at = (t.q0 + (long long)tok) * a.Hq + h;
+    if (a.splits > 1) {
+      const long long part = at * a.splits + split;
+      *reinterpret_cast<f32x4*>(a.part_o + part * D + c) = y;
+      if (c == 0) {
+        a.part_ml[2 * part] = mr;
+        a.part_ml[2 * part + 1] = lr;
+      }
+    } else {
+      const float inv = mr == -INFINITY ? 0.f : 1.0f / lr;
+      const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
+      store_floats<T, 4>(static_cast<T*>(a.O) + (t.q0 + tok) * a.o_token + h * a.o_head + c, z);
+      if (a.lse && c == 0)
+        a.lse[at] = mr == -INFINITY ? -INFINITY
+                                    : fmaf(mr, a.scale_log2, __builtin_amdgcn_logf(lr)) * 0.69314718055994530942f;
+    }
+  }
+}
+
+// Joins the splits' parts, four outputs a thread, a workgroup for the 32 rows of a tile.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, long long slots) {
+  const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
+  if (id >= slots * a.Hk) return;
+  const int hk = (int)(id % a.Hk);
+  const Tile t = find_tile<kFewRows>(a, id / a.Hk);
+  if (t.none()) return;
+  const int here = (int)(t.rows - t.r0 < kFewRows ? t.rows - t.r0 : kFewRows), quads = a.D / 4;
+  for (int e = threadIdx.x; e < here * quads; e += 256) {
+    const int r = e / quads, c = 4 * (e - r * quads);
+    const long long rr = t.r0 + r;
+    const int tok = (int)(rr / a.group), h = hk * a.group + (int)(rr - (long long)tok * a.group);
+    const long long at = (t.q0 + (long long)tok) * a.Hq + h;
+    const float* ml = a.part_ml + 2 * at * a.splits;
+    const float* po = a.part_o + at * a.splits * a.D + c;
+    float m = -INFINITY, l = 0.f;
+    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[2 * s]);
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s) {
+      const float ms = ml[2 * s];
+      if (ms == -INFINITY) continue;                     // (a part without keys)
+      const float f = __builtin_amdgcn_exp2f((ms - m) * a.scale_log2);
+      l = fmaf(ml[2 * s + 1], f, l);
+      y += *reinterpret_cast<const f32x4*>(po + (long long)s * a.D) * f;
+    }
+    const float inv = m == -INFINITY ? 0.f : 1.0f / l;
+    const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
+    store_floats<T, 4>(static_cast<T*>(a.O) + (t.q0 + tok) * a.o_token + h * a.o_head + c, z);
+    if (a.lse && c == 0)
+      a.lse[at] = m == -INFINITY ? -INFINITY : fmaf(m, a.scale_log2, __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+  }
+}
+
+// Which way a call goes, from what the host knows of it.
+struct AttendPlan {
+  bool few;
+  int splits;
+};
+static AttendPlan attend_plan(long long Tq, long long Tk, int S, int Hq, int Hk) {
+  AttendPlan p = {false, 1};
+  const long long g = Hq / Hk;
+  if (Tq * g > 32ll * S) return p;
+  p.few = true;
+  // enough workgroups for 512 at a time to even out sequences of different lengths, as long as
+  // each has a few hundred keys
+  const long long most = Tk / S / 256, base = (long long)S * Hk;
+  long long n = 2048 / base;
+  if (n > most) n = most;
+  if (n > 128) n = 128;
+  if (n > 1) p.splits = (int)n;
+  return p;
+}
+
+static size_t part_ml_bytes(long long Tq, int Hq, int splits) {
+  return ((size_t)Tq * Hq * splits * 2 * sizeof(float) + 255) & ~(size_t)255;
+}
+
+size_t attention_workspace(long long Tq, long long Tk, int S, int Hq, int Hk, int D) {
+  const AttendPlan p = attend_plan(Tq, Tk, S, Hq, Hk);
+  if (p.splits <= 1) return 0;
+  return part_ml_bytes(Tq, Hq, p.splits) + (size_t)Tq * Hq * p.splits * D * sizeof(float);
+}
+
+static dim3 two_axes(long long n) {                      // an axis of a grid holds fewer than 2^32 threads
+  const long long axis = 1 << 22;
+  return dim3(n < axis ? (unsigned)n : (unsigned)axis, (unsigned)((n + axis - 1) / axis));
 }
 
 template <typename T, int DP>
-static void launch_attend(const AttendArgs& a, hipStream_t st) {
-  const long long slots = a.Tq * a.group / 128 + a.S;
-  const long long total = slots * a.Hk, axis = 1 << 22;
-  const dim3 grid(total < axis ? (unsigned)total : (unsigned)axis, (unsigned)((total + axis - 1) / axis));
-  hipLaunchKernelGGL((k_attend<T, DP>), grid, dim3(256), 0, st, a, slots);
+static void launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
+  if (p.few) {
+    const long long slots = a.Tq * a.group / kFewRows + a.S;
+    hipLaunchKernelGGL((k_attend_few<T, DP>), two_axes(slots * a.Hk * p.splits), dim3(256), 0, st, a, slots);
+    if (p.splits > 1) hipLaunchKernelGGL((k_attend_join<T>), two_axes(slots * a.Hk), dim3(256), 0, st, a, slots);
+  } else {
+    const long long slots = a.Tq * a.group / 128 + a.S;
+    hipLaunchKernelGGL((k_attend<T, DP>), two_axes(slots * a.Hk), dim3(256), 0, st, a, slots);
+  }
 }
-
-size_t attention_workspace(long long, long long, int, int, int, int) { return 0; }
 
 hipError_t launch_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, tdq_dtype dt, long long Tq,
                             long long Tk, int S, const int* cu_q, const int* cu_k, int Hq, int Hk, int D, float scale,
-                            bool causal, const tdq_heads* O, float* lse, void*, hipStream_t st) {
+                            bool causal, const tdq_heads* O, float* lse, void* workspace, hipStream_t st) {
+  const AttendPlan p = attend_plan(Tq, Tk, S, Hq, Hk);
   AttendArgs a;
   a.Q = Q->data;
   a.K = K->data;
@@ -453,13 +750,19 @@ hipError_t launch_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_he
   a.group = Hq / Hk;
   a.D = D;
   a.causal = causal;
-  a.scale_log2 = (float)((double)scale * 1.44269504088896340736);
+  const double c = fabs((double)scale) * 1.44269504088896340736;
+  a.scale_log2 = c > 1e-30 ? (float)c : 1e-30f;
+  a.flip = scale < 0.f ? 0x80008000u : 0u;
+  a.splits = p.splits;
+  a.part_ml = static_cast<float*>(workspace);
+  a.part_o = p.splits > 1 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + part_ml_bytes(Tq, Hq, p.splits))
+                          : nullptr;
 #define TDQ_ATTEND(T)                                  \
   do {                                                 \
-    if (D <= 32) launch_attend<T, 32>(a, st);          \
-    else if (D <= 64) launch_attend<T, 64>(a, st);     \
-    else if (D <= 128) launch_attend<T, 128>(a, st);   \
-    else launch_attend<T, 256>(a, st);                 \
+    if (D <= 32) launch_attend<T, 32>(a, p, st);       \
+    else if (D <= 64) launch_attend<T, 64>(a, p, st);  \
+    else if (D <= 128) launch_attend<T, 128>(a, p, st); \
+    else launch_attend<T, 256>(a, p, st);              \
   } while (0)
   if (dt == TDQ_F16) TDQ_ATTEND(_Float16);
   else TDQ_ATTEND(__bf16);
