@@ -460,12 +460,13 @@ typedef struct tdq_heads {
 /*
  * Norm of every query and key head and the rotation by position, in one pass:
  *   y[d] = x[d] / sqrt(mean_d x[d]^2 + eps) * weight[d]        (weight NULL: y = x)
- * then pair p < R / 2 of the first R elements by the angle w = pos[axis[p], t] * freq[p]:
+ * then pair p < R / 2 of the first R elements by the angle w = pos[axis[p], t] * freq[p], a
+ * product rounded to binary32 as in the tables that models are trained with:
  *   (a, b) -> (a cos w - b sin w, b cos w + a sin w)
  * where (a, b) are elements (2 p, 2 p + 1) if interleaved, else (p, p + R / 2); elements from R
  * on are not turned.  Several position axes (time, height, width): axis [R / 2] says which axis
  * turns a pair (values outside 0 .. axes - 1 are taken as the nearest), NULL = the first.
- * Angles are reduced in binary64.
+ * Cosine and sine of that angle are as exact as binary32, however far the position.
  *
  * Q, K: T tokens of Hq and Hk heads of D elements of dt (any of the three); K may be NULL with
  * Hk = 0.  D and R multiples of 8, R <= D <= TDQ_MAX_HEAD.  q_weight, k_weight [D] floats or

@@ -13,8 +13,8 @@ namespace tdq {
 // angle pos[axis of p] * freq[p]:  (a, b) -> (a cos - b sin, b cos + a sin).
 // One pass: the rows are read and written once, bound by memory.  The angles of a token serve
 // all its heads, so a workgroup takes a few whole tokens and leaves their cosines and sines in
-// LDS.  An angle is reduced as a fraction of a turn in binary64: a binary32 product of a
-// position of 100000 is off by up to 0.004 radians, more than bfloat16's rounding.
+// LDS.  The product pos * freq is rounded to binary32, as in the tables that models are trained
+// with; from there on the angle is exact: it is reduced as a fraction of a turn in binary64.
 struct RotateArgs {
   const void* in[2];
   void* out[2];
@@ -44,7 +44,8 @@ __global__ __launch_bounds__(kRotateThreads) void k_norm_rotate(RotateArgs a, in
     const int t = i / P, p = i - t * P;
     int ax = a.axis ? a.axis[p] : 0;
     ax = ax < 0 ? 0 : ax < a.axes ? ax : a.axes - 1;
-    const double turns = (double)a.pos[ax * a.ld_pos + t0 + t] * ((double)a.freq[p] * 0.15915494309189533577);
+    const float angle = (float)a.pos[ax * a.ld_pos + t0 + t] * a.freq[p];
+    const double turns = (double)angle * 0.15915494309189533577;
     float s, c;
     sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
     turn[t][2 * p] = c;

@@ -81,7 +81,8 @@ def norm_rotate(x, w, eps, pos, freq, axis, interleaved):
     P = 0 if freq is None else freq.numel()
     for p in range(P):
         row = 0 if axis is None else int(axis[p])
-        a = (pos.view(-1, x.shape[0])[row].double() * freq[p].double())[:, None]
+        # (the angle is a binary32 product by definition)
+        a = (pos.view(-1, x.shape[0])[row].float() * freq[p]).double()[:, None]
         i, j = (2 * p, 2 * p + 1) if interleaved else (p, p + P)
         y[..., i] = x[..., i] * a.cos() - x[..., j] * a.sin()
         y[..., j] = x[..., j] * a.cos() + x[..., i] * a.sin()
