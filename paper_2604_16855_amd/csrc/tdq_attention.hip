@@ -280,15 +280,35 @@ struct Rows {
     l = 0.f;
   }
 
-  // Products of 32 keys from row r of a tile on: element j is key 8 (j / 4) + 4 (lane / 32) + j % 4.
-  __device__ __forceinline__ f32x16 scores(u32 lk, int r) const {
-    const int lane = threadIdx.x & 63, row = r + (lane & 31);
+  // LDS addresses that this lane reads of a tile, of K's 16 elements i and of V's 32 outputs i; the
+  // rows of a tile from 32 n on are at the same places 32 n rows further.
+  u32 ka[DP / 16], va[DP / 32];
+  __device__ __forceinline__ void addresses(u32 lk, u32 lv) {
+    const int lane = threadIdx.x & 63, row = lane & 31, half = lane >> 5, tr = lane & 15;
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) ka[i] = lk + row * (2 * DP) + 16 * ((2 * i + half) ^ place_k<DP>(row));
+    const int key = 4 * half + (tr >> 2);              // (place_v is the same every four rows)
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) {
+      const int c = 4 * i + 2 * ((lane >> 4) & 1) + ((tr & 3) >> 1);
+      va[i] = lv + key * (2 * DP) + 16 * (c ^ place_v<DP>(key)) + 8 * (tr & 1);
+    }
+  }
+  __device__ __forceinline__ void move(int by) {
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) ka[i] += by;
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) va[i] += by;
+  }
+
+  // Products of 32 keys from row r (a multiple of 32) of a tile on: element j is key
+  // 8 (j / 4) + 4 (lane / 32) + j % 4.
+  __device__ __forceinline__ f32x16 scores(int r) const {
     f32x16 s;
 #pragma unroll
     for (int j = 0; j < 16; ++j) s[j] = 0.f;
 #pragma unroll
-    for (int i = 0; i < DP / 16; ++i)
-      s = Mfma<T>::mul(read_lds16(lk + row * (2 * DP) + 16 * ((2 * i + (lane >> 5)) ^ place_k<DP>(row))), q[i], s);
+    for (int i = 0; i < DP / 16; ++i) s = Mfma<T>::mul(read_lds16(ka[i] + r * (2 * DP)), q[i], s);
     return s;
   }
 
@@ -335,20 +355,17 @@ struct Rows {
     l += sum;
   }
 
-  // O^T += V^T P^T for 32 keys from row r of a tile on: an operand has 16 keys, a lane's 8 of
-  // them 4 half .. + 3 and 8 + 4 half .. + 3, as its probabilities lie.
-  __device__ __forceinline__ void values(u32 lv, int r, const u32 (&p)[8]) {
-    const int lane = threadIdx.x & 63, half = lane >> 5, tr = lane & 15;
+  // O^T += V^T P^T for 32 keys from row r (a multiple of 32) of a tile on: an operand has 16 keys,
+  // a lane's 8 of them 4 half .. + 3 and 8 + 4 half .. + 3, as its probabilities lie.
+  __device__ __forceinline__ void values(int r, const u32 (&p)[8]) {
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       const u32x4 pb = {p[4 * n], p[4 * n + 1], p[4 * n + 2], p[4 * n + 3]};
 #pragma unroll
       for (int i = 0; i < DP / 32; ++i) {
-        const int c = 4 * i + 2 * ((lane >> 4) & 1) + ((tr & 3) >> 1);      // 16-byte piece of this lane's four columns
-        const int ra = r + 16 * n + 4 * half + (tr >> 2), rb = ra + 8;
-        const u32x2 va = read_column(lv + ra * (2 * DP) + 16 * (c ^ place_v<DP>(ra)) + 8 * (tr & 1));
-        const u32x2 vb = read_column(lv + rb * (2 * DP) + 16 * (c ^ place_v<DP>(rb)) + 8 * (tr & 1));
-        o[i] = Mfma<T>::mul(u32x4{va[0], va[1], vb[0], vb[1]}, pb, o[i]);
+        const u32x2 x = read_column(va[i] + (r + 16 * n) * (2 * DP));
+        const u32x2 y = read_column(va[i] + (r + 16 * n + 8) * (2 * DP));
+        o[i] = Mfma<T>::mul(u32x4{x[0], x[1], y[0], y[1]}, pb, o[i]);
       }
     }
   }
@@ -430,11 +447,12 @@ constexpr int kKeys = 64;              // keys of a tile
 // Many rows: 128 of them by four wavefronts that share tiles of 64 keys, the next tile on its way
 // while one is worked on.
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void k_attend(AttendArgs a, long long slots) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 2 : 1))) void k_attend(AttendArgs a,
+                                                                                               long long slots) {
   constexpr int BM = 128, ROW = DP * 2;                // bytes of a row in LDS
   constexpr int ROWS_PER_COPY = 512 / DP, COPIES = kKeys / ROWS_PER_COPY / 4;   // per wavefront
   constexpr int STAGES = DP <= 128 ? 2 : 1;
-  __shared__ __attribute__((aligned(1024))) uint8_t sk[STAGES][kKeys * ROW], sv[STAGES][kKeys * ROW];
+  __shared__ __attribute__((aligned(1024))) uint8_t kv[STAGES][2][kKeys * ROW];
 
   const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
   if (id >= slots * a.Hk) return;
@@ -459,7 +477,7 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a, long long slots) {
   const T* kp = static_cast<const T*>(a.K) + t.k0 * a.k_token + hk * a.k_head;
   const T* vp = static_cast<const T*>(a.V) + t.k0 * a.v_token + hk * a.v_head;
   auto copy_tile = [&](int j0, int stage) {
-    const u32 lk = lds_address(sk[stage]), lv = lds_address(sv[stage]);
+    const u32 lk = lds_address(kv[stage][0]), lv = lds_address(kv[stage][1]);
     const T *kt = kp + j0 * a.k_token, *vt = vp + j0 * a.v_token;
 #pragma unroll
     for (int i = 0; i < COPIES; ++i) {
@@ -468,6 +486,7 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a, long long slots) {
       copy_rows<T, DP, place_v<DP>>(vt, a.v_token, r, t.nk - j0, D, lv + c * 1024);
     }
   };
+  w.addresses(lds_address(kv[0][0]), lds_address(kv[0][1]));
   if (STAGES == 2 && end > 0) copy_tile(0, 0);
   for (int j0 = 0; j0 < end; j0 += kKeys) {
     const int stage = STAGES == 2 ? (j0 / kKeys) & 1 : 0;
@@ -479,15 +498,15 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a, long long slots) {
     __syncthreads();
     if (STAGES == 2 && j0 + kKeys < end) copy_tile(j0 + kKeys, stage ^ 1);
     if (j0 < last) {
-      const u32 lk = lds_address(sk[stage]), lv = lds_address(sv[stage]);
       f32x16 s[2];
       u32 p[2][8];
-      s[0] = w.scores(lk, 0);
-      s[1] = w.scores(lk, 32);
+      s[0] = w.scores(0);
+      s[1] = w.scores(32);
       w.softmax(s, p, a.scale_log2, j0, sees, j0 + kKeys > all);
-      w.values(lv, 0, p[0]);
-      w.values(lv, 32, p[1]);
+      w.values(0, p[0]);
+      w.values(32, p[1]);
     }
+    if (STAGES == 2) w.move(stage ? -(int)sizeof(kv[0]) : (int)sizeof(kv[0]));
   }
 
   const float l = w.l + other_half(w.l);
@@ -524,7 +543,8 @@ struct FewShared {
 };
 
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void k_attend_few(AttendArgs a, long long slots) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 2 : 1))) void k_attend_few(
+    AttendArgs a, long long slots) {
   constexpr int ROWS_PER_COPY = 512 / DP, COPIES = kFewKeys / ROWS_PER_COPY;
   __shared__ __attribute__((aligned(1024))) FewShared<DP> sh;
 
@@ -563,6 +583,7 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a, long long slot
     for (int c = 0; c < COPIES; ++c)
       copy_rows<T, DP, place_v<DP>>(vt, a.v_token, c * ROWS_PER_COPY, t.nk - i * kFewKeys, D, lv + c * 1024);
   };
+  w.addresses(lk, lv);
   int i = split * share + wave;
   if (i < stop) {
     copy_k(i);
@@ -574,13 +595,13 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a, long long slot
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
     f32x16 s[1];
     u32 p[1][8];
-    s[0] = w.scores(lk, 0);
+    s[0] = w.scores(0);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // K has been read
     if (more) copy_k(i + 4);
     w.softmax(s, p, a.scale_log2, i * kFewKeys, sees, (i + 1) * kFewKeys > all);
     if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
     else wait_copies();
-    w.values(lv, 0, p[0]);
+    w.values(0, p[0]);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // V has been read
     if (more) copy_v(i + 4);
   }
