@@ -339,7 +339,14 @@ struct Rows {
 #pragma unroll
       for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) o[i][j] *= keep;
+        for (int j = 0; j < 16; ++j) {
+          // (in place: from an ordinary product the compiler makes a copy of all of O in every
+          // pass, 64 moves.  What it reads was written by matrix instructions before those of the
+          // scores, which the condition has waited for.)
+          float e = o[i][j];
+          asm volatile("v_mul_f32 %0, %1, %0" : "+v"(e) : "v"(keep));
+          o[i][j] = e;
+        }
     }
     const float base = m == -INFINITY ? 0.f : -m * c;
     float sum = 0.f;
@@ -442,6 +449,30 @@ __device__ __forceinline__ void copy_rows(const T* first, long long token, int r
   copy_to_lds(row < left && 8 * piece < D ? (const void*)p : (const void*)kZeros, lds);
 }
 
+// The same for whole tiles, of N copies one after the other: offsets of this lane from the first
+// row, so that a copy costs no vector instruction.
+template <int DP, int N, int PLACE(int)>
+struct CopyOffsets {
+  u32 off[N];
+  __device__ __forceinline__ CopyOffsets(long long token, int r) {
+    constexpr int PIECES = DP / 8, ROWS = 64 / PIECES;
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int row = r + i * ROWS + lane / PIECES;
+      off[i] = (u32)(row * token * 2) + 16 * ((lane % PIECES) ^ PLACE(row));
+    }
+  }
+  __device__ __forceinline__ void copy(const void* first, u32 lds) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) copy_to_lds(first, off[i], lds + 1024 * i);
+  }
+};
+// Whether rows of a tile are within 32-bit offsets, and as long as in LDS.
+__device__ __forceinline__ bool whole_rows(const AttendArgs& a, int DP) {
+  return a.D == DP && a.k_token >= 0 && a.v_token >= 0 && a.k_token < 1 << 24 && a.v_token < 1 << 24;
+}
+
 constexpr int kKeys = 64;              // keys of a tile
 
 // Many rows: 128 of them by four wavefronts that share tiles of 64 keys, the next tile on its way
@@ -476,9 +507,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   w.start(static_cast<const T*>(a.Q) + (t.q0 + token) * a.q_token + head * a.q_head, D, a.flip);
   const T* kp = static_cast<const T*>(a.K) + t.k0 * a.k_token + hk * a.k_head;
   const T* vp = static_cast<const T*>(a.V) + t.k0 * a.v_token + hk * a.v_head;
+  const bool quick = whole_rows(a, DP);
+  const CopyOffsets<DP, COPIES, place_k<DP>> ko(a.k_token, wave * COPIES * ROWS_PER_COPY);
+  const CopyOffsets<DP, COPIES, place_v<DP>> vo(a.v_token, wave * COPIES * ROWS_PER_COPY);
   auto copy_tile = [&](int j0, int stage) {
     const u32 lk = lds_address(kv[stage][0]), lv = lds_address(kv[stage][1]);
     const T *kt = kp + j0 * a.k_token, *vt = vp + j0 * a.v_token;
+    if (quick && j0 + kKeys <= t.nk) {
+      ko.copy(kt, lk + wave * COPIES * 1024);
+      vo.copy(vt, lv + wave * COPIES * 1024);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < COPIES; ++i) {
       const int c = wave * COPIES + i, r = c * ROWS_PER_COPY;
@@ -571,14 +610,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   const T* kp = static_cast<const T*>(a.K) + t.k0 * a.k_token + hk * a.k_head;
   const T* vp = static_cast<const T*>(a.V) + t.k0 * a.v_token + hk * a.v_head;
   const u32 lk = lds_address(sh.kv[wave][0]), lv = lds_address(sh.kv[wave][1]);
+  const bool quick = whole_rows(a, DP);
+  const CopyOffsets<DP, COPIES, place_k<DP>> ko(a.k_token, 0);
+  const CopyOffsets<DP, COPIES, place_v<DP>> vo(a.v_token, 0);
   auto copy_k = [&](int i) {
     const T* kt = kp + (long long)i * kFewKeys * a.k_token;
+    if (quick && (i + 1) * kFewKeys <= t.nk) return ko.copy(kt, lk);
 #pragma unroll
     for (int c = 0; c < COPIES; ++c)
       copy_rows<T, DP, place_k<DP>>(kt, a.k_token, c * ROWS_PER_COPY, t.nk - i * kFewKeys, D, lk + c * 1024);
   };
   auto copy_v = [&](int i) {
     const T* vt = vp + (long long)i * kFewKeys * a.v_token;
+    if (quick && (i + 1) * kFewKeys <= t.nk) return vo.copy(vt, lv);
 #pragma unroll
     for (int c = 0; c < COPIES; ++c)
       copy_rows<T, DP, place_v<DP>>(vt, a.v_token, c * ROWS_PER_COPY, t.nk - i * kFewKeys, D, lv + c * 1024);
