@@ -57,8 +57,11 @@ __global__ __launch_bounds__(kRotateThreads) void k_norm_rotate(RotateArgs a, in
   const bool mine = 8 * sub < D, turned = 8 * sub < R;
   // 8 elements of a lane: neighbours, or 4 of the first half of the turned ones and their partners
   const int e0 = PAIRS || !turned ? 8 * sub : 4 * sub, e1 = PAIRS || !turned ? e0 + 4 : P + 4 * sub;
-  for (int i = threadIdx.x / L; i < here * heads; i += kRotateThreads / L) {
-    const int t = i / heads, hh = i - t * heads, which = hh >= a.heads[0], h = which ? hh - a.heads[0] : hh;
+  const int first = threadIdx.x / L;
+  // (token and head of the i-th item; the quotient of small numbers by a reciprocal just above 1 / heads)
+  const float per = 1.0f / (float)heads * 1.000001f;
+  for (int i = first; i < here * heads; i += kRotateThreads / L) {
+    const int t = (int)((float)i * per), hh = i - t * heads, which = hh >= a.heads[0], h = which ? hh - a.heads[0] : hh;
     const T* src = static_cast<const T*>(a.in[which]) + (t0 + t) * a.in_token[which] + h * a.in_head[which];
     T* dst = static_cast<T*>(a.out[which]) + (t0 + t) * a.out_token[which] + h * a.out_head[which];
     const float* w = a.weight[which];
@@ -707,37 +710,70 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   }
 }
 
-// Joins the splits' parts, four outputs a thread, a workgroup for the 32 rows of a tile.
+// Joins the splits' parts, a wavefront a row: its lanes take four outputs each of 256 / D' parts at a
+// time (D' the next power of two), their weights found before, so that all parts are on their way
+// at once.
+constexpr int kMaxSplits = 128;
 template <typename T>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, long long slots) {
+  __shared__ float weight[4][kMaxSplits];
   const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
   if (id >= slots * a.Hk) return;
   const int hk = (int)(id % a.Hk);
   const Tile t = find_tile<kFewRows>(a, id / a.Hk);
   if (t.none()) return;
-  const int here = (int)(t.rows - t.r0 < kFewRows ? t.rows - t.r0 : kFewRows), quads = a.D / 4;
-  for (int e = threadIdx.x; e < here * quads; e += 256) {
-    const int r = e / quads, c = 4 * (e - r * quads);
+  const int here = (int)(t.rows - t.r0 < kFewRows ? t.rows - t.r0 : kFewRows);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int quads = a.D <= 32 ? 8 : a.D <= 64 ? 16 : a.D <= 128 ? 32 : 64;
+  const int c = 4 * (lane & (quads - 1)), group = lane / quads, groups = 64 / quads;
+  for (int r = wave; r < here; r += 4) {
     const long long rr = t.r0 + r;
     const int tok = (int)(rr / a.group), h = hk * a.group + (int)(rr - (long long)tok * a.group);
     const long long at = (t.q0 + (long long)tok) * a.Hq + h;
     const float* ml = a.part_ml + 2 * at * a.splits;
-    const float* po = a.part_o + at * a.splits * a.D + c;
-    float m = -INFINITY, l = 0.f;
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[2 * s]);
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) {
-      const float ms = ml[2 * s];
-      if (ms == -INFINITY) continue;                     // (a part without keys)
-      const float f = __builtin_amdgcn_exp2f((ms - m) * a.scale_log2);
-      l = fmaf(ml[2 * s + 1], f, l);
-      y += *reinterpret_cast<const f32x4*>(po + (long long)s * a.D) * f;
+    float ms[kMaxSplits / 64], m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < kMaxSplits / 64; ++i) {
+      const int s = lane + 64 * i;
+      ms[i] = s < a.splits ? ml[2 * s] : -INFINITY;
+      m = fmaxf(m, ms[i]);
     }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+#pragma unroll
+    for (int i = 0; i < kMaxSplits / 64; ++i) {
+      const int s = lane + 64 * i;
+      // (a part without keys has a maximum of -inf, no sum and no output)
+      const float f = ms[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ms[i] - m) * a.scale_log2);
+      if (s < a.splits) {
+        weight[wave][s] = f;
+        if (f != 0.f) l = fmaf(ml[2 * s + 1], f, l);
+      }
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
+    __builtin_amdgcn_wave_barrier();
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    if (c < a.D) {
+      const float* po = a.part_o + at * a.splits * a.D + c;
+#pragma unroll 8
+      for (int s = group; s < a.splits; s += groups) {
+        const float f = weight[wave][s];
+        // (what a part without keys left in memory may be anything)
+        if (f != 0.f) y += *reinterpret_cast<const f32x4*>(po + (long long)s * a.D) * f;
+      }
+    }
+    for (int d = 32; d >= quads; d >>= 1)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] += __shfl_xor(y[i], d, 64);
     const float inv = m == -INFINITY ? 0.f : 1.0f / l;
-    const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
-    store_floats<T, 4>(static_cast<T*>(a.O) + (t.q0 + tok) * a.o_token + h * a.o_head + c, z);
-    if (a.lse && c == 0)
-      a.lse[at] = m == -INFINITY ? -INFINITY : fmaf(m, a.scale_log2, __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+    if (group == 0 && c < a.D) {
+      const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
+      store_floats<T, 4>(static_cast<T*>(a.O) + (t.q0 + tok) * a.o_token + h * a.o_head + c, z);
+      if (a.lse && lane == 0)
+        a.lse[at] = m == -INFINITY ? -INFINITY : fmaf(m, a.scale_log2, __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+    }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -756,7 +792,7 @@ static AttendPlan attend_plan(long long Tq, long long Tk, int S, int Hq, int Hk)
   const long long most = Tk / S / 256, base = (long long)S * Hk;
   long long n = 2048 / base;
   if (n > most) n = most;
-  if (n > 128) n = 128;
+  if (n > kMaxSplits) n = kMaxSplits;
   if (n > 1) p.splits = (int)n;
   return p;
 }

@@ -8,7 +8,6 @@ library is missing — there is no fallback.
 from __future__ import annotations
 
 import ctypes as C
-import math
 import os
 from typing import Optional, Tuple
 
@@ -128,7 +127,7 @@ def lib() -> C.CDLL:
                                         vp, vp, vp, vp]
     L.tdq_probe.restype = C.c_int
     L.tdq_probe.argtypes = [C.c_int32, vp, sz, C.c_int32, C.c_int32, vp]
-    hp, f32 = C.POINTER(Heads), C.c_float
+    hp, f32 = vp, C.c_float                  # (hp: const tdq_heads*)
     L.tdq_quantize_act_f8.restype = C.c_int
     L.tdq_quantize_act_f8.argtypes = [vp, C.c_int, i64, i32, i64, vp, i64, vp, i64, vp]
     L.tdq_quantize_weight_f8.restype = C.c_int
@@ -613,70 +612,76 @@ MAX_HEAD = 256              # TDQ_MAX_HEAD
 _WIDE_DTYPES = {torch.float16: TDQ_F16, torch.float32: TDQ_F32, torch.bfloat16: TDQ_BF16}
 
 
-def _wdt(t: torch.Tensor) -> int:
-    dt = _WIDE_DTYPES.get(t.dtype)
+# A call of a small kernel takes the GPU 5 us, and every look at a tensor costs the host 0.1 to 0.2: the checks below
+# look at each shape, stride and type once.
+def _wdt(dtype) -> int:
+    dt = _WIDE_DTYPES.get(dtype)
     if dt is None:
-        raise TypeError(f"unsupported dtype {t.dtype}")
+        raise TypeError(f"unsupported dtype {dtype}")
     return dt
 
 
-def _expect(t: Optional[torch.Tensor], dtype, name: str) -> None:
-    if t is not None and t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+def _wrong_type(name: str, t: torch.Tensor, dtype) -> TypeError:
+    return TypeError(f"{name} must be {dtype}, not {t.dtype}")
 
 
 def _matrix(X: torch.Tensor, name: str) -> Tuple[int, int, int]:
     """(rows, columns, leading dimension) of [R, C], or of [B, T, C] with a uniform row stride."""
-    if X.dim() == 3:
+    shape = X.shape
+    if len(shape) == 3:
         B, T, Cc, ld = _btc(X)
         return B * T, Cc, ld
-    if X.dim() != 2 or (X.shape[1] > 1 and X.stride(1) != 1):
+    if len(shape) != 2:
+        raise ValueError(f"{name} must be a matrix with contiguous rows")
+    R, Cc = shape
+    ld, step = X.stride()
+    if step != 1 and Cc > 1:
         raise ValueError(f"{name} must be a matrix with contiguous rows")
     # the stride of an axis of extent 1 addresses nothing
-    return X.shape[0], X.shape[1], X.stride(0) if X.shape[0] > 1 else max(X.shape[1], 1)
+    return R, Cc, ld if R > 1 else max(Cc, 1)
 
 
 def _rows_of(t: torch.Tensor, rows: int, cols: int, dtype, name: str) -> int:
     """Leading dimension of a matrix of `dtype` with at least rows x cols elements."""
-    _expect(t, dtype, name)
-    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] < cols or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must be [{rows}, {cols}] or larger, with contiguous rows")
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+    if t.dtype is not dtype:
+        raise _wrong_type(name, t, dtype)
+    shape = t.shape
+    if len(shape) != 2 or shape[0] < rows or shape[1] < cols:
+        raise ValueError(f"{name} must be [{rows}, {cols}] or larger")
+    ld, step = t.stride()
+    if step != 1 and shape[1] > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return ld if shape[0] > 1 else max(shape[1], ld)
 
 
 def f8_row_bytes(K: int) -> int:
     """Leading dimension of the e4m3 codes of K channels."""
-    return 16 * ((K + 15) // 16)
+    return (K + 15) & ~15
 
 
-def _f8_out(rows: int, step_rows: int, K: int, device, out):
-    KB = (K + BLOCK_F8 - 1) // BLOCK_F8
+def _quantize_f8(X: torch.Tensor, high: int, out, where: str):
+    R, K, ld = _matrix(X, "X")
+    RB, KB, row = (R + high - 1) // high, (K + BLOCK_F8 - 1) // BLOCK_F8, (K + 15) & ~15
     if out is None:
-        out = (torch.empty((rows, f8_row_bytes(K)), dtype=torch.uint8, device=device),
-               torch.empty((step_rows, KB), dtype=torch.float32, device=device))
+        out = (torch.empty((R, row), dtype=torch.uint8, device=X.device),
+               torch.empty((RB, KB), dtype=torch.float32, device=X.device))
     Q, step = out
-    return Q, step, _rows_of(Q, rows, f8_row_bytes(K), torch.uint8, "codes"), _rows_of(step, step_rows, KB,
-                                                                                   torch.float32, "step")
+    ld_q, ld_s = _rows_of(Q, R, row, torch.uint8, "codes"), _rows_of(step, RB, KB, torch.float32, "step")
+    rc = getattr(_lib or lib(), where)(X.data_ptr(), _wdt(X.dtype), R, K, ld, Q.data_ptr(), ld_q, step.data_ptr(),
+                                       ld_s, _stream())
+    if rc:
+        raise TdqError(rc, where)
+    return Q, step
 
 
 def tdq_quantize_act_f8(X: torch.Tensor, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
     """X[M, K] or [B, T, K] -> (codes[M, 16 ceil(K/16)] uint8 (e4m3), step[M, ceil(K/128)] f32)."""
-    M, K, ld = _matrix(X, "X")
-    Q, step, ld_q, ld_s = _f8_out(M, M, K, X.device, out)
-    rc = lib().tdq_quantize_act_f8(X.data_ptr(), _wdt(X), M, K, ld, Q.data_ptr(), ld_q, step.data_ptr(), ld_s,
-                                   _stream())
-    _check(rc, "tdq_quantize_act_f8")
-    return Q, step
+    return _quantize_f8(X, 1, out, "tdq_quantize_act_f8")
 
 
 def tdq_quantize_weight_f8(W: torch.Tensor, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
     """W[N, K] -> (codes[N, 16 ceil(K/16)] uint8 (e4m3), step[ceil(N/128), ceil(K/128)] f32)."""
-    N, K, ld = _matrix(W, "W")
-    Q, step, ld_q, ld_s = _f8_out(N, (N + BLOCK_F8 - 1) // BLOCK_F8, K, W.device, out)
-    rc = lib().tdq_quantize_weight_f8(W.data_ptr(), _wdt(W), N, K, ld, Q.data_ptr(), ld_q, step.data_ptr(), ld_s,
-                                      _stream())
-    _check(rc, "tdq_quantize_weight_f8")
-    return Q, step
+    return _quantize_f8(W, BLOCK_F8, out, "tdq_quantize_weight_f8")
 
 
 def tdq_linear_f8(Qx: torch.Tensor, x_step: torch.Tensor, K: int, Qw: torch.Tensor, w_step: torch.Tensor,
@@ -686,22 +691,33 @@ def tdq_linear_f8(Qx: torch.Tensor, x_step: torch.Tensor, K: int, Qw: torch.Tens
     M, N, KB = Qx.shape[0], Qw.shape[0], (K + BLOCK_F8 - 1) // BLOCK_F8
     if out is None:
         out = torch.empty((M, N), dtype=out_dtype, device=Qx.device)
-    if bias is not None and (bias.dtype != torch.float32 or bias.shape != (N,) or not bias.is_contiguous()):
+    if bias is not None and (bias.dtype is not torch.float32 or bias.shape != (N,) or not bias.is_contiguous()):
         raise ValueError("bias must be contiguous float32 [N]")
-    rc = lib().tdq_linear_f8(Qx.data_ptr(), _rows_of(Qx, M, K, torch.uint8, "Qx"), x_step.data_ptr(),
-                             _rows_of(x_step, M, KB, torch.float32, "x_step"), M, K, N, Qw.data_ptr(),
-                             _rows_of(Qw, N, K, torch.uint8, "Qw"), w_step.data_ptr(),
-                             _rows_of(w_step, (N + BLOCK_F8 - 1) // BLOCK_F8, KB, torch.float32, "w_step"), _ptr(bias),
-                             out.data_ptr(), _wdt(out), _rows_of(out, M, N, out.dtype, "out"), _stream())
-    _check(rc, "tdq_linear_f8")
+    y = out.dtype
+    rc = (_lib or lib()).tdq_linear_f8(
+        Qx.data_ptr(), _rows_of(Qx, M, K, torch.uint8, "Qx"), x_step.data_ptr(),
+        _rows_of(x_step, M, KB, torch.float32, "x_step"), M, K, N, Qw.data_ptr(),
+        _rows_of(Qw, N, K, torch.uint8, "Qw"), w_step.data_ptr(),
+        _rows_of(w_step, (N + BLOCK_F8 - 1) // BLOCK_F8, KB, torch.float32, "w_step"),
+        None if bias is None else bias.data_ptr(), out.data_ptr(), _wdt(y), _rows_of(out, M, N, y, "out"), _stream())
+    if rc:
+        raise TdqError(rc, "tdq_linear_f8")
     return out
 
 
-def _heads(X: torch.Tensor, name: str) -> Heads:
-    if X.dim() != 3 or (X.shape[2] > 1 and X.stride(2) != 1):
+_HEADS_BYTES = C.sizeof(Heads)
+_FourHeads = C.c_int64 * 12     # four of tdq_heads one after the other
+
+
+def _strides(X: torch.Tensor, name: str) -> Tuple[int, int]:
+    """Token and head strides of [tokens, heads, D]."""
+    s = X.stride()
+    if len(s) != 3 or (s[2] != 1 and X.shape[2] > 1):
         raise ValueError(f"{name} must be [tokens, heads, D] with contiguous heads")
-    # (the stride of an axis of extent 1 addresses nothing; torch may report any value for it)
-    return Heads(X.data_ptr(), X.stride(0) if X.shape[0] > 1 else 0, X.stride(1) if X.shape[1] > 1 else 0)
+    if (s[0] | s[1]) & 7:
+        # (the stride of an axis of extent 1 addresses nothing; torch may report any value for it)
+        return s[0] if X.shape[0] > 1 else 0, s[1] if X.shape[1] > 1 else 0
+    return s[0], s[1]
 
 
 def tdq_norm_rotate(Q: torch.Tensor, K: Optional[torch.Tensor], pos: Optional[torch.Tensor],
@@ -710,39 +726,65 @@ def tdq_norm_rotate(Q: torch.Tensor, K: Optional[torch.Tensor], pos: Optional[to
                     axis: Optional[torch.Tensor] = None, interleaved: bool = False, out=None):
     """Q[T, Hq, D], K[T, Hk, D] or None -> (Qo, Ko): heads normed (where a weight is given) and turned by
     pos[axes, T] (or [T]) * freq[R/2].  out = (Q, K) works in place."""
-    T, Hq, D = Q.shape
-    Hk = 0 if K is None else K.shape[1]
-    if K is not None and (K.shape[0] != T or K.shape[2] != D or K.dtype != Q.dtype):
+    q_shape, dtype = Q.shape, Q.dtype
+    T, Hq, D = q_shape
+    k_shape = None if K is None else K.shape
+    Hk = 0 if K is None else k_shape[1]
+    if K is not None and (k_shape[0] != T or k_shape[2] != D or K.dtype is not dtype):
         raise ValueError("K must have Q's tokens, head size and type")
-    R, axes, ld_pos = 0, 1, 0
-    if freq is not None and freq.numel() > 0:
-        _expect(freq, torch.float32, "freq")
-        _expect(pos, torch.int32, "pos")
-        _expect(axis, torch.int32, "axis")
-        R = 2 * freq.numel()
-        if pos is None or pos.shape[-1] != T or pos.dim() not in (1, 2) or (T > 1 and pos.stride(-1) != 1):
+    R, axes, ld_pos, p_pos, p_axis, p_freq = 0, 1, 0, None, None, None
+    P = 0 if freq is None else freq.numel()
+    if P > 0:
+        if freq.dtype is not torch.float32:
+            raise _wrong_type("freq", freq, torch.float32)
+        if pos is None:
+            raise ValueError("pos must be [T] or [axes, T]")
+        if pos.dtype is not torch.int32:
+            raise _wrong_type("pos", pos, torch.int32)
+        R, n, at = 2 * P, pos.shape, pos.stride()
+        if len(n) not in (1, 2) or n[-1] != T or (T > 1 and at[-1] != 1):
             raise ValueError("pos must be [T] or [axes, T] with contiguous rows")
-        axes = pos.shape[0] if pos.dim() == 2 else 1
-        ld_pos = pos.stride(0) if axes > 1 else T
-        if axis is not None and axis.numel() != freq.numel():
-            raise ValueError("axis must name an axis for each of freq")
-        if not freq.is_contiguous() or (axis is not None and not axis.is_contiguous()):
-            raise ValueError("freq and axis must be contiguous")
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None and (w.dtype != torch.float32 or w.numel() != D or not w.is_contiguous()):
-            raise ValueError(f"{name} must be contiguous float32 [D]")
+        axes = n[0] if len(n) == 2 else 1
+        ld_pos = at[0] if axes > 1 else T
+        if not freq.is_contiguous():
+            raise ValueError("freq must be contiguous")
+        p_pos, p_freq = pos.data_ptr(), freq.data_ptr()
+        if axis is not None:
+            if axis.dtype is not torch.int32:
+                raise _wrong_type("axis", axis, torch.int32)
+            if axis.numel() != P or not axis.is_contiguous():
+                raise ValueError("axis must be contiguous and name an axis for each of freq")
+            p_axis = axis.data_ptr()
+    p_wq = p_wk = None
+    if q_weight is not None:
+        if q_weight.dtype is not torch.float32 or q_weight.numel() != D or not q_weight.is_contiguous():
+            raise ValueError("q_weight must be contiguous float32 [D]")
+        p_wq = q_weight.data_ptr()
+    if k_weight is not None:
+        if k_weight.dtype is not torch.float32 or k_weight.numel() != D or not k_weight.is_contiguous():
+            raise ValueError("k_weight must be contiguous float32 [D]")
+        p_wk = k_weight.data_ptr()
     if out is None:
-        out = (torch.empty((T, Hq, D), dtype=Q.dtype, device=Q.device),
-               None if K is None else torch.empty((T, Hk, D), dtype=K.dtype, device=K.device))
+        out = (torch.empty(q_shape, dtype=dtype, device=Q.device),
+               None if K is None else torch.empty(k_shape, dtype=dtype, device=K.device))
     Qo, Ko = out
-    if Qo.shape != Q.shape or Qo.dtype != Q.dtype or (K is not None and (Ko.shape != K.shape or Ko.dtype != K.dtype)):
+    if Qo.shape != q_shape or Qo.dtype is not dtype:
         raise ValueError("out must have the shapes and types of Q and K")
-    kin, kout = (None, None) if K is None else (C.byref(_heads(K, "K")), C.byref(_heads(Ko, "out K")))
-    rc = lib().tdq_norm_rotate(C.byref(_heads(Q, "Q")), kin, _wdt(Q), T, Hq, Hk, D, _ptr(q_weight), _ptr(k_weight),
-                               eps, R, int(interleaved), _ptr(pos), ld_pos, axes, _ptr(axis), _ptr(freq),
-                               C.byref(_heads(Qo, "out Q")), kout, _stream())
-    _check(rc, "tdq_norm_rotate")
-    return Qo, Ko
+    if K is None:
+        h = _FourHeads(Q.data_ptr(), *_strides(Q, "Q"), Qo.data_ptr(), *_strides(Qo, "out Q"))
+    else:
+        if Ko.shape != k_shape or Ko.dtype is not dtype:
+            raise ValueError("out must have the shapes and types of Q and K")
+        h = _FourHeads(Q.data_ptr(), *_strides(Q, "Q"), Qo.data_ptr(), *_strides(Qo, "out Q"), K.data_ptr(),
+                       *_strides(K, "K"), Ko.data_ptr(), *_strides(Ko, "out K"))
+    at = C.addressof(h)
+    kin, kout = (None, None) if K is None else (at + 2 * _HEADS_BYTES, at + 3 * _HEADS_BYTES)
+    rc = (_lib or lib()).tdq_norm_rotate(at, kin, _wdt(dtype), T, Hq, Hk, D, p_wq, p_wk, eps, R,
+                                         1 if interleaved else 0, p_pos, ld_pos, axes, p_axis, p_freq,
+                                         at + _HEADS_BYTES, kout, _stream())
+    if rc:
+        raise TdqError(rc, "tdq_norm_rotate")
+    return out
 
 
 def tdq_attention_workspace_bytes(Tq: int, Tk: int, S: int, Hq: int, Hk: int, D: int) -> int:
@@ -755,32 +797,41 @@ def tdq_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, cu_q: torch
                   workspace: Optional[torch.Tensor] = None):
     """Q[Tq, Hq, D], K and V[Tk, Hk, D], cu_q and cu_k[S + 1] int32 -> (O[Tq, Hq, D], lse[Tq, Hq] f32 or None).
     scale: 1 / sqrt(D) if None."""
-    Tq, Hq, D = Q.shape
-    Tk, Hk = K.shape[0], K.shape[1]
-    if K.shape != V.shape or K.shape[2] != D or K.dtype != Q.dtype or V.dtype != Q.dtype:
+    q_shape, k_shape, dtype = Q.shape, K.shape, Q.dtype
+    Tq, Hq, D = q_shape
+    Tk, Hk = k_shape[0], k_shape[1]
+    if V.shape != k_shape or k_shape[2] != D or K.dtype is not dtype or V.dtype is not dtype:
         raise ValueError("K and V must have the same shape, and Q's head size and type")
-    _expect(cu_q, torch.int32, "cu_q")
-    _expect(cu_k, torch.int32, "cu_k")
+    if cu_q.dtype is not torch.int32:
+        raise _wrong_type("cu_q", cu_q, torch.int32)
+    if cu_k.dtype is not torch.int32:
+        raise _wrong_type("cu_k", cu_k, torch.int32)
     S = cu_q.numel() - 1
     if cu_k.numel() != S + 1 or not cu_q.is_contiguous() or not cu_k.is_contiguous():
         raise ValueError("cu_q and cu_k must be contiguous, one longer than the number of sequences")
     if out is None:
-        out = torch.empty((Tq, Hq, D), dtype=Q.dtype, device=Q.device)
-    if out.shape != Q.shape or out.dtype != Q.dtype:
+        out = torch.empty(q_shape, dtype=dtype, device=Q.device)
+    elif out.shape != q_shape or out.dtype is not dtype:
         raise ValueError("out must have the shape and type of Q")
-    if lse is None and want_lse:
-        lse = torch.empty((Tq, Hq), dtype=torch.float32, device=Q.device)
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (Tq, Hq) or not lse.is_contiguous()):
+    if lse is None:
+        if want_lse:
+            lse = torch.empty((Tq, Hq), dtype=torch.float32, device=Q.device)
+    elif lse.dtype is not torch.float32 or lse.shape != (Tq, Hq) or not lse.is_contiguous():
         raise ValueError("lse must be contiguous float32 [Tq, Hq]")
+    L = _lib or lib()
     if workspace is None:
-        n = tdq_attention_workspace_bytes(Tq, Tk, S, Hq, Hk, D)
+        n = L.tdq_attention_workspace_bytes(Tq, Tk, S, Hq, Hk, D)
         workspace = torch.empty(n, dtype=torch.uint8, device=Q.device) if n else None
-    rc = lib().tdq_attention(C.byref(_heads(Q, "Q")), C.byref(_heads(K, "K")), C.byref(_heads(V, "V")), _wdt(Q), Tq,
-                             Tk, S, cu_q.data_ptr(), cu_k.data_ptr(), Hq, Hk, D,
-                             1.0 / math.sqrt(D) if scale is None else scale, int(causal),
-                             C.byref(_heads(out, "out")), _ptr(lse), _ptr(workspace),
-                             0 if workspace is None else workspace.numel(), _stream())
-    _check(rc, "tdq_attention")
+    p_work, n_work = (None, 0) if workspace is None else (workspace.data_ptr(),
+                                                          workspace.numel() * workspace.element_size())
+    h = _FourHeads(Q.data_ptr(), *_strides(Q, "Q"), K.data_ptr(), *_strides(K, "K"), V.data_ptr(), *_strides(V, "V"),
+                   out.data_ptr(), *_strides(out, "out"))
+    at = C.addressof(h)
+    rc = L.tdq_attention(at, at + _HEADS_BYTES, at + 2 * _HEADS_BYTES, _wdt(dtype), Tq, Tk, S, cu_q.data_ptr(),
+                         cu_k.data_ptr(), Hq, Hk, D, D ** -0.5 if scale is None else scale, 1 if causal else 0,
+                         at + 3 * _HEADS_BYTES, None if lse is None else lse.data_ptr(), p_work, n_work, _stream())
+    if rc:
+        raise TdqError(rc, "tdq_attention")
     return out, lse
 
 
