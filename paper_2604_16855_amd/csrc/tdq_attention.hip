@@ -40,6 +40,27 @@ __global__ __launch_bounds__(kRotateThreads) void k_norm_rotate(RotateArgs a, in
   const int P = a.R >> 1;
   const long long t0 = (long long)blockIdx.x * tokens;
   const int here = (int)(a.T - t0 < tokens ? a.T - t0 : tokens);
+  const int sub = threadIdx.x & (L - 1), heads = a.heads[0] + a.heads[1];
+  const int D = a.D, R = a.R;
+  const bool mine = 8 * sub < D, turned = 8 * sub < R;
+  // 8 elements of a lane: neighbours, or 4 of the first half of the turned ones and their partners
+  const int e0 = PAIRS || !turned ? 8 * sub : 4 * sub, e1 = PAIRS || !turned ? e0 + 4 : P + 4 * sub;
+  // token and head of an item: the quotient of small numbers by a reciprocal just above 1 / heads
+  const float per = 1.0f / (float)heads * 1.000001f;
+  struct Item {
+    float x[4], y[4];
+  };
+  auto load = [&](int i, Item& v) {
+    const int t = (int)((float)i * per), hh = i - t * heads, which = hh >= a.heads[0], h = which ? hh - a.heads[0] : hh;
+    const T* src = static_cast<const T*>(a.in[which]) + (t0 + t) * a.in_token[which] + h * a.in_head[which];
+    load_floats<T, 4>(src + e0, v.x);
+    load_floats<T, 4>(src + e1, v.y);
+  };
+  // The first items are on their way while the angles are computed, each next one while one is
+  // worked on.
+  const int first = threadIdx.x / L, items = here * heads;
+  Item next = {};
+  if (mine && first < items) load(first, next);
   for (int i = threadIdx.x; i < here * P; i += kRotateThreads) {
     const int t = i / P, p = i - t * P;
     int ax = a.axis ? a.axis[p] : 0;
@@ -52,24 +73,14 @@ __global__ __launch_bounds__(kRotateThreads) void k_norm_rotate(RotateArgs a, in
     turn[t][2 * p + 1] = s;
   }
   __syncthreads();
-  const int sub = threadIdx.x & (L - 1), heads = a.heads[0] + a.heads[1];
-  const int D = a.D, R = a.R;
-  const bool mine = 8 * sub < D, turned = 8 * sub < R;
-  // 8 elements of a lane: neighbours, or 4 of the first half of the turned ones and their partners
-  const int e0 = PAIRS || !turned ? 8 * sub : 4 * sub, e1 = PAIRS || !turned ? e0 + 4 : P + 4 * sub;
-  const int first = threadIdx.x / L;
-  // (token and head of the i-th item; the quotient of small numbers by a reciprocal just above 1 / heads)
-  const float per = 1.0f / (float)heads * 1.000001f;
-  for (int i = first; i < here * heads; i += kRotateThreads / L) {
+  for (int i = first; i < items; i += kRotateThreads / L) {
+    Item v = next;
+    if (mine && i + kRotateThreads / L < items) load(i + kRotateThreads / L, next);
+    float(&x)[4] = v.x;
+    float(&y)[4] = v.y;
     const int t = (int)((float)i * per), hh = i - t * heads, which = hh >= a.heads[0], h = which ? hh - a.heads[0] : hh;
-    const T* src = static_cast<const T*>(a.in[which]) + (t0 + t) * a.in_token[which] + h * a.in_head[which];
     T* dst = static_cast<T*>(a.out[which]) + (t0 + t) * a.out_token[which] + h * a.out_head[which];
     const float* w = a.weight[which];
-    float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
-    if (mine) {
-      load_floats<T, 4>(src + e0, x);
-      load_floats<T, 4>(src + e1, y);
-    }
     if (w) {
       float sum = 0.f;
 #pragma unroll
@@ -93,11 +104,11 @@ __global__ __launch_bounds__(kRotateThreads) void k_norm_rotate(RotateArgs a, in
       if constexpr (PAIRS) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const float p = x[2 * j], q = x[2 * j + 1], u = y[2 * j], v = y[2 * j + 1];
+          const float p = x[2 * j], q = x[2 * j + 1], u = y[2 * j], v2 = y[2 * j + 1];
           x[2 * j] = fmaf(p, z[2 * j], -(q * z[2 * j + 1]));
           x[2 * j + 1] = fmaf(q, z[2 * j], p * z[2 * j + 1]);
-          y[2 * j] = fmaf(u, z[4 + 2 * j], -(v * z[5 + 2 * j]));
-          y[2 * j + 1] = fmaf(v, z[4 + 2 * j], u * z[5 + 2 * j]);
+          y[2 * j] = fmaf(u, z[4 + 2 * j], -(v2 * z[5 + 2 * j]));
+          y[2 * j + 1] = fmaf(v2, z[4 + 2 * j], u * z[5 + 2 * j]);
         }
       } else {
 #pragma unroll
