@@ -186,3 +186,27 @@ def test_repeats_and_streams():
     torch.cuda.current_stream().wait_stream(s)
     for O, lse in got:
         assert torch.equal(O, want[0]) and torch.equal(lse, want[1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("ql,kl,Hq,Hk,D", [([130], [130], 2, 1, 64), ([70, 40], [200, 41], 4, 4, 128), ([7], [300], 4, 1, 128),
+                                           ([4, 3], [40, 1000], 8, 2, 32), ([90], [90], 1, 1, 200)])
+def test_keys_behind_the_causal_edge_may_be_anything(ql, kl, Hq, Hk, D, bad, dtype):
+    """The last queries of a sequence see its last keys, which are NaN (or give NaN scores): the queries before them
+    stay as they are, bit for bit."""
+    Q, K, V = _inputs(ql, kl, Hq, Hk, D, dtype)
+    cu_q, cu_k = L.starts(ql), L.starts(kl)
+    print(f"[attention] {bad} behind the edge {ql} {kl} D={D} {dtype}", flush=True)
+    want = tdq.tdq_attention(Q, K, V, cu_q, cu_k, want_lse=True)
+    K2, touched = K.clone(), torch.zeros(Q.shape[0], dtype=torch.bool, device="cuda")
+    for nq, q1, k1 in zip(ql, cu_q.tolist()[1:], cu_k.tolist()[1:]):
+        late = nq // 2
+        K2[k1 - late:k1, :, 0] = bad
+        K2[k1 - late:k1, :, 1] = -bad
+        touched[q1 - late:q1] = True
+    Q2 = Q.clone()
+    Q2[touched] = Q2[touched].abs()                          # (infinities of both signs: NaN)
+    O, lse = tdq.tdq_attention(Q2, K2, V, cu_q, cu_k, want_lse=True)
+    assert torch.equal(O[~touched], want[0][~touched]) and torch.equal(lse[~touched], want[1][~touched])
+    assert bool(O[touched].float().isnan().all())
