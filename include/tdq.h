@@ -484,7 +484,8 @@ int tdq_norm_rotate(const tdq_heads* Q, const tdq_heads* K, tdq_dtype dt, int64_
  *   O[t, h] = sum_j p_j V[j, h / g],  p = softmax_j(scale * Q[t, h] . K[j, h / g]),  g = Hq / Hk
  * over the keys j of t's sequence; sequence s has the queries cu_q[s] .. cu_q[s + 1] - 1 and the
  * keys cu_k[s] .. cu_k[s + 1] - 1 (device arrays of S + 1, ascending, within 0 .. Tq and 0 .. Tk;
- * what lies outside is cut off).  causal: the last query of a sequence sees all of its keys, the
+ * what lies outside is cut off).  len_k [S] (device) or NULL: of the keys of sequence s only the
+ * first len_k[s] are used, as in a cache that leaves every sequence room to grow.  causal: the last query of a sequence sees all of its keys, the
  * one before it all but the last, and so on.  A query that sees no key gets O = 0 and lse = -inf.
  * Keys that a query does not see do not matter, whatever they hold; what lies outside its sequence
  * neither, keys or values.  A value of its own sequence that is not finite may reach it, though it
@@ -500,8 +501,8 @@ int tdq_norm_rotate(const tdq_heads* Q, const tdq_heads* K, tdq_dtype dt, int64_
  */
 size_t tdq_attention_workspace_bytes(int64_t Tq, int64_t Tk, int32_t S, int32_t Hq, int32_t Hk, int32_t D);
 int tdq_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, tdq_dtype dt, int64_t Tq, int64_t Tk,
-                  int32_t S, const int32_t* cu_q, const int32_t* cu_k, int32_t Hq, int32_t Hk, int32_t D, float scale,
-                  int32_t causal, const tdq_heads* O, float* lse, void* workspace, size_t workspace_bytes,
+                  int32_t S, const int32_t* cu_q, const int32_t* cu_k, const int32_t* len_k, int32_t Hq, int32_t Hk,
+                  int32_t D, float scale, int32_t causal, const tdq_heads* O, float* lse, void* workspace, size_t workspace_bytes,
                   void* stream);
 
 #ifdef __cplusplus

@@ -973,8 +973,8 @@ size_t tdq_attention_workspace_bytes(int64_t Tq, int64_t Tk, int32_t S, int32_t 
 }
 
 int tdq_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, tdq_dtype dt, int64_t Tq, int64_t Tk,
-                  int32_t S, const int32_t* cu_q, const int32_t* cu_k, int32_t Hq, int32_t Hk, int32_t D, float scale,
-                  int32_t causal, const tdq_heads* O, float* lse, void* workspace, size_t workspace_bytes,
+                  int32_t S, const int32_t* cu_q, const int32_t* cu_k, const int32_t* len_k, int32_t Hq, int32_t Hk,
+                  int32_t D, float scale, int32_t causal, const tdq_heads* O, float* lse, void* workspace, size_t workspace_bytes,
                   void* stream) {
   if (!Q || !K || !V || !O || !cu_q || !cu_k || !Q->data || !O->data) return TDQ_ERR_NULL;
   if (Tk > 0 && (!K->data || !V->data)) return TDQ_ERR_NULL;
@@ -983,10 +983,10 @@ int tdq_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, td
   if (!isfinite(scale)) return TDQ_ERR_PARAM;
   for (const tdq_heads* t : {Q, K, V, O})
     if (misaligned(t->data, 16) || t->token % 8 || t->head % 8) return TDQ_ERR_ALIGN;
-  if (misaligned(cu_q, 4) || misaligned(cu_k, 4) || misaligned(lse, 4)) return TDQ_ERR_ALIGN;
+  if (misaligned(cu_q, 4) || misaligned(cu_k, 4) || misaligned(len_k, 4) || misaligned(lse, 4)) return TDQ_ERR_ALIGN;
   const size_t need = attention_workspace(Tq, Tk, S, Hq, Hk, D);
   if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 256))) return TDQ_ERR_WORKSPACE;
-  if (launch_attention(Q, K, V, dt, Tq, Tk, S, cu_q, cu_k, Hq, Hk, D, scale, causal != 0, O, lse, workspace,
+  if (launch_attention(Q, K, V, dt, Tq, Tk, S, cu_q, cu_k, len_k, Hq, Hk, D, scale, causal != 0, O, lse, workspace,
                        static_cast<hipStream_t>(stream)) != hipSuccess)
     return TDQ_ERR_HIP;
   return TDQ_OK;

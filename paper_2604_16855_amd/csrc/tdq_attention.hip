@@ -209,7 +209,7 @@ struct AttendArgs {
   const void *Q, *K, *V;
   void* O;
   float* lse;
-  const int *cu_q, *cu_k;
+  const int *cu_q, *cu_k, *len_k;      // (len_k: nullptr, or how many of a sequence's keys are used)
   long long q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;
   long long Tq, Tk;
   int S, Hq, Hk, group, D, causal;
@@ -446,6 +446,10 @@ __device__ __forceinline__ Tile find_tile(const AttendArgs& a, long long slot) {
   t.nq = clamp_start(a.cu_q, s.seq + 1, a.Tq) - t.q0;
   t.k0 = clamp_start(a.cu_k, s.seq, a.Tk);
   t.nk = clamp_start(a.cu_k, s.seq + 1, a.Tk) - t.k0;
+  if (a.len_k) {
+    const int used = a.len_k[s.seq];
+    t.nk = used < t.nk ? used : t.nk;
+  }
   t.nk = t.nk > 0 ? t.nk : 0;
   t.rows = t.nq > 0 ? (long long)t.nq * a.group : 0;
   t.r0 = (long long)s.tile * BM;
@@ -836,7 +840,7 @@ static void launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t 
 }
 
 hipError_t launch_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, tdq_dtype dt, long long Tq,
-                            long long Tk, int S, const int* cu_q, const int* cu_k, int Hq, int Hk, int D, float scale,
+                            long long Tk, int S, const int* cu_q, const int* cu_k, const int* len_k, int Hq, int Hk, int D, float scale,
                             bool causal, const tdq_heads* O, float* lse, void* workspace, hipStream_t st) {
   const AttendPlan p = attend_plan(Tq, Tk, S, Hq, Hk);
   AttendArgs a;
@@ -847,6 +851,7 @@ hipError_t launch_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_he
   a.lse = lse;
   a.cu_q = cu_q;
   a.cu_k = cu_k;
+  a.len_k = len_k;
   a.q_token = Q->token;
   a.q_head = Q->head;
   a.k_token = K->token;

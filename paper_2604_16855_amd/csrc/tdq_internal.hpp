@@ -247,7 +247,7 @@ hipError_t launch_norm_rotate(const tdq_heads* Q, const tdq_heads* K, tdq_dtype 
                               const tdq_heads* Qo, const tdq_heads* Ko, hipStream_t st);
 size_t attention_workspace(long long Tq, long long Tk, int S, int Hq, int Hk, int D);
 hipError_t launch_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, tdq_dtype dt, long long Tq,
-                            long long Tk, int S, const int* cu_q, const int* cu_k, int Hq, int Hk, int D, float scale,
+                            long long Tk, int S, const int* cu_q, const int* cu_k, const int* len_k, int Hq, int Hk, int D, float scale,
                             bool causal, const tdq_heads* O, float* lse, void* workspace, hipStream_t st);
 
 }  // namespace tdq

@@ -140,7 +140,7 @@ def lib() -> C.CDLL:
     L.tdq_attention_workspace_bytes.restype = sz
     L.tdq_attention_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32]
     L.tdq_attention.restype = C.c_int
-    L.tdq_attention.argtypes = [hp, hp, hp, C.c_int, i64, i64, i32, vp, vp, i32, i32, i32, f32, i32, hp, vp, vp,
+    L.tdq_attention.argtypes = [hp, hp, hp, C.c_int, i64, i64, i32, vp, vp, vp, i32, i32, i32, f32, i32, hp, vp, vp,
                                 sz, vp]
     L.tdq_quantize_weight.restype = C.c_int
     L.tdq_quantize_weight.argtypes = [vp, i32, i32, i64, vp, i64, vp, vp]
@@ -794,9 +794,9 @@ def tdq_attention_workspace_bytes(Tq: int, Tk: int, S: int, Hq: int, Hk: int, D:
 def tdq_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, cu_q: torch.Tensor, cu_k: torch.Tensor,
                   scale: Optional[float] = None, causal: bool = True, out: Optional[torch.Tensor] = None,
                   lse: Optional[torch.Tensor] = None, want_lse: bool = False,
-                  workspace: Optional[torch.Tensor] = None):
+                  workspace: Optional[torch.Tensor] = None, len_k: Optional[torch.Tensor] = None):
     """Q[Tq, Hq, D], K and V[Tk, Hk, D], cu_q and cu_k[S + 1] int32 -> (O[Tq, Hq, D], lse[Tq, Hq] f32 or None).
-    scale: 1 / sqrt(D) if None."""
+    scale: 1 / sqrt(D) if None.  len_k[S] int32: how many of a sequence's keys are used."""
     q_shape, k_shape, dtype = Q.shape, K.shape, Q.dtype
     Tq, Hq, D = q_shape
     Tk, Hk = k_shape[0], k_shape[1]
@@ -809,6 +809,11 @@ def tdq_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, cu_q: torch
     S = cu_q.numel() - 1
     if cu_k.numel() != S + 1 or not cu_q.is_contiguous() or not cu_k.is_contiguous():
         raise ValueError("cu_q and cu_k must be contiguous, one longer than the number of sequences")
+    if len_k is not None:
+        if len_k.dtype is not torch.int32:
+            raise _wrong_type("len_k", len_k, torch.int32)
+        if len_k.numel() != S or not len_k.is_contiguous():
+            raise ValueError("len_k must be contiguous, one for each sequence")
     if out is None:
         out = torch.empty(q_shape, dtype=dtype, device=Q.device)
     elif out.shape != q_shape or out.dtype is not dtype:
@@ -828,7 +833,7 @@ def tdq_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, cu_q: torch
                    out.data_ptr(), *_strides(out, "out"))
     at = C.addressof(h)
     rc = L.tdq_attention(at, at + _HEADS_BYTES, at + 2 * _HEADS_BYTES, _wdt(dtype), Tq, Tk, S, cu_q.data_ptr(),
-                         cu_k.data_ptr(), Hq, Hk, D, D ** -0.5 if scale is None else scale, 1 if causal else 0,
+                         cu_k.data_ptr(), None if len_k is None else len_k.data_ptr(), Hq, Hk, D, D ** -0.5 if scale is None else scale, 1 if causal else 0,
                          at + 3 * _HEADS_BYTES, None if lse is None else lse.data_ptr(), p_work, n_work, _stream())
     if rc:
         raise TdqError(rc, "tdq_attention")

@@ -80,7 +80,7 @@ def test_norm_rotate():
 
 def test_attention():
     L = tdq.lib()
-    ok = dict(Q=_h(), K=_h(), V=_h(), dt=0, Tq=10, Tk=20, S=2, cq=FAKE, ck=FAKE, Hq=4, Hk=2, D=64, scale=0.125,
+    ok = dict(Q=_h(), K=_h(), V=_h(), dt=0, Tq=10, Tk=20, S=2, cq=FAKE, ck=FAKE, lk=None, Hq=4, Hk=2, D=64, scale=0.125,
               causal=1, O=_h(), lse=None, ws=FAKE, wsb=1 << 40, st=None)
     call = _caller(L.tdq_attention, ok)
     for kw in (dict(Q=None), dict(K=None), dict(V=None), dict(O=None), dict(cq=None), dict(ck=None), dict(Q=_h(None)),
@@ -100,7 +100,7 @@ def test_attention():
     for k in ("Q", "K", "V", "O"):
         for bad in (_h(FAKE + 8), _h(token=260), _h(head=60)):
             assert call(**{k: bad}) == tdq.ERR_ALIGN
-    for kw in (dict(cq=FAKE + 2), dict(ck=FAKE + 2), dict(lse=FAKE + 2)):
+    for kw in (dict(cq=FAKE + 2), dict(ck=FAKE + 2), dict(lk=FAKE + 2), dict(lse=FAKE + 2)):
         assert call(**kw) == tdq.ERR_ALIGN, kw
 
 
@@ -111,7 +111,7 @@ def test_attention_workspace():
     need = L.tdq_attention_workspace_bytes(*shape)
     if need:
         for ws, n in ((None, need), (FAKE, need - 1), (FAKE + 128, need)):
-            assert L.tdq_attention(_h(), _h(), _h(), 0, 1, 100000, 1, FAKE, FAKE, 8, 8, 128, 0.1, 1, _h(), None, ws, n,
+            assert L.tdq_attention(_h(), _h(), _h(), 0, 1, 100000, 1, FAKE, FAKE, None, 8, 8, 128, 0.1, 1, _h(), None, ws, n,
                                    None) == tdq.ERR_WORKSPACE
 
 
@@ -152,3 +152,7 @@ def test_binding_refuses_what_does_not_fit():
         tdq.tdq_attention(x, x, x, c.long(), c)
     with pytest.raises(ValueError):
         tdq.tdq_attention(x, x, x, c, c, lse=t(5, 3, dt=torch.float32))
+    with pytest.raises(ValueError):
+        tdq.tdq_attention(x, x, x, c, c, len_k=t(2, dt=torch.int32))
+    with pytest.raises(TypeError):
+        tdq.tdq_attention(x, x, x, c, c, len_k=t(1, dt=torch.int64))

@@ -210,3 +210,24 @@ def test_keys_behind_the_causal_edge_may_be_anything(ql, kl, Hq, Hk, D, bad, dty
     O, lse = tdq.tdq_attention(Q2, K2, V, cu_q, cu_k, want_lse=True)
     assert torch.equal(O[~touched], want[0][~touched]) and torch.equal(lse[~touched], want[1][~touched])
     assert bool(O[touched].float().isnan().all())
+
+
+@pytest.mark.parametrize("nq", [1, 3, 40])
+def test_cache_with_room(nq):
+    """Sequences in equal rooms of a cache, of which the first few keys are used: the same as packed."""
+    S, room, Hq, Hk, D = 5, 700, 8, 2, 64
+    used = [700, 0, 1, 333, 64]
+    Q, K, V = _inputs([nq] * S, [room] * S, Hq, Hk, D, torch.bfloat16)
+    cu_q, cu_k = L.starts([nq] * S), L.starts([room] * S)
+    keep = torch.cat([torch.arange(s * room, s * room + n, device="cuda") for s, n in enumerate(used)])
+    want = L.attention(Q, K[keep], V[keep], [nq] * S, used, D ** -0.5, True)
+    rest = torch.ones(S * room, dtype=torch.bool, device="cuda")
+    rest[keep] = False
+    K[rest], V[rest] = float("nan"), float("inf")
+    n = torch.tensor(used, dtype=torch.int32, device="cuda")
+    L.check_attention(tdq.tdq_attention(Q, K, V, cu_q, cu_k, len_k=n, want_lse=True), want)
+    more = n + 10000                                         # more than there is room for: all of it; fewer than none: none
+    a = tdq.tdq_attention(Q, K, V, cu_q, cu_k, len_k=more)[0]
+    b = tdq.tdq_attention(Q, K, V, cu_q, cu_k)[0]
+    assert torch.equal(a.isnan(), b.isnan())
+    assert bool((tdq.tdq_attention(Q, K, V, cu_q, cu_k, len_k=-n - 1)[0] == 0).all())
