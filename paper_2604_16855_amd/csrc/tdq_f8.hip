@@ -411,6 +411,14 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_f8(
   static_assert(32 * (COLS + V) * sizeof(OUT) * WAVES <= sizeof(stage), "room for the results");
   OUT* out = reinterpret_cast<OUT*>(&stage[0][0]) + wave * 32 * (COLS + V);
   const int nw = n0 + wn * COLS;
+  float b[TN][16];                                     // (read once, for all of the wavefront's tokens)
+#pragma unroll
+  for (int u = 0; u < TN; ++u)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int n = nw + 32 * u + 8 * (i / 4) + 4 * fh + i % 4;
+      b[u][i] = bias && n < N ? bias[n] : 0.f;
+    }
 #pragma unroll
   for (int t = 0; t < TM; ++t) {
 #pragma unroll
@@ -420,10 +428,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_f8(
         const int c = 32 * u + 8 * q + 4 * fh;
         float y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          y[i] = acc[u][t][4 * q + i];
-          if (bias && nw + c + i < N) y[i] = y[i] + bias[nw + c + i];
-        }
+        for (int i = 0; i < 4; ++i) y[i] = bias ? acc[u][t][4 * q + i] + b[u][4 * q + i] : acc[u][t][4 * q + i];
         store_floats<OUT, 4>(out + fr * (COLS + V) + c, y);
       }
     __builtin_amdgcn_wave_barrier();
