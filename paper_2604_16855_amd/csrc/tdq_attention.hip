@@ -11,7 +11,8 @@ namespace tdq {
 // ---------------------------------------------------------------------------
 // y = x / sqrt(mean x^2 + eps) * w over a head's D elements, then pair p of the first R by the
 // angle pos[axis of p] * freq[p]:  (a, b) -> (a cos - b sin, b cos + a sin).
-// One pass: the rows are read and written once, bound by memory.  The angles of a token serve
+// One pass: the rows are read and written once, bound by memory (32768 tokens of 32 heads of 64,
+// binary16, in 60 us, 4.5 TB/s).  The angles of a token serve
 // all its heads, so a workgroup takes a few whole tokens and leaves their cosines and sines in
 // LDS.  The product pos * freq is rounded to binary32, as in the tables that models are trained
 // with; from there on the angle is exact: it is reduced as a fraction of a turn in binary64.
@@ -38,7 +39,8 @@ template <typename T, int L, bool PAIRS>
 __global__ __launch_bounds__(kRotateThreads) void k_norm_rotate(RotateArgs a, int tokens) {
   __shared__ float turn[kRotateTokens][kMaxHead];      // cosine and sine of each pair
   const int P = a.R >> 1;
-  const long long t0 = (long long)blockIdx.x * tokens;
+  const long long t0 = (blockIdx.x + (long long)blockIdx.y * gridDim.x) * tokens;
+  if (t0 >= a.T) return;                               // (a last row of workgroups may be longer than needed)
   const int here = (int)(a.T - t0 < tokens ? a.T - t0 : tokens);
   const int sub = threadIdx.x & (L - 1), heads = a.heads[0] + a.heads[1];
   const int D = a.D, R = a.R;
@@ -165,9 +167,9 @@ hipError_t launch_norm_rotate(const tdq_heads* Q, const tdq_heads* K, tdq_dtype 
   const RotateArgs a =
       rotate_args(Q, K, T, Hq, Hk, D, q_weight, k_weight, eps, R, pos, ld_pos, axes, axis, freq, Qo, Ko);
   const int tokens = T >= 1024 * kRotateTokens ? kRotateTokens : 1;
-  const unsigned grid = (unsigned)((T + tokens - 1) / tokens);
+  const dim3 grid = two_axes((T + tokens - 1) / tokens);
 #define TDQ_ROTATE_LP(T_, L, PAIRS) \
-  hipLaunchKernelGGL((k_norm_rotate<T_, L, PAIRS>), dim3(grid), dim3(kRotateThreads), 0, st, a, tokens)
+  hipLaunchKernelGGL((k_norm_rotate<T_, L, PAIRS>), grid, dim3(kRotateThreads), 0, st, a, tokens)
 #define TDQ_ROTATE_L(T_, L)                    \
   do {                                         \
     if (interleaved) TDQ_ROTATE_LP(T_, L, true); \
@@ -494,7 +496,8 @@ __device__ __forceinline__ bool whole_rows(const AttendArgs& a, int DP) {
 constexpr int kKeys = 64;              // keys of a tile
 
 // Many rows: 128 of them by four wavefronts that share tiles of 64 keys, the next tile on its way
-// while one is worked on.
+// while one is worked on.  Bound by the matrix and the vector unit (45 and 53 % of the cycles, hardly
+// at the same time): 8 causal prompts of up to 4096, 32/8 heads of 128, in 645 us, 910 TFLOP/s.
 template <typename T, int DP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 2 : 1))) void k_attend(AttendArgs a,
                                                                                                long long slots) {
@@ -588,7 +591,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
 // Few rows (single tokens over a cache): 32 of them, and it is the keys that are shared out, to
 // `splits` workgroups and in each to four wavefronts.  Bound by reading K and V once: a wavefront
 // copies its own tiles of 32 keys, K of the next while it works on V of this and the other way
-// round, and waits for nobody until the end, where the wavefronts' parts are joined in LDS.
+// round, and waits for nobody until the end, where the wavefronts' parts are joined in LDS.  16 tokens
+// over 4000 to 32000 keys, 32/8 heads of 128: 224 us, 5.3 TB/s (a wavefront of rows for all keys: 1354).
 constexpr int kFewRows = 32, kFewKeys = 32;
 template <int DP>
 struct FewShared {
@@ -820,11 +824,6 @@ size_t attention_workspace(long long Tq, long long Tk, int S, int Hq, int Hk, in
   const AttendPlan p = attend_plan(Tq, Tk, S, Hq, Hk);
   if (p.splits <= 1) return 0;
   return part_ml_bytes(Tq, Hq, p.splits) + (size_t)Tq * Hq * p.splits * D * sizeof(float);
-}
-
-static dim3 two_axes(long long n) {                      // an axis of a grid holds fewer than 2^32 threads
-  const long long axis = 1 << 22;
-  return dim3(n < axis ? (unsigned)n : (unsigned)axis, (unsigned)((n + axis - 1) / axis));
 }
 
 template <typename T, int DP>

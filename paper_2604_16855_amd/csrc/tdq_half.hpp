@@ -22,6 +22,12 @@ typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
 typedef u32 u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef u32 u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 
+// Grid of n workgroups: an axis holds fewer than 2^32 threads (workgroups past the last return).
+inline dim3 two_axes(long long n) {
+  const long long axis = 1 << 22;
+  return dim3(n < axis ? (unsigned)n : (unsigned)axis, (unsigned)((n + axis - 1) / axis));
+}
+
 // Two adjacent 16-bit elements as floats, and back (to nearest, ties to even).
 template <typename T>
 __device__ __forceinline__ f32x2 two_floats(u32 w);
