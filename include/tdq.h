@@ -486,7 +486,8 @@ int tdq_norm_rotate(const tdq_heads* Q, const tdq_heads* K, tdq_dtype dt, int64_
  * keys cu_k[s] .. cu_k[s + 1] - 1 (device arrays of S + 1, ascending, within 0 .. Tq and 0 .. Tk;
  * what lies outside is cut off).  len_k [S] (device) or NULL: of the keys of sequence s only the
  * first len_k[s] are used, as in a cache that leaves every sequence room to grow.  causal: the last query of a sequence sees all of its keys, the
- * one before it all but the last, and so on.  A query that sees no key gets O = 0 and lse = -inf.
+ * one before it all but the last, and so on.  A query that sees no key gets O = 0 and lse = -inf; one
+ * that is NaN, or sees a key that is, gets NaN in both.
  * Keys that a query does not see do not matter, whatever they hold; what lies outside its sequence
  * neither, keys or values.  A value of its own sequence that is not finite may reach it, though it
  * does not see it: the weight 0 times that value is NaN.

@@ -250,6 +250,14 @@ __device__ __forceinline__ float max_of_halves(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// Whether a row with maximum m and sum l has no key, or none with a score above -inf.  The maximum
+// alone does not say: it passes over NaN, which the sum does not.
+__device__ __forceinline__ bool no_weight(float m, float l) { return m == -INFINITY && l == 0.f; }
+// Log of the sum of exp(scale * score).
+__device__ __forceinline__ float log_sum(float m, float l, float scale_log2) {
+  return no_weight(m, l) ? -INFINITY : fmaf(m, scale_log2, __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+}
+
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 // Four elements down a column: 16 lanes give the addresses of 4 rows x 16 columns (a lane 4
 // columns of row lane / 4), lane i gets column i.
@@ -571,7 +579,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
 
   const float l = w.l + other_half(w.l);
   if (!real) return;
-  const float inv = w.m == -INFINITY ? 0.f : 1.0f / l;   // a row that sees no key: zeros, and -inf
+  const float inv = no_weight(w.m, l) ? 0.f : 1.0f / l;   // a row that sees no key: zeros, and -inf
   T* op = static_cast<T*>(a.O) + (t.q0 + token) * a.o_token + head * a.o_head;
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i)
@@ -583,9 +591,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
         store_floats<T, 4>(op + c, y);
       }
     }
-  if (a.lse && half == 0)
-    a.lse[(t.q0 + (long long)token) * a.Hq + head] =
-        w.m == -INFINITY ? -INFINITY : fmaf(w.m, a.scale_log2, __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+  if (a.lse && half == 0) a.lse[(t.q0 + (long long)token) * a.Hq + head] = log_sum(w.m, l, a.scale_log2);
 }
 
 // Few rows (single tokens over a cache): 32 of them, and it is the keys that are shared out, to
@@ -684,10 +690,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   for (int v = 0; v < 4; ++v) m = fmaxf(m, sh.ml[v][lane & 31][0]);
 #pragma unroll
   for (int v = 0; v < 4; ++v) {
-    const float mv = sh.ml[v][lane & 31][0];
-    if (mv != -INFINITY) sum += sh.ml[v][lane & 31][1] * __builtin_amdgcn_exp2f((mv - m) * a.scale_log2);
+    const float mv = sh.ml[v][lane & 31][0], lv = sh.ml[v][lane & 31][1];
+    if (!no_weight(mv, lv)) sum += lv * __builtin_amdgcn_exp2f((mv - m) * a.scale_log2);
   }
-  const float keep = w.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((w.m - m) * a.scale_log2);
+  const float keep = no_weight(w.m, l) ? 0.f : __builtin_amdgcn_exp2f((w.m - m) * a.scale_log2);
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
@@ -719,12 +725,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
         a.part_ml[2 * part + 1] = lr;
       }
     } else {
-      const float inv = mr == -INFINITY ? 0.f : 1.0f / lr;
+      const float inv = no_weight(mr, lr) ? 0.f : 1.0f / lr;
       const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
       store_floats<T, 4>(static_cast<T*>(a.O) + (t.q0 + tok) * a.o_token + h * a.o_head + c, z);
-      if (a.lse && c == 0)
-        a.lse[at] = mr == -INFINITY ? -INFINITY
-                                    : fmaf(mr, a.scale_log2, __builtin_amdgcn_logf(lr)) * 0.69314718055994530942f;
+      if (a.lse && c == 0) a.lse[at] = log_sum(mr, lr, a.scale_log2);
     }
   }
 }
@@ -750,11 +754,12 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, long long slo
     const int tok = (int)(rr / a.group), h = hk * a.group + (int)(rr - (long long)tok * a.group);
     const long long at = (t.q0 + (long long)tok) * a.Hq + h;
     const float* ml = a.part_ml + 2 * at * a.splits;
-    float ms[kMaxSplits / 64], m = -INFINITY, l = 0.f;
+    float ms[kMaxSplits / 64], ls[kMaxSplits / 64], m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int i = 0; i < kMaxSplits / 64; ++i) {
       const int s = lane + 64 * i;
       ms[i] = s < a.splits ? ml[2 * s] : -INFINITY;
+      ls[i] = s < a.splits ? ml[2 * s + 1] : 0.f;
       m = fmaxf(m, ms[i]);
     }
 #pragma unroll
@@ -762,11 +767,14 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, long long slo
 #pragma unroll
     for (int i = 0; i < kMaxSplits / 64; ++i) {
       const int s = lane + 64 * i;
-      // (a part without keys has a maximum of -inf, no sum and no output)
-      const float f = ms[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ms[i] - m) * a.scale_log2);
+      // (a part without keys has a maximum of -inf, no sum and no output; one of nothing but NaN has
+      // the same maximum, and its sum makes the row NaN)
+      const float f = no_weight(ms[i], ls[i]) ? 0.f
+                      : ls[i] != ls[i]        ? ls[i]
+                                              : __builtin_amdgcn_exp2f((ms[i] - m) * a.scale_log2);
       if (s < a.splits) {
         weight[wave][s] = f;
-        if (f != 0.f) l = fmaf(ml[2 * s + 1], f, l);
+        if (f != 0.f) l = fmaf(ls[i], f, l);
       }
     }
 #pragma unroll
@@ -785,12 +793,12 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, long long slo
     for (int d = 32; d >= quads; d >>= 1)
 #pragma unroll
       for (int i = 0; i < 4; ++i) y[i] += __shfl_xor(y[i], d, 64);
-    const float inv = m == -INFINITY ? 0.f : 1.0f / l;
+    const float inv = no_weight(m, l) ? 0.f : 1.0f / l;
     if (group == 0 && c < a.D) {
       const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
       store_floats<T, 4>(static_cast<T*>(a.O) + (t.q0 + tok) * a.o_token + h * a.o_head + c, z);
       if (a.lse && lane == 0)
-        a.lse[at] = m == -INFINITY ? -INFINITY : fmaf(m, a.scale_log2, __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+        a.lse[at] = log_sum(m, l, a.scale_log2);
     }
     __builtin_amdgcn_wave_barrier();
   }
