@@ -489,8 +489,8 @@ int tdq_norm_rotate(const tdq_heads* Q, const tdq_heads* K, tdq_dtype dt, int64_
  * one before it all but the last, and so on.  A query that sees no key gets O = 0 and lse = -inf; one
  * that is NaN, or sees a key that is, gets NaN in both.
  * Keys that a query does not see do not matter, whatever they hold; what lies outside its sequence
- * neither, keys or values.  A value of its own sequence that is not finite may reach it, though it
- * does not see it: the weight 0 times that value is NaN.
+ * neither, keys or values.  A value of its own sequence that is not finite may reach a query that
+ * sees other keys, though not this one: the weight 0 times that value is NaN.
  * lse [Tq, Hq] floats or NULL: log of the sum of exp(scale * score).
  * Scores, maxima, sums and O are held in binary32; the probabilities are rounded to the type of
  * V for the product with it.

@@ -579,7 +579,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
 
   const float l = w.l + other_half(w.l);
   if (!real) return;
-  const float inv = no_weight(w.m, l) ? 0.f : 1.0f / l;   // a row that sees no key: zeros, and -inf
+  // a row that sees no key: zeros, and -inf (its sums may hold 0 * NaN from values that others see)
+  const bool none = no_weight(w.m, l);
+  const float inv = 1.0f / l;
   T* op = static_cast<T*>(a.O) + (t.q0 + token) * a.o_token + head * a.o_head;
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i)
@@ -587,7 +589,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     for (int j = 0; j < 16; j += 4) {
       const int c = 32 * i + 2 * j + 4 * half;
       if (c < D) {
-        const float y[4] = {w.o[i][j] * inv, w.o[i][j + 1] * inv, w.o[i][j + 2] * inv, w.o[i][j + 3] * inv};
+        float y[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) y[u] = none ? 0.f : w.o[i][j + u] * inv;
         store_floats<T, 4>(op + c, y);
       }
     }
@@ -693,13 +697,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     const float mv = sh.ml[v][lane & 31][0], lv = sh.ml[v][lane & 31][1];
     if (!no_weight(mv, lv)) sum += lv * __builtin_amdgcn_exp2f((mv - m) * a.scale_log2);
   }
-  const float keep = no_weight(w.m, l) ? 0.f : __builtin_amdgcn_exp2f((w.m - m) * a.scale_log2);
+  // (a part in which a row sees no key is 0: its sums may hold 0 * NaN from values that others see)
+  const bool none = no_weight(w.m, l);
+  const float keep = __builtin_amdgcn_exp2f((w.m - m) * a.scale_log2);
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-    for (int j = 0; j < 16; j += 4)
-      *reinterpret_cast<f32x4*>(&sh.o[wave][lane & 31][32 * d + 2 * j + 4 * (lane >> 5)]) =
-          f32x4{w.o[d][j] * keep, w.o[d][j + 1] * keep, w.o[d][j + 2] * keep, w.o[d][j + 3] * keep};
+    for (int j = 0; j < 16; j += 4) {
+      f32x4 y;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) y[u] = none ? 0.f : w.o[d][j + u] * keep;
+      *reinterpret_cast<f32x4*>(&sh.o[wave][lane & 31][32 * d + 2 * j + 4 * (lane >> 5)]) = y;
+    }
   __syncthreads();
   if (wave == 0 && lane < 32) {                          // for the threads that store a row
     sh.ml[0][lane][0] = m;

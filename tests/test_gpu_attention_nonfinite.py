@@ -85,3 +85,19 @@ def test_infinite_scores(way, dtype):
     K2[5, :, 7] = math.inf
     O, _ = _run(Q, K2, V, cu_q, cu_k)
     assert bool(O[:ql[0]].float().isnan().all()) and bool(O[ql[0]:].isfinite().all())
+
+
+@pytest.mark.parametrize("way", [([4, 1], [2, 3000], 8, 2, 128), ([10, 3], [4, 0], 4, 2, 64), ([70, 5], [40, 0], 4, 2, 64)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_rows_without_a_key_among_values_that_are_not_finite(way, bad):
+    """The first queries of a sequence with fewer keys than queries see none: zeros, and -inf, whatever the values."""
+    ql, kl, Hq, Hk, D = way
+    Q, K, V = (L.randn(n, h, D, seed=i, dtype=torch.float16) for i, (n, h) in
+               enumerate([(sum(ql), Hq), (sum(kl), Hk), (sum(kl), Hk)]))
+    V[:kl[0]] = bad
+    O, lse = _run(Q, K, V, L.starts(ql), L.starts(kl), causal=True)
+    none = ql[0] - kl[0]
+    assert bool((O[:none] == 0).all()) and bool((lse[:none] == -math.inf).all())
+    assert not bool(O[none:ql[0]].isfinite().any()) and bool(lse[none:ql[0]].isfinite().all())
+    rest = O[ql[0]:]
+    assert bool(rest.isfinite().all()) and (kl[1] > 0 or bool((rest == 0).all()))
