@@ -776,14 +776,14 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, long long slo
 #pragma unroll
     for (int i = 0; i < kMaxSplits / 64; ++i) {
       const int s = lane + 64 * i;
-      // (a part without keys has a maximum of -inf, no sum and no output; one of nothing but NaN has
-      // the same maximum, and its sum makes the row NaN)
-      const float f = no_weight(ms[i], ls[i]) ? 0.f
-                      : ls[i] != ls[i]        ? ls[i]
-                                              : __builtin_amdgcn_exp2f((ms[i] - m) * a.scale_log2);
+      // A part without keys is left out, marked by a negative weight.  One of nothing but NaN has the
+      // same maximum of -inf, and its sum makes the row NaN; one whose weight rounds to 0 still counts,
+      // as its values may not be finite.
+      const bool none = no_weight(ms[i], ls[i]);
+      const float f = ls[i] != ls[i] ? ls[i] : __builtin_amdgcn_exp2f((ms[i] - m) * a.scale_log2);
       if (s < a.splits) {
-        weight[wave][s] = f;
-        if (f != 0.f) l = fmaf(ls[i], f, l);
+        weight[wave][s] = none ? -1.f : f;
+        if (!none) l = fmaf(ls[i], f, l);
       }
     }
 #pragma unroll
@@ -795,8 +795,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, long long slo
 #pragma unroll 8
       for (int s = group; s < a.splits; s += groups) {
         const float f = weight[wave][s];
-        // (what a part without keys left in memory may be anything)
-        if (f != 0.f) y += *reinterpret_cast<const f32x4*>(po + (long long)s * a.D) * f;
+        if (!(f < 0.f)) y += *reinterpret_cast<const f32x4*>(po + (long long)s * a.D) * f;
       }
     }
     for (int d = 32; d >= quads; d >>= 1)

@@ -101,3 +101,22 @@ def test_rows_without_a_key_among_values_that_are_not_finite(way, bad):
     assert not bool(O[none:ql[0]].isfinite().any()) and bool(lse[none:ql[0]].isfinite().all())
     rest = O[ql[0]:]
     assert bool(rest.isfinite().all()) and (kl[1] > 0 or bool((rest == 0).all()))
+
+
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("part", ["first half", "second half", "whole parts"])
+def test_values_of_no_weight_still_count(way, bad, part):
+    """Keys whose scores are 2000 below the others' and whose values are not finite: 0 * NaN is NaN."""
+    ql, kl, Hq, Hk, D = way
+    Q, K, V, cu_q, cu_k = _inputs(way, torch.bfloat16)
+    Q[:], K[:] = 1.0, 0.0
+    n = kl[0]
+    half = {"first half": slice(0, n // 2), "second half": slice(n // 2, n),
+            "whole parts": slice(min(384, n // 3), min(1152, n - 1))}[part]
+    K[half, :, 0] = -2000.0
+    want = _run(Q, K, V, cu_q, cu_k, scale=1.0)
+    V[half] = bad
+    O, lse = _run(Q, K, V, cu_q, cu_k, scale=1.0)
+    assert bool(O[:ql[0]].float().isnan().all()) and torch.equal(lse, want[1])
+    assert torch.equal(O[ql[0]:], want[0][ql[0]:])
