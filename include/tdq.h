@@ -493,7 +493,7 @@ int tdq_norm_rotate(const tdq_heads* Q, const tdq_heads* K, tdq_dtype dt, int64_
  * sees other keys, though not this one: the weight 0 times that value is NaN.
  * lse [Tq, Hq] floats or NULL: log of the sum of exp(scale * score).
  * Scores, maxima, sums and O are held in binary32; the probabilities are rounded to the type of
- * V for the product with it.
+ * V for the product with it (binary16: those below 2^-32 of the largest are lost).
  *
  * Q [Tq, Hq, D], K, V [Tk, Hk, D], O [Tq, Hq, D] of dt = TDQ_F16 or TDQ_BF16, all 16-byte aligned
  * with strides that are multiples of 8.  D a multiple of 8 up to TDQ_MAX_HEAD, Hk divides Hq,

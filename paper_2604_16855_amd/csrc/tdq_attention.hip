@@ -206,6 +206,9 @@ hipError_t launch_norm_rotate(const tdq_heads* Q, const tdq_heads* K, tdq_dtype 
 //                     within an instruction is free as long as V^T is read in the same order
 // The maximum m that P refers to is raised, and O rescaled, only when a score exceeds it by 8
 // octaves: the quotient O / sum is the same for any m, and 2^8 leaves every type its precision.
+// Binary16 ends 25 octaves below 1, where many keys of a long cache may still have a weight together:
+// its probabilities are held 2^7 times as large (at most 2^15), so that they end 32 octaves below the
+// largest; O and the sum have that factor in common, and lse takes it out again.
 // The sum of the probabilities is taken before their rounding.
 struct AttendArgs {
   const void *Q, *K, *V;
@@ -253,9 +256,14 @@ __device__ __forceinline__ float max_of_halves(float x) {
 // Whether a row with maximum m and sum l has no key, or none with a score above -inf.  The maximum
 // alone does not say: it passes over NaN, which the sum does not.
 __device__ __forceinline__ bool no_weight(float m, float l) { return m == -INFINITY && l == 0.f; }
+// Octaves that probabilities of a type are held above their size.
+template <typename T>
+constexpr int kLift = __is_same(T, _Float16) ? 7 : 0;
 // Log of the sum of exp(scale * score).
+template <typename T>
 __device__ __forceinline__ float log_sum(float m, float l, float scale_log2) {
-  return no_weight(m, l) ? -INFINITY : fmaf(m, scale_log2, __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+  constexpr float down = 1.0f / (1 << kLift<T>);
+  return no_weight(m, l) ? -INFINITY : fmaf(m, scale_log2, __builtin_amdgcn_logf(l * down)) * 0.69314718055994530942f;
 }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -372,7 +380,7 @@ struct Rows {
           o[i][j] = e;
         }
     }
-    const float base = m == -INFINITY ? 0.f : -m * c;
+    const float base = m == -INFINITY ? 0.f : fmaf(-m, c, (float)kLift<T>);
     float sum = 0.f;
 #pragma unroll
     for (int n = 0; n < N; ++n)
@@ -595,7 +603,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
         store_floats<T, 4>(op + c, y);
       }
     }
-  if (a.lse && half == 0) a.lse[(t.q0 + (long long)token) * a.Hq + head] = log_sum(w.m, l, a.scale_log2);
+  if (a.lse && half == 0) a.lse[(t.q0 + (long long)token) * a.Hq + head] = log_sum<T>(w.m, l, a.scale_log2);
 }
 
 // Few rows (single tokens over a cache): 32 of them, and it is the keys that are shared out, to
@@ -737,7 +745,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
       const float inv = no_weight(mr, lr) ? 0.f : 1.0f / lr;
       const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
       store_floats<T, 4>(static_cast<T*>(a.O) + (t.q0 + tok) * a.o_token + h * a.o_head + c, z);
-      if (a.lse && c == 0) a.lse[at] = log_sum(mr, lr, a.scale_log2);
+      if (a.lse && c == 0) a.lse[at] = log_sum<T>(mr, lr, a.scale_log2);
     }
   }
 }
@@ -806,7 +814,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, long long slo
       const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
       store_floats<T, 4>(static_cast<T*>(a.O) + (t.q0 + tok) * a.o_token + h * a.o_head + c, z);
       if (a.lse && lane == 0)
-        a.lse[at] = log_sum(m, l, a.scale_log2);
+        a.lse[at] = log_sum<T>(m, l, a.scale_log2);
     }
     __builtin_amdgcn_wave_barrier();
   }
