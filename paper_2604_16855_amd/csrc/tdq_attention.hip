@@ -207,8 +207,8 @@ hipError_t launch_norm_rotate(const tdq_heads* Q, const tdq_heads* K, tdq_dtype 
 // The maximum m that P refers to is raised, and O rescaled, only when a score exceeds it by 8
 // octaves: the quotient O / sum is the same for any m, and 2^8 leaves every type its precision.
 // Binary16 ends 25 octaves below 1, where many keys of a long cache may still have a weight together:
-// its probabilities are held 2^7 times as large (at most 2^15), so that they end 32 octaves below the
-// largest; O and the sum have that factor in common, and lse takes it out again.
+// its m is 7 octaves below the largest score, so that probabilities (at most 2^15) end 32 octaves
+// below the largest.
 // The sum of the probabilities is taken before their rounding.
 struct AttendArgs {
   const void *Q, *K, *V;
@@ -219,6 +219,7 @@ struct AttendArgs {
   long long Tq, Tk;
   int S, Hq, Hk, group, D, causal;
   float scale_log2;                    // |scale| log2(e), at least 1e-30 (a masked score stays -inf)
+  float lift;                          // kLift octaves as a score
   u32 flip;                            // sign bits of two elements if the scale is negative: Q is negated
   int splits;                          // parts that the keys of a sequence are cut into
   float *part_o, *part_ml;             // [Tq Hq][splits][D], and maximum and sum [Tq Hq][splits][2]
@@ -256,14 +257,12 @@ __device__ __forceinline__ float max_of_halves(float x) {
 // Whether a row with maximum m and sum l has no key, or none with a score above -inf.  The maximum
 // alone does not say: it passes over NaN, which the sum does not.
 __device__ __forceinline__ bool no_weight(float m, float l) { return m == -INFINITY && l == 0.f; }
-// Octaves that probabilities of a type are held above their size.
+// Octaves that the reference m is set below the largest score.
 template <typename T>
 constexpr int kLift = __is_same(T, _Float16) ? 7 : 0;
 // Log of the sum of exp(scale * score).
-template <typename T>
 __device__ __forceinline__ float log_sum(float m, float l, float scale_log2) {
-  constexpr float down = 1.0f / (1 << kLift<T>);
-  return no_weight(m, l) ? -INFINITY : fmaf(m, scale_log2, __builtin_amdgcn_logf(l * down)) * 0.69314718055994530942f;
+  return no_weight(m, l) ? -INFINITY : fmaf(m, scale_log2, __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
 }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -345,9 +344,10 @@ struct Rows {
   }
 
   // Scores -> probabilities, of N times 32 keys from key j0 on; `sees`: how many keys the row
-  // sees (looked at only where `masked`).
+  // sees (looked at only where `masked`).  lift: kLift octaves as a score.
   template <int N>
-  __device__ __forceinline__ void softmax(f32x16 (&s)[N], u32 (&p)[N][8], float c, int j0, int sees, bool masked) {
+  __device__ __forceinline__ void softmax(f32x16 (&s)[N], u32 (&p)[N][8], float c, float lift, int j0, int sees,
+                                          bool masked) {
     const int half = (threadIdx.x >> 5) & 1;
     if (masked) {
 #pragma unroll
@@ -362,8 +362,8 @@ struct Rows {
 #pragma unroll
       for (int j = 0; j < 16; ++j) top = fmaxf(top, s[n][j]);
     top = max_of_halves(top);
-    if (__ballot((top - m) * c > 8.0f || (m == -INFINITY && top > m))) {
-      const float m_new = fmaxf(m, top);
+    if (__ballot((top - m) * c > 8.0f + kLift<T> || (m == -INFINITY && top > m))) {
+      const float m_new = fmaxf(m, kLift<T> == 0 ? top : top - lift);
       // (rows that have seen no key yet keep their zeros)
       const float keep = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - m_new) * c);
       m = m_new;
@@ -380,7 +380,7 @@ struct Rows {
           o[i][j] = e;
         }
     }
-    const float base = m == -INFINITY ? 0.f : fmaf(-m, c, (float)kLift<T>);
+    const float base = m == -INFINITY ? 0.f : -m * c;
     float sum = 0.f;
 #pragma unroll
     for (int n = 0; n < N; ++n)
@@ -578,7 +578,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
       u32 p[2][8];
       s[0] = w.scores(0);
       s[1] = w.scores(32);
-      w.softmax(s, p, a.scale_log2, j0, sees, j0 + kKeys > all);
+      w.softmax(s, p, a.scale_log2, a.lift, j0, sees, j0 + kKeys > all);
       w.values(0, p[0]);
       w.values(32, p[1]);
     }
@@ -589,7 +589,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   if (!real) return;
   // a row that sees no key: zeros, and -inf (its sums may hold 0 * NaN from values that others see)
   const bool none = no_weight(w.m, l);
-  const float inv = 1.0f / l;
+  if (__ballot(none)) {                                // (hardly ever: no select in the ordinary way)
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) w.o[i][j] = none ? 0.f : w.o[i][j];
+  }
+  const float inv = none ? 0.f : 1.0f / l;
   T* op = static_cast<T*>(a.O) + (t.q0 + token) * a.o_token + head * a.o_head;
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i)
@@ -597,13 +603,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     for (int j = 0; j < 16; j += 4) {
       const int c = 32 * i + 2 * j + 4 * half;
       if (c < D) {
-        float y[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) y[u] = none ? 0.f : w.o[i][j + u] * inv;
+        const float y[4] = {w.o[i][j] * inv, w.o[i][j + 1] * inv, w.o[i][j + 2] * inv, w.o[i][j + 3] * inv};
         store_floats<T, 4>(op + c, y);
       }
     }
-  if (a.lse && half == 0) a.lse[(t.q0 + (long long)token) * a.Hq + head] = log_sum<T>(w.m, l, a.scale_log2);
+  if (a.lse && half == 0) a.lse[(t.q0 + (long long)token) * a.Hq + head] = log_sum(w.m, l, a.scale_log2);
 }
 
 // Few rows (single tokens over a cache): 32 of them, and it is the keys that are shared out, to
@@ -682,7 +686,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     s[0] = w.scores(0);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // K has been read
     if (more) copy_k(i + 4);
-    w.softmax(s, p, a.scale_log2, i * kFewKeys, sees, (i + 1) * kFewKeys > all);
+    w.softmax(s, p, a.scale_log2, a.lift, i * kFewKeys, sees, (i + 1) * kFewKeys > all);
     if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
     else wait_copies();
     w.values(0, p[0]);
@@ -745,7 +749,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
       const float inv = no_weight(mr, lr) ? 0.f : 1.0f / lr;
       const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
       store_floats<T, 4>(static_cast<T*>(a.O) + (t.q0 + tok) * a.o_token + h * a.o_head + c, z);
-      if (a.lse && c == 0) a.lse[at] = log_sum<T>(mr, lr, a.scale_log2);
+      if (a.lse && c == 0) a.lse[at] = log_sum(mr, lr, a.scale_log2);
     }
   }
 }
@@ -814,7 +818,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, long long slo
       const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
       store_floats<T, 4>(static_cast<T*>(a.O) + (t.q0 + tok) * a.o_token + h * a.o_head + c, z);
       if (a.lse && lane == 0)
-        a.lse[at] = log_sum<T>(m, l, a.scale_log2);
+        a.lse[at] = log_sum(m, l, a.scale_log2);
     }
     __builtin_amdgcn_wave_barrier();
   }
@@ -893,6 +897,7 @@ hipError_t launch_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_he
   a.causal = causal;
   const double c = fabs((double)scale) * 1.44269504088896340736;
   a.scale_log2 = c > 1e-30 ? (float)c : 1e-30f;
+  a.lift = (dt == TDQ_F16 ? kLift<_Float16> : kLift<__bf16>) / a.scale_log2;
   a.flip = scale < 0.f ? 0x80008000u : 0u;
   a.splits = p.splits;
   a.part_ml = static_cast<float*>(workspace);
