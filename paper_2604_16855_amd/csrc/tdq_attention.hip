@@ -369,16 +369,20 @@ struct Rows {
       m = m_new;
       l *= keep;
 #pragma unroll
-      for (int i = 0; i < DP / 32; ++i)
+      for (int i = 0; i < DP / 32; ++i) {
+        // In place: from an ordinary product the compiler makes a copy of all of O in every pass, 64
+        // moves.  It does not see what these instructions read and write, so the wait states that it
+        // would put between matrix instructions and them are here, tied to the values: 20 before the
+        // first, as many as the longest matrix instruction needs, and two behind the last.
+        asm volatile("s_nop 15\n\ts_nop 3" : "+v"(o[i]));
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          // (in place: from an ordinary product the compiler makes a copy of all of O in every
-          // pass, 64 moves.  What it reads was written by matrix instructions before those of the
-          // scores, which the condition has waited for.)
           float e = o[i][j];
           asm volatile("v_mul_f32 %0, %1, %0" : "+v"(e) : "v"(keep));
           o[i][j] = e;
         }
+        asm volatile("s_nop 1" : "+v"(o[i]));
+      }
     }
     const float base = m == -INFINITY ? 0.f : -m * c;
     float sum = 0.f;
