@@ -62,17 +62,44 @@ class Cache:
     """Keys and values of S sequences, `room` tokens each, and how many are there."""
 
     def __init__(self, S: int, room: int, Hk: int, D: int, dtype, device):
-        self.K = torch.empty((S * room, Hk, D), dtype=dtype, device=device)
-        self.V = torch.empty_like(self.K)
+        # (a row behind the last sequence takes what has no place)
+        self._K = torch.empty((S * room + 1, Hk, D), dtype=dtype, device=device)
+        self._V = torch.empty_like(self._K)
+        self.K, self.V = self._K[:-1], self._V[:-1]
+        self.S, self.room = S, room
         self.cu = room * torch.arange(S + 1, dtype=torch.int32, device=device)
-        self.used = torch.zeros((S,), dtype=torch.int32, device=device)
+        # one entry more: tokens that belong to no sequence, which fit nowhere
+        self._first = self.cu.long()
+        self._end = torch.cat([self._first[1:], torch.full_like(self._first[:1], -(1 << 62))])
+        self._used = torch.zeros_like(self.cu)
+        self.used = self._used[:-1]
+        self._most = 0                   # no sequence has more tokens, as far as the host can tell
 
     def append(self, K: torch.Tensor, V: torch.Tensor, cu: torch.Tensor) -> None:
-        """New tokens of every sequence, packed by cu.  (Whoever fills a cache sees to it that they have room.)"""
+        """New tokens of every sequence, packed by cu [S + 1] from 0 on.  A sequence without room for its own is
+        refused, and the cache left as it is.  The host counts T more for every sequence; only when that would not fit
+        does it ask the device for the true numbers.  (A replayed graph does not ask: there, what has no room is left
+        out, and the next call that asks is refused.)"""
+        T = K.shape[0]
+        if cu.shape != (self.S + 1,) or V.shape[0] != T:
+            raise ValueError("cu must be one longer than the number of sequences, K and V as long as each other")
+        most = self._most + T
+        if most > self.room:
+            new = cu.tolist()
+            total = [u + b - a for u, a, b in zip(self.used.tolist(), new, new[1:])]
+            most = max(total)
+            if most > self.room:
+                raise ValueError(f"sequence {total.index(most)} would have {most} tokens in a room of {self.room}")
+        self._write(K, V, cu)
+        self._most = most
+
+    def _write(self, K: torch.Tensor, V: torch.Tensor, cu: torch.Tensor) -> None:
         t = torch.arange(K.shape[0], dtype=torch.int32, device=K.device)
-        s = torch.searchsorted(cu, t, right=True) - 1
-        at = (self.cu[s] + self.used[s] + t - cu[s]).long()
-        self.K[at], self.V[at] = K, V
+        s = torch.searchsorted(cu, t, right=True).sub_(1)        # (in front of the first: -1, the last entry as well)
+        at = (self._first + self._used - cu)[s] + t
+        at = torch.where(at < self._end[s], at, self.S * self.room)
+        self._K.index_copy_(0, at, K)
+        self._V.index_copy_(0, at, V)
         self.used += cu[1:] - cu[:-1]
 
 
