@@ -433,7 +433,9 @@ int tdq_quantize_weight_f8(const void* W, tdq_dtype dt, int32_t N, int32_t K, in
 /*
  * Linear on such codes:
  *   Y[m, n] = sum_b x_step[m, b] * w_step[n / 128, b] * sum_{i in block b} Qx[m, i] Qw[n, i] (+ bias[n])
- * Blocks are added in binary32, b ascending, and the result is rounded once.  Binary16 and
+ * Blocks are added in binary32 and the result is rounded once.  More than 32 tokens: b ascending.
+ * Up to 32: eight sums, of the blocks b = w, w + 8, w + 16 .. ascending, which are added w ascending;
+ * so a token's last bits may differ between a call of 32 tokens and one of more.  Binary16 and
  * bfloat16 results take the 8-bit matrix instruction, which adds the products of a few
  * neighbouring channels with about 16 bits below the largest (some 2e-5 of the result's norm,
  * below a tenth of what the result's own rounding costs); binary32 results take the codes as

@@ -1,0 +1,26 @@
+"""The sums of the 8-bit linear."""
+import pytest
+import torch
+
+from paper_2604_16855_amd import tdq
+
+import layer_util as L
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+@pytest.mark.parametrize("K,N", [(1025, 64), (4096, 200), (8190, 640)])
+def test_few_and_more_tokens_agree(K, N, dtype):
+    """Up to 32 tokens the blocks of K are added in eight partial sums: the same within the bound of either order."""
+    X = L.randn(33, K, seed=K)
+    qx, xs = tdq.tdq_quantize_act_f8(X)
+    qw, ws = tdq.tdq_quantize_weight_f8(0.05 * L.randn(N, K, seed=2))
+    more = tdq.tdq_linear_f8(qx, xs, K, qw, ws, out_dtype=dtype).double()
+    _, mag = L.linear(qx, xs, K, qw, ws)
+    tol = 2 * (-(-K // 128) + 128 + 4) * 2.0 ** -24 * mag
+    if dtype != torch.float32:
+        tol = tol + 2 * 2.0 ** -13 * mag + 2 * L.UNIT[dtype] * more.abs() + L.TINY[dtype]
+    for M in (32, 16, 1):
+        few = tdq.tdq_linear_f8(qx[:M], xs[:M], K, qw, ws, out_dtype=dtype).double()
+        assert bool(((few - more[:M]).abs() <= tol[:M]).all())
