@@ -468,12 +468,14 @@ typedef struct tdq_heads {
  * where (a, b) are elements (2 p, 2 p + 1) if interleaved, else (p, p + R / 2); elements from R
  * on are not turned.  Several position axes (time, height, width): axis [R / 2] says which axis
  * turns a pair (values outside 0 .. axes - 1 are taken as the nearest), NULL = the first.
- * Cosine and sine of that angle are as exact as binary32, however far the position.
+ * Cosine and sine of that angle are as exact as binary32, however far the position.  The squares
+ * are added in binary32.
  *
  * Q, K: T tokens of Hq and Hk heads of D elements of dt (any of the three); K may be NULL with
  * Hk = 0.  D and R multiples of 8, R <= D <= TDQ_MAX_HEAD.  q_weight, k_weight [D] floats or
  * NULL.  pos [axes, ld_pos] int32, ld_pos >= T.  freq [R / 2] floats; R = 0 turns nothing (pos
- * and freq may be NULL then).  Qo, Ko as Q, K; they may be the same tensors as Q and K.
+ * and freq may be NULL then).  Qo, Ko as Q, K; they may be the same tensors as Q and K, but not overlap
+ * them in another way.
  * T <= 2^30, Hq + Hk <= 4096.
  */
 int tdq_norm_rotate(const tdq_heads* Q, const tdq_heads* K, tdq_dtype dt, int64_t T, int32_t Hq, int32_t Hk,
@@ -487,9 +489,10 @@ int tdq_norm_rotate(const tdq_heads* Q, const tdq_heads* K, tdq_dtype dt, int64_
  * over the keys j of t's sequence; sequence s has the queries cu_q[s] .. cu_q[s + 1] - 1 and the
  * keys cu_k[s] .. cu_k[s + 1] - 1 (device arrays of S + 1, ascending, within 0 .. Tq and 0 .. Tk;
  * what lies outside is cut off).  len_k [S] (device) or NULL: of the keys of sequence s only the
- * first len_k[s] are used, as in a cache that leaves every sequence room to grow.  causal: the last query of a sequence sees all of its keys, the
- * one before it all but the last, and so on.  A query that sees no key gets O = 0 and lse = -inf; one
- * that is NaN, or sees a key that is, gets NaN in both.
+ * first len_k[s] are used, as in a cache that leaves every sequence room to grow.  Queries of no
+ * sequence keep what their rows of O and lse hold.  causal: the last query of a sequence sees all
+ * of its keys, the one before it all but the last, and so on.  A query that sees no key gets O = 0
+ * and lse = -inf; one that is NaN, or sees a key that is, gets NaN in both.
  * Keys that a query does not see do not matter, whatever they hold; what lies outside its sequence
  * neither, keys or values.  A value of its own sequence that is not finite may reach a query that
  * sees other keys, though not this one: the weight 0 times that value is NaN.
@@ -505,8 +508,8 @@ int tdq_norm_rotate(const tdq_heads* Q, const tdq_heads* K, tdq_dtype dt, int64_
 size_t tdq_attention_workspace_bytes(int64_t Tq, int64_t Tk, int32_t S, int32_t Hq, int32_t Hk, int32_t D);
 int tdq_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, tdq_dtype dt, int64_t Tq, int64_t Tk,
                   int32_t S, const int32_t* cu_q, const int32_t* cu_k, const int32_t* len_k, int32_t Hq, int32_t Hk,
-                  int32_t D, float scale, int32_t causal, const tdq_heads* O, float* lse, void* workspace, size_t workspace_bytes,
-                  void* stream);
+                  int32_t D, float scale, int32_t causal, const tdq_heads* O, float* lse, void* workspace,
+                  size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

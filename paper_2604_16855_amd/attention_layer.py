@@ -24,7 +24,8 @@ class AttentionLayer:
 
     def __init__(self, w_qkv: torch.Tensor, w_out: torch.Tensor, Hq: int, Hk: int, D: int, freq: torch.Tensor,
                  axis: Optional[torch.Tensor] = None, q_norm: Optional[torch.Tensor] = None,
-                 k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False, causal: bool = True):
+                 k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
+                 causal: bool = True):
         if w_qkv.shape[0] != (Hq + 2 * Hk) * D or w_out.shape[1] != Hq * D:
             raise ValueError("the weights do not fit the heads")
         self.qkv, self.out = tdq.tdq_quantize_weight_f8(w_qkv), tdq.tdq_quantize_weight_f8(w_out)
@@ -51,7 +52,8 @@ class AttentionLayer:
         return self._project(tdq.tdq_attention(Q, K, V, cu, cu, causal=self.causal)[0])
 
     def step(self, X: torch.Tensor, pos: torch.Tensor, cu: torch.Tensor, cache: "Cache") -> torch.Tensor:
-        """The next tokens of every sequence of a cache: X[T, C], packed by cu [S + 1]; their keys and values join it."""
+        """The next tokens of every sequence of a cache: X[T, C], packed by cu [S + 1]; their keys and values join it
+        (refused where a sequence has no room for them)."""
         Q, K, V = self._heads(X, pos)
         cache.append(K, V, cu)
         O, _ = tdq.tdq_attention(Q, cache.K, cache.V, cu, cache.cu, len_k=cache.used, causal=self.causal)
@@ -114,7 +116,7 @@ def main() -> None:
     layer = AttentionLayer(0.02 * randn((Hq + 2 * Hk) * D, C), 0.02 * randn(C, Hq * D), Hq, Hk, D, freq, q_norm=ones,
                            k_norm=ones)
     whole = [randn(n + more, C).bfloat16() for n in lengths]
-    pack = lambda a, b: torch.cat([x[n + a:n + b] if a >= 0 else x[:n + b] for x, n in zip(whole, lengths)])  # noqa: E731
+    pack = lambda a, b: torch.cat([x[n + a if a >= 0 else 0:n + b] for x, n in zip(whole, lengths)])  # noqa: E731
 
     def places(counts, first):
         cu = torch.tensor([0] + counts, device="cuda").cumsum(0).to(torch.int32)

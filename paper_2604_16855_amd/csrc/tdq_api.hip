@@ -974,8 +974,8 @@ size_t tdq_attention_workspace_bytes(int64_t Tq, int64_t Tk, int32_t S, int32_t 
 
 int tdq_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, tdq_dtype dt, int64_t Tq, int64_t Tk,
                   int32_t S, const int32_t* cu_q, const int32_t* cu_k, const int32_t* len_k, int32_t Hq, int32_t Hk,
-                  int32_t D, float scale, int32_t causal, const tdq_heads* O, float* lse, void* workspace, size_t workspace_bytes,
-                  void* stream) {
+                  int32_t D, float scale, int32_t causal, const tdq_heads* O, float* lse, void* workspace,
+                  size_t workspace_bytes, void* stream) {
   if (!Q || !K || !V || !O || !cu_q || !cu_k || !Q->data || !O->data) return TDQ_ERR_NULL;
   if (Tk > 0 && (!K->data || !V->data)) return TDQ_ERR_NULL;
   if (dt != TDQ_F16 && dt != TDQ_BF16) return TDQ_ERR_DTYPE;

@@ -241,7 +241,8 @@ template <>
 struct Mfma<__bf16> {
   typedef b16x8 frag;
   __device__ static __forceinline__ f32x16 mul(u32x4 a, u32x4 b, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(frag, a), __builtin_bit_cast(frag, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(frag, a), __builtin_bit_cast(frag, b), c, 0, 0,
+                                                   0);
   }
 };
 
@@ -292,7 +293,8 @@ __device__ __forceinline__ int place_v(int r) {
 template <typename T, int DP>
 struct Rows {
   u32x4 q[DP / 16];                    // operand columns: row lane % 32, elements 16 i + 8 (lane / 32) ..
-  f32x16 o[DP / 32];                   // element j of o[i]: row lane % 32, output 32 i + 8 (j / 4) + 4 (lane / 32) + j % 4
+  // element j of o[i]: row lane % 32, output 32 i + 8 (j / 4) + 4 (lane / 32) + j % 4
+  f32x16 o[DP / 32];
   float m, l;                          // reference of the exponents (of the row), sum (of this lane's keys)
 
   __device__ __forceinline__ void start(const T* qp, int D, u32 flip) {
@@ -517,7 +519,10 @@ constexpr int kKeys = 64;              // keys of a tile
 
 // Many rows: 128 of them by four wavefronts that share tiles of 64 keys, the next tile on its way
 // while one is worked on.  Bound by the matrix and the vector unit (45 and 53 % of the cycles, hardly
-// at the same time): 8 causal prompts of up to 4096, 32/8 heads of 128, in 645 us, 910 TFLOP/s.
+// at the same time): 8 causal prompts of up to 4096, 32/8 heads of 128, in 631 us, 930 TFLOP/s.
+// With D up to 128 padded to a power of two (80 takes 586 us there, 96 605, at 620 and 730 TFLOP/s
+// of what they need); beyond, tiles have one stage and a SIMD one wavefront: 16/4 heads of 256 865 us,
+// 680 TFLOP/s.
 template <typename T, int DP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 2 : 1))) void k_attend(AttendArgs a,
                                                                                                long long slots) {
@@ -618,7 +623,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
 // `splits` workgroups and in each to four wavefronts.  Bound by reading K and V once: a wavefront
 // copies its own tiles of 32 keys, K of the next while it works on V of this and the other way
 // round, and waits for nobody until the end, where the wavefronts' parts are joined in LDS.  16 tokens
-// over 4000 to 32000 keys, 32/8 heads of 128: 224 us, 5.3 TB/s (a wavefront of rows for all keys: 1354).
+// over 4000 to 32000 keys, 32/8 heads of 128: 222 us, 5.3 TB/s (a wavefront of rows for all keys: 1354);
+// 16/4 heads of 256, with 17 registers in scratch, 3.1 TB/s.
 constexpr int kFewRows = 32, kFewKeys = 32;
 template <int DP>
 struct FewShared {
@@ -828,7 +834,11 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, long long slo
   }
 }
 
-// Which way a call goes, from what the host knows of it.
+// Which way a call goes, from what the host knows of it: the totals, not the sequences.  Keys are
+// shared out where there are up to 32 rows a sequence on average, by the average of its keys.  Beyond
+// that a workgroup goes through all keys of its 128 rows, which leaves most of the chip idle where
+// there are few such tiles: one sequence over 30000 keys, 32/8 heads of 128, 8 tokens 192 us (160 of
+// it the join, which has one workgroup for the rows of a tile), 9 tokens 534; 15 single tokens over 32000 keys 366 us, and 631 with a prompt of 2000 (54) in the same call.
 struct AttendPlan {
   bool few;
   int splits;
@@ -871,8 +881,8 @@ static void launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t 
 }
 
 hipError_t launch_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, tdq_dtype dt, long long Tq,
-                            long long Tk, int S, const int* cu_q, const int* cu_k, const int* len_k, int Hq, int Hk, int D, float scale,
-                            bool causal, const tdq_heads* O, float* lse, void* workspace, hipStream_t st) {
+                            long long Tk, int S, const int* cu_q, const int* cu_k, const int* len_k, int Hq, int Hk,
+                            int D, float scale, bool causal, const tdq_heads* O, float* lse, void* workspace, hipStream_t st) {
   const AttendPlan p = attend_plan(Tq, Tk, S, Hq, Hk);
   AttendArgs a;
   a.Q = Q->data;

@@ -196,7 +196,7 @@ hipError_t launch_quantize_f8_tiles(const void* W, tdq_dtype dt, int N, int K, l
 // ---------------------------------------------------------------------------
 // linear
 // ---------------------------------------------------------------------------
-// Bytes [at, at + 8) of a row: those at K and beyond become code 0.
+// Bytes [at, at + 4) of a row: those at K and beyond become code 0.
 __device__ __forceinline__ void mask_codes(u32& w, int at, int K) {
   const int keep = K - at;
   if (keep < 4) w = keep <= 0 ? 0u : w & ((1u << (8 * keep)) - 1u);
@@ -279,8 +279,10 @@ __device__ __forceinline__ void store_run(OUT* p, u32x4 v, int left) {
 // block's rescale needs one step product per 32 tokens and lane.
 // LDS: rows of 128 codes (one block), the 16-byte piece p of row r at position p ^ (r / 2 % 8):
 // the 16 rows that a fragment read takes at a time fall on 16 different groups of banks.
-// Bound by the clock under this load (1.8 GHz) and by what a block's start costs all wavefronts at
-// once: 2.3 PFLOP/s at 8192^3 (472 us), 1.7 at 131072 x 1024 x 4096 (658).
+// At 8192^3 (483 us, 2.3 PFLOP/s) the matrix units work 58 % of the cycles, at 1.9 GHz under this
+// load: a block's start costs all wavefronts at once.  131072 x 1024 x 4096 (655 us, 1.7 PFLOP/s) has
+// as many products and 42 %: of the 20 us of a tile 6 are its start and end, which nothing covers, and
+// the stage that is copied behind the last block and not used.
 template <typename OUT, bool FINE, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void k_linear_f8(
     const uint8_t* __restrict__ Qx, long long ld_q, const float* __restrict__ xs, long long ld_xs, int M, int K, int N,
@@ -340,7 +342,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_f8(
       copy_to_lds(c * 8 < BM ? xb : wb, row_off[i] + at, base + c * 1024);
     }
     if (part == 0 && wave * 64 < BM)
-      copy_float_to_lds(xs + m0 * ld_xs + (kb < KB ? kb : KB - 1), step_off, steps0 + (u32)((kb & 1) * (BM < 64 ? 64 : BM) + wave * 64) * 4);
+      copy_float_to_lds(xs + m0 * ld_xs + (kb < KB ? kb : KB - 1), step_off,
+                        steps0 + (u32)((kb & 1) * (BM < 64 ? 64 : BM) + wave * 64) * 4);
   };
 
   f32x16 acc[TN][TM];
@@ -450,7 +453,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_f8(
 // Few tokens: bound by reading the weight once.  A workgroup has 16 outputs and all tokens, its
 // wavefronts share out the blocks of K: each reads its blocks of 16 x 128 codes straight to
 // registers, a lane 32 bytes and four lanes a whole line, several blocks at a time, and the
-// wavefronts' sums are joined in LDS.  One token, 4096 -> 4096: 5.7 us, by 64 x 64 tiles 14.
+// wavefronts' sums are joined in LDS.  One token, 4096 -> 4096: 5.8 us, by 64 x 64 tiles 14.
 constexpr int kFewWaves = 8;
 template <typename OUT, bool FINE, int TM>
 __global__ __launch_bounds__(64 * kFewWaves) void k_linear_f8_few(
@@ -557,6 +560,8 @@ static void launch_linear(const uint8_t* Qx, long long ld_q, const float* xs, lo
 //   128 x 256  1.15 for each 256 tiles; binary32 1.9
 //   256 x 256  1.75 for each 256 tiles (8192 x 8192 x 8192: 472, 128 x 256 586, 64 x 64 951)
 //   128 x 128  (binary32, whose operands as binary16 spill from a 256 x 256 tile) 1.17, 4.3 for each 1000
+// No tile cuts K, so that few tiles over a long K leave most of the chip idle: 4096 x 4096 takes 9.7 us
+// with 32 tokens and 13.8 with 33 (floor 2.7), 8192 -> 1024 25 us with 64, 4096 -> 512 14 us with 968.
 enum { kFew16, kFew32, k64x64, k128x256, kLargest };
 static int linear_way(long long M, long long N, bool fine) {
   if (M <= 32) return M <= 16 ? kFew16 : kFew32;

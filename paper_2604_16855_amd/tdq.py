@@ -796,7 +796,8 @@ def tdq_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, cu_q: torch
                   lse: Optional[torch.Tensor] = None, want_lse: bool = False,
                   workspace: Optional[torch.Tensor] = None, len_k: Optional[torch.Tensor] = None):
     """Q[Tq, Hq, D], K and V[Tk, Hk, D], cu_q and cu_k[S + 1] int32 -> (O[Tq, Hq, D], lse[Tq, Hq] f32 or None).
-    scale: 1 / sqrt(D) if None.  len_k[S] int32: how many of a sequence's keys are used."""
+    scale: 1 / sqrt(D) if None.  len_k[S] int32: how many of a sequence's keys are used.  Rows of queries outside
+    cu_q are not written."""
     q_shape, k_shape, dtype = Q.shape, K.shape, Q.dtype
     Tq, Hq, D = q_shape
     Tk, Hk = k_shape[0], k_shape[1]
@@ -833,8 +834,8 @@ def tdq_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, cu_q: torch
                    out.data_ptr(), *_strides(out, "out"))
     at = C.addressof(h)
     rc = L.tdq_attention(at, at + _HEADS_BYTES, at + 2 * _HEADS_BYTES, _wdt(dtype), Tq, Tk, S, cu_q.data_ptr(),
-                         cu_k.data_ptr(), None if len_k is None else len_k.data_ptr(), Hq, Hk, D, D ** -0.5 if scale is None else scale, 1 if causal else 0,
-                         at + 3 * _HEADS_BYTES, None if lse is None else lse.data_ptr(), p_work, n_work, _stream())
+                         cu_k.data_ptr(), None if len_k is None else len_k.data_ptr(), Hq, Hk, D,
+                         D ** -0.5 if scale is None else scale, 1 if causal else 0, at + 3 * _HEADS_BYTES, None if lse is None else lse.data_ptr(), p_work, n_work, _stream())
     if rc:
         raise TdqError(rc, "tdq_attention")
     return out, lse
