@@ -511,6 +511,123 @@ int tdq_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, td
                   int32_t D, float scale, int32_t causal, const tdq_heads* O, float* lse, void* workspace,
                   size_t workspace_bytes, void* stream);
 
+/*
+ * A cache of keys and values in pages, for serving many sequences: new tokens written to it, the
+ * choice of the pages that a token attends to, and the attention over chosen pages or whole sequences.
+ */
+
+/* Element d of head h of row r of page p is data[p page + r token + h head + d], strides in elements. */
+typedef struct tdq_pages {
+  void* data;
+  int64_t page, token, head;
+} tdq_pages;
+
+/* S sequences whose keys lie in the pages of a cache (all arrays on the device):
+ *   cu_q  [S + 1]  the queries (new tokens) of sequence s are cu_q[s] .. cu_q[s + 1] - 1: ascending, what
+ *                  lies outside 0 .. Tq is cut off; queries of no sequence are left alone everywhere
+ *   len_k [S]      its keys, those of its queries with them (the last ones); no more are used than its
+ *                  line of the table has room for, columns * page_size
+ *   table [S, ld_table]  key j of sequence s is row j % page_size of page table[s][j / page_size].  A page
+ *                  outside 0 .. n_pages - 1 is not there: nobody sees its keys, nothing is written to it.
+ * page_size a power of two from 16 to 1024, columns >= 1, columns * page_size <= 2^30, n_pages >= 1,
+ * 1 <= S <= 2^20.  Entries of a line past its sequence's last key are not looked at. */
+typedef struct tdq_sequences {
+  const int32_t *cu_q, *len_k, *table;
+  int64_t ld_table;
+  int32_t S, columns, n_pages, page_size;
+} tdq_sequences;
+
+/*
+ * tdq_norm_rotate on the queries and keys of new tokens, on the way to a cache: query i of n of a
+ * sequence with len keys is its key j = len - n + i, and
+ *   Qo[t]                                          = rotate(norm(Q[t]))
+ *   Kc[table[s][j / page_size]][j % page_size]     = rotate(norm(K[t]))
+ *   Vc[table[s][j / page_size]][j % page_size]     = V[t]
+ * with the formulas of tdq_norm_rotate.  pos NULL: a token's position is j (axes 1, ld_pos ignored).
+ * Keys and values without a place (j < 0, or past the line's room, a page that is not there) are not
+ * written.  No two tokens of a call may have the same place.
+ *
+ * Q [T, Hq, D], K, V [T, Hk, D] of dt = TDQ_F16 or TDQ_BF16; Q and Qo may be NULL with Hq = 0.  Qo may be Q,
+ * but not overlap it in another way.  Kc, Vc: the cache's pages [n_pages, page_size, Hk, D] of dt.
+ * D and R multiples of 8, R <= D <= TDQ_MAX_HEAD, 1 <= Hk, Hq + 2 Hk <= 4096, T <= 2^30; seq->cu_q not NULL.
+ */
+int tdq_cache_append(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, tdq_dtype dt, int64_t T,
+                     const tdq_sequences* seq, int32_t Hq, int32_t Hk, int32_t D, const float* q_weight,
+                     const float* k_weight, float eps, int32_t R, int32_t interleaved, const int32_t* pos,
+                     int64_t ld_pos, int32_t axes, const int32_t* axis, const float* freq, const tdq_heads* Qo,
+                     const tdq_pages* Kc, const tdq_pages* Vc, void* stream);
+
+/*
+ * Bounds of pages, for tdq_select_pages: lo[p, h, d] and hi[p, h, d] the smallest and largest value of
+ * channel d over the keys in use (j < len) of page p, NaN where one of them is.  seq->cu_q NULL: all pages
+ * of all sequences; else the pages that hold a sequence's last n keys, n its queries (T: all of them, an
+ * upper bound).  Other pages' bounds are left alone.  A page that two sequences share has to hold the same
+ * number of keys for both.
+ *
+ * Kc as in tdq_cache_append, data and strides aligned to 2 bytes; lo, hi: tdq_heads with a page for a token,
+ * [n_pages, Hk, D] of dt.  1 <= Hk <= 4096, D a multiple of 8 up to TDQ_MAX_HEAD, 0 <= T <= 2^30.
+ */
+int tdq_page_bounds(const tdq_pages* Kc, tdq_dtype dt, int64_t T, const tdq_sequences* seq, int32_t Hk, int32_t D,
+                    const tdq_heads* lo, const tdq_heads* hi, void* stream);
+
+/*
+ * The pages that a token attends to, for each of its key heads: of the pages b that hold a key it sees
+ * (causal: the last query of a sequence sees all keys, the one before it all but the last, and so on),
+ * the first `first`, the last `last`, and the best of the others up to `count` in all, by
+ *   score[t, h, b] = max over the query heads e of h of sum_d max(Q[t, e, d], 0) hi[p, h, d] + min(Q[t, e, d], 0) lo[p, h, d]
+ * with p = table[s][b]: no key of the page has a larger product with one of the queries (for a positive
+ * scale).  Sums are held in binary64 and rounded to binary32; NaN counts as largest; of equal scores the
+ * lower b is better.  Pages that are not there are not taken.
+ * chosen [Tq, Hk, count] int32: the places b in the sequence's line, ascending, -1 behind them; those of
+ * tokens of no sequence are not written.
+ *
+ * Q [Tq, Hq, D] of dt = TDQ_F16 or TDQ_BF16, lo and hi as tdq_page_bounds writes them.  0 <= first, last;
+ * max(1, first + last) <= count <= 2^20.  D a multiple of 8 up to TDQ_MAX_HEAD, Hk divides Hq, Hq <= 4096,
+ * 1 <= Tq <= 2^30.  workspace: device scratch of tdq_select_pages_workspace_bytes(Tq, Hk, columns), 256-byte
+ * aligned.
+ */
+size_t tdq_select_pages_workspace_bytes(int64_t Tq, int32_t Hk, int32_t columns);
+int tdq_select_pages(const tdq_heads* Q, const tdq_heads* lo, const tdq_heads* hi, tdq_dtype dt, int64_t Tq,
+                     const tdq_sequences* seq, int32_t Hq, int32_t Hk, int32_t D, int32_t causal, int32_t first,
+                     int32_t last, int32_t count, int32_t* chosen, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
+/*
+ * tdq_attention over the keys of chosen pages: token t and key head h see, of the keys that t sees, those of
+ * the pages chosen[t, h, 0 .. count - 1] of their sequence's line, in any order.  Values outside the line's
+ * pages in use (-1) name none; the keys of a page that is named twice count twice.  O, lse, scale, causal and
+ * what is rounded as in tdq_attention; the same holds for keys that nobody sees and values that are not finite.
+ *
+ * Kc, Vc [n_pages, page_size, Hk, D], 16-byte aligned, strides multiples of 8; 1 <= count <= 2^20, count *
+ * page_size <= 2^30; the other arguments as in tdq_attention.  workspace: device scratch of
+ * tdq_attention_selected_workspace_bytes(Tq, Hq, Hk, D, page_size, count), 256-byte aligned (NULL if that is 0).
+ */
+size_t tdq_attention_selected_workspace_bytes(int64_t Tq, int32_t Hq, int32_t Hk, int32_t D, int32_t page_size,
+                                              int32_t count);
+int tdq_attention_selected(const tdq_heads* Q, const tdq_pages* Kc, const tdq_pages* Vc, tdq_dtype dt, int64_t Tq,
+                           const tdq_sequences* seq, int32_t Hq, int32_t Hk, int32_t D, float scale, int32_t causal,
+                           const int32_t* chosen, int32_t count, const tdq_heads* O, float* lse, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/*
+ * tdq_attention over whole sequences in pages.  prefix NULL: the keys of a sequence are its own.  Else the
+ * keys of a prefix stand in front of them: prefix->cu_q [prefix->S + 1] counts sequences, prefix g belongs to
+ * the sequences cu_q[g] .. cu_q[g + 1] - 1 (of none: no prefix), has prefix->len_k[g] keys in the pages of
+ * prefix->table, and every query of its sequences sees all of them, causal or not: only a sequence's own
+ * keys are hidden from its earlier queries.  A prefix is read once for all of its sequences.
+ * n_pages and page_size are the same for both.
+ *
+ * O, lse, scale, causal, rounding, keys that nobody sees and values that are not finite as in tdq_attention.
+ * Kc, Vc [n_pages, page_size, Hk, D], 16-byte aligned, strides multiples of 8; Tq * (Hq / Hk) <= 2^31;
+ * the other arguments as in tdq_attention.  workspace: device scratch of
+ * tdq_attention_paged_workspace_bytes(Tq, S, prefixes, Hq, Hk, D), 256-byte aligned.
+ */
+size_t tdq_attention_paged_workspace_bytes(int64_t Tq, int32_t S, int32_t prefixes, int32_t Hq, int32_t Hk, int32_t D);
+int tdq_attention_paged(const tdq_heads* Q, const tdq_pages* Kc, const tdq_pages* Vc, tdq_dtype dt, int64_t Tq,
+                        const tdq_sequences* seq, const tdq_sequences* prefix, int32_t Hq, int32_t Hk, int32_t D,
+                        float scale, int32_t causal, const tdq_heads* O, float* lse, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

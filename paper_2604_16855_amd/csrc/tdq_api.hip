@@ -992,4 +992,165 @@ int tdq_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, td
   return TDQ_OK;
 }
 
+// ---- a cache in pages ----------------------------------------------------------
+
+// Sequences (queries: with their cu_q; else it may be NULL) whose pages lie in the given tensors.
+static int check_sequences(const tdq_sequences* q, bool queries) {
+  if (!q || !q->len_k || !q->table || (queries && !q->cu_q)) return TDQ_ERR_NULL;
+  if (q->S < 1 || q->S > 1 << 20 || q->columns < 1 || q->ld_table < q->columns || q->n_pages < 1) return TDQ_ERR_SHAPE;
+  const int32_t p = q->page_size;
+  if (p < 16 || p > 1024 || (p & (p - 1)) != 0 || (int64_t)q->columns * p > (int64_t)1 << 30) return TDQ_ERR_SHAPE;
+  if (misaligned(q->cu_q, 4) || misaligned(q->len_k, 4) || misaligned(q->table, 4)) return TDQ_ERR_ALIGN;
+  return TDQ_OK;
+}
+static bool half_type(tdq_dtype dt) { return dt == TDQ_F16 || dt == TDQ_BF16; }
+static bool loose_heads(const tdq_heads* t) { return misaligned(t->data, 16) || t->token % 8 || t->head % 8; }
+static bool loose_pages(const tdq_pages* t) {
+  return misaligned(t->data, 16) || t->page % 8 || t->token % 8 || t->head % 8;
+}
+
+int tdq_cache_append(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, tdq_dtype dt, int64_t T,
+                     const tdq_sequences* seq, int32_t Hq, int32_t Hk, int32_t D, const float* q_weight,
+                     const float* k_weight, float eps, int32_t R, int32_t interleaved, const int32_t* pos,
+                     int64_t ld_pos, int32_t axes, const int32_t* axis, const float* freq, const tdq_heads* Qo,
+                     const tdq_pages* Kc, const tdq_pages* Vc, void* stream) {
+  if (!K || !V || !Kc || !Vc || !K->data || !V->data || !Kc->data || !Vc->data) return TDQ_ERR_NULL;
+  if (Hq > 0 && (!Q || !Qo || !Q->data || !Qo->data)) return TDQ_ERR_NULL;
+  if (R > 0 && !freq) return TDQ_ERR_NULL;
+  const int rc = check_sequences(seq, true);
+  if (rc != TDQ_OK) return rc;
+  if (!half_type(dt)) return TDQ_ERR_DTYPE;
+  if (T < 1 || T > (int64_t)1 << 30 || Hq < 0 || Hk < 1 || Hq > 4096 || Hk > 4096 || Hq + 2 * Hk > 4096)
+    return TDQ_ERR_SHAPE;
+  if (D < 8 || D > TDQ_MAX_HEAD || D % 8 || R < 0 || R > D || R % 8) return TDQ_ERR_SHAPE;
+  if (R > 0 && pos && (axes < 1 || ld_pos < T)) return TDQ_ERR_SHAPE;
+  if (!(eps >= 0.f) || !isfinite(eps)) return TDQ_ERR_PARAM;
+  if (misaligned(K->data, 2) || misaligned(V->data, 2) || misaligned(Kc->data, 2) || misaligned(Vc->data, 2))
+    return TDQ_ERR_ALIGN;
+  if (Hq > 0 && (misaligned(Q->data, 2) || misaligned(Qo->data, 2))) return TDQ_ERR_ALIGN;
+  if (misaligned(q_weight, 4) || misaligned(k_weight, 4) || misaligned(pos, 4) || misaligned(axis, 4) ||
+      misaligned(freq, 4))
+    return TDQ_ERR_ALIGN;
+  // (a token's place turns all pairs alike)
+  if (launch_append(Hq > 0 ? Q : nullptr, K, V, dt, T, seq, Hq, Hk, D, q_weight, k_weight, eps, R, interleaved != 0,
+                    pos, ld_pos, pos ? axes : 1, axis, freq, Hq > 0 ? Qo : nullptr, Kc, Vc,
+                    static_cast<hipStream_t>(stream)) != hipSuccess)
+    return TDQ_ERR_HIP;
+  return TDQ_OK;
+}
+
+int tdq_page_bounds(const tdq_pages* Kc, tdq_dtype dt, int64_t T, const tdq_sequences* seq, int32_t Hk, int32_t D,
+                    const tdq_heads* lo, const tdq_heads* hi, void* stream) {
+  if (!Kc || !lo || !hi || !Kc->data || !lo->data || !hi->data) return TDQ_ERR_NULL;
+  const int rc = check_sequences(seq, false);
+  if (rc != TDQ_OK) return rc;
+  if (!half_type(dt)) return TDQ_ERR_DTYPE;
+  if (T < 0 || T > (int64_t)1 << 30 || Hk < 1 || Hk > 4096 || D < 8 || D > TDQ_MAX_HEAD || D % 8) return TDQ_ERR_SHAPE;
+  if (misaligned(Kc->data, 2) || misaligned(lo->data, 2) || misaligned(hi->data, 2)) return TDQ_ERR_ALIGN;
+  if (launch_bounds(Kc, dt, T, seq, Hk, D, lo, hi, static_cast<hipStream_t>(stream)) != hipSuccess) return TDQ_ERR_HIP;
+  return TDQ_OK;
+}
+
+static bool paged_shape(int64_t Tq, int32_t Hq, int32_t Hk, int32_t D) {
+  return Tq >= 1 && Tq <= (int64_t)1 << 30 && Hq >= 1 && Hq <= 4096 && Hk >= 1 && Hq % Hk == 0 && D >= 8 &&
+         D <= TDQ_MAX_HEAD && D % 8 == 0;
+}
+
+size_t tdq_select_pages_workspace_bytes(int64_t Tq, int32_t Hk, int32_t columns) {
+  if (Tq < 1 || Tq > (int64_t)1 << 30 || Hk < 1 || Hk > 4096 || columns < 1 || columns > 1 << 26) return 0;
+  return choice_workspace(Tq, Hk, columns);
+}
+
+int tdq_select_pages(const tdq_heads* Q, const tdq_heads* lo, const tdq_heads* hi, tdq_dtype dt, int64_t Tq,
+                     const tdq_sequences* seq, int32_t Hq, int32_t Hk, int32_t D, int32_t causal, int32_t first,
+                     int32_t last, int32_t count, int32_t* chosen, void* workspace, size_t workspace_bytes,
+                     void* stream) {
+  if (!Q || !lo || !hi || !chosen || !Q->data || !lo->data || !hi->data) return TDQ_ERR_NULL;
+  const int rc = check_sequences(seq, true);
+  if (rc != TDQ_OK) return rc;
+  if (!half_type(dt)) return TDQ_ERR_DTYPE;
+  if (!paged_shape(Tq, Hq, Hk, D)) return TDQ_ERR_SHAPE;
+  if (count < 1 || count > 1 << 20 || first < 0 || last < 0 || (int64_t)first + last > count) return TDQ_ERR_PARAM;
+  if (misaligned(Q->data, 2) || misaligned(lo->data, 2) || misaligned(hi->data, 2) || misaligned(chosen, 4))
+    return TDQ_ERR_ALIGN;
+  const size_t need = choice_workspace(Tq, Hk, seq->columns);
+  if (!workspace || workspace_bytes < need || misaligned(workspace, 256)) return TDQ_ERR_WORKSPACE;
+  if (launch_choice(Q, lo, hi, dt, Tq, seq, Hq, Hk, D, causal != 0, first, last, count, chosen, workspace,
+                    static_cast<hipStream_t>(stream)) != hipSuccess)
+    return TDQ_ERR_HIP;
+  return TDQ_OK;
+}
+
+static int check_paged(const tdq_heads* Q, const tdq_pages* Kc, const tdq_pages* Vc, tdq_dtype dt, int64_t Tq,
+                       const tdq_sequences* seq, int32_t Hq, int32_t Hk, int32_t D, float scale, const tdq_heads* O,
+                       const float* lse) {
+  if (!Q || !Kc || !Vc || !O || !Q->data || !Kc->data || !Vc->data || !O->data) return TDQ_ERR_NULL;
+  const int rc = check_sequences(seq, true);
+  if (rc != TDQ_OK) return rc;
+  if (!half_type(dt)) return TDQ_ERR_DTYPE;
+  if (!paged_shape(Tq, Hq, Hk, D)) return TDQ_ERR_SHAPE;
+  if (!isfinite(scale)) return TDQ_ERR_PARAM;
+  if (loose_heads(Q) || loose_heads(O) || loose_pages(Kc) || loose_pages(Vc) || misaligned(lse, 4)) return TDQ_ERR_ALIGN;
+  return TDQ_OK;
+}
+
+static bool chosen_shape(int32_t page_size, int32_t count) {
+  return page_size >= 16 && page_size <= 1024 && (page_size & (page_size - 1)) == 0 && count >= 1 && count <= 1 << 20 &&
+         (int64_t)count * page_size <= (int64_t)1 << 30;
+}
+
+size_t tdq_attention_selected_workspace_bytes(int64_t Tq, int32_t Hq, int32_t Hk, int32_t D, int32_t page_size,
+                                              int32_t count) {
+  return paged_shape(Tq, Hq, Hk, D) && chosen_shape(page_size, count)
+             ? chosen_workspace(Tq, Hq, Hk, D, page_size, count)
+             : 0;
+}
+
+int tdq_attention_selected(const tdq_heads* Q, const tdq_pages* Kc, const tdq_pages* Vc, tdq_dtype dt, int64_t Tq,
+                           const tdq_sequences* seq, int32_t Hq, int32_t Hk, int32_t D, float scale, int32_t causal,
+                           const int32_t* chosen, int32_t count, const tdq_heads* O, float* lse, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  if (!chosen) return TDQ_ERR_NULL;
+  const int rc = check_paged(Q, Kc, Vc, dt, Tq, seq, Hq, Hk, D, scale, O, lse);
+  if (rc != TDQ_OK) return rc;
+  if (!chosen_shape(seq->page_size, count)) return TDQ_ERR_SHAPE;
+  if (misaligned(chosen, 4)) return TDQ_ERR_ALIGN;
+  const size_t need = chosen_workspace(Tq, Hq, Hk, D, seq->page_size, count);
+  if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 256))) return TDQ_ERR_WORKSPACE;
+  if (launch_chosen(Q, Kc, Vc, dt, Tq, seq, Hq, Hk, D, scale, causal != 0, chosen, count, O, lse, workspace,
+                    static_cast<hipStream_t>(stream)) != hipSuccess)
+    return TDQ_ERR_HIP;
+  return TDQ_OK;
+}
+
+// (rows of a line of work are counted in 32 bits)
+static bool paged_rows(int64_t Tq, int32_t Hq, int32_t Hk) { return Tq * (Hq / Hk) <= (int64_t)1 << 31; }
+
+size_t tdq_attention_paged_workspace_bytes(int64_t Tq, int32_t S, int32_t prefixes, int32_t Hq, int32_t Hk, int32_t D) {
+  return paged_shape(Tq, Hq, Hk, D) && paged_rows(Tq, Hq, Hk) && S >= 1 && S <= 1 << 20 && prefixes >= 0 &&
+                 prefixes <= 1 << 20
+             ? paged_workspace(Tq, S, prefixes, Hq, Hk, D)
+             : 0;
+}
+
+int tdq_attention_paged(const tdq_heads* Q, const tdq_pages* Kc, const tdq_pages* Vc, tdq_dtype dt, int64_t Tq,
+                        const tdq_sequences* seq, const tdq_sequences* prefix, int32_t Hq, int32_t Hk, int32_t D,
+                        float scale, int32_t causal, const tdq_heads* O, float* lse, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  int rc = check_paged(Q, Kc, Vc, dt, Tq, seq, Hq, Hk, D, scale, O, lse);
+  if (rc != TDQ_OK) return rc;
+  if (!paged_rows(Tq, Hq, Hk)) return TDQ_ERR_SHAPE;
+  if (prefix) {
+    rc = check_sequences(prefix, true);
+    if (rc != TDQ_OK) return rc;
+    if (prefix->page_size != seq->page_size || prefix->n_pages != seq->n_pages) return TDQ_ERR_SHAPE;
+  }
+  const size_t need = paged_workspace(Tq, seq->S, prefix ? prefix->S : 0, Hq, Hk, D);
+  if (!workspace || workspace_bytes < need || misaligned(workspace, 256)) return TDQ_ERR_WORKSPACE;
+  if (launch_paged(Q, Kc, Vc, dt, Tq, seq, prefix, Hq, Hk, D, scale, causal != 0, O, lse, workspace,
+                   static_cast<hipStream_t>(stream)) != hipSuccess)
+    return TDQ_ERR_HIP;
+  return TDQ_OK;
+}
+
 }  // extern "C"

@@ -2,7 +2,8 @@
 // heads over packed sequences.
 #include <math.h>
 
-#include "tdq_half.hpp"
+#include "tdq_attend.hpp"
+#include "tdq_rotate.hpp"
 
 namespace tdq {
 
@@ -68,9 +69,8 @@ __global__ __launch_bounds__(kRotateThreads) void k_norm_rotate(RotateArgs a, in
     int ax = a.axis ? a.axis[p] : 0;
     ax = ax < 0 ? 0 : ax < a.axes ? ax : a.axes - 1;
     const float angle = (float)a.pos[ax * a.ld_pos + t0 + t] * a.freq[p];
-    const double turns = (double)angle * 0.15915494309189533577;
     float s, c;
-    sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
+    turn_of(angle, &c, &s);
     turn[t][2 * p] = c;
     turn[t][2 * p + 1] = s;
   }
@@ -82,45 +82,7 @@ __global__ __launch_bounds__(kRotateThreads) void k_norm_rotate(RotateArgs a, in
     float(&y)[4] = v.y;
     const int t = (int)((float)i * per), hh = i - t * heads, which = hh >= a.heads[0], h = which ? hh - a.heads[0] : hh;
     T* dst = static_cast<T*>(a.out[which]) + (t0 + t) * a.out_token[which] + h * a.out_head[which];
-    const float* w = a.weight[which];
-    if (w) {
-      float sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sum = fmaf(x[j], x[j], fmaf(y[j], y[j], sum));
-#pragma unroll
-      for (int d = L / 2; d >= 1; d >>= 1) sum += __shfl_xor(sum, d, L);
-      const float r = 1.0f / sqrtf(sum / (float)D + a.eps);
-      if (mine) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          x[j] = x[j] * r * w[e0 + j];
-          y[j] = y[j] * r * w[e1 + j];
-        }
-      }
-    }
-    if (turned) {
-      const float* cs = &turn[t][8 * sub];
-      float z[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) z[j] = cs[j];
-      if constexpr (PAIRS) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float p = x[2 * j], q = x[2 * j + 1], u = y[2 * j], v2 = y[2 * j + 1];
-          x[2 * j] = fmaf(p, z[2 * j], -(q * z[2 * j + 1]));
-          x[2 * j + 1] = fmaf(q, z[2 * j], p * z[2 * j + 1]);
-          y[2 * j] = fmaf(u, z[4 + 2 * j], -(v2 * z[5 + 2 * j]));
-          y[2 * j + 1] = fmaf(v2, z[4 + 2 * j], u * z[5 + 2 * j]);
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float p = x[j], q = y[j];
-          x[j] = fmaf(p, z[2 * j], -(q * z[2 * j + 1]));
-          y[j] = fmaf(q, z[2 * j], p * z[2 * j + 1]);
-        }
-      }
-    }
+    norm_and_turn<L, PAIRS>(x, y, a.weight[which], e0, e1, D, a.eps, mine, turned, &turn[t][8 * sub]);
     if (mine) {
       store_floats<T, 4>(dst + e0, x);
       store_floats<T, 4>(dst + e1, y);
@@ -223,197 +185,6 @@ struct AttendArgs {
   u32 flip;                            // sign bits of two elements if the scale is negative: Q is negated
   int splits;                          // parts that the keys of a sequence are cut into
   float *part_o, *part_ml;             // [Tq Hq][splits][D], and maximum and sum [Tq Hq][splits][2]
-};
-
-// What keys and values past the end of a sequence, or past D, are copied from.
-__device__ u32x4 kZeros[4];
-
-template <typename T>
-struct Mfma;
-template <>
-struct Mfma<_Float16> {
-  typedef h16x8 frag;
-  __device__ static __forceinline__ f32x16 mul(u32x4 a, u32x4 b, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(frag, a), __builtin_bit_cast(frag, b), c, 0, 0, 0);
-  }
-};
-template <>
-struct Mfma<__bf16> {
-  typedef b16x8 frag;
-  __device__ static __forceinline__ f32x16 mul(u32x4 a, u32x4 b, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(frag, a), __builtin_bit_cast(frag, b), c, 0, 0,
-                                                   0);
-  }
-};
-
-__device__ __forceinline__ float other_half(float x) {   // the value of lane ^ 32
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
-}
-__device__ __forceinline__ float max_of_halves(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-
-// Whether a row with maximum m and sum l has no key, or none with a score above -inf.  The maximum
-// alone does not say: it passes over NaN, which the sum does not.
-__device__ __forceinline__ bool no_weight(float m, float l) { return m == -INFINITY && l == 0.f; }
-// Octaves that the reference m is set below the largest score.
-template <typename T>
-constexpr int kLift = __is_same(T, _Float16) ? 7 : 0;
-// Log of the sum of exp(scale * score).
-__device__ __forceinline__ float log_sum(float m, float l, float scale_log2) {
-  return no_weight(m, l) ? -INFINITY : fmaf(m, scale_log2, __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
-}
-
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-// Four elements down a column: 16 lanes give the addresses of 4 rows x 16 columns (a lane 4
-// columns of row lane / 4), lane i gets column i.
-__device__ __forceinline__ u32x2 read_column(u32 lds) {
-  const s16x4 r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)lds);
-  return __builtin_bit_cast(u32x2, r);
-}
-__device__ __forceinline__ u32x4 read_lds16(u32 lds) {
-  return *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)lds;
-}
-
-// Where the 16-byte piece c of row r lies in a row of LDS (c ^ place), so that what an
-// instruction reads at a time spreads over the banks: K by 16 rows of one piece, V by 4 rows of
-// 64 bytes.
-template <int DP>
-__device__ __forceinline__ int place_k(int r) {
-  return DP >= 128 ? r & 15 : DP == 64 ? (r >> 1) & 7 : (r >> 2) & 3;
-}
-template <int DP>
-__device__ __forceinline__ int place_v(int r) {
-  return DP >= 128 ? 4 * (r & 3) : DP == 64 ? 4 * ((r >> 1) & 1) : 0;
-}
-
-// A wavefront's 32 rows: their queries, and the softmax and output so far.
-template <typename T, int DP>
-struct Rows {
-  u32x4 q[DP / 16];                    // operand columns: row lane % 32, elements 16 i + 8 (lane / 32) ..
-  // element j of o[i]: row lane % 32, output 32 i + 8 (j / 4) + 4 (lane / 32) + j % 4
-  f32x16 o[DP / 32];
-  float m, l;                          // reference of the exponents (of the row), sum (of this lane's keys)
-
-  __device__ __forceinline__ void start(const T* qp, int D, u32 flip) {
-    const int half = (threadIdx.x >> 5) & 1;
-#pragma unroll
-    for (int i = 0; i < DP / 16; ++i) {
-      const int c = 16 * i + 8 * half;
-      q[i] = u32x4{0, 0, 0, 0};
-      if (c < D) q[i] = *reinterpret_cast<const u32x4*>(qp + c) ^ flip;
-    }
-#pragma unroll
-    for (int i = 0; i < DP / 32; ++i)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
-    m = -INFINITY;
-    l = 0.f;
-  }
-
-  // LDS addresses that this lane reads of a tile, of K's 16 elements i and of V's 32 outputs i; the
-  // rows of a tile from 32 n on are at the same places 32 n rows further.
-  u32 ka[DP / 16], va[DP / 32];
-  __device__ __forceinline__ void addresses(u32 lk, u32 lv) {
-    const int lane = threadIdx.x & 63, row = lane & 31, half = lane >> 5, tr = lane & 15;
-#pragma unroll
-    for (int i = 0; i < DP / 16; ++i) ka[i] = lk + row * (2 * DP) + 16 * ((2 * i + half) ^ place_k<DP>(row));
-    const int key = 4 * half + (tr >> 2);              // (place_v is the same every four rows)
-#pragma unroll
-    for (int i = 0; i < DP / 32; ++i) {
-      const int c = 4 * i + 2 * ((lane >> 4) & 1) + ((tr & 3) >> 1);
-      va[i] = lv + key * (2 * DP) + 16 * (c ^ place_v<DP>(key)) + 8 * (tr & 1);
-    }
-  }
-  __device__ __forceinline__ void move(int by) {
-#pragma unroll
-    for (int i = 0; i < DP / 16; ++i) ka[i] += by;
-#pragma unroll
-    for (int i = 0; i < DP / 32; ++i) va[i] += by;
-  }
-
-  // Products of 32 keys from row r (a multiple of 32) of a tile on: element j is key
-  // 8 (j / 4) + 4 (lane / 32) + j % 4.
-  __device__ __forceinline__ f32x16 scores(int r) const {
-    f32x16 s;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) s[j] = 0.f;
-#pragma unroll
-    for (int i = 0; i < DP / 16; ++i) s = Mfma<T>::mul(read_lds16(ka[i] + r * (2 * DP)), q[i], s);
-    return s;
-  }
-
-  // Scores -> probabilities, of N times 32 keys from key j0 on; `sees`: how many keys the row
-  // sees (looked at only where `masked`).  lift: kLift octaves as a score.
-  template <int N>
-  __device__ __forceinline__ void softmax(f32x16 (&s)[N], u32 (&p)[N][8], float c, float lift, int j0, int sees,
-                                          bool masked) {
-    const int half = (threadIdx.x >> 5) & 1;
-    if (masked) {
-#pragma unroll
-      for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-          s[n][j] = j0 + 32 * n + 8 * (j / 4) + 4 * half + j % 4 < sees ? s[n][j] : -INFINITY;
-    }
-    float top = s[0][0];
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) top = fmaxf(top, s[n][j]);
-    top = max_of_halves(top);
-    if (__ballot((top - m) * c > 8.0f + kLift<T> || (m == -INFINITY && top > m))) {
-      const float m_new = fmaxf(m, kLift<T> == 0 ? top : top - lift);
-      // (rows that have seen no key yet keep their zeros)
-      const float keep = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - m_new) * c);
-      m = m_new;
-      l *= keep;
-#pragma unroll
-      for (int i = 0; i < DP / 32; ++i) {
-        // In place: from an ordinary product the compiler makes a copy of all of O in every pass, 64
-        // moves.  It does not see what these instructions read and write, so the wait states that it
-        // would put between matrix instructions and them are here, tied to the values: 20 before the
-        // first, as many as the longest matrix instruction needs, and two behind the last.
-        asm volatile("s_nop 15\n\ts_nop 3" : "+v"(o[i]));
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          float e = o[i][j];
-          asm volatile("v_mul_f32 %0, %1, %0" : "+v"(e) : "v"(keep));
-          o[i][j] = e;
-        }
-        asm volatile("s_nop 1" : "+v"(o[i]));
-      }
-    }
-    const float base = m == -INFINITY ? 0.f : -m * c;
-    float sum = 0.f;
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-      for (int j = 0; j < 16; j += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[n][j], c, base));
-        const float p1 = __builtin_amdgcn_exp2f(fmaf(s[n][j + 1], c, base));
-        sum += p0 + p1;
-        p[n][j / 2] = two_rounded<T>(p0, p1);
-      }
-    l += sum;
-  }
-
-  // O^T += V^T P^T for 32 keys from row r (a multiple of 32) of a tile on: an operand has 16 keys,
-  // a lane's 8 of them 4 half .. + 3 and 8 + 4 half .. + 3, as its probabilities lie.
-  __device__ __forceinline__ void values(int r, const u32 (&p)[8]) {
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      const u32x4 pb = {p[4 * n], p[4 * n + 1], p[4 * n + 2], p[4 * n + 3]};
-#pragma unroll
-      for (int i = 0; i < DP / 32; ++i) {
-        const u32x2 x = read_column(va[i] + (r + 16 * n) * (2 * DP));
-        const u32x2 y = read_column(va[i] + (r + 16 * n + 8) * (2 * DP));
-        o[i] = Mfma<T>::mul(u32x4{x[0], x[1], y[0], y[1]}, pb, o[i]);
-      }
-    }
-  }
 };
 
 // The sequence and the tile of a slot: sequence s has the slots from floor(first row / BM) + s
@@ -587,7 +358,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
       u32 p[2][8];
       s[0] = w.scores(0);
       s[1] = w.scores(32);
-      w.softmax(s, p, a.scale_log2, a.lift, j0, sees, j0 + kKeys > all);
+      w.softmax(s, p, a.scale_log2, a.lift, j0 + kKeys > all, [&](int k) { return j0 + k < sees; });
       w.values(0, p[0]);
       w.values(32, p[1]);
     }
@@ -696,7 +467,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     s[0] = w.scores(0);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // K has been read
     if (more) copy_k(i + 4);
-    w.softmax(s, p, a.scale_log2, a.lift, i * kFewKeys, sees, (i + 1) * kFewKeys > all);
+    w.softmax(s, p, a.scale_log2, a.lift, (i + 1) * kFewKeys > all,
+              [&](int k) { return i * kFewKeys + k < sees; });
     if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
     else wait_copies();
     w.values(0, p[0]);

@@ -1,0 +1,566 @@
+// A cache of keys and values in pages: new tokens written to it with norm and rotation on the way, the
+// bounds of its pages, and the pages that a token attends to.
+#include "tdq_pages.hpp"
+#include "tdq_rotate.hpp"
+
+namespace tdq {
+
+// ---------------------------------------------------------------------------
+// append
+// ---------------------------------------------------------------------------
+// The arithmetic of the head norm (tdq_attention.hip) on the rows of a token's queries and keys; its
+// values are copied.  A token is key len - n + i of its sequence (i of n new ones), which says where its
+// keys and values go and, if no other is given, its position.  Every row is read and written once.  A
+// workgroup takes a few whole tokens; a wavefront finds the place of each while the rows are on their
+// way.
+struct AppendArgs {
+  const void* in[3];                   // Q, K, V
+  long long in_token[3], in_head[3];
+  void* out[3];                        // Qo, pages of K, pages of V
+  long long out_token[3], out_head[3], page[3];
+  const float* weight[2];
+  int heads[3];                        // ends of the heads of Q, K and V in a token's row of all
+  Sequences seq;
+  long long T;
+  int D, R, axes;
+  float eps;
+  const int* pos;                      // (nullptr: a token's place in its sequence)
+  long long ld_pos;
+  const int* axis;
+  const float* freq;
+};
+
+constexpr int kAppendThreads = 256;
+constexpr int kAppendTokens = 4;       // most tokens of a workgroup: one a wavefront
+
+template <typename T, int L, bool PAIRS>
+__global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a, int tokens) {
+  __shared__ float turn[kAppendTokens][TDQ_MAX_HEAD];  // cosine and sine of each pair
+  __shared__ int place[kAppendTokens], page[kAppendTokens];   // key of its sequence, page (negative: nowhere, -2: no sequence)
+  const int P = a.R >> 1;
+  const long long t0 = (blockIdx.x + (long long)blockIdx.y * gridDim.x) * tokens;
+  if (t0 >= a.T) return;                               // (a last row of workgroups may be longer than needed)
+  const int here = (int)(a.T - t0 < tokens ? a.T - t0 : tokens);
+  const int sub = threadIdx.x & (L - 1), heads = a.heads[2];
+  const int D = a.D, R = a.R;
+  const bool mine = 8 * sub < D, turned = 8 * sub < R;
+  // 8 elements of a lane: neighbours, or 4 of the first half of the turned ones and their partners
+  const int e0 = PAIRS || !turned ? 8 * sub : 4 * sub, e1 = PAIRS || !turned ? e0 + 4 : P + 4 * sub;
+  // token and head of an item: the quotient of small numbers by a reciprocal just above 1 / heads
+  const float per = 1.0f / (float)heads * 1.000001f;
+  struct Item {
+    u32x2 a, b;
+  };
+  struct Head {
+    int t, which, h;
+  };
+  auto head_of = [&](int i) {
+    const int t = (int)((float)i * per), hh = i - t * heads;
+    const int which = (hh >= a.heads[0]) + (hh >= a.heads[1]);
+    return Head{t, which, which ? hh - a.heads[which - 1] : hh};
+  };
+  auto load = [&](int i, Item& v) {
+    const Head x = head_of(i);
+    const T* src = static_cast<const T*>(a.in[x.which]) + (t0 + x.t) * a.in_token[x.which] + x.h * a.in_head[x.which];
+    v.a = *reinterpret_cast<const u32x2_any*>(src + e0);
+    v.b = *reinterpret_cast<const u32x2_any*>(src + e1);
+  };
+  // The first items are on their way while the places are found and the angles computed, each next
+  // one while one is worked on.
+  const int first = threadIdx.x / L, items = here * heads;
+  Item next = {};
+  if (mine && first < items) load(first, next);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (wave < here) {
+    const Sequences& q = a.seq;
+    const long long t = t0 + wave;
+    const int s = last_at_most(q.S, t, [&](int i) { return start_of(q.cu, i, a.T); });
+    const int from = start_of(q.cu, s, a.T), to = start_of(q.cu, s + 1, a.T);
+    int j = -1, p = -2;
+    if (t >= from && t < to) {
+      const int n = q.len[s];
+      j = (int)((long long)n - to + t);
+      p = -1;
+      if (n >= 0 && j >= 0 && j >> q.shift < q.columns) p = q.table[s * q.ld + (j >> q.shift)];
+      p = p >= 0 && p < q.n_pages ? p : -1;
+    }
+    if ((threadIdx.x & 63) == 0) {
+      place[wave] = j;
+      page[wave] = p;
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < here * P; i += kAppendThreads) {
+    const int t = i / P, p = i - t * P;
+    int ax = a.axis ? a.axis[p] : 0;
+    ax = ax < 0 ? 0 : ax < a.axes ? ax : a.axes - 1;
+    const float angle = (float)(a.pos ? a.pos[ax * a.ld_pos + t0 + t] : place[t]) * a.freq[p];
+    float s, c;
+    turn_of(angle, &c, &s);
+    turn[t][2 * p] = c;
+    turn[t][2 * p + 1] = s;
+  }
+  __syncthreads();
+  const int slots = (1 << a.seq.shift) - 1;
+  for (int i = first; i < items; i += kAppendThreads / L) {
+    const Item v = next;
+    if (mine && i + kAppendThreads / L < items) load(i + kAppendThreads / L, next);
+    const Head at = head_of(i);
+    const int to = page[at.t];
+    if (to < (at.which ? 0 : -1)) continue;            // (the same in all lanes of a head)
+    const long long row = at.which ? to * a.page[at.which] + (place[at.t] & slots) * a.out_token[at.which]
+                                   : (t0 + at.t) * a.out_token[0];
+    T* dst = static_cast<T*>(a.out[at.which]) + row + at.h * a.out_head[at.which];
+    if (at.which == 2) {
+      if (mine) {
+        *reinterpret_cast<u32x2_any*>(dst + e0) = v.a;
+        *reinterpret_cast<u32x2_any*>(dst + e1) = v.b;
+      }
+      continue;
+    }
+    float x[4], y[4];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const f32x2 f = two_floats<T>(v.a[j]), g = two_floats<T>(v.b[j]);
+      x[2 * j] = f[0];
+      x[2 * j + 1] = f[1];
+      y[2 * j] = g[0];
+      y[2 * j + 1] = g[1];
+    }
+    norm_and_turn<L, PAIRS>(x, y, a.weight[at.which], e0, e1, D, a.eps, mine, turned, &turn[at.t][8 * sub]);
+    if (mine) {
+      store_floats<T, 4>(dst + e0, x);
+      store_floats<T, 4>(dst + e1, y);
+    }
+  }
+}
+
+hipError_t launch_append(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, tdq_dtype dt, long long T,
+                         const tdq_sequences* seq, int Hq, int Hk, int D, const float* q_weight, const float* k_weight,
+                         float eps, int R, bool interleaved, const int* pos, long long ld_pos, int axes,
+                         const int* axis, const float* freq, const tdq_heads* Qo, const tdq_pages* Kp,
+                         const tdq_pages* Vp, hipStream_t st) {
+  AppendArgs a;
+  const tdq_heads none = {nullptr, 0, 0};
+  const tdq_heads* in[3] = {Q ? Q : &none, K, V};
+  for (int i = 0; i < 3; ++i) {
+    a.in[i] = in[i]->data;
+    a.in_token[i] = in[i]->token;
+    a.in_head[i] = in[i]->head;
+  }
+  const tdq_heads* q = Qo ? Qo : &none;
+  a.out[0] = q->data;
+  a.out_token[0] = q->token;
+  a.out_head[0] = q->head;
+  a.page[0] = 0;
+  const tdq_pages* out[2] = {Kp, Vp};
+  for (int i = 0; i < 2; ++i) {
+    a.out[i + 1] = out[i]->data;
+    a.out_token[i + 1] = out[i]->token;
+    a.out_head[i + 1] = out[i]->head;
+    a.page[i + 1] = out[i]->page;
+  }
+  a.weight[0] = q_weight;
+  a.weight[1] = k_weight;
+  a.heads[0] = Hq;
+  a.heads[1] = Hq + Hk;
+  a.heads[2] = Hq + 2 * Hk;
+  a.seq = sequences_of(seq);
+  a.T = T;
+  a.D = D;
+  a.R = R;
+  a.axes = axes;
+  a.eps = eps;
+  a.pos = pos;
+  a.ld_pos = ld_pos;
+  a.axis = axis;
+  a.freq = freq;
+  const int tokens = T >= 1024 * kAppendTokens ? kAppendTokens : 1;
+  const dim3 grid = two_axes((T + tokens - 1) / tokens);
+#define TDQ_APPEND_LP(T_, L, PAIRS) \
+  hipLaunchKernelGGL((k_append<T_, L, PAIRS>), grid, dim3(kAppendThreads), 0, st, a, tokens)
+#define TDQ_APPEND_L(T_, L)                      \
+  do {                                           \
+    if (interleaved) TDQ_APPEND_LP(T_, L, true); \
+    else TDQ_APPEND_LP(T_, L, false);            \
+  } while (0)
+#define TDQ_APPEND(T_)                         \
+  do {                                         \
+    if (D <= 32) TDQ_APPEND_L(T_, 4);          \
+    else if (D <= 64) TDQ_APPEND_L(T_, 8);     \
+    else if (D <= 128) TDQ_APPEND_L(T_, 16);   \
+    else TDQ_APPEND_L(T_, 32);                 \
+  } while (0)
+  if (dt == TDQ_F16) TDQ_APPEND(_Float16);
+  else TDQ_APPEND(__bf16);
+#undef TDQ_APPEND
+#undef TDQ_APPEND_L
+#undef TDQ_APPEND_LP
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// bounds of pages
+// ---------------------------------------------------------------------------
+// Smallest and largest value of every channel over the keys of a page that are in use; NaN where one
+// is.  A workgroup has a page and a key head: a lane 8 channels of every 16th row or so (all of them on
+// their way at once), joined in the wavefront by exchanges and between wavefronts in LDS.
+struct BoundsArgs {
+  const void* K;
+  void *lo, *hi;
+  long long k_page, k_token, k_head, lo_page, lo_head, hi_page, hi_head;
+  Sequences seq;
+  long long T, slots;
+  int Hk, D;
+};
+
+// (minimum and maximum that are NaN where one of the two is)
+__device__ __forceinline__ float least(float a, float b) { return __builtin_elementwise_minimum(a, b); }
+__device__ __forceinline__ float most(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+template <typename T, int L>
+__global__ __launch_bounds__(256) void k_bounds(BoundsArgs a) {
+  constexpr int GROUPS = 256 / L;                      // rows at a time
+  __shared__ float part[3][2][8 * L];
+  const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
+  const int h = (int)(id % a.Hk);
+  const long long slot = id / a.Hk;
+  if (slot >= a.slots) return;
+  const Sequences& q = a.seq;
+  int s, b;                                            // sequence and page of it
+  if (q.cu) {
+    // n new tokens lie in no more than n / P + 2 pages: sequence s has the slots from
+    // floor(first token / P) + 2 s on
+    s = last_at_most(q.S, slot, [&](int i) { return (long long)(start_of(q.cu, i, a.T) >> q.shift) + 2ll * i; });
+    const int from = start_of(q.cu, s, a.T), n = start_of(q.cu, s + 1, a.T) - from, len = keys_of(q, s);
+    if (n <= 0) return;
+    const long long i = slot - ((from >> q.shift) + 2ll * s);
+    if (i < 0 || i >= q.columns) return;
+    b = (int)i + ((len > n ? len - n : 0) >> q.shift);
+  } else {
+    s = (int)(slot / q.columns);
+    b = (int)(slot - (long long)s * q.columns);
+  }
+  const int len = keys_of(q, s);
+  if (b >= q.columns || b << q.shift >= len) return;
+  const int page = q.table[s * q.ld + b];
+  if (page < 0 || page >= q.n_pages) return;
+  const int rest = len - (b << q.shift), rows = rest < 1 << q.shift ? rest : 1 << q.shift;
+  const int sub = threadIdx.x & (L - 1), group = threadIdx.x / L, wave = threadIdx.x >> 6;
+  const bool mine = 8 * sub < a.D;
+  float lo[8], hi[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    lo[j] = INFINITY;
+    hi[j] = -INFINITY;
+  }
+  const T* src = static_cast<const T*>(a.K) + page * a.k_page + h * a.k_head + 8 * sub;
+  if (mine) {
+#pragma unroll 4
+    for (int r = group; r < rows; r += GROUPS) {
+      float x[8];
+      load_floats<T, 8>(src + r * a.k_token, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        lo[j] = least(lo[j], x[j]);
+        hi[j] = most(hi[j], x[j]);
+      }
+    }
+  }
+#pragma unroll
+  for (int d = L; d < 64; d <<= 1)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      lo[j] = least(lo[j], __shfl_xor(lo[j], d, 64));
+      hi[j] = most(hi[j], __shfl_xor(hi[j], d, 64));
+    }
+  if (wave > 0 && (threadIdx.x & 63) < L) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      part[wave - 1][0][8 * sub + j] = lo[j];
+      part[wave - 1][1][8 * sub + j] = hi[j];
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < L && mine) {
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        lo[j] = least(lo[j], part[w][0][8 * sub + j]);
+        hi[j] = most(hi[j], part[w][1][8 * sub + j]);
+      }
+    store_floats<T, 8>(static_cast<T*>(a.lo) + page * a.lo_page + h * a.lo_head + 8 * sub, lo);
+    store_floats<T, 8>(static_cast<T*>(a.hi) + page * a.hi_page + h * a.hi_head + 8 * sub, hi);
+  }
+}
+
+hipError_t launch_bounds(const tdq_pages* K, tdq_dtype dt, long long T, const tdq_sequences* seq, int Hk, int D,
+                         const tdq_heads* lo, const tdq_heads* hi, hipStream_t st) {
+  BoundsArgs a;
+  a.K = K->data;
+  a.k_page = K->page;
+  a.k_token = K->token;
+  a.k_head = K->head;
+  a.lo = lo->data;
+  a.lo_page = lo->token;
+  a.lo_head = lo->head;
+  a.hi = hi->data;
+  a.hi_page = hi->token;
+  a.hi_head = hi->head;
+  a.seq = sequences_of(seq);
+  a.T = T;
+  a.slots = a.seq.cu ? (T >> a.seq.shift) + 2ll * a.seq.S : (long long)a.seq.S * a.seq.columns;
+  a.Hk = Hk;
+  a.D = D;
+  const dim3 grid = two_axes(a.slots * Hk);
+#define TDQ_BOUNDS(T_)                                                                      \
+  do {                                                                                      \
+    if (D <= 32) hipLaunchKernelGGL((k_bounds<T_, 4>), grid, dim3(256), 0, st, a);          \
+    else if (D <= 64) hipLaunchKernelGGL((k_bounds<T_, 8>), grid, dim3(256), 0, st, a);     \
+    else if (D <= 128) hipLaunchKernelGGL((k_bounds<T_, 16>), grid, dim3(256), 0, st, a);   \
+    else hipLaunchKernelGGL((k_bounds<T_, 32>), grid, dim3(256), 0, st, a);                 \
+  } while (0)
+  if (dt == TDQ_F16) TDQ_BOUNDS(_Float16);
+  else TDQ_BOUNDS(__bf16);
+#undef TDQ_BOUNDS
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// choice of pages
+// ---------------------------------------------------------------------------
+//   score[t, h, b] = max over the query heads e of h of sum_d max(q_d, 0) hi_d + min(q_d, 0) lo_d
+// with q = Q[t, e] and the bounds of page b: no product of q with a key of the page is larger.
+// The choice depends on which of two scores is larger, so they must not depend on the order of the sum:
+// products of two 16-bit types are added in binary64, which holds nearly all such sums without rounding,
+// and the result is rounded to binary32.  L lanes have a page's 16 bytes each of both bounds, HEADS heads
+// share them; the heads' parts stay in registers for all pages.
+struct ChoiceArgs {
+  const void *Q, *lo, *hi;
+  long long q_token, q_head, lo_page, lo_head, hi_page, hi_head;
+  Sequences seq;
+  long long Tq;
+  int Hk, group, D, causal, first, last, count, chunks;
+  float* score;                        // [Tq Hk, columns]
+  int* chosen;                         // [Tq Hk, count]
+};
+
+// The sequence of a token and how many keys it sees (none: a token of no sequence).
+struct Seen {
+  int seq, keys;
+};
+__device__ __forceinline__ Seen seen_by(const Sequences& q, long long t, long long T, int causal) {
+  const int s = last_at_most(q.S, t, [&](int i) { return start_of(q.cu, i, T); });
+  const int from = start_of(q.cu, s, T), to = start_of(q.cu, s + 1, T), n = keys_of(q, s);
+  if (t < from || t >= to) return {s, -1};
+  const long long e = causal ? n - to + t + 1 : n;
+  return {s, e < 0 ? 0 : (int)e};
+}
+
+constexpr int kScorePages = 128;       // pages of a workgroup
+
+template <typename T, int L, int HEADS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_score(ChoiceArgs a) {
+  __shared__ float top[kScorePages];
+  const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
+  const int h = (int)(id % a.Hk), chunk = (int)(id / a.Hk % a.chunks);
+  const long long t = id / a.Hk / a.chunks;
+  if (t >= a.Tq) return;
+  const Sequences& q = a.seq;
+  const Seen me = seen_by(q, t, a.Tq, a.causal);
+  const int pages = me.keys <= 0 ? 0 : ((me.keys - 1) >> q.shift) + 1, b0 = chunk * kScorePages;
+  if (b0 >= pages) return;
+  const int here = pages - b0 < kScorePages ? pages - b0 : kScorePages;
+  const int sub = threadIdx.x & (L - 1), group = threadIdx.x / L;
+  const bool mine = 8 * sub < a.D;
+  const int* line = q.table + me.seq * q.ld + b0;
+  float* out = a.score + (t * a.Hk + h) * q.columns + b0;
+  for (int e0 = 0; e0 < a.group; e0 += HEADS) {
+    double up[HEADS][8], down[HEADS][8];
+#pragma unroll
+    for (int e = 0; e < HEADS; ++e) {
+      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      // (past the last head: the last again, which changes no maximum)
+      const int head = h * a.group + (e0 + e < a.group ? e0 + e : a.group - 1);
+      if (mine) load_floats<T, 8>(static_cast<const T*>(a.Q) + t * a.q_token + head * a.q_head + 8 * sub, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        up[e][j] = x[j] < 0.f ? 0.0 : (double)x[j];
+        down[e][j] = x[j] > 0.f ? 0.0 : (double)x[j];
+      }
+    }
+    for (int b = group; b < here; b += 256 / L) {
+      const int page = line[b];
+      if (page < 0 || page >= q.n_pages) continue;       // (the same in the L lanes)
+      float lo[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, hi[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (mine) {
+        load_floats<T, 8>(static_cast<const T*>(a.lo) + page * a.lo_page + h * a.lo_head + 8 * sub, lo);
+        load_floats<T, 8>(static_cast<const T*>(a.hi) + page * a.hi_page + h * a.hi_head + 8 * sub, hi);
+      }
+      float best = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < HEADS; ++e) {
+        double sum = 0.0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum = fma(up[e][j], (double)hi[j], fma(down[e][j], (double)lo[j], sum));
+#pragma unroll
+        for (int d = L / 2; d >= 1; d >>= 1) sum += __shfl_xor(sum, d, L);
+        best = most(best, (float)sum);
+      }
+      if (sub == 0) {
+        if (e0 > 0) best = most(best, top[b]);
+        top[b] = best;                                   // (read by this lane alone)
+        if (e0 + HEADS >= a.group) out[b] = best;
+      }
+    }
+  }
+}
+
+// The pages of a token and key head: a radix select of the count-th largest key among the scores'
+// bit patterns (8 bits a pass), then the pages above it and the first ones at it, ascending.  Keys of up
+// to 2048 pages stay in registers.
+__global__ __launch_bounds__(256) void k_choose(ChoiceArgs a) {
+  constexpr int HELD = 8;
+  __shared__ u32 bins[256];
+  __shared__ u32 found[2];                               // digit, how many of the larger ones
+  __shared__ int count[2][4];
+  const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
+  if (id >= a.Tq * a.Hk) return;
+  const Sequences& q = a.seq;
+  const Seen me = seen_by(q, id / a.Hk, a.Tq, a.causal);
+  if (me.keys < 0) return;                               // (no sequence: its pages are left as they are)
+  const int pages = me.keys == 0 ? 0 : ((me.keys - 1) >> q.shift) + 1;
+  const int* line = q.table + me.seq * q.ld;
+  const float* score = a.score + id * q.columns;
+  int* out = a.chosen + id * a.count;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  // larger for a larger score; 0: not there; the largest: always taken; NaN above all numbers
+  auto read = [&](int b) -> u32 {
+    if (b >= pages) return 0;
+    const int page = line[b];
+    if (page < 0 || page >= q.n_pages) return 0;
+    if (b < a.first || b >= pages - a.last) return 0xFFFFFFFFu;
+    const float s = score[b];
+    if (s != s) return 0xFFFFFFFEu;
+    const u32 u = __float_as_uint(s + 0.f);              // (-0 as 0)
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+  };
+  u32 held[HELD];
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) held[i] = read(256 * i + tid);
+  auto each = [&](auto f) {                              // all pages, 256 at a time
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+      if (256 * i < pages) f(256 * i + tid, held[i]);
+    for (int b = 256 * HELD; b < pages; b += 256) f(b + tid, read(b + tid));
+  };
+  u32 prefix = 0, want = (u32)a.count;                   // the want-th largest of the keys that begin with prefix
+  bool all = pages <= a.count;
+  for (int shift = 24; shift >= 0 && !all; shift -= 8) {
+    bins[tid] = 0;
+    __syncthreads();
+    each([&](int, u32 k) {
+      if (k != 0 && (shift == 24 || k >> (shift + 8) == prefix >> (shift + 8))) atomicAdd(&bins[k >> shift & 255], 1u);
+    });
+    __syncthreads();
+    if (wave == 0) {
+      u32 c[4], sum = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        c[i] = bins[4 * lane + i];
+        sum += c[i];
+      }
+      u32 upto = sum;                                    // of this lane's bins and all larger ones
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const u32 o = __shfl_down(upto, d, 64);
+        if (lane + d < 64) upto += o;
+      }
+      u32 above = upto - sum;
+      if (lane == 0 && upto < want) found[0] = 256;      // fewer keys than wanted: all of them
+#pragma unroll
+      for (int i = 3; i >= 0; --i) {
+        if (above < want && above + c[i] >= want) {
+          found[0] = 4 * lane + i;
+          found[1] = above;
+        }
+        above += c[i];
+      }
+    }
+    __syncthreads();
+    if (found[0] == 256) {
+      all = true;
+    } else {
+      prefix |= found[0] << shift;
+      want -= found[1];
+    }
+    __syncthreads();
+  }
+  // all: every key that is there; else those above prefix, and the first `want` of those that are equal
+  const u32 limit = all ? 0 : prefix;
+  int taken = 0, equal = 0;
+  each([&](int b, u32 k) {
+    const bool same = !all && k == limit;
+    const unsigned long long eq = __ballot(same);
+    if (lane == 0) count[0][wave] = __popcll(eq);
+    __syncthreads();
+    int before = equal;
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) before += count[0][w];
+      equal += count[0][w];
+    }
+    const unsigned long long below = (1ull << lane) - 1;
+    const bool take = k > limit || (same && before + __popcll(eq & below) < (int)want);
+    const unsigned long long tk = __ballot(take);
+    if (lane == 0) count[1][wave] = __popcll(tk);
+    __syncthreads();
+    int at = taken;
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) at += count[1][w];
+      taken += count[1][w];
+    }
+    if (take) out[at + __popcll(tk & below)] = b;
+  });
+  for (int i = taken + tid; i < a.count; i += 256) out[i] = -1;
+}
+
+size_t choice_workspace(long long Tq, int Hk, int columns) { return (size_t)Tq * Hk * columns * sizeof(float); }
+
+hipError_t launch_choice(const tdq_heads* Q, const tdq_heads* lo, const tdq_heads* hi, tdq_dtype dt, long long Tq,
+                         const tdq_sequences* seq, int Hq, int Hk, int D, bool causal, int first, int last, int count,
+                         int* chosen, void* workspace, hipStream_t st) {
+  ChoiceArgs a;
+  a.Q = Q->data;
+  a.q_token = Q->token;
+  a.q_head = Q->head;
+  a.lo = lo->data;
+  a.lo_page = lo->token;
+  a.lo_head = lo->head;
+  a.hi = hi->data;
+  a.hi_page = hi->token;
+  a.hi_head = hi->head;
+  a.seq = sequences_of(seq);
+  a.Tq = Tq;
+  a.Hk = Hk;
+  a.group = Hq / Hk;
+  a.D = D;
+  a.causal = causal;
+  a.first = first;
+  a.last = last;
+  a.count = count;
+  a.chunks = (seq->columns + kScorePages - 1) / kScorePages;
+  a.score = static_cast<float*>(workspace);
+  a.chosen = chosen;
+  const dim3 grid = two_axes(Tq * Hk * a.chunks);
+#define TDQ_SCORE_L(T_, L)                                                                                      do {                                                                                                            if (a.group == 1) hipLaunchKernelGGL((k_score<T_, L, 1>), grid, dim3(256), 0, st, a);                         else if (a.group == 2) hipLaunchKernelGGL((k_score<T_, L, 2>), grid, dim3(256), 0, st, a);                    else hipLaunchKernelGGL((k_score<T_, L, 4>), grid, dim3(256), 0, st, a);                                    } while (0)
+#define TDQ_SCORE(T_)                          do {                                           if (D <= 32) TDQ_SCORE_L(T_, 4);             else if (D <= 64) TDQ_SCORE_L(T_, 8);        else if (D <= 128) TDQ_SCORE_L(T_, 16);      else TDQ_SCORE_L(T_, 32);                  } while (0)
+  if (dt == TDQ_F16) TDQ_SCORE(_Float16);
+  else TDQ_SCORE(__bf16);
+#undef TDQ_SCORE
+#undef TDQ_SCORE_L
+  hipLaunchKernelGGL(k_choose, two_axes(Tq * Hk), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace tdq

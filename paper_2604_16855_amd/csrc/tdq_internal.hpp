@@ -250,4 +250,25 @@ hipError_t launch_attention(const tdq_heads* Q, const tdq_heads* K, const tdq_he
                             long long Tk, int S, const int* cu_q, const int* cu_k, const int* len_k, int Hq, int Hk, int D, float scale,
                             bool causal, const tdq_heads* O, float* lse, void* workspace, hipStream_t st);
 
+// ---- a cache in pages ----------------------------------------------------------
+hipError_t launch_append(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V, tdq_dtype dt, long long T,
+                         const tdq_sequences* seq, int Hq, int Hk, int D, const float* q_weight, const float* k_weight,
+                         float eps, int R, bool interleaved, const int* pos, long long ld_pos, int axes,
+                         const int* axis, const float* freq, const tdq_heads* Qo, const tdq_pages* Kp,
+                         const tdq_pages* Vp, hipStream_t st);
+hipError_t launch_bounds(const tdq_pages* K, tdq_dtype dt, long long T, const tdq_sequences* seq, int Hk, int D,
+                         const tdq_heads* lo, const tdq_heads* hi, hipStream_t st);
+size_t choice_workspace(long long Tq, int Hk, int columns);
+hipError_t launch_choice(const tdq_heads* Q, const tdq_heads* lo, const tdq_heads* hi, tdq_dtype dt, long long Tq,
+                         const tdq_sequences* seq, int Hq, int Hk, int D, bool causal, int first, int last, int count,
+                         int* chosen, void* workspace, hipStream_t st);
+size_t chosen_workspace(long long Tq, int Hq, int Hk, int D, int page_size, int count);
+hipError_t launch_chosen(const tdq_heads* Q, const tdq_pages* K, const tdq_pages* V, tdq_dtype dt, long long Tq,
+                         const tdq_sequences* seq, int Hq, int Hk, int D, float scale, bool causal, const int* chosen,
+                         int count, const tdq_heads* O, float* lse, void* workspace, hipStream_t st);
+size_t paged_workspace(long long Tq, int S, int prefixes, int Hq, int Hk, int D);
+hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages* V, tdq_dtype dt, long long Tq,
+                        const tdq_sequences* seq, const tdq_sequences* prefix, int Hq, int Hk, int D, float scale,
+                        bool causal, const tdq_heads* O, float* lse, void* workspace, hipStream_t st);
+
 }  // namespace tdq

@@ -1,0 +1,999 @@
+// Softmax attention over the keys and values of a cache in pages: whole sequences behind prefixes that
+// they may share, and the pages chosen for every token and key head.
+//
+// Rows, tiles and arithmetic are those of the packed attention (tdq_attention.hip): the query heads of a
+// key head are rows of one tile, a wavefront has 32 of them.  Here the keys of a tile come in granules of
+// 16, the smallest page, each from where the table says.
+#include "tdq_attend.hpp"
+#include "tdq_pages.hpp"
+
+namespace tdq {
+
+constexpr int kGranule = 16, kGranuleBits = 4;
+constexpr int kNowhere = 1 << 30;      // key of a granule that no row sees (a page that is not there)
+
+// Where a granule is: its page (negative: not there), and the key that its first row is.
+struct Granule {
+  int page, key;
+};
+
+// One of the cache's two tensors.
+struct Pages {
+  const void* data;
+  long long page, token, head;
+};
+
+// Copies of a granule's rows to LDS, 64 lanes with 16 bytes each a copy; rows of LDS have DP elements,
+// their pieces at PLACE.
+template <typename T, int DP, int PLACE(int)>
+struct GranuleCopy {
+  static constexpr int PIECES = DP / 8, ROWS = 64 / PIECES, N = kGranule / ROWS;
+  u32 off[N];                          // bytes from the granule's first row (whole granules)
+  u32 mine;                            // bit i: whether the head has what this lane copies in copy i
+
+  __device__ __forceinline__ GranuleCopy(long long token, int D) {
+    const int lane = threadIdx.x & 63;
+    mine = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int row = i * ROWS + lane / PIECES, piece = (lane % PIECES) ^ PLACE(row);
+      off[i] = (u32)(row * token * 2) + 16 * piece;
+      mine |= (u32)(8 * piece < D) << i;
+    }
+  }
+  // All rows; where D < DP the pieces past it keep what LDS holds.
+  __device__ __forceinline__ void whole(const T* first, u32 lds, bool full) const {
+    if (full) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) copy_to_lds(first, off[i], lds + 1024 * i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (mine >> i & 1) copy_to_lds(first, off[i], lds + 1024 * i);
+    }
+  }
+  // The first `left` rows, zeros behind them and past D.
+  __device__ __forceinline__ void some(const T* first, long long token, int left, u32 lds) const {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int row = i * ROWS + lane / PIECES, piece = (lane % PIECES) ^ PLACE(row);
+      const T* p = first + row * token + 8 * piece;
+      copy_to_lds(row < left && (mine >> i & 1) ? (const void*)p : (const void*)kZeros, lds + 1024 * i);
+    }
+  }
+};
+
+// The granules of a sequence, in order.
+struct Line {
+  const int* table;                    // the sequence's pages
+  int shift, n_pages, keys;
+  __device__ __forceinline__ Granule operator()(int i) const {   // (any i, as long as there is a key)
+    const int last = (keys - 1) >> kGranuleBits, at = i < last ? i : last;
+    const int page = load_scalar(table + (at >> (shift - kGranuleBits)));
+    const bool there = i <= last && page >= 0 && page < n_pages;
+    return {there ? page : -1, there ? i << kGranuleBits : kNowhere};
+  }
+};
+
+// The granules of a list of pages of a sequence.
+struct Chosen {
+  const int *list, *table;
+  int count, shift, n_pages, keys;
+  __device__ __forceinline__ Granule operator()(int i) const {
+    const int bits = shift - kGranuleBits, n = i >> bits, at = n < count ? n : count - 1;
+    const int b = load_scalar(list + at), last = (keys - 1) >> shift;
+    const int page = load_scalar(table + (b < 0 ? 0 : b < last ? b : last));
+    const bool there = n < count && b >= 0 && b <= last && page >= 0 && page < n_pages;
+    return {there ? page : -1, there ? (b << shift) + ((i << kGranuleBits) & ((1 << shift) - 1)) : kNowhere};
+  }
+};
+
+// What copies and reads the granules of one key head.
+template <typename T, int DP>
+struct Store {
+  const T *K, *V;                      // of this head
+  long long k_page, k_token, v_page, v_token;
+  int shift, D;
+  bool quick;                          // 16 rows are within 32-bit offsets
+  GranuleCopy<T, DP, place_k<DP>> ko;
+  GranuleCopy<T, DP, place_v<DP>> vo;
+  __device__ __forceinline__ Store(const Pages& k, const Pages& v, int h, int shift, int D)
+      : K(static_cast<const T*>(k.data) + h * k.head),
+        V(static_cast<const T*>(v.data) + h * v.head),
+        k_page(k.page),
+        k_token(k.token),
+        v_page(v.page),
+        v_token(v.token),
+        shift(shift),
+        D(D),
+        quick(k.token >= 0 && v.token >= 0 && k.token < 1 << 24 && v.token < 1 << 24),
+        ko(k.token, D),
+        vo(v.token, D) {}
+  __device__ __forceinline__ int row(const Granule& g) const { return g.key & ((1 << shift) - 1); }
+  // rows of the sequence in a granule; none of one that is not there
+  __device__ __forceinline__ void copy_k(const Granule& g, int keys, u32 lds) const {
+    const T* first = K + (g.page < 0 ? 0 : g.page * k_page + row(g) * k_token);
+    if (quick && keys - g.key >= kGranule) ko.whole(first, lds, D == DP);
+    else ko.some(first, k_token, keys - g.key, lds);
+  }
+  __device__ __forceinline__ void copy_v(const Granule& g, int keys, u32 lds) const {
+    const T* first = V + (g.page < 0 ? 0 : g.page * v_page + row(g) * v_token);
+    if (quick && keys - g.key >= kGranule) vo.whole(first, lds, D == DP);
+    else vo.some(first, v_token, keys - g.key, lds);
+  }
+};
+
+// Where a tile's result goes: to O and lse, or, of a part of the keys, its sums in binary32.
+template <typename T>
+struct Target {
+  T* O;                                // of the tile's first token and the key head's first query head
+  float* lse;
+  long long o_token, o_head;
+  int Hq, group, first;                // first: row of the first token that the tile begins with
+  float *po, *pml;                     // parts (or nullptr): row r at r * D and 2 * r
+  float scale_log2;
+  int D;
+  __device__ __forceinline__ void split(int r, int* token, int* head) const {
+    *token = (first + r) / group;
+    *head = first + r - *token * group;
+  }
+};
+
+constexpr int kTileKeys = 64, kManyRows = 128, kFewRows = 32, kFewKeys = 32;
+template <int DP>
+constexpr int kStages = DP <= 128 ? 2 : 1;
+template <int DP>
+struct Shared {
+  union {
+    uint8_t many[kStages<DP>][2][kTileKeys * 2 * DP];  // [stage][K, V]
+    uint8_t few[4][2][kFewKeys * 2 * DP];              // [wavefront][K, V]
+    float o[4][32][DP + 4];                            // parts of the output, rows 16 bytes apart in the banks
+  };
+  float ml[4][32][2];
+};
+
+// Zeros where a whole granule's copies leave LDS alone and products of K read it.
+template <int DP>
+__device__ __forceinline__ void clear(Shared<DP>& sh) {
+  __syncthreads();
+  u32x4* p = reinterpret_cast<u32x4*>(&sh);
+  for (int i = threadIdx.x; i < (int)(sizeof(sh.few) / 16); i += 256) p[i] = u32x4{0, 0, 0, 0};
+  __syncthreads();
+}
+
+// Up to 128 rows by four wavefronts that share tiles of 64 keys, the next tile on its way while one is
+// worked on; key tiles from lo to hi.  A wavefront copies one granule of each tile.
+template <typename T, int DP, int DC, typename G>
+__device__ __forceinline__ void attend_many(Shared<DP>& sh, const Store<T, DP>& store, const G& where, const T* qp,
+                                            int sees, int all, int last, int keys, int lo, int hi, int rows, u32 flip,
+                                            float lift, const Target<T>& to) {
+  constexpr int BYTES = kGranule * 2 * DP;             // of a granule in LDS
+  constexpr int STAGES = kStages<DP>;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+  Rows<T, DP, DC> w;
+  w.start(qp, store.D, flip);
+  w.addresses(lds_address(sh.many[0][0]), lds_address(sh.many[0][1]));
+  struct Four {
+    Granule own;
+    int key[4];
+  };
+  auto look = [&](int i) {
+    Four f;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) f.key[g] = where(4 * i + g).key;
+    f.own = where(4 * i + wave);
+    return f;
+  };
+  auto copy = [&](const Granule& g, int stage) {
+    store.copy_k(g, keys, lds_address(sh.many[stage][0]) + wave * BYTES);
+    store.copy_v(g, keys, lds_address(sh.many[stage][1]) + wave * BYTES);
+  };
+  Four now = {}, next = {};
+  if (lo < hi) now = look(lo);
+  if (STAGES == 2 && lo < hi) {
+    copy(now.own, 0);
+    if (lo + 1 < hi) next = look(lo + 1);
+  }
+  for (int i = lo; i < hi; ++i) {
+    const int stage = STAGES == 2 ? (i - lo) & 1 : 0;
+    if (STAGES == 1) {
+      __syncthreads();                                 // the last tile has been read
+      copy(now.own, 0);
+      if (i + 1 < hi) next = look(i + 1);
+    }
+    wait_copies();
+    __syncthreads();
+    if (STAGES == 2 && i + 1 < hi) copy(next.own, stage ^ 1);
+    if (i * kTileKeys < last) {
+      f32x16 s[2];
+      u32 p[2][8];
+      s[0] = w.scores(0);
+      s[1] = w.scores(32);
+      bool masked = false;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) masked |= now.key[g] + kGranule > all;
+      w.softmax(s, p, to.scale_log2, lift, masked,
+                [&](int k) { return now.key[k / kGranule] + k % kGranule < sees; });
+      w.values(0, p[0]);
+      w.values(32, p[1]);
+    }
+    now = next;
+    if (STAGES == 2) {
+      if (i + 2 < hi) next = look(i + 2);
+      w.move(stage ? -(int)sizeof(sh.many[0]) : (int)sizeof(sh.many[0]));
+    }
+  }
+
+  const float l = w.l + other_half(w.l);
+  const int r = wave * 32 + (lane & 31);
+  if (r >= rows) return;
+  // a row that sees no key: zeros, and -inf (its sums may hold 0 * NaN from values that others see)
+  const bool none = no_weight(w.m, l);
+  if (__ballot(none)) {                                // (hardly ever: no select in the ordinary way)
+#pragma unroll
+    for (int i = 0; i < DC / 32; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) w.o[i][j] = none ? 0.f : w.o[i][j];
+  }
+  if (to.po) {
+    float* po = to.po + (long long)r * to.D;
+#pragma unroll
+    for (int i = 0; i < DC / 32; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; j += 4) {
+        const int c = 32 * i + 2 * j + 4 * half;
+        if (c < to.D) *reinterpret_cast<f32x4*>(po + c) = f32x4{w.o[i][j], w.o[i][j + 1], w.o[i][j + 2], w.o[i][j + 3]};
+      }
+    if (half == 0) *reinterpret_cast<f32x2*>(to.pml + 2 * r) = f32x2{w.m, l};
+    return;
+  }
+  const float inv = none ? 0.f : 1.0f / l;
+  int token, head;
+  to.split(r, &token, &head);
+  T* op = to.O + token * to.o_token + head * to.o_head;
+#pragma unroll
+  for (int i = 0; i < DC / 32; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; j += 4) {
+      const int c = 32 * i + 2 * j + 4 * half;
+      if (c < to.D) {
+        const float y[4] = {w.o[i][j] * inv, w.o[i][j + 1] * inv, w.o[i][j + 2] * inv, w.o[i][j + 3] * inv};
+        store_floats<T, 4>(op + c, y);
+      }
+    }
+  if (to.lse && half == 0) to.lse[(long long)token * to.Hq + head] = log_sum(w.m, l, to.scale_log2);
+}
+
+// Up to 32 rows: the wavefronts share out the tiles of 32 keys from lo to hi, each copying its own, K of
+// the next while it works on V of this and the other way round; their parts are joined in LDS.
+template <typename T, int DP, int DC, typename G>
+__device__ __forceinline__ void attend_few(Shared<DP>& sh, const Store<T, DP>& store, const G& where, const T* qp,
+                                           int sees, int all, int keys, int lo, int hi, int rows, u32 flip, float lift,
+                                           const Target<T>& to) {
+  constexpr int BYTES = kGranule * 2 * DP, COPIES = 2 * GranuleCopy<T, DP, place_k<DP>>::N;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Rows<T, DP, DC> w;
+  w.start(qp, store.D, flip);
+  const u32 lk = lds_address(sh.few[wave][0]), lv = lds_address(sh.few[wave][1]);
+  w.addresses(lk, lv);
+  struct Two {
+    Granule g[2];
+  };
+  auto look = [&](int i) { return Two{{where(2 * i), where(2 * i + 1)}}; };
+  auto copy_k = [&](const Two& t) {
+    store.copy_k(t.g[0], keys, lk);
+    store.copy_k(t.g[1], keys, lk + BYTES);
+  };
+  auto copy_v = [&](const Two& t) {
+    store.copy_v(t.g[0], keys, lv);
+    store.copy_v(t.g[1], keys, lv + BYTES);
+  };
+  int i = lo + wave;
+  if (i < hi) {
+    Two now = look(i), next = now;
+    copy_k(now);
+    copy_v(now);
+    if (i + 4 < hi) next = look(i + 4);
+    for (; i < hi; i += 4) {
+      const bool more = i + 4 < hi;
+      // (copies arrive in order: all but the last COPIES, those of V, are there)
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
+      f32x16 s[1];
+      u32 p[1][8];
+      s[0] = w.scores(0);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // K has been read
+      if (more) copy_k(next);
+      const bool masked = now.g[0].key + kGranule > all || now.g[1].key + kGranule > all;
+      w.softmax(s, p, to.scale_log2, lift, masked,
+                [&](int k) { return now.g[k / kGranule].key + k % kGranule < sees; });
+      if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
+      else wait_copies();
+      w.values(0, p[0]);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // V has been read
+      if (more) copy_v(next);
+      now = next;
+      if (i + 8 < hi) next = look(i + 8);
+    }
+  }
+
+  // join the wavefronts' parts: they refer to different maxima
+  const float l = w.l + other_half(w.l);
+  if (lane < 32) {
+    sh.ml[wave][lane][0] = w.m;
+    sh.ml[wave][lane][1] = l;
+  }
+  __syncthreads();                                       // (nobody reads K and V any more)
+  float m = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int v = 0; v < 4; ++v) m = fmaxf(m, sh.ml[v][lane & 31][0]);
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    const float mv = sh.ml[v][lane & 31][0], lv = sh.ml[v][lane & 31][1];
+    if (!no_weight(mv, lv)) sum += lv * __builtin_amdgcn_exp2f((mv - m) * to.scale_log2);
+  }
+  // (a part in which a row sees no key is 0: its sums may hold 0 * NaN from values that others see)
+  const bool none = no_weight(w.m, l);
+  const float keep = __builtin_amdgcn_exp2f((w.m - m) * to.scale_log2);
+  if ((lane & 31) < rows) {
+#pragma unroll
+    for (int d = 0; d < DC / 32; ++d)
+#pragma unroll
+      for (int j = 0; j < 16; j += 4) {
+        f32x4 y;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) y[u] = none ? 0.f : w.o[d][j + u] * keep;
+        *reinterpret_cast<f32x4*>(&sh.o[wave][lane & 31][32 * d + 2 * j + 4 * (lane >> 5)]) = y;
+      }
+  }
+  __syncthreads();
+  if (wave == 0 && lane < 32) {                          // for the threads that store a row
+    sh.ml[0][lane][0] = m;
+    sh.ml[0][lane][1] = sum;
+  }
+  __syncthreads();
+  constexpr int QUADS = DC / 4;
+  for (int e = threadIdx.x; e < rows * QUADS; e += 256) {
+    const int r = e / QUADS, c = 4 * (e % QUADS);
+    if (c >= to.D) continue;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int v = 0; v < 4; ++v) y += *reinterpret_cast<const f32x4*>(&sh.o[v][r][c]);
+    const float mr = sh.ml[0][r][0], lr = sh.ml[0][r][1];
+    if (to.po) {
+      *reinterpret_cast<f32x4*>(to.po + (long long)r * to.D + c) = y;
+      if (c == 0) *reinterpret_cast<f32x2*>(to.pml + 2 * r) = f32x2{mr, lr};
+    } else {
+      const float inv = no_weight(mr, lr) ? 0.f : 1.0f / lr;
+      const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
+      int token, head;
+      to.split(r, &token, &head);
+      store_floats<T, 4>(to.O + token * to.o_token + head * to.o_head + c, z);
+      if (to.lse && c == 0) to.lse[(long long)token * to.Hq + head] = log_sum(mr, lr, to.scale_log2);
+    }
+  }
+  __syncthreads();                                       // (LDS is free for a next tile)
+}
+
+// Joins the parts of a row, by a wavefront: `part(i)` says where the sums and the values of part i < n are
+// (nullptr: there is none).  A group of lanes has four outputs each of one part, as many parts at a time
+// as there are groups, all of them on their way at once; weights were found before, a lane a part.
+struct Part {
+  const float *ml, *o;
+};
+constexpr int kMaxParts = 512 + 4;
+template <typename T, typename F>
+__device__ __forceinline__ void join_row(float* weight, int n, F part, int D, float scale_log2, T* op, float* lse) {
+  const int lane = threadIdx.x & 63;
+  float m = -INFINITY;
+  for (int i = lane; i < n; i += 64) {
+    const Part p = part(i);
+    const float mi = p.ml ? p.ml[0] : -INFINITY;
+    m = fmaxf(m, mi);
+  }
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+  float l = 0.f;
+  for (int i = lane; i < n; i += 64) {
+    const Part p = part(i);
+    const float mi = p.ml ? p.ml[0] : -INFINITY, li = p.ml ? p.ml[1] : 0.f;
+    // A part without keys is left out, marked by a negative weight.  One of nothing but NaN has the
+    // same maximum of -inf, and its sum makes the row NaN; one whose weight rounds to 0 still counts,
+    // as its values may not be finite.
+    const bool none = no_weight(mi, li);
+    const float f = li != li ? li : __builtin_amdgcn_exp2f((mi - m) * scale_log2);
+    weight[i] = none ? -1.f : f;
+    if (!none) l = fmaf(li, f, l);
+  }
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
+  __builtin_amdgcn_wave_barrier();
+  const int quads = D <= 32 ? 8 : D <= 64 ? 16 : D <= 128 ? 32 : 64;
+  const int c = 4 * (lane & (quads - 1)), group = lane / quads, groups = 64 / quads;
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  if (c < D) {
+#pragma unroll 4
+    for (int i = group; i < n; i += groups) {
+      const float f = weight[i];
+      if (!(f < 0.f)) y += *reinterpret_cast<const f32x4*>(part(i).o + c) * f;
+    }
+  }
+  for (int d = 32; d >= quads; d >>= 1)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] += __shfl_xor(y[i], d, 64);
+  const float inv = no_weight(m, l) ? 0.f : 1.0f / l;
+  if (group == 0 && c < D) {
+    const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
+    store_floats<T, 4>(op + c, z);
+    if (lse && lane == 0) *lse = log_sum(m, l, scale_log2);
+  }
+  __builtin_amdgcn_wave_barrier();
+}
+
+// ---------------------------------------------------------------------------
+// whole sequences
+// ---------------------------------------------------------------------------
+// The work is laid out on a line, for every key head the same: first the prefixes (each with the rows of
+// all its sequences), then the sequences with their own keys, of each its tiles of 128 rows, of each tile
+// its keys.  A workgroup takes an equal piece of that line, whatever it holds of many short or parts of
+// few long ones; a tile that lies in several pieces is joined by the second kernel.  Every workgroup finds
+// the line's length and its own place on it from the lengths (a sum over them by all threads), so that
+// nothing of the plan depends on the host, which does not know them.
+struct PagedArgs {
+  const void* Q;
+  void* O;
+  float* lse;
+  Pages K, V;
+  Sequences own, pre;                  // (pre.S = 0: none; pre.cu counts sequences)
+  long long q_token, q_head, o_token, o_head;
+  long long Tq;
+  int Hq, Hk, group, D, causal;
+  float scale_log2, lift;
+  u32 flip;
+  int pieces;                          // most pieces of a line
+  int cap;                             // rows of a part: as many as a tile may have
+  long long* plan;                     // [prefixes and sequences]: the places on the line that they begin at, then its length
+  float *part_o, *part_ml;             // [pieces Hk][2][cap]: of tiles that begin before a piece, and that end behind it
+  float *whole_o, *whole_ml;           // with prefixes: [2][Tq Hq], of tiles of one (prefixes, sequences) in one piece
+};
+
+constexpr int kTileCost = 2;           // what a tile takes beside its keys, in tiles of 64 keys
+constexpr int kLeastPiece = 4;
+
+// A prefix or a sequence: its rows, and its keys.
+struct Item {
+  int t0, tokens, keys;                // first token
+  long long rows, tiles;
+  int ahead;                           // token i sees the keys up to i + ahead
+  long long skip;                      // tiles none of whose rows sees a key
+  int group;
+  double more;                         // keys that a tile sees beyond the one before it, half of them
+  __device__ __forceinline__ int sees(long long row) const {
+    const long long e = row / group + ahead + 1;
+    return e < 0 ? 0 : e < keys ? (int)e : keys;
+  }
+  // Cost of the first r tiles: kTileCost each, and the sum of what their last rows see in tiles of 64
+  // keys, over skip < i <= r of 128 i / group + ahead (or ahead, where all see the same).
+  __device__ __forceinline__ long long cost(long long r) const {
+    const long long m = r > skip ? r - skip : 0;
+    const double first = (double)(r - m), end = (double)r;
+    const double keys_seen = (double)m * ahead + more * (end * (end + 1.0) - first * (first + 1.0));
+    return kTileCost * r + (long long)(keys_seen * (1.0 / kTileKeys));
+  }
+};
+__device__ __forceinline__ Item item_of(const PagedArgs& a, int v) {
+  Item x;
+  x.group = a.group;
+  int end;
+  if (v < a.pre.S) {
+    x.t0 = start_of(a.own.cu, start_of(a.pre.cu, v, a.own.S), a.Tq);
+    end = start_of(a.own.cu, start_of(a.pre.cu, v + 1, a.own.S), a.Tq);
+    x.keys = keys_of(a.pre, v);
+  } else {
+    x.t0 = start_of(a.own.cu, v - a.pre.S, a.Tq);
+    end = start_of(a.own.cu, v - a.pre.S + 1, a.Tq);
+    x.keys = keys_of(a.own, v - a.pre.S);
+  }
+  x.tokens = end > x.t0 ? end - x.t0 : 0;
+  x.rows = (long long)x.tokens * a.group;
+  x.tiles = (x.rows + kManyRows - 1) / kManyRows;
+  // (what sees everything: as if all its tokens stood at the end)
+  const bool causal = a.causal && v >= a.pre.S;
+  x.ahead = causal ? x.keys - x.tokens : x.keys;
+  x.more = causal ? kManyRows * 0.5 / a.group : 0.0;
+  x.skip = 0;
+  if (x.ahead < 0) {
+    x.skip = (long long)-x.ahead * a.group / kManyRows;
+    x.skip = x.skip < x.tiles ? x.skip : x.tiles;
+  }
+  return x;
+}
+
+// The tile of an item, and the place of it on the line.
+struct Stretch {
+  long long begin, end;
+  int tiles;                           // of keys, one at least
+  __device__ __forceinline__ int at(long long x) const {   // first tile of keys behind a place
+    if (x <= begin) return 0;
+    if (x >= end) return tiles;
+    return (int)((x - begin) * tiles / (end - begin));
+  }
+};
+__device__ __forceinline__ Stretch stretch_of(const Item& x, long long start, long long r) {
+  Stretch s;
+  s.begin = start + x.cost(r);
+  s.end = start + x.cost(r + 1);
+  const long long last = (r + 1) * kManyRows < x.rows ? (r + 1) * kManyRows : x.rows;
+  const int n = x.sees(last - 1);
+  s.tiles = n > 0 ? (n + kTileKeys - 1) / kTileKeys : 1;
+  return s;
+}
+__device__ __forceinline__ int pieces_of(const PagedArgs& a, long long total) {
+  const long long n = total / kLeastPiece;
+  return n < 1 ? 1 : n < a.pieces ? (int)n : a.pieces;
+}
+// Where piece k of n begins.
+__device__ __forceinline__ long long piece_at(long long total, int k, int n) { return total * k / n; }
+
+template <typename T, int DP, int DC>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 2 : 1))) void k_attend_pages(
+    PagedArgs a) {
+  __shared__ __attribute__((aligned(1024))) Shared<DP> sh;
+  __shared__ long long wave_sum[4];
+  __shared__ long long found[2];                         // item, and the place it begins at
+  const int hk = (int)(blockIdx.x % (unsigned)a.Hk), k = (int)(blockIdx.x / (unsigned)a.Hk);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  // the line
+  const int items = a.pre.S + a.own.S, each = (items + 255) / 256;
+  const int v0 = tid * each < items ? tid * each : items, v1 = v0 + each < items ? v0 + each : items;
+  long long mine = 0;
+  for (int v = v0; v < v1; ++v) {
+    const Item x = item_of(a, v);
+    mine += x.cost(x.tiles);
+  }
+  long long upto = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const long long o = __shfl_up(upto, d, 64);
+    if (lane >= d) upto += o;
+  }
+  if (lane == 63) wave_sum[wave] = upto;
+  __syncthreads();
+  long long before = upto - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) before += wave_sum[w];
+    total += wave_sum[w];
+  }
+  const int n = pieces_of(a, total);
+  if (total == 0 || k >= n) {
+    if (blockIdx.x == 0 && tid == 0) a.plan[items] = 0;
+    return;
+  }
+  const long long from = piece_at(total, k, n), to = piece_at(total, k + 1, n);
+  for (int v = v0; v < v1; ++v) {
+    const Item x = item_of(a, v);
+    const long long next = before + x.cost(x.tiles);
+    if (before <= from && from < next) {
+      found[0] = v;
+      found[1] = before;
+    }
+    if (blockIdx.x == 0) a.plan[v] = before;
+    before = next;
+  }
+  if (blockIdx.x == 0 && tid == 0) a.plan[items] = total;
+  __syncthreads();
+
+  int v = __builtin_amdgcn_readfirstlane((int)found[0]);
+  long long start = found[1];
+  Item x = item_of(a, v);
+  long long r = 0;
+  for (long long count = x.tiles; count > 1;) {          // the last tile that begins no later than the piece
+    const long long half = count / 2;
+    if (start + x.cost(r + half) <= from) {
+      r += half;
+      count -= half;
+    } else {
+      count = half;
+    }
+  }
+  for (;;) {
+    const Stretch s = stretch_of(x, start, r);
+    if (s.begin >= to) break;
+    const int lo = __builtin_amdgcn_readfirstlane(s.at(from)), hi = __builtin_amdgcn_readfirstlane(s.at(to));
+    if (lo < hi) {
+      const bool prefix = v < a.pre.S;
+      const Sequences& q = prefix ? a.pre : a.own;
+      const int line = prefix ? v : v - a.pre.S;
+      const long long r0 = r * kManyRows;
+      const int rows = __builtin_amdgcn_readfirstlane((int)(x.rows - r0 < kManyRows ? x.rows - r0 : kManyRows));
+      const int token0 = __builtin_amdgcn_readfirstlane((int)(r0 / a.group));
+      const int first = __builtin_amdgcn_readfirstlane((int)(r0 - (long long)token0 * a.group));
+      const int t0 = __builtin_amdgcn_readfirstlane(x.t0) + token0;
+      const int keys = __builtin_amdgcn_readfirstlane(x.keys);
+      const int ahead = __builtin_amdgcn_readfirstlane(x.ahead) + token0 + 1;   // of row r of the tile: + (first + r) / group
+      auto sees = [&](int row) {
+        const int e = (first + row) / a.group + ahead;
+        return e < 0 ? 0 : e < keys ? e : keys;
+      };
+      const Line where = {q.table + line * q.ld, q.shift, q.n_pages, keys};
+      const Store<T, DP> store(a.K, a.V, hk, q.shift, a.D);
+      Target<T> target;
+      target.O = static_cast<T*>(a.O) + t0 * a.o_token + (long long)hk * a.group * a.o_head;
+      target.lse = a.lse ? a.lse + (long long)t0 * a.Hq + hk * a.group : nullptr;
+      target.o_token = a.o_token;
+      target.o_head = a.o_head;
+      target.Hq = a.Hq;
+      target.group = a.group;
+      target.first = first;
+      target.scale_log2 = a.scale_log2;
+      target.D = a.D;
+      target.po = target.pml = nullptr;
+      if (lo > 0 || hi < s.tiles) {
+        const long long slot = 2ll * blockIdx.x + (lo > 0 ? 0 : 1);
+        target.po = a.part_o + slot * a.cap * a.D;
+        target.pml = a.part_ml + slot * a.cap * 2;
+      } else if (a.pre.S > 0) {
+        // (rows of a key head one after the other)
+        const long long at = ((prefix ? 0 : a.Hk) + hk) * a.Tq * a.group + (long long)t0 * a.group + first;
+        target.po = a.whole_o + at * a.D;
+        target.pml = a.whole_ml + at * 2;
+      }
+      if (a.D < DC) clear<DP>(sh);
+      else __syncthreads();
+      const bool few = rows <= kFewRows;
+      const int mine_row = few ? lane & 31 : wave * 32 + (lane & 31);
+      const int row = mine_row < rows ? mine_row : rows - 1;
+      const int token = (first + row) / a.group, head = first + row - token * a.group;
+      const T* qp = static_cast<const T*>(a.Q) + (long long)(t0 + token) * a.q_token +
+                    (long long)(hk * a.group + head) * a.q_head;
+      if (few) {
+        const int end = __builtin_amdgcn_readfirstlane(sees(rows - 1)), all = __builtin_amdgcn_readfirstlane(sees(0));
+        const int tiles = (end + kFewKeys - 1) / kFewKeys, stop = 2 * hi < tiles ? 2 * hi : tiles;
+        attend_few<T, DP, DC>(sh, store, where, qp, sees(row), all, keys, 2 * lo, stop, rows, a.flip, a.lift, target);
+      } else {
+        const int from_row = wave * 32 < rows ? wave * 32 : rows - 1;
+        const int last_row = wave * 32 + 31 < rows ? wave * 32 + 31 : rows - 1;
+        const int last = wave * 32 < rows ? __builtin_amdgcn_readfirstlane(sees(last_row)) : 0;
+        const int all = __builtin_amdgcn_readfirstlane(sees(from_row));
+        const int end = __builtin_amdgcn_readfirstlane(sees(rows - 1));
+        const int tiles = (end + kTileKeys - 1) / kTileKeys, stop = hi < tiles ? hi : tiles;
+        attend_many<T, DP, DC>(sh, store, where, qp, sees(row), all, last, keys, lo, stop, rows, a.flip, a.lift, target);
+      }
+    }
+    if (s.end >= to) break;
+    if (++r >= x.tiles) {
+      start += x.cost(x.tiles);
+      r = 0;
+      do {
+        if (++v >= items) return;
+        x = item_of(a, v);
+      } while (x.tiles == 0);
+    }
+  }
+}
+
+// Joins the tiles that lie in several pieces, and prefixes with sequences: a wavefront a row, some rows
+// each.
+template <typename T>
+__global__ __launch_bounds__(256) void k_join_pages(PagedArgs a, int heads, int chunks) {
+  __shared__ float weight[4][kMaxParts];
+  const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
+  const long long t = id / chunks;
+  if (t >= a.Tq) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h0 = ((int)(id % chunks) * 4 + wave) * heads, h1 = h0 + heads < a.Hq ? h0 + heads : a.Hq;
+  const int items = a.pre.S + a.own.S;
+  const long long total = a.plan[items];
+  if (total <= 0) return;
+  const int n = pieces_of(a, total);
+  const int s = last_at_most(a.own.S, t, [&](int i) { return start_of(a.own.cu, i, a.Tq); });
+  if (t < start_of(a.own.cu, s, a.Tq) || t >= start_of(a.own.cu, s + 1, a.Tq)) return;
+  int p = -1;                                            // the sequence's prefix
+  if (a.pre.S > 0) {
+    p = last_at_most(a.pre.S, s, [&](int i) { return start_of(a.pre.cu, i, a.own.S); });
+    if (s < start_of(a.pre.cu, p, a.own.S) || s >= start_of(a.pre.cu, p + 1, a.own.S)) p = -1;
+  }
+  // of the prefix and of the sequence: the tile that a row lies in, and its pieces
+  struct Pieces {
+    Stretch s;
+    int first, count, row;
+    long long whole;                                     // row among those of tiles in one piece
+  };
+  const Item own = item_of(a, a.pre.S + s), pre = p < 0 ? own : item_of(a, p);
+  const long long own_start = a.plan[a.pre.S + s], pre_start = p < 0 ? 0 : a.plan[p];
+  auto pieces = [&](const Item& x, long long start, int hk, int e) {
+    Pieces q;
+    const long long row = (t - x.t0) * a.group + e, r = row / kManyRows;
+    q.row = (int)(row - r * kManyRows);
+    q.s = stretch_of(x, start, r);
+    int k0 = (int)(q.s.begin * n / total), k1 = (int)((q.s.end - 1) * n / total);
+    while (k0 > 0 && piece_at(total, k0, n) > q.s.begin) --k0;
+    while (k0 + 1 < n && piece_at(total, k0 + 1, n) <= q.s.begin) ++k0;
+    while (k1 > k0 && piece_at(total, k1, n) >= q.s.end) --k1;
+    while (k1 + 1 < n && piece_at(total, k1 + 1, n) < q.s.end) ++k1;
+    q.first = k0;
+    q.count = k1 - k0 + 1;
+    q.whole = hk * a.Tq * a.group + t * a.group + e;
+    return q;
+  };
+  for (int h = h0; h < h1; ++h) {
+    const int hk = h / a.group, e = h - hk * a.group;
+    const Pieces of_own = pieces(own, own_start, a.pre.S > 0 ? a.Hk + hk : hk, e);
+    Pieces of_pre = of_own;
+    if (p >= 0) of_pre = pieces(pre, pre_start, hk, e);
+    const int before = p < 0 ? 0 : of_pre.count;
+    if (a.pre.S == 0) {
+      // (one piece has all the keys: it has written the output)
+      bool whole = false;
+      for (int i = lane; i < of_own.count; i += 64) {
+        const int k = of_own.first + i;
+        whole |= of_own.s.at(piece_at(total, k, n)) == 0 && of_own.s.at(piece_at(total, k + 1, n)) == of_own.s.tiles;
+      }
+      if (__ballot(whole)) continue;
+    }
+    auto of_piece = [&](const Pieces& q, int k) -> Part {
+      const int lo = q.s.at(piece_at(total, k, n)), hi = q.s.at(piece_at(total, k + 1, n));
+      if (lo >= hi) return {nullptr, nullptr};
+      if (lo > 0 || hi < q.s.tiles) {
+        const long long at = (2 * ((long long)k * a.Hk + hk) + (lo > 0 ? 0 : 1)) * a.cap + q.row;
+        return {a.part_ml + 2 * at, a.part_o + at * a.D};
+      }
+      return {a.whole_ml + 2 * q.whole, a.whole_o + q.whole * a.D};
+    };
+    auto part = [&](int i) -> Part {
+      return i < before ? of_piece(of_pre, of_pre.first + i) : of_piece(of_own, of_own.first + i - before);
+    };
+    join_row<T>(weight[wave], before + of_own.count, part, a.D, a.scale_log2,
+                static_cast<T*>(a.O) + t * a.o_token + h * a.o_head, a.lse ? a.lse + t * a.Hq + h : nullptr);
+  }
+}
+
+// Pieces for each key head's line: a workgroup each, as many as run at a time.
+static int paged_pieces(int Hk, int D) {
+  const int at_a_time = D <= 128 ? 512 : 256;
+  return at_a_time / Hk > 0 ? at_a_time / Hk : 1;
+}
+
+struct PagedLayout {
+  size_t plan, ml, o, whole_ml, whole_o, total;
+  int pieces, cap;
+};
+static PagedLayout paged_layout(long long Tq, int S, int prefixes, int Hq, int Hk, int D) {
+  PagedLayout l;
+  const long long rows = Tq * (Hq / Hk);
+  l.cap = (int)(rows < kManyRows ? rows : kManyRows);
+  l.pieces = paged_pieces(Hk, D);
+  const size_t parts = 2ull * l.pieces * Hk * l.cap, whole = prefixes > 0 ? 2ull * Tq * Hq : 0;
+  auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
+  l.plan = 0;
+  l.ml = up((size_t)(S + prefixes + 1) * sizeof(long long));
+  l.o = l.ml + up(parts * 2 * sizeof(float));
+  l.whole_ml = l.o + up(parts * D * sizeof(float));
+  l.whole_o = l.whole_ml + up(whole * 2 * sizeof(float));
+  l.total = l.whole_o + up(whole * D * sizeof(float));
+  return l;
+}
+size_t paged_workspace(long long Tq, int S, int prefixes, int Hq, int Hk, int D) {
+  return paged_layout(Tq, S, prefixes, Hq, Hk, D).total;
+}
+
+static Pages pages_of(const tdq_pages* p) { return {p->data, p->page, p->token, p->head}; }
+static void scale_of(float scale, tdq_dtype dt, float* scale_log2, float* lift, u32* flip) {
+  const double c = fabs((double)scale) * 1.44269504088896340736;
+  *scale_log2 = c > 1e-30 ? (float)c : 1e-30f;           // (a masked score stays -inf)
+  *lift = (dt == TDQ_F16 ? kLift<_Float16> : kLift<__bf16>) / *scale_log2;
+  *flip = scale < 0.f ? 0x80008000u : 0u;                // (Q is negated)
+}
+
+// Kernels for a head of D elements: rows of LDS of a power of two, products of a multiple of 32.
+#define TDQ_BY_HEAD(F, T)              \
+  do {                                 \
+    if (D <= 32) F(T, 32, 32);         \
+    else if (D <= 64) F(T, 64, 64);    \
+    else if (D <= 96) F(T, 128, 96);   \
+    else if (D <= 128) F(T, 128, 128); \
+    else if (D <= 192) F(T, 256, 192); \
+    else F(T, 256, 256);               \
+  } while (0)
+
+hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages* V, tdq_dtype dt, long long Tq,
+                        const tdq_sequences* seq, const tdq_sequences* prefix, int Hq, int Hk, int D, float scale,
+                        bool causal, const tdq_heads* O, float* lse, void* workspace, hipStream_t st) {
+  PagedArgs a;
+  a.Q = Q->data;
+  a.O = O->data;
+  a.lse = lse;
+  a.K = pages_of(K);
+  a.V = pages_of(V);
+  a.own = sequences_of(seq);
+  if (prefix) {
+    a.pre = sequences_of(prefix);
+  } else {
+    a.pre = a.own;
+    a.pre.S = 0;
+  }
+  a.q_token = Q->token;
+  a.q_head = Q->head;
+  a.o_token = O->token;
+  a.o_head = O->head;
+  a.Tq = Tq;
+  a.Hq = Hq;
+  a.Hk = Hk;
+  a.group = Hq / Hk;
+  a.D = D;
+  a.causal = causal;
+  scale_of(scale, dt, &a.scale_log2, &a.lift, &a.flip);
+  const PagedLayout l = paged_layout(Tq, seq->S, a.pre.S, Hq, Hk, D);
+  a.pieces = l.pieces;
+  a.cap = l.cap;
+  char* w = static_cast<char*>(workspace);
+  a.plan = reinterpret_cast<long long*>(w + l.plan);
+  a.part_ml = reinterpret_cast<float*>(w + l.ml);
+  a.part_o = reinterpret_cast<float*>(w + l.o);
+  a.whole_ml = reinterpret_cast<float*>(w + l.whole_ml);
+  a.whole_o = reinterpret_cast<float*>(w + l.whole_o);
+  const dim3 grid((unsigned)(a.pieces * Hk));
+#define TDQ_PAGED(T, DP, DC) hipLaunchKernelGGL((k_attend_pages<T, DP, DC>), grid, dim3(256), 0, st, a)
+  if (dt == TDQ_F16) TDQ_BY_HEAD(TDQ_PAGED, _Float16);
+  else TDQ_BY_HEAD(TDQ_PAGED, __bf16);
+#undef TDQ_PAGED
+  const int heads = Tq * Hq > 16384 ? 4 : 1, chunks = (Hq + 4 * heads - 1) / (4 * heads);
+  const dim3 join = two_axes(Tq * chunks);
+  if (dt == TDQ_F16) hipLaunchKernelGGL((k_join_pages<_Float16>), join, dim3(256), 0, st, a, heads, chunks);
+  else hipLaunchKernelGGL((k_join_pages<__bf16>), join, dim3(256), 0, st, a, heads, chunks);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// chosen pages
+// ---------------------------------------------------------------------------
+// Every token and key head has a list of pages of its own, so a tile has the group's rows and no more;
+// its pages are shared out to `splits` workgroups, and in each to four wavefronts.
+struct ChosenArgs {
+  const void* Q;
+  void* O;
+  float* lse;
+  Pages K, V;
+  Sequences seq;
+  const int* chosen;                   // [Tq Hk, count]
+  long long q_token, q_head, o_token, o_head;
+  long long Tq;
+  int Hq, Hk, group, D, causal, count;
+  float scale_log2, lift;
+  u32 flip;
+  int splits, tiles;                   // tiles of 32 rows of a group
+  float *part_o, *part_ml;             // [Tq Hq][splits]
+};
+
+template <typename T, int DP, int DC>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 2 : 1))) void k_attend_chosen(
+    ChosenArgs a) {
+  __shared__ __attribute__((aligned(1024))) Shared<DP> sh;
+  const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
+  const int hk = (int)(id % a.Hk), split = (int)(id / a.Hk % a.splits);
+  const long long rest = id / a.Hk / a.splits;
+  const int tile = (int)(rest % a.tiles);
+  const long long t = rest / a.tiles;
+  if (t >= a.Tq) return;
+  const Sequences& q = a.seq;
+  const int s = last_at_most(q.S, t, [&](int i) { return start_of(q.cu, i, a.Tq); });
+  const int from = start_of(q.cu, s, a.Tq), to = start_of(q.cu, s + 1, a.Tq);
+  const int keys = __builtin_amdgcn_readfirstlane(keys_of(q, s));
+  if (t < from || t >= to) return;
+  const long long e = a.causal ? keys - to + t + 1 : keys;
+  const int sees = __builtin_amdgcn_readfirstlane(e < 0 ? 0 : (int)e);
+  const int rows = a.group - tile * kFewRows < kFewRows ? a.group - tile * kFewRows : kFewRows;
+  const int lane = threadIdx.x & 63, row = (lane & 31) < rows ? lane & 31 : rows - 1;
+  const int h0 = hk * a.group + tile * kFewRows;
+  const Chosen where = {a.chosen + (t * a.Hk + hk) * a.count, q.table + s * q.ld, a.count, q.shift, q.n_pages, keys};
+  const Store<T, DP> store(a.K, a.V, hk, q.shift, a.D);
+  Target<T> target;
+  target.O = static_cast<T*>(a.O) + t * a.o_token + h0 * a.o_head;
+  target.lse = a.lse ? a.lse + t * a.Hq + h0 : nullptr;
+  target.o_token = a.o_token;
+  target.o_head = a.o_head;
+  target.Hq = a.Hq;
+  target.group = kFewRows;                               // (all rows are heads of one token)
+  target.first = 0;
+  target.scale_log2 = a.scale_log2;
+  target.D = a.D;
+  target.po = target.pml = nullptr;
+  if (a.splits > 1) {
+    // (rows of a split one after the other)
+    const long long at = (split * a.Tq + t) * a.Hq + h0;
+    target.po = a.part_o + at * a.D;
+    target.pml = a.part_ml + 2 * at;
+  }
+  int used = 0;                                          // the list up to its last page that is named
+  for (int i = lane; i < a.count; i += 64) used = where.list[i] >= 0 ? i + 1 : used;
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) used = max(used, __shfl_xor(used, d, 64));
+  used = __builtin_amdgcn_readfirstlane(used);
+  const int tiles = sees > 0 ? (int)((((long long)used << q.shift) + kFewKeys - 1) / kFewKeys) : 0;
+  const int share = (tiles + a.splits - 1) / a.splits;
+  const int lo = split * share < tiles ? split * share : tiles, hi = lo + share < tiles ? lo + share : tiles;
+  if (a.D < DC) clear<DP>(sh);
+  attend_few<T, DP, DC>(sh, store, where, static_cast<const T*>(a.Q) + t * a.q_token + (h0 + row) * a.q_head, sees, sees,
+                        keys, lo, hi, rows, a.flip, a.lift, target);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_join_chosen(ChosenArgs a) {
+  __shared__ float weight[4][kMaxParts];
+  const long long row = 4 * (blockIdx.x + (long long)blockIdx.y * gridDim.x) + (threadIdx.x >> 6);
+  if (row >= a.Tq * a.Hq) return;
+  const long long t = row / a.Hq;
+  const int h = (int)(row - t * a.Hq);
+  const Sequences& q = a.seq;
+  const int s = last_at_most(q.S, t, [&](int i) { return start_of(q.cu, i, a.Tq); });
+  if (t < start_of(q.cu, s, a.Tq) || t >= start_of(q.cu, s + 1, a.Tq)) return;
+  auto part = [&](int i) -> Part {
+    const long long at = i * a.Tq * a.Hq + row;
+    return {a.part_ml + 2 * at, a.part_o + at * a.D};
+  };
+  join_row<T>(weight[threadIdx.x >> 6], a.splits, part, a.D, a.scale_log2,
+              static_cast<T*>(a.O) + t * a.o_token + h * a.o_head, a.lse ? a.lse + row : nullptr);
+}
+
+// Enough workgroups to fill the chip, as long as each has 256 keys.
+static int chosen_splits(long long Tq, int Hq, int Hk, int page_size, int count) {
+  const long long base = Tq * Hk * ((Hq / Hk + kFewRows - 1) / kFewRows), most = (long long)count * page_size / 256;
+  long long n = 1024 / base;
+  if (n > most) n = most;
+  if (n > 64) n = 64;
+  return n > 1 ? (int)n : 1;
+}
+static size_t chosen_ml_bytes(long long Tq, int Hq, int splits) {
+  return ((size_t)Tq * Hq * splits * 2 * sizeof(float) + 255) & ~(size_t)255;
+}
+size_t chosen_workspace(long long Tq, int Hq, int Hk, int D, int page_size, int count) {
+  const int splits = chosen_splits(Tq, Hq, Hk, page_size, count);
+  return splits > 1 ? chosen_ml_bytes(Tq, Hq, splits) + (size_t)Tq * Hq * splits * D * sizeof(float) : 0;
+}
+
+hipError_t launch_chosen(const tdq_heads* Q, const tdq_pages* K, const tdq_pages* V, tdq_dtype dt, long long Tq,
+                         const tdq_sequences* seq, int Hq, int Hk, int D, float scale, bool causal, const int* chosen,
+                         int count, const tdq_heads* O, float* lse, void* workspace, hipStream_t st) {
+  ChosenArgs a;
+  a.Q = Q->data;
+  a.O = O->data;
+  a.lse = lse;
+  a.K = pages_of(K);
+  a.V = pages_of(V);
+  a.seq = sequences_of(seq);
+  a.chosen = chosen;
+  a.q_token = Q->token;
+  a.q_head = Q->head;
+  a.o_token = O->token;
+  a.o_head = O->head;
+  a.Tq = Tq;
+  a.Hq = Hq;
+  a.Hk = Hk;
+  a.group = Hq / Hk;
+  a.D = D;
+  a.causal = causal;
+  a.count = count;
+  scale_of(scale, dt, &a.scale_log2, &a.lift, &a.flip);
+  a.splits = chosen_splits(Tq, Hq, Hk, seq->page_size, count);
+  a.tiles = (a.group + kFewRows - 1) / kFewRows;
+  a.part_ml = static_cast<float*>(workspace);
+  a.part_o = a.splits > 1
+                 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + chosen_ml_bytes(Tq, Hq, a.splits))
+                 : nullptr;
+  const dim3 grid = two_axes(Tq * a.tiles * a.splits * Hk);
+#define TDQ_CHOSEN(T, DP, DC) hipLaunchKernelGGL((k_attend_chosen<T, DP, DC>), grid, dim3(256), 0, st, a)
+  if (dt == TDQ_F16) TDQ_BY_HEAD(TDQ_CHOSEN, _Float16);
+  else TDQ_BY_HEAD(TDQ_CHOSEN, __bf16);
+#undef TDQ_CHOSEN
+  if (a.splits > 1) {
+    const dim3 join = two_axes((Tq * Hq + 3) / 4);
+    if (dt == TDQ_F16) hipLaunchKernelGGL((k_join_chosen<_Float16>), join, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_join_chosen<__bf16>), join, dim3(256), 0, st, a);
+  }
+  return hipGetLastError();
+}
+#undef TDQ_BY_HEAD
+
+}  // namespace tdq

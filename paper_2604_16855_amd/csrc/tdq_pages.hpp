@@ -1,0 +1,64 @@
+// Sequences whose keys and values lie in the pages of a cache: what the kernels that write, sum up,
+// choose and read pages share.
+#pragma once
+
+#include "tdq_half.hpp"
+
+namespace tdq {
+
+// tdq_sequences as the kernels take it.  Key j of sequence s is row j % P of page table[s][j / P].
+struct Sequences {
+  const int *cu, *len, *table;
+  long long ld;
+  int S, columns, n_pages, shift;      // page size P = 2^shift
+};
+inline Sequences sequences_of(const tdq_sequences* q) {
+  Sequences s;
+  s.cu = q->cu_q;
+  s.len = q->len_k;
+  s.table = q->table;
+  s.ld = q->ld_table;
+  s.S = q->S;
+  s.columns = q->columns;
+  s.n_pages = q->n_pages;
+  s.shift = __builtin_ctz((unsigned)q->page_size);
+  return s;
+}
+
+// A value that no kernel of this call writes, from an address that is the same in every lane.
+__device__ __forceinline__ int load_scalar(const int* p) {
+  return *(const __attribute__((address_space(4))) int*)(uintptr_t)p;
+}
+
+// cu[i] within 0 .. total.
+__device__ __forceinline__ int start_of(const int* cu, long long i, long long total) {
+  const int c = cu[i];
+  return c < 0 ? 0 : c < total ? c : (int)total;
+}
+// Keys of sequence s: no more than its line of the table has room for.
+__device__ __forceinline__ int keys_of(const Sequences& q, int s) {
+  const int n = q.len[s], room = q.columns << q.shift;
+  return n < 0 ? 0 : n < room ? n : room;
+}
+
+// The last i < n with first(i) <= at, for an ascending `first` with first(0) <= at: 64 places at a
+// time, a lane each.  Every lane gets the answer.
+template <typename F>
+__device__ __forceinline__ int last_at_most(int n, long long at, F first) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0;
+  while (n > 0) {
+    const int step = (n + 63) / 64;
+    const int i = lo + lane * step;
+    const bool le = lane * step < n && first(i) <= at;
+    const int count = __popcll(__ballot(le));            // (ascending: a run of lanes from 0 on)
+    if (count == 0) break;
+    const int base = lo + (count - 1) * step, rest = lo + n - base;
+    lo = base;
+    if (step == 1) break;
+    n = rest < step ? rest : step;
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+}  // namespace tdq

@@ -48,6 +48,19 @@ class Heads(C.Structure):
     _fields_ = [("data", C.c_void_p), ("token", C.c_int64), ("head", C.c_int64)]
 
 
+class Pages(C.Structure):
+    """Mirror of tdq_pages: a cache's tensor [pages, page_size, heads, D] with contiguous heads."""
+
+    _fields_ = [("data", C.c_void_p), ("page", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class Sequences(C.Structure):
+    """Mirror of tdq_sequences."""
+
+    _fields_ = [("cu_q", C.c_void_p), ("len_k", C.c_void_p), ("table", C.c_void_p), ("ld_table", C.c_int64),
+                ("S", C.c_int32), ("columns", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32)]
+
+
 class TdqError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -142,6 +155,25 @@ def lib() -> C.CDLL:
     L.tdq_attention.restype = C.c_int
     L.tdq_attention.argtypes = [hp, hp, hp, C.c_int, i64, i64, i32, vp, vp, vp, i32, i32, i32, f32, i32, hp, vp, vp,
                                 sz, vp]
+    pp, sp = vp, vp                          # (const tdq_pages*, const tdq_sequences*)
+    L.tdq_cache_append.restype = C.c_int
+    L.tdq_cache_append.argtypes = [hp, hp, hp, C.c_int, i64, sp, i32, i32, i32, vp, vp, f32, i32, i32, vp, i64, i32,
+                                   vp, vp, hp, pp, pp, vp]
+    L.tdq_page_bounds.restype = C.c_int
+    L.tdq_page_bounds.argtypes = [pp, C.c_int, i64, sp, i32, i32, hp, hp, vp]
+    L.tdq_select_pages_workspace_bytes.restype = sz
+    L.tdq_select_pages_workspace_bytes.argtypes = [i64, i32, i32]
+    L.tdq_select_pages.restype = C.c_int
+    L.tdq_select_pages.argtypes = [hp, hp, hp, C.c_int, i64, sp, i32, i32, i32, i32, i32, i32, i32, vp, vp, sz, vp]
+    L.tdq_attention_selected_workspace_bytes.restype = sz
+    L.tdq_attention_selected_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32]
+    L.tdq_attention_selected.restype = C.c_int
+    L.tdq_attention_selected.argtypes = [hp, pp, pp, C.c_int, i64, sp, i32, i32, i32, f32, i32, vp, i32, hp, vp, vp, sz,
+                                         vp]
+    L.tdq_attention_paged_workspace_bytes.restype = sz
+    L.tdq_attention_paged_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32]
+    L.tdq_attention_paged.restype = C.c_int
+    L.tdq_attention_paged.argtypes = [hp, pp, pp, C.c_int, i64, sp, sp, i32, i32, i32, f32, i32, hp, vp, vp, sz, vp]
     L.tdq_quantize_weight.restype = C.c_int
     L.tdq_quantize_weight.argtypes = [vp, i32, i32, i64, vp, i64, vp, vp]
     _lib = L
@@ -838,6 +870,290 @@ def tdq_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, cu_q: torch
                          D ** -0.5 if scale is None else scale, 1 if causal else 0, at + 3 * _HEADS_BYTES, None if lse is None else lse.data_ptr(), p_work, n_work, _stream())
     if rc:
         raise TdqError(rc, "tdq_attention")
+    return out, lse
+
+
+# --------------------------------------------------------------------------------------
+# a cache of keys and values in pages
+# --------------------------------------------------------------------------------------
+# The structures of a call one after the other: their places in an array of 64-bit numbers, in bytes.
+_HEADS, _PAGES, _SEQUENCES = 24, 32, 48
+
+
+def _same_device(*tensors) -> None:
+    """The library runs on the current device: an address of another one would fault it."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        at = t.get_device()                  # (-1: the host)
+        if dev is None and at >= 0:
+            dev = _get_device() if _get_device is not None else torch.cuda.current_device()
+        if at < 0 or at != dev:
+            raise ValueError("all tensors must be on the current GPU")
+
+
+def _ints(t: torch.Tensor, name: str, n: Optional[int] = None) -> torch.Tensor:
+    if t.dtype is not torch.int32:
+        raise _wrong_type(name, t, torch.int32)
+    if t.dim() != 1 or not t.is_contiguous() or (n is not None and t.shape[0] != n):
+        raise ValueError(f"{name} must be contiguous" + ("" if n is None else f" [{n}]"))
+    return t
+
+
+def _cache(X: torch.Tensor, name: str, like=None) -> Tuple[int, int, int, int]:
+    """(address, page, token and head strides) of [pages, page_size, heads, D]."""
+    shape, s = X.shape, X.stride()
+    if len(shape) != 4 or (s[3] != 1 and shape[3] > 1):
+        raise ValueError(f"{name} must be [pages, page_size, heads, D] with contiguous heads")
+    if like is not None and (shape != like.shape or X.dtype is not like.dtype):
+        raise ValueError("the caches of keys and values must have the same shape and type")
+    # (the stride of an axis of extent 1 addresses nothing; torch may report any value for it)
+    return (X.data_ptr(),) + tuple(s[i] if shape[i] > 1 else 0 for i in range(3))
+
+
+def _sequences(cu: Optional[torch.Tensor], table: torch.Tensor, len_k: torch.Tensor, cache_shape, what: str):
+    """tdq_sequences as six 64-bit numbers."""
+    if table.dtype is not torch.int32:
+        raise _wrong_type(what + "table", table, torch.int32)
+    shape, at = table.shape, table.stride()
+    if len(shape) != 2 or (at[1] != 1 and shape[1] > 1):
+        raise ValueError(what + "table must be [sequences, pages] with contiguous rows")
+    S, columns = shape
+    _ints(len_k, what + "len_k", S)
+    if cu is not None:
+        _ints(cu, what + "cu_q", S + 1)
+    return (0 if cu is None else cu.data_ptr(), len_k.data_ptr(), table.data_ptr(), at[0] if S > 1 else max(columns, 1),
+            S | columns << 32, cache_shape[0] | cache_shape[1] << 32)
+
+
+def tdq_cache_append(Q: Optional[torch.Tensor], K: torch.Tensor, V: torch.Tensor, cache_k: torch.Tensor,
+                     cache_v: torch.Tensor, cu_q: torch.Tensor, table: torch.Tensor, len_k: torch.Tensor,
+                     freq: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+                     q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                     eps: float = 1e-6, axis: Optional[torch.Tensor] = None, interleaved: bool = False,
+                     out: Optional[torch.Tensor] = None):
+    """Q[T, Hq, D] or None, K and V[T, Hk, D], packed by cu_q[S + 1], to cache_k and cache_v[pages, page_size, Hk, D]
+    by table[S, pages] and len_k[S] (the new tokens with them): heads normed (where a weight is given) and turned by
+    pos[axes, T] (or [T]; None: a token's place in its sequence) * freq[R/2].  -> Qo[T, Hq, D] (out; out = Q works in
+    place), whose rows of tokens of no sequence are not written."""
+    k_shape, dtype = K.shape, K.dtype
+    T, Hk, D = k_shape
+    if V.shape != k_shape or V.dtype is not dtype:
+        raise ValueError("K and V must have the same shape and type")
+    shape = cache_k.shape
+    if len(shape) != 4 or shape[2] != Hk or shape[3] != D or cache_k.dtype is not dtype:
+        raise ValueError("the cache must be [pages, page_size, heads, D] with K's heads, head size and type")
+    Hq, q = 0, (0,) * 6
+    if Q is not None:
+        q_shape = Q.shape
+        Hq = q_shape[1]
+        if q_shape[0] != T or q_shape[2] != D or Q.dtype is not dtype:
+            raise ValueError("Q must have K's tokens, head size and type")
+        if out is None:
+            out = torch.empty(q_shape, dtype=dtype, device=Q.device)
+        elif out.shape != q_shape or out.dtype is not dtype:
+            raise ValueError("out must have the shape and type of Q")
+        q = (Q.data_ptr(), *_strides(Q, "Q"), out.data_ptr(), *_strides(out, "out"))
+    R, axes, ld_pos, p_pos, p_axis, p_freq = 0, 1, 0, None, None, None
+    P = 0 if freq is None else freq.numel()
+    if P > 0:
+        if freq.dtype is not torch.float32:
+            raise _wrong_type("freq", freq, torch.float32)
+        if not freq.is_contiguous():
+            raise ValueError("freq must be contiguous")
+        R, p_freq = 2 * P, freq.data_ptr()
+        if pos is not None:
+            if pos.dtype is not torch.int32:
+                raise _wrong_type("pos", pos, torch.int32)
+            n, at = pos.shape, pos.stride()
+            if len(n) not in (1, 2) or n[-1] != T or (T > 1 and at[-1] != 1):
+                raise ValueError("pos must be [T] or [axes, T] with contiguous rows")
+            axes = n[0] if len(n) == 2 else 1
+            ld_pos = at[0] if axes > 1 else T
+            p_pos = pos.data_ptr()
+        if axis is not None:
+            if axis.dtype is not torch.int32:
+                raise _wrong_type("axis", axis, torch.int32)
+            if axis.numel() != P or not axis.is_contiguous():
+                raise ValueError("axis must be contiguous and name an axis for each of freq")
+            p_axis = axis.data_ptr()
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None and (w.dtype is not torch.float32 or w.numel() != D or not w.is_contiguous()):
+            raise ValueError(name + " must be contiguous float32 [D]")
+    h = (C.c_int64 * 26)(*q, K.data_ptr(), *_strides(K, "K"), V.data_ptr(), *_strides(V, "V"),
+                         *_cache(cache_k, "cache_k"), *_cache(cache_v, "cache_v", cache_k),
+                         *_sequences(cu_q, table, len_k, shape, ""))
+    _same_device(Q, K, V, cache_k, cache_v, cu_q, table, len_k, freq, pos, q_weight, k_weight, axis, out)
+    at = C.addressof(h)
+    rc = (_lib or lib()).tdq_cache_append(
+        at if Hq else None, at + 2 * _HEADS, at + 3 * _HEADS, _wdt(dtype), T, at + 4 * _HEADS + 2 * _PAGES, Hq, Hk, D,
+        _ptr(q_weight), _ptr(k_weight), eps, R, 1 if interleaved else 0, p_pos, ld_pos, axes, p_axis, p_freq,
+        at + _HEADS if Hq else None, at + 4 * _HEADS, at + 4 * _HEADS + _PAGES, _stream())
+    if rc:
+        raise TdqError(rc, "tdq_cache_append")
+    return out
+
+
+def tdq_page_bounds(cache_k: torch.Tensor, table: torch.Tensor, len_k: torch.Tensor,
+                    cu_q: Optional[torch.Tensor] = None, Tq: Optional[int] = None,
+                    out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
+    """cache_k[pages, page_size, Hk, D] -> (lo, hi)[pages, Hk, D]: smallest and largest value of every channel over the
+    keys in use of a page.  cu_q None: of all pages that the table and len_k name; else of those that hold each
+    sequence's last cu_q[s + 1] - cu_q[s] keys, Tq in all (or more).  The others are left as they are (zeros in a new
+    `out`)."""
+    shape, dtype = cache_k.shape, cache_k.dtype
+    c = _cache(cache_k, "cache_k")
+    pages, _, Hk, D = shape
+    if cu_q is not None and Tq is None:
+        raise ValueError("cu_q needs Tq, the number of new tokens")
+    if out is None:
+        out = (torch.zeros((pages, Hk, D), dtype=dtype, device=cache_k.device),
+               torch.zeros((pages, Hk, D), dtype=dtype, device=cache_k.device))
+    lo, hi = out
+    for x in out:
+        if x.shape != (pages, Hk, D) or x.dtype is not dtype:
+            raise ValueError("out must be two of [pages, heads, D] of the cache's type")
+    h = (C.c_int64 * 16)(*c, lo.data_ptr(), *_strides(lo, "lo"), hi.data_ptr(), *_strides(hi, "hi"),
+                         *_sequences(cu_q, table, len_k, shape, ""))
+    _same_device(cache_k, lo, hi, cu_q, table, len_k)
+    at = C.addressof(h)
+    rc = (_lib or lib()).tdq_page_bounds(at, _wdt(dtype), Tq or 0, at + _PAGES + 2 * _HEADS, Hk, D, at + _PAGES,
+                                         at + _PAGES + _HEADS, _stream())
+    if rc:
+        raise TdqError(rc, "tdq_page_bounds")
+    return out
+
+
+def _scratch(workspace: Optional[torch.Tensor], n: int, device) -> Tuple[Optional[torch.Tensor], Optional[int], int]:
+    if workspace is None:
+        workspace = torch.empty(n, dtype=torch.uint8, device=device) if n else None
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return (None, None, 0) if workspace is None else (workspace, workspace.data_ptr(),
+                                                      workspace.numel() * workspace.element_size())
+
+
+def tdq_select_pages_workspace_bytes(Tq: int, Hk: int, columns: int) -> int:
+    return int((_lib or lib()).tdq_select_pages_workspace_bytes(Tq, Hk, columns))
+
+
+def tdq_select_pages(Q: torch.Tensor, lo: torch.Tensor, hi: torch.Tensor, cu_q: torch.Tensor, table: torch.Tensor,
+                     len_k: torch.Tensor, page_size: int, count: int, first: int = 1, last: int = 1,
+                     causal: bool = True, out: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Q[Tq, Hq, D], lo and hi[pages, Hk, D] (tdq_page_bounds) -> [Tq, Hk, count] int32: the places in its sequence's
+    line of the table of the pages that each token and key head attends to: the first, the last and the best others,
+    ascending, -1 behind them.  Rows of tokens of no sequence are not written."""
+    Tq, Hq, D = Q.shape
+    b_shape, dtype = lo.shape, Q.dtype
+    if len(b_shape) != 3 or b_shape[2] != D or hi.shape != b_shape or lo.dtype is not dtype or hi.dtype is not dtype:
+        raise ValueError("lo and hi must be [pages, heads, D] with Q's head size and type")
+    Hk = b_shape[1]
+    if out is None:
+        out = torch.empty((Tq, Hk, count), dtype=torch.int32, device=Q.device)
+    elif out.dtype is not torch.int32 or out.shape != (Tq, Hk, count) or not out.is_contiguous():
+        raise ValueError("out must be contiguous int32 [Tq, heads, count]")
+    L = _lib or lib()
+    h = (C.c_int64 * 15)(Q.data_ptr(), *_strides(Q, "Q"), lo.data_ptr(), *_strides(lo, "lo"), hi.data_ptr(),
+                         *_strides(hi, "hi"), *_sequences(cu_q, table, len_k, (b_shape[0], page_size), ""))
+    n = L.tdq_select_pages_workspace_bytes(Tq, Hk, table.shape[1]) if workspace is None else 0
+    workspace, p_work, n_work = _scratch(workspace, n, Q.device)
+    _same_device(Q, lo, hi, cu_q, table, len_k, out, workspace)
+    at = C.addressof(h)
+    rc = L.tdq_select_pages(at, at + _HEADS, at + 2 * _HEADS, _wdt(dtype), Tq, at + 3 * _HEADS, Hq, Hk, D,
+                            1 if causal else 0, first, last, count, out.data_ptr(), p_work, n_work, _stream())
+    if rc:
+        raise TdqError(rc, "tdq_select_pages")
+    return out
+
+
+def _paged_call(Q, cache_k, cache_v, cu_q, table, len_k, out, lse, want_lse, more=()):
+    """(structures Q, O, K, V, sequences and `more` one after the other, Tq, Hq, Hk, D, out, lse)."""
+    q_shape, dtype, shape = Q.shape, Q.dtype, cache_k.shape
+    Tq, Hq, D = q_shape
+    if len(shape) != 4 or shape[3] != D or cache_k.dtype is not dtype:
+        raise ValueError("the cache must be [pages, page_size, heads, D] with Q's head size and type")
+    if out is None:
+        out = torch.empty(q_shape, dtype=dtype, device=Q.device)
+    elif out.shape != q_shape or out.dtype is not dtype:
+        raise ValueError("out must have the shape and type of Q")
+    if lse is None:
+        if want_lse:
+            lse = torch.empty((Tq, Hq), dtype=torch.float32, device=Q.device)
+    elif lse.dtype is not torch.float32 or lse.shape != (Tq, Hq) or not lse.is_contiguous():
+        raise ValueError("lse must be contiguous float32 [Tq, Hq]")
+    h = (C.c_int64 * (20 + len(more)))(
+        Q.data_ptr(), *_strides(Q, "Q"), out.data_ptr(), *_strides(out, "out"), *_cache(cache_k, "cache_k"),
+        *_cache(cache_v, "cache_v", cache_k), *_sequences(cu_q, table, len_k, shape, ""), *more)
+    return h, Tq, Hq, shape[2], D, out, lse
+
+
+_KC, _VC, _SEQ, _PRE = 2 * _HEADS, 2 * _HEADS + _PAGES, 2 * _HEADS + 2 * _PAGES, 2 * _HEADS + 2 * _PAGES + _SEQUENCES
+
+
+def tdq_attention_selected_workspace_bytes(Tq: int, Hq: int, Hk: int, D: int, page_size: int, count: int) -> int:
+    return int((_lib or lib()).tdq_attention_selected_workspace_bytes(Tq, Hq, Hk, D, page_size, count))
+
+
+def tdq_attention_selected(Q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tensor, chosen: torch.Tensor,
+                           cu_q: torch.Tensor, table: torch.Tensor, len_k: torch.Tensor,
+                           scale: Optional[float] = None, causal: bool = True, out: Optional[torch.Tensor] = None,
+                           lse: Optional[torch.Tensor] = None, want_lse: bool = False,
+                           workspace: Optional[torch.Tensor] = None):
+    """Q[Tq, Hq, D] over the pages chosen[Tq, Hk, count] of each token's sequence (tdq_select_pages) in cache_k and
+    cache_v[pages, page_size, Hk, D] -> (O[Tq, Hq, D], lse[Tq, Hq] f32 or None).  scale: 1 / sqrt(D) if None."""
+    if chosen.dtype is not torch.int32:
+        raise _wrong_type("chosen", chosen, torch.int32)
+    h, Tq, Hq, Hk, D, out, lse = _paged_call(Q, cache_k, cache_v, cu_q, table, len_k, out, lse, want_lse)
+    n = chosen.shape
+    if len(n) != 3 or n[0] != Tq or n[1] != Hk or not chosen.is_contiguous():
+        raise ValueError("chosen must be contiguous [Tq, heads of the cache, count]")
+    L, count = _lib or lib(), n[2]
+    need = 0
+    if workspace is None:
+        need = L.tdq_attention_selected_workspace_bytes(Tq, Hq, Hk, D, cache_k.shape[1], count)
+    workspace, p_work, n_work = _scratch(workspace, need, Q.device)
+    _same_device(Q, cache_k, cache_v, chosen, cu_q, table, len_k, out, lse, workspace)
+    at = C.addressof(h)
+    rc = L.tdq_attention_selected(at, at + _KC, at + _VC, _wdt(Q.dtype), Tq, at + _SEQ, Hq, Hk, D,
+                                  D ** -0.5 if scale is None else scale, 1 if causal else 0, chosen.data_ptr(), count,
+                                  at + _HEADS, _ptr(lse), p_work, n_work, _stream())
+    if rc:
+        raise TdqError(rc, "tdq_attention_selected")
+    return out, lse
+
+
+def tdq_attention_paged_workspace_bytes(Tq: int, S: int, prefixes: int, Hq: int, Hk: int, D: int) -> int:
+    return int((_lib or lib()).tdq_attention_paged_workspace_bytes(Tq, S, prefixes, Hq, Hk, D))
+
+
+def tdq_attention_paged(Q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tensor, cu_q: torch.Tensor,
+                        table: torch.Tensor, len_k: torch.Tensor, prefix=None, scale: Optional[float] = None,
+                        causal: bool = True, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                        want_lse: bool = False, workspace: Optional[torch.Tensor] = None):
+    """Q[Tq, Hq, D], packed by cu_q[S + 1], over the len_k[S] keys of each sequence in the pages table[S, pages] of
+    cache_k and cache_v[pages, page_size, Hk, D] -> (O[Tq, Hq, D], lse[Tq, Hq] f32 or None).  prefix: None, or (first
+    sequence of each prefix and the end [G + 1], its table [G, pages], its keys [G]), all int32: keys that stand in
+    front of those of its sequences.  scale: 1 / sqrt(D) if None.  Rows of queries of no sequence are not written."""
+    more, tensors, G = (), (), 0
+    if prefix is not None:
+        tensors = tuple(prefix)
+        if len(tensors) != 3:
+            raise ValueError("prefix must be (first sequences, table, keys)")
+        more = _sequences(*tensors, cache_k.shape, "prefix ")
+        G = tensors[1].shape[0]
+    h, Tq, Hq, Hk, D, out, lse = _paged_call(Q, cache_k, cache_v, cu_q, table, len_k, out, lse, want_lse, more)
+    L = _lib or lib()
+    need = L.tdq_attention_paged_workspace_bytes(Tq, table.shape[0], G, Hq, Hk, D) if workspace is None else 0
+    workspace, p_work, n_work = _scratch(workspace, need, Q.device)
+    _same_device(Q, cache_k, cache_v, cu_q, table, len_k, out, lse, workspace, *tensors)
+    at = C.addressof(h)
+    rc = L.tdq_attention_paged(at, at + _KC, at + _VC, _wdt(Q.dtype), Tq, at + _SEQ, at + _PRE if more else None, Hq, Hk,
+                               D, D ** -0.5 if scale is None else scale, 1 if causal else 0, at + _HEADS, _ptr(lse),
+                               p_work, n_work, _stream())
+    if rc:
+        raise TdqError(rc, "tdq_attention_paged")
     return out, lse
 
 
