@@ -66,18 +66,31 @@ struct GranuleCopy {
 
 // The granules of a sequence, in order.
 struct Line {
+  static constexpr bool kInOrder = true;               // granule i is keys 16 i .. 16 i + 15
   const int* table;                    // the sequence's pages
   int shift, n_pages, keys;
+  bool sure;                           // all pages of interest are there
   __device__ __forceinline__ Granule operator()(int i) const {   // (any i, as long as there is a key)
     const int last = (keys - 1) >> kGranuleBits, at = i < last ? i : last;
     const int page = load_scalar(table + (at >> (shift - kGranuleBits)));
     const bool there = i <= last && page >= 0 && page < n_pages;
     return {there ? page : -1, there ? i << kGranuleBits : kNowhere};
   }
+  // Looks at the pages of granules lo to hi.
+  __device__ __forceinline__ void look_over(int lo, int hi) {
+    sure = true;
+    if (keys <= 0) return;
+    const int bits = shift - kGranuleBits, last = (keys - 1) >> shift;
+    int end = (hi - 1) >> bits;
+    end = end < last ? end : last;
+    for (int b = (lo >> bits) + (threadIdx.x & 63); b <= end; b += 64) sure = sure && table[b] >= 0 && table[b] < n_pages;
+    sure = __ballot(!sure) == 0;
+  }
 };
 
 // The granules of a list of pages of a sequence.
 struct Chosen {
+  static constexpr bool kInOrder = false;
   const int *list, *table;
   int count, shift, n_pages, keys;
   __device__ __forceinline__ Granule operator()(int i) const {
@@ -164,8 +177,8 @@ __device__ __forceinline__ void clear(Shared<DP>& sh) {
 
 // Up to 128 rows by four wavefronts that share tiles of 64 keys, the next tile on its way while one is
 // worked on; key tiles from lo to hi.  A wavefront copies one granule of each tile.
-template <typename T, int DP, int DC, typename G>
-__device__ __forceinline__ void attend_many(Shared<DP>& sh, const Store<T, DP>& store, const G& where, const T* qp,
+template <typename T, int DP, int DC>
+__device__ __forceinline__ void attend_many(Shared<DP>& sh, const Store<T, DP>& store, const Line& where, const T* qp,
                                             int sees, int all, int last, int keys, int lo, int hi, int rows, u32 flip,
                                             float lift, const Target<T>& to) {
   constexpr int BYTES = kGranule * 2 * DP;             // of a granule in LDS
@@ -174,53 +187,43 @@ __device__ __forceinline__ void attend_many(Shared<DP>& sh, const Store<T, DP>& 
   Rows<T, DP, DC> w;
   w.start(qp, store.D, flip);
   w.addresses(lds_address(sh.many[0][0]), lds_address(sh.many[0][1]));
-  struct Four {
-    Granule own;
-    int key[4];
-  };
-  auto look = [&](int i) {
-    Four f;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) f.key[g] = where(4 * i + g).key;
-    f.own = where(4 * i + wave);
-    return f;
-  };
   auto copy = [&](const Granule& g, int stage) {
     store.copy_k(g, keys, lds_address(sh.many[stage][0]) + wave * BYTES);
     store.copy_v(g, keys, lds_address(sh.many[stage][1]) + wave * BYTES);
   };
-  Four now = {}, next = {};
-  if (lo < hi) now = look(lo);
+  Granule next = {-1, kNowhere};
+  if (lo < hi) next = where(4 * lo + wave);
   if (STAGES == 2 && lo < hi) {
-    copy(now.own, 0);
-    if (lo + 1 < hi) next = look(lo + 1);
+    copy(next, 0);
+    if (lo + 1 < hi) next = where(4 * (lo + 1) + wave);
   }
   for (int i = lo; i < hi; ++i) {
     const int stage = STAGES == 2 ? (i - lo) & 1 : 0;
     if (STAGES == 1) {
       __syncthreads();                                 // the last tile has been read
-      copy(now.own, 0);
-      if (i + 1 < hi) next = look(i + 1);
+      copy(next, 0);
+      if (i + 1 < hi) next = where(4 * (i + 1) + wave);
     }
     wait_copies();
     __syncthreads();
-    if (STAGES == 2 && i + 1 < hi) copy(next.own, stage ^ 1);
+    if (STAGES == 2 && i + 1 < hi) copy(next, stage ^ 1);
     if (i * kTileKeys < last) {
       f32x16 s[2];
       u32 p[2][8];
       s[0] = w.scores(0);
       s[1] = w.scores(32);
-      bool masked = false;
+      const bool masked = !where.sure || (i + 1) * kTileKeys > all;
+      int key[4] = {0, 0, 0, 0};
+      if (masked) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g) masked |= now.key[g] + kGranule > all;
-      w.softmax(s, p, to.scale_log2, lift, masked,
-                [&](int k) { return now.key[k / kGranule] + k % kGranule < sees; });
+        for (int g = 0; g < 4; ++g) key[g] = where.sure ? (4 * i + g) * kGranule : where(4 * i + g).key;
+      }
+      w.softmax(s, p, to.scale_log2, lift, masked, [&](int k) { return key[k / kGranule] + k % kGranule < sees; });
       w.values(0, p[0]);
       w.values(32, p[1]);
     }
-    now = next;
     if (STAGES == 2) {
-      if (i + 2 < hi) next = look(i + 2);
+      if (i + 2 < hi) next = where(4 * (i + 2) + wave);
       w.move(stage ? -(int)sizeof(sh.many[0]) : (int)sizeof(sh.many[0]));
     }
   }
@@ -304,9 +307,16 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const Store<T, DP>& s
       s[0] = w.scores(0);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // K has been read
       if (more) copy_k(next);
-      const bool masked = now.g[0].key + kGranule > all || now.g[1].key + kGranule > all;
-      w.softmax(s, p, to.scale_log2, lift, masked,
-                [&](int k) { return now.g[k / kGranule].key + k % kGranule < sees; });
+      bool masked = now.g[0].key + kGranule > all || now.g[1].key + kGranule > all;
+      int key[2] = {now.g[0].key, now.g[1].key};
+      if constexpr (G::kInOrder) {
+        masked = !where.sure || (i + 1) * kFewKeys > all;
+        if (masked) {
+#pragma unroll
+          for (int g = 0; g < 2; ++g) key[g] = where.sure ? (2 * i + g) * kGranule : where(2 * i + g).key;
+        }
+      }
+      w.softmax(s, p, to.scale_log2, lift, masked, [&](int k) { return key[k / kGranule] + k % kGranule < sees; });
       if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
       else wait_copies();
       w.values(0, p[0]);
@@ -375,35 +385,29 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const Store<T, DP>& s
   __syncthreads();                                       // (LDS is free for a next tile)
 }
 
-// Joins the parts of a row, by a wavefront: `part(i)` says where the sums and the values of part i < n are
-// (nullptr: there is none).  A group of lanes has four outputs each of one part, as many parts at a time
-// as there are groups, all of them on their way at once; weights were found before, a lane a part.
-struct Part {
-  const float *ml, *o;
-};
+// Joins the parts of a row, by a wavefront: part i < n has its sums at ml(i) and its values at o(i).  A
+// group of lanes has four outputs each of one part, as many parts at a time as there are groups, all of
+// them on their way at once; weights were found before, a lane a part.
 constexpr int kMaxParts = 512 + 4;
-template <typename T, typename F>
-__device__ __forceinline__ void join_row(float* weight, int n, F part, int D, float scale_log2, T* op, float* lse) {
+template <typename T, typename F, typename H>
+__device__ __forceinline__ void join_row(float* weight, int n, F ml, H o, int D, float scale_log2, T* op, float* lse) {
   const int lane = threadIdx.x & 63;
-  float m = -INFINITY;
-  for (int i = lane; i < n; i += 64) {
-    const Part p = part(i);
-    const float mi = p.ml ? p.ml[0] : -INFINITY;
-    m = fmaxf(m, mi);
-  }
+  f32x2 own = {-INFINITY, 0.f};                          // of part `lane`
+  if (lane < n) own = *reinterpret_cast<const f32x2*>(ml(lane));
+  float m = own[0];
+  for (int i = lane + 64; i < n; i += 64) m = fmaxf(m, ml(i)[0]);
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
   float l = 0.f;
   for (int i = lane; i < n; i += 64) {
-    const Part p = part(i);
-    const float mi = p.ml ? p.ml[0] : -INFINITY, li = p.ml ? p.ml[1] : 0.f;
+    const f32x2 x = i == lane ? own : *reinterpret_cast<const f32x2*>(ml(i));
     // A part without keys is left out, marked by a negative weight.  One of nothing but NaN has the
     // same maximum of -inf, and its sum makes the row NaN; one whose weight rounds to 0 still counts,
     // as its values may not be finite.
-    const bool none = no_weight(mi, li);
-    const float f = li != li ? li : __builtin_amdgcn_exp2f((mi - m) * scale_log2);
+    const bool none = no_weight(x[0], x[1]);
+    const float f = x[1] != x[1] ? x[1] : __builtin_amdgcn_exp2f((x[0] - m) * scale_log2);
     weight[i] = none ? -1.f : f;
-    if (!none) l = fmaf(li, f, l);
+    if (!none) l = fmaf(x[1], f, l);
   }
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
@@ -415,7 +419,7 @@ __device__ __forceinline__ void join_row(float* weight, int n, F part, int D, fl
 #pragma unroll 4
     for (int i = group; i < n; i += groups) {
       const float f = weight[i];
-      if (!(f < 0.f)) y += *reinterpret_cast<const f32x4*>(part(i).o + c) * f;
+      if (!(f < 0.f)) y += *reinterpret_cast<const f32x4*>(o(i) + c) * f;
     }
   }
   for (int d = 32; d >= quads; d >>= 1)
@@ -452,9 +456,18 @@ struct PagedArgs {
   u32 flip;
   int pieces;                          // most pieces of a line
   int cap;                             // rows of a part: as many as a tile may have
-  long long* plan;                     // [prefixes and sequences]: the places on the line that they begin at, then its length
+  int* first_tile;                     // [prefixes + 2]: of every prefix, of the first sequence, and the end
+  struct TileParts* tiles;             // [max_tiles][Hk]: where the parts of each are
+  long long max_tiles;
   float *part_o, *part_ml;             // [pieces Hk][2][cap]: of tiles that begin before a piece, and that end behind it
   float *whole_o, *whole_ml;           // with prefixes: [2][Tq Hq], of tiles of one (prefixes, sequences) in one piece
+};
+
+// What the second kernel needs to know of a tile.
+struct TileParts {
+  int piece, count;                    // its first piece, and how many it lies in
+  int t0, first, rows;                 // its first token, which of that one's heads is its first row
+  int seq, unused[2];
 };
 
 constexpr int kTileCost = 2;           // what a tile takes beside its keys, in tiles of 64 keys
@@ -540,7 +553,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     PagedArgs a) {
   __shared__ __attribute__((aligned(1024))) Shared<DP> sh;
   __shared__ long long wave_sum[4];
-  __shared__ long long found[2];                         // item, and the place it begins at
+  __shared__ int wave_tiles[4];
+  __shared__ long long found[3];                         // item, the place it begins at, its first tile
   const int hk = (int)(blockIdx.x % (unsigned)a.Hk), k = (int)(blockIdx.x / (unsigned)a.Hk);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
@@ -548,29 +562,45 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   const int items = a.pre.S + a.own.S, each = (items + 255) / 256;
   const int v0 = tid * each < items ? tid * each : items, v1 = v0 + each < items ? v0 + each : items;
   long long mine = 0;
+  int mine_tiles = 0;
   for (int v = v0; v < v1; ++v) {
     const Item x = item_of(a, v);
     mine += x.cost(x.tiles);
+    mine_tiles += (int)x.tiles;
   }
   long long upto = mine;
+  int tiles_upto = mine_tiles;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const long long o = __shfl_up(upto, d, 64);
-    if (lane >= d) upto += o;
+    const int ot = __shfl_up(tiles_upto, d, 64);
+    if (lane >= d) {
+      upto += o;
+      tiles_upto += ot;
+    }
   }
-  if (lane == 63) wave_sum[wave] = upto;
+  if (lane == 63) {
+    wave_sum[wave] = upto;
+    wave_tiles[wave] = tiles_upto;
+  }
   __syncthreads();
   long long before = upto - mine, total = 0;
+  int tiles_before = tiles_upto - mine_tiles, all_tiles = 0;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    if (w < wave) before += wave_sum[w];
+    if (w < wave) {
+      before += wave_sum[w];
+      tiles_before += wave_tiles[w];
+    }
     total += wave_sum[w];
+    all_tiles += wave_tiles[w];
   }
   const int n = pieces_of(a, total);
-  if (total == 0 || k >= n) {
-    if (blockIdx.x == 0 && tid == 0) a.plan[items] = 0;
-    return;
+  if (blockIdx.x == 0 && tid == 0) {
+    if (a.pre.S == 0 || total == 0) a.first_tile[a.pre.S] = 0;
+    a.first_tile[a.pre.S + 1] = all_tiles;
   }
+  if (total == 0 || k >= n) return;
   const long long from = piece_at(total, k, n), to = piece_at(total, k + 1, n);
   for (int v = v0; v < v1; ++v) {
     const Item x = item_of(a, v);
@@ -578,15 +608,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     if (before <= from && from < next) {
       found[0] = v;
       found[1] = before;
+      found[2] = tiles_before;
     }
-    if (blockIdx.x == 0) a.plan[v] = before;
+    if (blockIdx.x == 0 && v <= a.pre.S && a.pre.S > 0) a.first_tile[v] = tiles_before;
     before = next;
+    tiles_before += (int)x.tiles;
   }
-  if (blockIdx.x == 0 && tid == 0) a.plan[items] = total;
   __syncthreads();
 
   int v = __builtin_amdgcn_readfirstlane((int)found[0]);
   long long start = found[1];
+  int tile0 = __builtin_amdgcn_readfirstlane((int)found[2]);
   Item x = item_of(a, v);
   long long r = 0;
   for (long long count = x.tiles; count > 1;) {          // the last tile that begins no later than the piece
@@ -617,7 +649,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
         const int e = (first + row) / a.group + ahead;
         return e < 0 ? 0 : e < keys ? e : keys;
       };
-      const Line where = {q.table + line * q.ld, q.shift, q.n_pages, keys};
+      Line where = {q.table + line * q.ld, q.shift, q.n_pages, keys, true};
+      where.look_over(lo * (kTileKeys / kGranule), hi * (kTileKeys / kGranule));
+      if (lo == 0 && tid == 0 && tile0 + r < a.max_tiles) {
+        // the last piece that the tile lies in: of those that begin in front of its end
+        int last = (int)((s.end - 1) * n / total);
+        while (last > k && piece_at(total, last, n) >= s.end) --last;
+        while (last + 1 < n && piece_at(total, last + 1, n) < s.end) ++last;
+        a.tiles[(tile0 + r) * a.Hk + hk] = TileParts{k, last - k + 1, t0, first, rows, line, {0, 0}};
+      }
       const Store<T, DP> store(a.K, a.V, hk, q.shift, a.D);
       Target<T> target;
       target.O = static_cast<T*>(a.O) + t0 * a.o_token + (long long)hk * a.group * a.o_head;
@@ -631,7 +671,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
       target.D = a.D;
       target.po = target.pml = nullptr;
       if (lo > 0 || hi < s.tiles) {
-        const long long slot = 2ll * blockIdx.x + (lo > 0 ? 0 : 1);
+        const long long slot = 2 * ((long long)k * a.Hk + hk) + (lo > 0 ? 0 : 1);
         target.po = a.part_o + slot * a.cap * a.D;
         target.pml = a.part_ml + slot * a.cap * 2;
       } else if (a.pre.S > 0) {
@@ -662,9 +702,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
         attend_many<T, DP, DC>(sh, store, where, qp, sees(row), all, last, keys, lo, stop, rows, a.flip, a.lift, target);
       }
     }
+    if (lo >= hi && lo > 0 && lo < s.tiles && tid < kManyRows && tid < x.rows - r * kManyRows) {
+      // (no keys of the tile for this piece, though some for those before and behind)
+      const long long slot = 2 * ((long long)k * a.Hk + hk);
+      *reinterpret_cast<f32x2*>(a.part_ml + (slot * a.cap + tid) * 2) = f32x2{-INFINITY, 0.f};
+    }
     if (s.end >= to) break;
     if (++r >= x.tiles) {
       start += x.cost(x.tiles);
+      tile0 += (int)x.tiles;
       r = 0;
       do {
         if (++v >= items) return;
@@ -674,78 +720,54 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   }
 }
 
-// Joins the tiles that lie in several pieces, and prefixes with sequences: a wavefront a row, some rows
-// each.
+// Joins the tiles that lie in several pieces, and prefixes with sequences: a wavefront a row, 16 rows of a
+// tile a workgroup.
+constexpr int kJoinRows = 16;
 template <typename T>
-__global__ __launch_bounds__(256) void k_join_pages(PagedArgs a, int heads, int chunks) {
+__global__ __launch_bounds__(256) void k_join_pages(PagedArgs a, int chunks) {
   __shared__ float weight[4][kMaxParts];
   const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
-  const long long t = id / chunks;
-  if (t >= a.Tq) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h0 = ((int)(id % chunks) * 4 + wave) * heads, h1 = h0 + heads < a.Hq ? h0 + heads : a.Hq;
-  const int items = a.pre.S + a.own.S;
-  const long long total = a.plan[items];
-  if (total <= 0) return;
-  const int n = pieces_of(a, total);
-  const int s = last_at_most(a.own.S, t, [&](int i) { return start_of(a.own.cu, i, a.Tq); });
-  if (t < start_of(a.own.cu, s, a.Tq) || t >= start_of(a.own.cu, s + 1, a.Tq)) return;
+  const int hk = (int)(id % a.Hk), chunk = (int)(id / a.Hk % chunks);
+  const long long first_own = a.first_tile[a.pre.S], tile = first_own + id / a.Hk / chunks;
+  if (tile >= a.first_tile[a.pre.S + 1] || tile >= a.max_tiles) return;
+  const TileParts own = a.tiles[tile * a.Hk + hk];
+  if (own.count == 1 && a.pre.S == 0) return;            // (its one piece has written the output)
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int p = -1;                                            // the sequence's prefix
+  long long pre_row = 0;                                 // the tile's first row among the prefix's
   if (a.pre.S > 0) {
-    p = last_at_most(a.pre.S, s, [&](int i) { return start_of(a.pre.cu, i, a.own.S); });
-    if (s < start_of(a.pre.cu, p, a.own.S) || s >= start_of(a.pre.cu, p + 1, a.own.S)) p = -1;
+    p = last_at_most(a.pre.S, own.seq, [&](int i) { return start_of(a.pre.cu, i, a.own.S); });
+    const int from = start_of(a.pre.cu, p, a.own.S);
+    if (own.seq < from || own.seq >= start_of(a.pre.cu, p + 1, a.own.S)) p = -1;
+    else pre_row = (long long)(own.t0 - start_of(a.own.cu, from, a.Tq)) * a.group + own.first;
   }
-  // of the prefix and of the sequence: the tile that a row lies in, and its pieces
-  struct Pieces {
-    Stretch s;
-    int first, count, row;
-    long long whole;                                     // row among those of tiles in one piece
-  };
-  const Item own = item_of(a, a.pre.S + s), pre = p < 0 ? own : item_of(a, p);
-  const long long own_start = a.plan[a.pre.S + s], pre_start = p < 0 ? 0 : a.plan[p];
-  auto pieces = [&](const Item& x, long long start, int hk, int e) {
-    Pieces q;
-    const long long row = (t - x.t0) * a.group + e, r = row / kManyRows;
-    q.row = (int)(row - r * kManyRows);
-    q.s = stretch_of(x, start, r);
-    int k0 = (int)(q.s.begin * n / total), k1 = (int)((q.s.end - 1) * n / total);
-    while (k0 > 0 && piece_at(total, k0, n) > q.s.begin) --k0;
-    while (k0 + 1 < n && piece_at(total, k0 + 1, n) <= q.s.begin) ++k0;
-    while (k1 > k0 && piece_at(total, k1, n) >= q.s.end) --k1;
-    while (k1 + 1 < n && piece_at(total, k1 + 1, n) < q.s.end) ++k1;
-    q.first = k0;
-    q.count = k1 - k0 + 1;
-    q.whole = hk * a.Tq * a.group + t * a.group + e;
-    return q;
-  };
-  for (int h = h0; h < h1; ++h) {
-    const int hk = h / a.group, e = h - hk * a.group;
-    const Pieces of_own = pieces(own, own_start, a.pre.S > 0 ? a.Hk + hk : hk, e);
-    Pieces of_pre = of_own;
-    if (p >= 0) of_pre = pieces(pre, pre_start, hk, e);
-    const int before = p < 0 ? 0 : of_pre.count;
-    if (a.pre.S == 0) {
-      // (one piece has all the keys: it has written the output)
-      bool whole = false;
-      for (int i = lane; i < of_own.count; i += 64) {
-        const int k = of_own.first + i;
-        whole |= of_own.s.at(piece_at(total, k, n)) == 0 && of_own.s.at(piece_at(total, k + 1, n)) == of_own.s.tiles;
-      }
-      if (__ballot(whole)) continue;
+  const int end = (chunk + 1) * kJoinRows < own.rows ? (chunk + 1) * kJoinRows : own.rows;
+  for (int r = chunk * kJoinRows + wave; r < end; r += 4) {
+    const int token = (own.first + r) / a.group, e = own.first + r - token * a.group;
+    const long long t = own.t0 + token, whole = hk * a.Tq * a.group + t * a.group + e;
+    // (parts of a tile: the first ends behind its piece, the others begin in front of theirs)
+    auto slot = [&](const TileParts& d, int i, int row) {
+      return (2 * ((long long)(d.piece + i) * a.Hk + hk) + (i == 0)) * a.cap + row;
+    };
+    TileParts pre = {};
+    int in_pre = 0;
+    if (p >= 0) {
+      const long long row = pre_row + r;
+      const long long of = a.first_tile[p] + row / kManyRows;
+      in_pre = (int)(row % kManyRows);
+      if (row >= 0 && of < first_own) pre = a.tiles[of * a.Hk + hk];
     }
-    auto of_piece = [&](const Pieces& q, int k) -> Part {
-      const int lo = q.s.at(piece_at(total, k, n)), hi = q.s.at(piece_at(total, k + 1, n));
-      if (lo >= hi) return {nullptr, nullptr};
-      if (lo > 0 || hi < q.s.tiles) {
-        const long long at = (2 * ((long long)k * a.Hk + hk) + (lo > 0 ? 0 : 1)) * a.cap + q.row;
-        return {a.part_ml + 2 * at, a.part_o + at * a.D};
-      }
-      return {a.whole_ml + 2 * q.whole, a.whole_o + q.whole * a.D};
+    const long long all = a.Tq * a.Hq;
+    auto ml = [&](int i) -> const float* {
+      if (i < pre.count) return pre.count == 1 ? a.whole_ml + 2 * whole : a.part_ml + 2 * slot(pre, i, in_pre);
+      return own.count == 1 ? a.whole_ml + 2 * (all + whole) : a.part_ml + 2 * slot(own, i - pre.count, r);
     };
-    auto part = [&](int i) -> Part {
-      return i < before ? of_piece(of_pre, of_pre.first + i) : of_piece(of_own, of_own.first + i - before);
+    auto o = [&](int i) -> const float* {
+      if (i < pre.count) return pre.count == 1 ? a.whole_o + whole * a.D : a.part_o + slot(pre, i, in_pre) * a.D;
+      return own.count == 1 ? a.whole_o + (all + whole) * a.D : a.part_o + slot(own, i - pre.count, r) * a.D;
     };
-    join_row<T>(weight[wave], before + of_own.count, part, a.D, a.scale_log2,
+    const int h = hk * a.group + e;
+    join_row<T>(weight[wave], pre.count + own.count, ml, o, a.D, a.scale_log2,
                 static_cast<T*>(a.O) + t * a.o_token + h * a.o_head, a.lse ? a.lse + t * a.Hq + h : nullptr);
   }
 }
@@ -757,8 +779,9 @@ static int paged_pieces(int Hk, int D) {
 }
 
 struct PagedLayout {
-  size_t plan, ml, o, whole_ml, whole_o, total;
+  size_t tiles, ml, o, whole_ml, whole_o, total;         // (the first tiles at 0)
   int pieces, cap;
+  long long own_tiles, max_tiles;                        // of all sequences, and with the prefixes, at most
 };
 static PagedLayout paged_layout(long long Tq, int S, int prefixes, int Hq, int Hk, int D) {
   PagedLayout l;
@@ -767,8 +790,10 @@ static PagedLayout paged_layout(long long Tq, int S, int prefixes, int Hq, int H
   l.pieces = paged_pieces(Hk, D);
   const size_t parts = 2ull * l.pieces * Hk * l.cap, whole = prefixes > 0 ? 2ull * Tq * Hq : 0;
   auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
-  l.plan = 0;
-  l.ml = up((size_t)(S + prefixes + 1) * sizeof(long long));
+  l.own_tiles = rows / kManyRows + S;
+  l.tiles = up((size_t)(prefixes + 2) * sizeof(int));
+  l.max_tiles = l.own_tiles + (prefixes > 0 ? rows / kManyRows + prefixes : 0);
+  l.ml = l.tiles + up((size_t)l.max_tiles * Hk * sizeof(TileParts));
   l.o = l.ml + up(parts * 2 * sizeof(float));
   l.whole_ml = l.o + up(parts * D * sizeof(float));
   l.whole_o = l.whole_ml + up(whole * 2 * sizeof(float));
@@ -829,7 +854,9 @@ hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages*
   a.pieces = l.pieces;
   a.cap = l.cap;
   char* w = static_cast<char*>(workspace);
-  a.plan = reinterpret_cast<long long*>(w + l.plan);
+  a.first_tile = reinterpret_cast<int*>(w);
+  a.tiles = reinterpret_cast<TileParts*>(w + l.tiles);
+  a.max_tiles = l.max_tiles;
   a.part_ml = reinterpret_cast<float*>(w + l.ml);
   a.part_o = reinterpret_cast<float*>(w + l.o);
   a.whole_ml = reinterpret_cast<float*>(w + l.whole_ml);
@@ -839,10 +866,10 @@ hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages*
   if (dt == TDQ_F16) TDQ_BY_HEAD(TDQ_PAGED, _Float16);
   else TDQ_BY_HEAD(TDQ_PAGED, __bf16);
 #undef TDQ_PAGED
-  const int heads = Tq * Hq > 16384 ? 4 : 1, chunks = (Hq + 4 * heads - 1) / (4 * heads);
-  const dim3 join = two_axes(Tq * chunks);
-  if (dt == TDQ_F16) hipLaunchKernelGGL((k_join_pages<_Float16>), join, dim3(256), 0, st, a, heads, chunks);
-  else hipLaunchKernelGGL((k_join_pages<__bf16>), join, dim3(256), 0, st, a, heads, chunks);
+  const int chunks = (l.cap + kJoinRows - 1) / kJoinRows;
+  const dim3 join = two_axes(l.own_tiles * Hk * chunks);
+  if (dt == TDQ_F16) hipLaunchKernelGGL((k_join_pages<_Float16>), join, dim3(256), 0, st, a, chunks);
+  else hipLaunchKernelGGL((k_join_pages<__bf16>), join, dim3(256), 0, st, a, chunks);
   return hipGetLastError();
 }
 
@@ -929,11 +956,9 @@ __global__ __launch_bounds__(256) void k_join_chosen(ChosenArgs a) {
   const Sequences& q = a.seq;
   const int s = last_at_most(q.S, t, [&](int i) { return start_of(q.cu, i, a.Tq); });
   if (t < start_of(q.cu, s, a.Tq) || t >= start_of(q.cu, s + 1, a.Tq)) return;
-  auto part = [&](int i) -> Part {
-    const long long at = i * a.Tq * a.Hq + row;
-    return {a.part_ml + 2 * at, a.part_o + at * a.D};
-  };
-  join_row<T>(weight[threadIdx.x >> 6], a.splits, part, a.D, a.scale_log2,
+  auto at = [&](int i) { return i * a.Tq * a.Hq + row; };
+  join_row<T>(weight[threadIdx.x >> 6], a.splits, [&](int i) { return a.part_ml + 2 * at(i); },
+              [&](int i) { return a.part_o + at(i) * a.D; }, a.D, a.scale_log2,
               static_cast<T*>(a.O) + t * a.o_token + h * a.o_head, a.lse ? a.lse + row : nullptr);
 }
 
