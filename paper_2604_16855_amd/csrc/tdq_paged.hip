@@ -385,22 +385,48 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const Store<T, DP>& s
   __syncthreads();                                       // (LDS is free for a next tile)
 }
 
-// Joins the parts of a row, by a wavefront: part i < n has its sums at ml(i) and its values at o(i).  A
-// group of lanes has four outputs each of one part, as many parts at a time as there are groups, all of
-// them on their way at once; weights were found before, a lane a part.
+// Parts of a row: of the first one the sums are at ml and the values at o, the others' `step` rows behind
+// each other from `gap` rows in front of it on.
+struct Run {
+  const float *ml, *o;
+  long long step, gap;
+  int count;
+};
+
+// Joins the parts of two runs for a row, by a wavefront.  A group of lanes has four outputs each of one
+// part, as many parts at a time as there are groups, the first ones on their way with the sums; weights are
+// found before, a lane a part.
 constexpr int kMaxParts = 512 + 4;
-template <typename T, typename F, typename H>
-__device__ __forceinline__ void join_row(float* weight, int n, F ml, H o, int D, float scale_log2, T* op, float* lse) {
-  const int lane = threadIdx.x & 63;
+template <typename T>
+__device__ __forceinline__ void join_row(float* weight, const Run& a, const Run& b, int D, float scale_log2, T* op,
+                                         float* lse) {
+  constexpr int AHEAD = 4;
+  const int lane = threadIdx.x & 63, n = a.count + b.count;
+  const int quads = D <= 32 ? 8 : D <= 64 ? 16 : D <= 128 ? 32 : 64;
+  const int c = 4 * (lane & (quads - 1)), group = lane / quads, groups = 64 / quads;
+  auto row = [&](int i) {                                // of its run
+    const bool first = i < a.count;
+    const int at = first ? i : i - a.count;
+    return at == 0 ? 0 : at * (first ? a.step : b.step) - (first ? a.gap : b.gap);
+  };
+  auto ml = [&](int i) { return *reinterpret_cast<const f32x2*>((i < a.count ? a.ml : b.ml) + 2 * row(i)); };
+  auto value = [&](int i) { return *reinterpret_cast<const f32x4*>((i < a.count ? a.o : b.o) + row(i) * D + c); };
+  f32x4 early[AHEAD];
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j) {
+    const int i = group + j * groups;
+    early[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (c < D && i < n) early[j] = value(i);
+  }
   f32x2 own = {-INFINITY, 0.f};                          // of part `lane`
-  if (lane < n) own = *reinterpret_cast<const f32x2*>(ml(lane));
+  if (lane < n) own = ml(lane);
   float m = own[0];
   for (int i = lane + 64; i < n; i += 64) m = fmaxf(m, ml(i)[0]);
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
   float l = 0.f;
   for (int i = lane; i < n; i += 64) {
-    const f32x2 x = i == lane ? own : *reinterpret_cast<const f32x2*>(ml(i));
+    const f32x2 x = i == lane ? own : ml(i);
     // A part without keys is left out, marked by a negative weight.  One of nothing but NaN has the
     // same maximum of -inf, and its sum makes the row NaN; one whose weight rounds to 0 still counts,
     // as its values may not be finite.
@@ -412,14 +438,19 @@ __device__ __forceinline__ void join_row(float* weight, int n, F ml, H o, int D,
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
   __builtin_amdgcn_wave_barrier();
-  const int quads = D <= 32 ? 8 : D <= 64 ? 16 : D <= 128 ? 32 : 64;
-  const int c = 4 * (lane & (quads - 1)), group = lane / quads, groups = 64 / quads;
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
   if (c < D) {
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const int i = group + j * groups;
+      const float f = i < n ? weight[i] : -1.f;
+      if (!(f < 0.f)) y += early[j] * f;
+    }
 #pragma unroll 4
-    for (int i = group; i < n; i += groups) {
+    for (int i = group + AHEAD * groups; i < n; i += groups) {
+      const f32x4 x = value(i);
       const float f = weight[i];
-      if (!(f < 0.f)) y += *reinterpret_cast<const f32x4*>(o(i) + c) * f;
+      if (!(f < 0.f)) y += x * f;
     }
   }
   for (int d = 32; d >= quads; d >>= 1)
@@ -456,18 +487,18 @@ struct PagedArgs {
   u32 flip;
   int pieces;                          // most pieces of a line
   int cap;                             // rows of a part: as many as a tile may have
-  int* first_tile;                     // [prefixes + 2]: of every prefix, of the first sequence, and the end
-  struct TileParts* tiles;             // [max_tiles][Hk]: where the parts of each are
-  long long max_tiles;
+  int* first_tile;                     // [prefixes + 2]: tiles of the sequences, of the prefixes, and in front of each
+  struct TileParts* tiles;             // [own_tiles + pre_tiles][Hk]: where the parts of each are, sequences first
+  long long own_tiles, pre_tiles;      // (room for so many)
+  int2* place;                         // [Tq]: tile and row of it of a token's first row
   float *part_o, *part_ml;             // [pieces Hk][2][cap]: of tiles that begin before a piece, and that end behind it
   float *whole_o, *whole_ml;           // with prefixes: [2][Tq Hq], of tiles of one (prefixes, sequences) in one piece
 };
 
-// What the second kernel needs to know of a tile.
+// What the second kernel needs to know of a tile: its first piece, and how many it lies in, and the
+// sequence (or prefix).
 struct TileParts {
-  int piece, count;                    // its first piece, and how many it lies in
-  int t0, first, rows;                 // its first token, which of that one's heads is its first row
-  int seq, unused[2];
+  int piece, count, line, unused;
 };
 
 constexpr int kTileCost = 2;           // what a tile takes beside its keys, in tiles of 64 keys
@@ -554,7 +585,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   __shared__ __attribute__((aligned(1024))) Shared<DP> sh;
   __shared__ long long wave_sum[4];
   __shared__ int wave_tiles[4];
-  __shared__ long long found[3];                         // item, the place it begins at, its first tile
+  __shared__ long long found[4];                         // item, the place it begins at, its first tile, tiles of prefixes
   const int hk = (int)(blockIdx.x % (unsigned)a.Hk), k = (int)(blockIdx.x / (unsigned)a.Hk);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
@@ -596,11 +627,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     all_tiles += wave_tiles[w];
   }
   const int n = pieces_of(a, total);
-  if (blockIdx.x == 0 && tid == 0) {
-    if (a.pre.S == 0 || total == 0) a.first_tile[a.pre.S] = 0;
-    a.first_tile[a.pre.S + 1] = all_tiles;
+  if (total == 0 || k >= n) {
+    if (blockIdx.x == 0 && tid == 0) a.first_tile[0] = 0;
+    return;
   }
-  if (total == 0 || k >= n) return;
   const long long from = piece_at(total, k, n), to = piece_at(total, k + 1, n);
   for (int v = v0; v < v1; ++v) {
     const Item x = item_of(a, v);
@@ -610,7 +640,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
       found[1] = before;
       found[2] = tiles_before;
     }
-    if (blockIdx.x == 0 && v <= a.pre.S && a.pre.S > 0) a.first_tile[v] = tiles_before;
+    if (v == a.pre.S) found[3] = tiles_before;           // tiles of prefixes
+    if (blockIdx.x == 0 && v < a.pre.S) a.first_tile[v + 2] = tiles_before;
     before = next;
     tiles_before += (int)x.tiles;
   }
@@ -619,6 +650,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   int v = __builtin_amdgcn_readfirstlane((int)found[0]);
   long long start = found[1];
   int tile0 = __builtin_amdgcn_readfirstlane((int)found[2]);
+  const int pre_tiles = __builtin_amdgcn_readfirstlane((int)found[3]);
+  if (blockIdx.x == 0 && tid == 0) {
+    a.first_tile[0] = all_tiles - pre_tiles;
+    a.first_tile[1] = pre_tiles;
+  }
   Item x = item_of(a, v);
   long long r = 0;
   for (long long count = x.tiles; count > 1;) {          // the last tile that begins no later than the piece
@@ -651,12 +687,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
       };
       Line where = {q.table + line * q.ld, q.shift, q.n_pages, keys, true};
       where.look_over(lo * (kTileKeys / kGranule), hi * (kTileKeys / kGranule));
-      if (lo == 0 && tid == 0 && tile0 + r < a.max_tiles) {
+      const long long tile = prefix ? a.own_tiles + tile0 + r : tile0 - pre_tiles + r;
+      if (lo == 0 && tid == 0 && tile < (prefix ? a.own_tiles + a.pre_tiles : a.own_tiles)) {
         // the last piece that the tile lies in: of those that begin in front of its end
         int last = (int)((s.end - 1) * n / total);
         while (last > k && piece_at(total, last, n) >= s.end) --last;
         while (last + 1 < n && piece_at(total, last + 1, n) < s.end) ++last;
-        a.tiles[(tile0 + r) * a.Hk + hk] = TileParts{k, last - k + 1, t0, first, rows, line, {0, 0}};
+        a.tiles[tile * a.Hk + hk] = TileParts{k, last - k + 1, line, 0};
+      }
+      if (lo == 0 && hk == 0 && !prefix) {
+        // (tokens whose first row lies in the tile)
+        const int row = tid * a.group - first;
+        if (row >= 0 && row < rows) a.place[t0 + tid] = make_int2(tile0 - pre_tiles + (int)r, row);
       }
       const Store<T, DP> store(a.K, a.V, hk, q.shift, a.D);
       Target<T> target;
@@ -720,56 +762,63 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   }
 }
 
-// Joins the tiles that lie in several pieces, and prefixes with sequences: a wavefront a row, 16 rows of a
-// tile a workgroup.
-constexpr int kJoinRows = 16;
+// Joins the tiles that lie in several pieces, and prefixes with sequences: a wavefront a row.
 template <typename T>
-__global__ __launch_bounds__(256) void k_join_pages(PagedArgs a, int chunks) {
+__global__ __launch_bounds__(256, 4) void k_join_pages(PagedArgs a, int chunks) {
   __shared__ float weight[4][kMaxParts];
   const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
-  const int hk = (int)(id % a.Hk), chunk = (int)(id / a.Hk % chunks);
-  const long long first_own = a.first_tile[a.pre.S], tile = first_own + id / a.Hk / chunks;
-  if (tile >= a.first_tile[a.pre.S + 1] || tile >= a.max_tiles) return;
+  const long long t = id / chunks;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = (int)(id % chunks) * 4 + wave;
+  if (t >= a.Tq || h >= a.Hq) return;
+  const int lane = threadIdx.x & 63, hk = h / a.group, e = h - hk * a.group;
+  // (all on their way at once; what lies there is looked at if the token is one of a sequence)
+  const int begin = start_of(a.own.cu, 0, a.Tq), end = start_of(a.own.cu, a.own.S, a.Tq);
+  const int tiles = a.first_tile[0], pre_tiles = a.first_tile[1];
+  const int2 place = a.place[t];
+  int from = 0, to = 0, first = 0;                       // of prefix `lane`: its sequences, its first tile
+  const bool few = a.pre.S <= 64;
+  if (lane < a.pre.S && few) {
+    from = start_of(a.pre.cu, lane, a.own.S);
+    to = start_of(a.pre.cu, lane + 1, a.own.S);
+    first = a.first_tile[2 + lane];
+  }
+  if (t < begin || t >= end) return;
+  const long long own_row = place.y + e, tile = place.x + own_row / kManyRows;
+  if (place.y < 0 || tile < 0 || tile >= tiles || tile >= a.own_tiles) return;
   const TileParts own = a.tiles[tile * a.Hk + hk];
   if (own.count == 1 && a.pre.S == 0) return;            // (its one piece has written the output)
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int p = -1;                                            // the sequence's prefix
-  long long pre_row = 0;                                 // the tile's first row among the prefix's
+  TileParts pre = {0, 0, 0, 0};
+  int pre_row = 0;
   if (a.pre.S > 0) {
-    p = last_at_most(a.pre.S, own.seq, [&](int i) { return start_of(a.pre.cu, i, a.own.S); });
-    const int from = start_of(a.pre.cu, p, a.own.S);
-    if (own.seq < from || own.seq >= start_of(a.pre.cu, p + 1, a.own.S)) p = -1;
-    else pre_row = (long long)(own.t0 - start_of(a.own.cu, from, a.Tq)) * a.group + own.first;
-  }
-  const int end = (chunk + 1) * kJoinRows < own.rows ? (chunk + 1) * kJoinRows : own.rows;
-  for (int r = chunk * kJoinRows + wave; r < end; r += 4) {
-    const int token = (own.first + r) / a.group, e = own.first + r - token * a.group;
-    const long long t = own.t0 + token, whole = hk * a.Tq * a.group + t * a.group + e;
-    // (parts of a tile: the first ends behind its piece, the others begin in front of theirs)
-    auto slot = [&](const TileParts& d, int i, int row) {
-      return (2 * ((long long)(d.piece + i) * a.Hk + hk) + (i == 0)) * a.cap + row;
-    };
-    TileParts pre = {};
-    int in_pre = 0;
-    if (p >= 0) {
-      const long long row = pre_row + r;
-      const long long of = a.first_tile[p] + row / kManyRows;
-      in_pre = (int)(row % kManyRows);
-      if (row >= 0 && of < first_own) pre = a.tiles[of * a.Hk + hk];
+    const int t0 = few ? start_of(a.own.cu, from, a.Tq) : 0;
+    bool there;                                          // whether the sequence has a prefix,
+    int pre_t0, pre_first;                               // and that one's first token and tile
+    if (few) {
+      const unsigned long long mine = __ballot(own.line >= from && own.line < to);
+      const int p = mine ? __builtin_ctzll(mine) : 0;
+      there = mine != 0;
+      pre_t0 = __shfl(t0, p, 64);
+      pre_first = __shfl(first, p, 64);
+    } else {
+      const int p = last_at_most(a.pre.S, own.line, [&](int i) { return start_of(a.pre.cu, i, a.own.S); });
+      const int s = start_of(a.pre.cu, p, a.own.S);
+      there = own.line >= s && own.line < start_of(a.pre.cu, p + 1, a.own.S);
+      pre_t0 = start_of(a.own.cu, s, a.Tq);
+      pre_first = a.first_tile[2 + p];
     }
-    const long long all = a.Tq * a.Hq;
-    auto ml = [&](int i) -> const float* {
-      if (i < pre.count) return pre.count == 1 ? a.whole_ml + 2 * whole : a.part_ml + 2 * slot(pre, i, in_pre);
-      return own.count == 1 ? a.whole_ml + 2 * (all + whole) : a.part_ml + 2 * slot(own, i - pre.count, r);
-    };
-    auto o = [&](int i) -> const float* {
-      if (i < pre.count) return pre.count == 1 ? a.whole_o + whole * a.D : a.part_o + slot(pre, i, in_pre) * a.D;
-      return own.count == 1 ? a.whole_o + (all + whole) * a.D : a.part_o + slot(own, i - pre.count, r) * a.D;
-    };
-    const int h = hk * a.group + e;
-    join_row<T>(weight[wave], pre.count + own.count, ml, o, a.D, a.scale_log2,
-                static_cast<T*>(a.O) + t * a.o_token + h * a.o_head, a.lse ? a.lse + t * a.Hq + h : nullptr);
+    const long long row = (t - pre_t0) * a.group + e, of = pre_first + row / kManyRows;
+    pre_row = (int)(row % kManyRows);
+    if (there && row >= 0 && of < pre_tiles && of < a.pre_tiles) pre = a.tiles[(a.own_tiles + of) * a.Hk + hk];
   }
+  const long long step = 2ll * a.Hk * a.cap, whole = hk * a.Tq * a.group + t * a.group + e;
+  // (parts of a tile: the first ends behind its piece, the others begin in front of theirs)
+  auto run = [&](const TileParts& d, int row, long long whole) {
+    const long long at = ((2ll * d.piece * a.Hk + 2 * hk) + 1) * a.cap + row;
+    return d.count == 1 ? Run{a.whole_ml + 2 * whole, a.whole_o + whole * a.D, 0, 0, 1}
+                        : Run{a.part_ml + 2 * at, a.part_o + at * a.D, step, a.cap, d.count};
+  };
+  join_row<T>(weight[wave], run(pre, pre_row, whole), run(own, (int)(own_row % kManyRows), a.Tq * a.Hq + whole), a.D,
+              a.scale_log2, static_cast<T*>(a.O) + t * a.o_token + h * a.o_head, a.lse ? a.lse + t * a.Hq + h : nullptr);
 }
 
 // Pieces for each key head's line: a workgroup each, as many as run at a time.
@@ -779,9 +828,9 @@ static int paged_pieces(int Hk, int D) {
 }
 
 struct PagedLayout {
-  size_t tiles, ml, o, whole_ml, whole_o, total;         // (the first tiles at 0)
+  size_t tiles, place, ml, o, whole_ml, whole_o, total;  // (the first tiles at 0)
   int pieces, cap;
-  long long own_tiles, max_tiles;                        // of all sequences, and with the prefixes, at most
+  long long own_tiles, pre_tiles;                        // at most
 };
 static PagedLayout paged_layout(long long Tq, int S, int prefixes, int Hq, int Hk, int D) {
   PagedLayout l;
@@ -792,8 +841,9 @@ static PagedLayout paged_layout(long long Tq, int S, int prefixes, int Hq, int H
   auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
   l.own_tiles = rows / kManyRows + S;
   l.tiles = up((size_t)(prefixes + 2) * sizeof(int));
-  l.max_tiles = l.own_tiles + (prefixes > 0 ? rows / kManyRows + prefixes : 0);
-  l.ml = l.tiles + up((size_t)l.max_tiles * Hk * sizeof(TileParts));
+  l.pre_tiles = prefixes > 0 ? rows / kManyRows + prefixes : 0;
+  l.place = l.tiles + up((size_t)(l.own_tiles + l.pre_tiles) * Hk * sizeof(TileParts));
+  l.ml = l.place + up((size_t)Tq * sizeof(int2));
   l.o = l.ml + up(parts * 2 * sizeof(float));
   l.whole_ml = l.o + up(parts * D * sizeof(float));
   l.whole_o = l.whole_ml + up(whole * 2 * sizeof(float));
@@ -856,7 +906,9 @@ hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages*
   char* w = static_cast<char*>(workspace);
   a.first_tile = reinterpret_cast<int*>(w);
   a.tiles = reinterpret_cast<TileParts*>(w + l.tiles);
-  a.max_tiles = l.max_tiles;
+  a.place = reinterpret_cast<int2*>(w + l.place);
+  a.own_tiles = l.own_tiles;
+  a.pre_tiles = l.pre_tiles;
   a.part_ml = reinterpret_cast<float*>(w + l.ml);
   a.part_o = reinterpret_cast<float*>(w + l.o);
   a.whole_ml = reinterpret_cast<float*>(w + l.whole_ml);
@@ -866,8 +918,8 @@ hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages*
   if (dt == TDQ_F16) TDQ_BY_HEAD(TDQ_PAGED, _Float16);
   else TDQ_BY_HEAD(TDQ_PAGED, __bf16);
 #undef TDQ_PAGED
-  const int chunks = (l.cap + kJoinRows - 1) / kJoinRows;
-  const dim3 join = two_axes(l.own_tiles * Hk * chunks);
+  const int chunks = (Hq + 3) / 4;
+  const dim3 join = two_axes(Tq * chunks);
   if (dt == TDQ_F16) hipLaunchKernelGGL((k_join_pages<_Float16>), join, dim3(256), 0, st, a, chunks);
   else hipLaunchKernelGGL((k_join_pages<__bf16>), join, dim3(256), 0, st, a, chunks);
   return hipGetLastError();
@@ -947,7 +999,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_join_chosen(ChosenArgs a) {
+__global__ __launch_bounds__(256, 4) void k_join_chosen(ChosenArgs a) {
   __shared__ float weight[4][kMaxParts];
   const long long row = 4 * (blockIdx.x + (long long)blockIdx.y * gridDim.x) + (threadIdx.x >> 6);
   if (row >= a.Tq * a.Hq) return;
@@ -956,9 +1008,8 @@ __global__ __launch_bounds__(256) void k_join_chosen(ChosenArgs a) {
   const Sequences& q = a.seq;
   const int s = last_at_most(q.S, t, [&](int i) { return start_of(q.cu, i, a.Tq); });
   if (t < start_of(q.cu, s, a.Tq) || t >= start_of(q.cu, s + 1, a.Tq)) return;
-  auto at = [&](int i) { return i * a.Tq * a.Hq + row; };
-  join_row<T>(weight[threadIdx.x >> 6], a.splits, [&](int i) { return a.part_ml + 2 * at(i); },
-              [&](int i) { return a.part_o + at(i) * a.D; }, a.D, a.scale_log2,
+  join_row<T>(weight[threadIdx.x >> 6], Run{}, Run{a.part_ml + 2 * row, a.part_o + row * a.D, a.Tq * a.Hq, 0, a.splits},
+              a.D, a.scale_log2,
               static_cast<T*>(a.O) + t * a.o_token + h * a.o_head, a.lse ? a.lse + row : nullptr);
 }
 
