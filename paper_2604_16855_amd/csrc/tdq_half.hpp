@@ -119,6 +119,13 @@ __device__ __forceinline__ void copy_to_lds(const void* base, u32 off, u32 lds_b
                : "v"(off), "s"(base), "s"(lds_base)
                : "memory");
 }
+// The same for what is read once: it takes no place in the caches from what others read again.
+__device__ __forceinline__ void stream_to_lds(const void* base, u32 off, u32 lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt"
+               :
+               : "v"(off), "s"(base), "s"(lds_base)
+               : "memory");
+}
 // 64 floats, one offset a lane, to 256 consecutive bytes of LDS.
 __device__ __forceinline__ void copy_float_to_lds(const void* base, u32 off, u32 lds_base) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"

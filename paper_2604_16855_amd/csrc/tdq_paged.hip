@@ -41,11 +41,18 @@ struct GranuleCopy {
       mine |= (u32)(8 * piece < D) << i;
     }
   }
-  // All rows; where D < DP the pieces past it keep what LDS holds.
-  __device__ __forceinline__ void whole(const T* first, u32 lds, bool full) const {
-    if (full) {
+  // All rows; where D < DP the pieces past it keep what LDS holds.  `once`: nobody else reads them.
+  __device__ __forceinline__ void whole(const T* first, u32 lds, bool full, bool once) const {
+    if (full && once) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) stream_to_lds(first, off[i], lds + 1024 * i);
+    } else if (full) {
 #pragma unroll
       for (int i = 0; i < N; ++i) copy_to_lds(first, off[i], lds + 1024 * i);
+    } else if (once) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (mine >> i & 1) stream_to_lds(first, off[i], lds + 1024 * i);
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i)
@@ -125,14 +132,14 @@ struct Store {
         vo(v.token, D) {}
   __device__ __forceinline__ int row(const Granule& g) const { return g.key & ((1 << shift) - 1); }
   // rows of the sequence in a granule; none of one that is not there
-  __device__ __forceinline__ void copy_k(const Granule& g, int keys, u32 lds) const {
+  __device__ __forceinline__ void copy_k(const Granule& g, int keys, u32 lds, bool once) const {
     const T* first = K + (g.page < 0 ? 0 : g.page * k_page + row(g) * k_token);
-    if (quick && keys - g.key >= kGranule) ko.whole(first, lds, D == DP);
+    if (quick && keys - g.key >= kGranule) ko.whole(first, lds, D == DP, once);
     else ko.some(first, k_token, keys - g.key, lds);
   }
-  __device__ __forceinline__ void copy_v(const Granule& g, int keys, u32 lds) const {
+  __device__ __forceinline__ void copy_v(const Granule& g, int keys, u32 lds, bool once) const {
     const T* first = V + (g.page < 0 ? 0 : g.page * v_page + row(g) * v_token);
-    if (quick && keys - g.key >= kGranule) vo.whole(first, lds, D == DP);
+    if (quick && keys - g.key >= kGranule) vo.whole(first, lds, D == DP, once);
     else vo.some(first, v_token, keys - g.key, lds);
   }
 };
@@ -188,8 +195,8 @@ __device__ __forceinline__ void attend_many(Shared<DP>& sh, const Store<T, DP>& 
   w.start(qp, store.D, flip);
   w.addresses(lds_address(sh.many[0][0]), lds_address(sh.many[0][1]));
   auto copy = [&](const Granule& g, int stage) {
-    store.copy_k(g, keys, lds_address(sh.many[stage][0]) + wave * BYTES);
-    store.copy_v(g, keys, lds_address(sh.many[stage][1]) + wave * BYTES);
+    store.copy_k(g, keys, lds_address(sh.many[stage][0]) + wave * BYTES, false);
+    store.copy_v(g, keys, lds_address(sh.many[stage][1]) + wave * BYTES, false);
   };
   Granule next = {-1, kNowhere};
   if (lo < hi) next = where(4 * lo + wave);
@@ -272,8 +279,8 @@ __device__ __forceinline__ void attend_many(Shared<DP>& sh, const Store<T, DP>& 
 // the next while it works on V of this and the other way round; their parts are joined in LDS.
 template <typename T, int DP, int DC, typename G>
 __device__ __forceinline__ void attend_few(Shared<DP>& sh, const Store<T, DP>& store, const G& where, const T* qp,
-                                           int sees, int all, int keys, int lo, int hi, int rows, u32 flip, float lift,
-                                           const Target<T>& to) {
+                                           int sees, int all, int keys, int lo, int hi, int rows, bool once, u32 flip,
+                                           float lift, const Target<T>& to) {
   constexpr int BYTES = kGranule * 2 * DP, COPIES = 2 * GranuleCopy<T, DP, place_k<DP>>::N;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Rows<T, DP, DC> w;
@@ -285,12 +292,12 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const Store<T, DP>& s
   };
   auto look = [&](int i) { return Two{{where(2 * i), where(2 * i + 1)}}; };
   auto copy_k = [&](const Two& t) {
-    store.copy_k(t.g[0], keys, lk);
-    store.copy_k(t.g[1], keys, lk + BYTES);
+    store.copy_k(t.g[0], keys, lk, once);
+    store.copy_k(t.g[1], keys, lk + BYTES, once);
   };
   auto copy_v = [&](const Two& t) {
-    store.copy_v(t.g[0], keys, lv);
-    store.copy_v(t.g[1], keys, lv + BYTES);
+    store.copy_v(t.g[0], keys, lv, once);
+    store.copy_v(t.g[1], keys, lv + BYTES, once);
   };
   int i = lo + wave;
   if (i < hi) {
@@ -501,7 +508,7 @@ struct TileParts {
   int piece, count, line, unused;
 };
 
-constexpr int kTileCost = 2;           // what a tile takes beside its keys, in tiles of 64 keys
+constexpr int kTileCost = 4;           // what a tile takes beside its keys, in tiles of 64 keys
 constexpr int kLeastPiece = 4;
 
 // A prefix or a sequence: its rows, and its keys.
@@ -733,7 +740,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
       if (few) {
         const int end = __builtin_amdgcn_readfirstlane(sees(rows - 1)), all = __builtin_amdgcn_readfirstlane(sees(0));
         const int tiles = (end + kFewKeys - 1) / kFewKeys, stop = 2 * hi < tiles ? 2 * hi : tiles;
-        attend_few<T, DP, DC>(sh, store, where, qp, sees(row), all, keys, 2 * lo, stop, rows, a.flip, a.lift, target);
+        attend_few<T, DP, DC>(sh, store, where, qp, sees(row), all, keys, 2 * lo, stop, rows, true, a.flip,
+                              a.lift, target);
       } else {
         const int from_row = wave * 32 < rows ? wave * 32 : rows - 1;
         const int last_row = wave * 32 + 31 < rows ? wave * 32 + 31 : rows - 1;
@@ -995,7 +1003,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   const int lo = split * share < tiles ? split * share : tiles, hi = lo + share < tiles ? lo + share : tiles;
   if (a.D < DC) clear<DP>(sh);
   attend_few<T, DP, DC>(sh, store, where, static_cast<const T*>(a.Q) + t * a.q_token + (h0 + row) * a.q_head, sees, sees,
-                        keys, lo, hi, rows, a.flip, a.lift, target);
+                        keys, lo, hi, rows, to - from == 1, a.flip, a.lift, target);
 }
 
 template <typename T>
