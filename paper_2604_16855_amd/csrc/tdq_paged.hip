@@ -95,54 +95,82 @@ struct Line {
   }
 };
 
-// The granules of a list of pages of a sequence.
+// The granules of a list of pages of a sequence.  A lane holds a page of 64 of the list at a time.
 struct Chosen {
   static constexpr bool kInOrder = false;
   const int *list, *table;
   int count, shift, n_pages, keys;
-  __device__ __forceinline__ Granule operator()(int i) const {
-    const int bits = shift - kGranuleBits, n = i >> bits, at = n < count ? n : count - 1;
-    const int b = load_scalar(list + at), last = (keys - 1) >> shift;
-    const int page = load_scalar(table + (b < 0 ? 0 : b < last ? b : last));
-    const bool there = n < count && b >= 0 && b <= last && page >= 0 && page < n_pages;
-    return {there ? page : -1, there ? (b << shift) + ((i << kGranuleBits) & ((1 << shift) - 1)) : kNowhere};
+  int base;                            // the 64 places of the list that the lanes hold
+  int page, key;                       // of place base + lane: page (negative: not there), its first key
+
+  __device__ __forceinline__ void hold(int from) {
+    base = from;
+    const int i = from + (threadIdx.x & 63), last = (keys - 1) >> shift;
+    const int b = i < count ? list[i] : -1;
+    page = table[b < 0 ? 0 : b < last ? b : last];
+    const bool there = b >= 0 && b <= last && page >= 0 && page < n_pages;
+    page = there ? page : -1;
+    key = there ? b << shift : kNowhere;
+  }
+  __device__ __forceinline__ Granule operator()(int i) {
+    const int n = i >> (shift - kGranuleBits);
+    if ((n & ~63) != base) hold(n & ~63);
+    const int page_of = __builtin_amdgcn_readlane(page, n & 63), first = __builtin_amdgcn_readlane(key, n & 63);
+    return {page_of, page_of < 0 ? kNowhere : first + ((i << kGranuleBits) & ((1 << shift) - 1))};
   }
 };
 
-// What copies and reads the granules of one key head.
-template <typename T, int DP>
+// The kernel's arguments, read again where they are asked for: the scalar registers do not hold all that a
+// loop over keys and what is around it need, and what the compiler puts aside costs a read through a
+// vector register each time.
+template <typename A>
+__device__ __forceinline__ const __attribute__((address_space(4))) A* arguments() {
+  auto p = (const __attribute__((address_space(4))) A*)__builtin_amdgcn_kernarg_segment_ptr();
+  if constexpr (A::kReadAgain) asm volatile("" : "+s"(p));
+  return p;
+}
+
+// A granule's first rows of one key head, and how many of its rows are the sequence's (kWhole: all, and
+// they are within 32-bit offsets).
+constexpr int kWhole = kGranule + 1;
+struct Spot {
+  const void *k, *v;
+  int rows, key;
+};
+
+// What copies the granules of key head h.
+template <typename A, typename T, int DP>
 struct Store {
-  const T *K, *V;                      // of this head
-  long long k_page, k_token, v_page, v_token;
-  int shift, D;
-  bool quick;                          // 16 rows are within 32-bit offsets
+  int h, shift, keys;
+  bool full;                           // D == DP
   GranuleCopy<T, DP, place_k<DP>> ko;
   GranuleCopy<T, DP, place_v<DP>> vo;
-  __device__ __forceinline__ Store(const Pages& k, const Pages& v, int h, int shift, int D)
-      : K(static_cast<const T*>(k.data) + h * k.head),
-        V(static_cast<const T*>(v.data) + h * v.head),
-        k_page(k.page),
-        k_token(k.token),
-        v_page(v.page),
-        v_token(v.token),
-        shift(shift),
-        D(D),
-        quick(k.token >= 0 && v.token >= 0 && k.token < 1 << 24 && v.token < 1 << 24),
-        ko(k.token, D),
-        vo(v.token, D) {}
-  __device__ __forceinline__ int row(const Granule& g) const { return g.key & ((1 << shift) - 1); }
-  // rows of the sequence in a granule; none of one that is not there
-  __device__ __forceinline__ void copy_k(const Granule& g, int keys, u32 lds, bool once) const {
-    const T* first = K + (g.page < 0 ? 0 : g.page * k_page + row(g) * k_token);
-    if (quick && keys - g.key >= kGranule) ko.whole(first, lds, D == DP, once);
-    else ko.some(first, k_token, keys - g.key, lds);
+  __device__ __forceinline__ Store(const A& a, int h, int shift, int keys)
+      : h(h), shift(shift), keys(keys), full(a.D == DP), ko(a.K.token, a.D), vo(a.V.token, a.D) {}
+  __device__ __forceinline__ Spot spot(const Granule& g) const {
+    const auto a = arguments<A>();
+    const long long page = g.page < 0 ? 0 : g.page, row = g.key & ((1 << shift) - 1);
+    Spot s;
+    s.k = static_cast<const T*>(a->K.data) + page * a->K.page + row * a->K.token + h * a->K.head;
+    s.v = static_cast<const T*>(a->V.data) + page * a->V.page + row * a->V.token + h * a->V.head;
+    const bool quick = (unsigned long long)a->K.token < 1 << 24 && (unsigned long long)a->V.token < 1 << 24;
+    const int left = keys - g.key;                       // (nothing of one that is not there)
+    s.rows = left >= kGranule && quick ? kWhole : left;
+    s.key = g.key;
+    return s;
   }
-  __device__ __forceinline__ void copy_v(const Granule& g, int keys, u32 lds, bool once) const {
-    const T* first = V + (g.page < 0 ? 0 : g.page * v_page + row(g) * v_token);
-    if (quick && keys - g.key >= kGranule) vo.whole(first, lds, D == DP, once);
-    else vo.some(first, v_token, keys - g.key, lds);
+  __device__ __forceinline__ void copy_k(const Spot& s, u32 lds, bool once) const {
+    if (s.rows == kWhole) ko.whole(static_cast<const T*>(s.k), lds, full, once);
+    else ko.some(static_cast<const T*>(s.k), arguments<A>()->K.token, s.rows, lds);
+  }
+  __device__ __forceinline__ void copy_v(const Spot& s, u32 lds, bool once) const {
+    if (s.rows == kWhole) vo.whole(static_cast<const T*>(s.v), lds, full, once);
+    else vo.some(static_cast<const T*>(s.v), arguments<A>()->V.token, s.rows, lds);
   }
 };
+
+// n / d of small numbers (n < 2^22), by 1 / d.
+__device__ __forceinline__ int quotient(int n, float inverse) { return (int)(((float)n + 0.5f) * inverse); }
 
 // Where a tile's result goes: to O and lse, or, of a part of the keys, its sums in binary32.
 template <typename T>
@@ -152,10 +180,9 @@ struct Target {
   long long o_token, o_head;
   int Hq, group, first;                // first: row of the first token that the tile begins with
   float *po, *pml;                     // parts (or nullptr): row r at r * D and 2 * r
-  float scale_log2;
   int D;
   __device__ __forceinline__ void split(int r, int* token, int* head) const {
-    *token = (first + r) / group;
+    *token = quotient(first + r, 1.0f / (float)group);
     *head = first + r - *token * group;
   }
 };
@@ -184,32 +211,34 @@ __device__ __forceinline__ void clear(Shared<DP>& sh) {
 
 // Up to 128 rows by four wavefronts that share tiles of 64 keys, the next tile on its way while one is
 // worked on; key tiles from lo to hi.  A wavefront copies one granule of each tile.
-template <typename T, int DP, int DC>
-__device__ __forceinline__ void attend_many(Shared<DP>& sh, const Store<T, DP>& store, const Line& where, const T* qp,
-                                            int sees, int all, int last, int keys, int lo, int hi, int rows, u32 flip,
-                                            float lift, const Target<T>& to) {
+template <typename A, typename T, int DP, int DC, typename F>
+__device__ __forceinline__ void attend_many(Shared<DP>& sh, const Store<A, T, DP>& store, Line where, const T* qp, int D,
+                                            int sees, int all, int last, int lo, int hi, int rows, u32 flip, float c,
+                                            float lift, F target) {
   constexpr int BYTES = kGranule * 2 * DP;             // of a granule in LDS
   constexpr int STAGES = kStages<DP>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-  Rows<T, DP, DC> w;
-  w.start(qp, store.D, flip);
-  w.addresses(lds_address(sh.many[0][0]), lds_address(sh.many[0][1]));
-  auto copy = [&](const Granule& g, int stage) {
-    store.copy_k(g, keys, lds_address(sh.many[stage][0]) + wave * BYTES, false);
-    store.copy_v(g, keys, lds_address(sh.many[stage][1]) + wave * BYTES, false);
+  auto look = [&](int i) { return store.spot(where(4 * i + wave)); };
+  auto copy = [&](const Spot& s, int stage) {
+    store.copy_k(s, lds_address(sh.many[stage][0]) + wave * BYTES, false);
+    store.copy_v(s, lds_address(sh.many[stage][1]) + wave * BYTES, false);
   };
-  Granule next = {-1, kNowhere};
-  if (lo < hi) next = where(4 * lo + wave);
+  Spot next = {nullptr, nullptr, 0, 0};
+  if (lo < hi) next = look(lo);
   if (STAGES == 2 && lo < hi) {
     copy(next, 0);
-    if (lo + 1 < hi) next = where(4 * (lo + 1) + wave);
+    if (lo + 1 < hi) next = look(lo + 1);
   }
+  Rows<T, DP, DC> w;
+  w.start(qp, D, flip);
+  w.addresses(lds_address(sh.many[0][0]), lds_address(sh.many[0][1]));
+  where.look_over(lo * (kTileKeys / kGranule), hi * (kTileKeys / kGranule));
   for (int i = lo; i < hi; ++i) {
     const int stage = STAGES == 2 ? (i - lo) & 1 : 0;
     if (STAGES == 1) {
       __syncthreads();                                 // the last tile has been read
       copy(next, 0);
-      if (i + 1 < hi) next = where(4 * (i + 1) + wave);
+      if (i + 1 < hi) next = look(i + 1);
     }
     wait_copies();
     __syncthreads();
@@ -225,15 +254,16 @@ __device__ __forceinline__ void attend_many(Shared<DP>& sh, const Store<T, DP>& 
 #pragma unroll
         for (int g = 0; g < 4; ++g) key[g] = where.sure ? (4 * i + g) * kGranule : where(4 * i + g).key;
       }
-      w.softmax(s, p, to.scale_log2, lift, masked, [&](int k) { return key[k / kGranule] + k % kGranule < sees; });
+      w.softmax(s, p, c, lift, masked, [&](int k) { return key[k / kGranule] + k % kGranule < sees; });
       w.values(0, p[0]);
       w.values(32, p[1]);
     }
     if (STAGES == 2) {
-      if (i + 2 < hi) next = where(4 * (i + 2) + wave);
+      if (i + 2 < hi) next = look(i + 2);
       w.move(stage ? -(int)sizeof(sh.many[0]) : (int)sizeof(sh.many[0]));
     }
   }
+  const Target<T> to = target();
 
   const float l = w.l + other_half(w.l);
   const int r = wave * 32 + (lane & 31);
@@ -252,8 +282,8 @@ __device__ __forceinline__ void attend_many(Shared<DP>& sh, const Store<T, DP>& 
     for (int i = 0; i < DC / 32; ++i)
 #pragma unroll
       for (int j = 0; j < 16; j += 4) {
-        const int c = 32 * i + 2 * j + 4 * half;
-        if (c < to.D) *reinterpret_cast<f32x4*>(po + c) = f32x4{w.o[i][j], w.o[i][j + 1], w.o[i][j + 2], w.o[i][j + 3]};
+        const int d = 32 * i + 2 * j + 4 * half;
+        if (d < to.D) *reinterpret_cast<f32x4*>(po + d) = f32x4{w.o[i][j], w.o[i][j + 1], w.o[i][j + 2], w.o[i][j + 3]};
       }
     if (half == 0) *reinterpret_cast<f32x2*>(to.pml + 2 * r) = f32x2{w.m, l};
     return;
@@ -266,70 +296,80 @@ __device__ __forceinline__ void attend_many(Shared<DP>& sh, const Store<T, DP>& 
   for (int i = 0; i < DC / 32; ++i)
 #pragma unroll
     for (int j = 0; j < 16; j += 4) {
-      const int c = 32 * i + 2 * j + 4 * half;
-      if (c < to.D) {
+      const int d = 32 * i + 2 * j + 4 * half;
+      if (d < to.D) {
         const float y[4] = {w.o[i][j] * inv, w.o[i][j + 1] * inv, w.o[i][j + 2] * inv, w.o[i][j + 3] * inv};
-        store_floats<T, 4>(op + c, y);
+        store_floats<T, 4>(op + d, y);
       }
     }
-  if (to.lse && half == 0) to.lse[(long long)token * to.Hq + head] = log_sum(w.m, l, to.scale_log2);
+  if (to.lse && half == 0) to.lse[(long long)token * to.Hq + head] = log_sum(w.m, l, c);
 }
 
 // Up to 32 rows: the wavefronts share out the tiles of 32 keys from lo to hi, each copying its own, K of
 // the next while it works on V of this and the other way round; their parts are joined in LDS.
-template <typename T, int DP, int DC, typename G>
-__device__ __forceinline__ void attend_few(Shared<DP>& sh, const Store<T, DP>& store, const G& where, const T* qp,
-                                           int sees, int all, int keys, int lo, int hi, int rows, bool once, u32 flip,
-                                           float lift, const Target<T>& to) {
+template <typename A, typename T, int DP, int DC, typename G, typename F>
+__device__ __forceinline__ void attend_few(Shared<DP>& sh, const Store<A, T, DP>& store, G where, const T* qp, int D,
+                                           int sees, int all, int lo, int hi, int rows, bool once, u32 flip, float c,
+                                           float lift, F target) {
   constexpr int BYTES = kGranule * 2 * DP, COPIES = 2 * GranuleCopy<T, DP, place_k<DP>>::N;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  Rows<T, DP, DC> w;
-  w.start(qp, store.D, flip);
   const u32 lk = lds_address(sh.few[wave][0]), lv = lds_address(sh.few[wave][1]);
-  w.addresses(lk, lv);
   struct Two {
-    Granule g[2];
+    Spot s[2];
   };
-  auto look = [&](int i) { return Two{{where(2 * i), where(2 * i + 1)}}; };
+  auto look = [&](int i) {
+    const Granule a = where(2 * i), b = where(2 * i + 1);
+    return Two{{store.spot(a), store.spot(b)}};
+  };
   auto copy_k = [&](const Two& t) {
-    store.copy_k(t.g[0], keys, lk, once);
-    store.copy_k(t.g[1], keys, lk + BYTES, once);
+    store.copy_k(t.s[0], lk, once);
+    store.copy_k(t.s[1], lk + BYTES, once);
   };
   auto copy_v = [&](const Two& t) {
-    store.copy_v(t.g[0], keys, lv, once);
-    store.copy_v(t.g[1], keys, lv + BYTES, once);
+    store.copy_v(t.s[0], lv, once);
+    store.copy_v(t.s[1], lv + BYTES, once);
   };
   int i = lo + wave;
+  Two next = {};
+  int key[2] = {0, 0};
   if (i < hi) {
-    Two now = look(i), next = now;
-    copy_k(now);
-    copy_v(now);
+    next = look(i);
+    copy_k(next);
+    copy_v(next);
+    key[0] = next.s[0].key;
+    key[1] = next.s[1].key;
     if (i + 4 < hi) next = look(i + 4);
-    for (; i < hi; i += 4) {
-      const bool more = i + 4 < hi;
-      // (copies arrive in order: all but the last COPIES, those of V, are there)
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
-      f32x16 s[1];
-      u32 p[1][8];
-      s[0] = w.scores(0);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // K has been read
-      if (more) copy_k(next);
-      bool masked = now.g[0].key + kGranule > all || now.g[1].key + kGranule > all;
-      int key[2] = {now.g[0].key, now.g[1].key};
-      if constexpr (G::kInOrder) {
-        masked = !where.sure || (i + 1) * kFewKeys > all;
-        if (masked) {
+  }
+  Rows<T, DP, DC> w;
+  w.start(qp, D, flip);
+  w.addresses(lk, lv);
+  if constexpr (G::kInOrder) where.look_over(2 * lo, 2 * hi);
+  for (; i < hi; i += 4) {
+    const bool more = i + 4 < hi;
+    // (copies arrive in order: all but the last COPIES, those of V, are there)
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
+    f32x16 s[1];
+    u32 p[1][8];
+    s[0] = w.scores(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // K has been read
+    if (more) copy_k(next);
+    bool masked = key[0] + kGranule > all || key[1] + kGranule > all;
+    if constexpr (G::kInOrder) {
+      masked = !where.sure || (i + 1) * kFewKeys > all;
+      if (masked) {
 #pragma unroll
-          for (int g = 0; g < 2; ++g) key[g] = where.sure ? (2 * i + g) * kGranule : where(2 * i + g).key;
-        }
+        for (int g = 0; g < 2; ++g) key[g] = where.sure ? (2 * i + g) * kGranule : where(2 * i + g).key;
       }
-      w.softmax(s, p, to.scale_log2, lift, masked, [&](int k) { return key[k / kGranule] + k % kGranule < sees; });
-      if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
-      else wait_copies();
-      w.values(0, p[0]);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // V has been read
-      if (more) copy_v(next);
-      now = next;
+    }
+    w.softmax(s, p, c, lift, masked, [&](int k) { return key[k / kGranule] + k % kGranule < sees; });
+    if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
+    else wait_copies();
+    w.values(0, p[0]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // V has been read
+    if (more) {
+      copy_v(next);
+      key[0] = next.s[0].key;
+      key[1] = next.s[1].key;
       if (i + 8 < hi) next = look(i + 8);
     }
   }
@@ -347,11 +387,11 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const Store<T, DP>& s
 #pragma unroll
   for (int v = 0; v < 4; ++v) {
     const float mv = sh.ml[v][lane & 31][0], lv = sh.ml[v][lane & 31][1];
-    if (!no_weight(mv, lv)) sum += lv * __builtin_amdgcn_exp2f((mv - m) * to.scale_log2);
+    if (!no_weight(mv, lv)) sum += lv * __builtin_amdgcn_exp2f((mv - m) * c);
   }
   // (a part in which a row sees no key is 0: its sums may hold 0 * NaN from values that others see)
   const bool none = no_weight(w.m, l);
-  const float keep = __builtin_amdgcn_exp2f((w.m - m) * to.scale_log2);
+  const float keep = __builtin_amdgcn_exp2f((w.m - m) * c);
   if ((lane & 31) < rows) {
 #pragma unroll
     for (int d = 0; d < DC / 32; ++d)
@@ -369,24 +409,25 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const Store<T, DP>& s
     sh.ml[0][lane][1] = sum;
   }
   __syncthreads();
+  const Target<T> to = target();
   constexpr int QUADS = DC / 4;
   for (int e = threadIdx.x; e < rows * QUADS; e += 256) {
-    const int r = e / QUADS, c = 4 * (e % QUADS);
-    if (c >= to.D) continue;
+    const int r = e / QUADS, d = 4 * (e % QUADS);
+    if (d >= to.D) continue;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int v = 0; v < 4; ++v) y += *reinterpret_cast<const f32x4*>(&sh.o[v][r][c]);
+    for (int v = 0; v < 4; ++v) y += *reinterpret_cast<const f32x4*>(&sh.o[v][r][d]);
     const float mr = sh.ml[0][r][0], lr = sh.ml[0][r][1];
     if (to.po) {
-      *reinterpret_cast<f32x4*>(to.po + (long long)r * to.D + c) = y;
-      if (c == 0) *reinterpret_cast<f32x2*>(to.pml + 2 * r) = f32x2{mr, lr};
+      *reinterpret_cast<f32x4*>(to.po + (long long)r * to.D + d) = y;
+      if (d == 0) *reinterpret_cast<f32x2*>(to.pml + 2 * r) = f32x2{mr, lr};
     } else {
       const float inv = no_weight(mr, lr) ? 0.f : 1.0f / lr;
       const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
       int token, head;
       to.split(r, &token, &head);
-      store_floats<T, 4>(to.O + token * to.o_token + head * to.o_head + c, z);
-      if (to.lse && c == 0) to.lse[(long long)token * to.Hq + head] = log_sum(mr, lr, to.scale_log2);
+      store_floats<T, 4>(to.O + token * to.o_token + head * to.o_head + d, z);
+      if (to.lse && d == 0) to.lse[(long long)token * to.Hq + head] = log_sum(mr, lr, c);
     }
   }
   __syncthreads();                                       // (LDS is free for a next tile)
@@ -472,6 +513,52 @@ __device__ __forceinline__ void join_row(float* weight, const Run& a, const Run&
   __builtin_amdgcn_wave_barrier();
 }
 
+// The same for up to kFewParts parts, by the lanes that have the row's outputs, each for itself.
+constexpr int kFewParts = 8;
+template <typename T>
+__device__ __forceinline__ void join_few(const Run& a, const Run& b, int c, int D, float scale_log2, T* op, float* lse) {
+  const int n = a.count + b.count;
+  f32x2 x[kFewParts];
+  f32x4 v[kFewParts];
+#pragma unroll
+  for (int i = 0; i < kFewParts; ++i) {
+    x[i] = f32x2{-INFINITY, 0.f};
+    v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (i < n && c < D) {
+      const bool first = i < a.count;
+      const int at = first ? i : i - a.count;
+      const long long row = at == 0 ? 0 : at * (first ? a.step : b.step) - (first ? a.gap : b.gap);
+      x[i] = *reinterpret_cast<const f32x2*>((first ? a.ml : b.ml) + 2 * row);
+      v[i] = *reinterpret_cast<const f32x4*>((first ? a.o : b.o) + row * D + c);
+    }
+  }
+  float m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < kFewParts; ++i) m = fmaxf(m, x[i][0]);
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kFewParts; ++i) {
+    // (what is left out and what is not: as above)
+    const bool none = no_weight(x[i][0], x[i][1]);
+    const float f = x[i][1] != x[i][1] ? x[i][1] : __builtin_amdgcn_exp2f((x[i][0] - m) * scale_log2);
+    if (!none) {
+      l = fmaf(x[i][1], f, l);
+      y += v[i] * f;
+    }
+  }
+  if (c < D) {
+    const float inv = no_weight(m, l) ? 0.f : 1.0f / l;
+    const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
+    store_floats<T, 4>(op + c, z);
+    if (lse && c == 0) *lse = log_sum(m, l, scale_log2);
+  }
+}
+// A run as lane `from` of the wavefront has it.
+__device__ __forceinline__ Run run_of(const Run& r, int from) {
+  return Run{(const float*)__shfl((unsigned long long)r.ml, from, 64), (const float*)__shfl((unsigned long long)r.o, from, 64),
+             __shfl(r.step, from, 64), __shfl(r.gap, from, 64), __shfl(r.count, from, 64)};
+}
+
 // ---------------------------------------------------------------------------
 // whole sequences
 // ---------------------------------------------------------------------------
@@ -482,6 +569,7 @@ __device__ __forceinline__ void join_row(float* weight, const Run& a, const Run&
 // the line's length and its own place on it from the lengths (a sum over them by all threads), so that
 // nothing of the plan depends on the host, which does not know them.
 struct PagedArgs {
+  static constexpr bool kReadAgain = true;
   const void* Q;
   void* O;
   float* lse;
@@ -492,6 +580,7 @@ struct PagedArgs {
   int Hq, Hk, group, D, causal;
   float scale_log2, lift;
   u32 flip;
+  double per_group, half_tile;         // 1 / group, and half of the tokens of a tile
   int pieces;                          // most pieces of a line
   int cap;                             // rows of a part: as many as a tile may have
   int* first_tile;                     // [prefixes + 2]: tiles of the sequences, of the prefixes, and in front of each
@@ -513,78 +602,86 @@ constexpr int kLeastPiece = 4;
 
 // A prefix or a sequence: its rows, and its keys.
 struct Item {
-  int t0, tokens, keys;                // first token
-  long long rows, tiles;
+  int t0, end, keys;                   // first token and the one behind the last
   int ahead;                           // token i sees the keys up to i + ahead
-  long long skip;                      // tiles none of whose rows sees a key
-  int group;
-  double more;                         // keys that a tile sees beyond the one before it, half of them
-  __device__ __forceinline__ int sees(long long row) const {
-    const long long e = row / group + ahead + 1;
-    return e < 0 ? 0 : e < keys ? (int)e : keys;
-  }
+  unsigned rows;
+  int tiles, skip;                     // tiles, and how many of them see no key
+  bool causal;
+
   // Cost of the first r tiles: kTileCost each, and the sum of what their last rows see in tiles of 64
   // keys, over skip < i <= r of 128 i / group + ahead (or ahead, where all see the same).
-  __device__ __forceinline__ long long cost(long long r) const {
-    const long long m = r > skip ? r - skip : 0;
+  __device__ __forceinline__ long long cost(const PagedArgs& a, int r) const {
+    const int m = r > skip ? r - skip : 0;
     const double first = (double)(r - m), end = (double)r;
-    const double keys_seen = (double)m * ahead + more * (end * (end + 1.0) - first * (first + 1.0));
-    return kTileCost * r + (long long)(keys_seen * (1.0 / kTileKeys));
+    double seen = (double)m * ahead;
+    if (causal) seen += a.half_tile * (end * (end + 1.0) - first * (first + 1.0));
+    return (long long)kTileCost * r + (long long)(seen * (1.0 / kTileKeys));
+  }
+  // Keys that a row sees.
+  __device__ __forceinline__ int sees(const PagedArgs& a, unsigned row) const {
+    const int e = (int)(((double)row + 0.5) * a.per_group) + ahead + 1;
+    return e < 0 ? 0 : e < keys ? e : keys;
   }
 };
-__device__ __forceinline__ Item item_of(const PagedArgs& a, int v) {
+__device__ __forceinline__ Item item_from(const PagedArgs& a, bool prefix, int t0, int end, int keys) {
   Item x;
-  x.group = a.group;
-  int end;
-  if (v < a.pre.S) {
-    x.t0 = start_of(a.own.cu, start_of(a.pre.cu, v, a.own.S), a.Tq);
-    end = start_of(a.own.cu, start_of(a.pre.cu, v + 1, a.own.S), a.Tq);
-    x.keys = keys_of(a.pre, v);
-  } else {
-    x.t0 = start_of(a.own.cu, v - a.pre.S, a.Tq);
-    end = start_of(a.own.cu, v - a.pre.S + 1, a.Tq);
-    x.keys = keys_of(a.own, v - a.pre.S);
-  }
-  x.tokens = end > x.t0 ? end - x.t0 : 0;
-  x.rows = (long long)x.tokens * a.group;
-  x.tiles = (x.rows + kManyRows - 1) / kManyRows;
+  x.t0 = t0;
+  x.end = end;
+  x.keys = keys;
+  const int tokens = end > t0 ? end - t0 : 0;
+  x.rows = (unsigned)tokens * (unsigned)a.group;
+  x.tiles = (int)((x.rows + (unsigned)(kManyRows - 1)) / kManyRows);
   // (what sees everything: as if all its tokens stood at the end)
-  const bool causal = a.causal && v >= a.pre.S;
-  x.ahead = causal ? x.keys - x.tokens : x.keys;
-  x.more = causal ? kManyRows * 0.5 / a.group : 0.0;
+  x.causal = a.causal && !prefix;
+  x.ahead = x.causal ? keys - tokens : keys;
   x.skip = 0;
   if (x.ahead < 0) {
-    x.skip = (long long)-x.ahead * a.group / kManyRows;
-    x.skip = x.skip < x.tiles ? x.skip : x.tiles;
+    const long long none = (long long)-x.ahead * a.group / kManyRows;
+    x.skip = none < x.tiles ? (int)none : x.tiles;
   }
   return x;
+}
+__device__ __forceinline__ Item item_of(const PagedArgs& a, int v) {
+  const bool prefix = v < a.pre.S;
+  int s = v - a.pre.S, next = s + 1;
+  if (prefix) {
+    s = start_of(a.pre.cu, v, a.own.S);
+    next = start_of(a.pre.cu, v + 1, a.own.S);
+  }
+  return item_from(a, prefix, start_of(a.own.cu, s, a.Tq), start_of(a.own.cu, next, a.Tq),
+                   prefix ? keys_of(a.pre, v) : keys_of(a.own, v - a.pre.S));
 }
 
 // The tile of an item, and the place of it on the line.
 struct Stretch {
   long long begin, end;
   int tiles;                           // of keys, one at least
+  double each;                         // of them for one place
   __device__ __forceinline__ int at(long long x) const {   // first tile of keys behind a place
     if (x <= begin) return 0;
     if (x >= end) return tiles;
-    return (int)((x - begin) * tiles / (end - begin));
+    const int n = (int)((double)(x - begin) * each);
+    return n < tiles ? n : tiles - 1;
   }
 };
-__device__ __forceinline__ Stretch stretch_of(const Item& x, long long start, long long r) {
+__device__ __forceinline__ Stretch stretch_of(const PagedArgs& a, const Item& x, long long start, int r) {
   Stretch s;
-  s.begin = start + x.cost(r);
-  s.end = start + x.cost(r + 1);
-  const long long last = (r + 1) * kManyRows < x.rows ? (r + 1) * kManyRows : x.rows;
-  const int n = x.sees(last - 1);
+  s.begin = start + x.cost(a, r);
+  s.end = start + x.cost(a, r + 1);
+  const unsigned behind = (unsigned)(r + 1) * kManyRows;
+  const int n = x.sees(a, (behind < x.rows ? behind : x.rows) - 1);
   s.tiles = n > 0 ? (n + kTileKeys - 1) / kTileKeys : 1;
+  s.each = (double)s.tiles / (double)(s.end - s.begin);
   return s;
 }
 __device__ __forceinline__ int pieces_of(const PagedArgs& a, long long total) {
   const long long n = total / kLeastPiece;
   return n < 1 ? 1 : n < a.pieces ? (int)n : a.pieces;
 }
-// Where piece k of n begins.
-__device__ __forceinline__ long long piece_at(long long total, int k, int n) { return total * k / n; }
+// Where piece k of n begins, `each` the length of one.
+__device__ __forceinline__ long long piece_at(long long total, double each, int k, int n) {
+  return k < n ? (long long)(each * k) : total;
+}
 
 template <typename T, int DP, int DC>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 2 : 1))) void k_attend_pages(
@@ -592,19 +689,22 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   __shared__ __attribute__((aligned(1024))) Shared<DP> sh;
   __shared__ long long wave_sum[4];
   __shared__ int wave_tiles[4];
-  __shared__ long long found[4];                         // item, the place it begins at, its first tile, tiles of prefixes
+  __shared__ int3 known[256];                            // first token, end and keys of items, if there are no more
+  __shared__ long long found_start;
+  __shared__ int found[3];                               // item, its first tile, tiles of prefixes
   const int hk = (int)(blockIdx.x % (unsigned)a.Hk), k = (int)(blockIdx.x / (unsigned)a.Hk);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
   // the line
-  const int items = a.pre.S + a.own.S, each = (items + 255) / 256;
-  const int v0 = tid * each < items ? tid * each : items, v1 = v0 + each < items ? v0 + each : items;
+  const int items = a.pre.S + a.own.S, share = (items + 255) / 256;
+  const int v0 = tid * share < items ? tid * share : items, v1 = v0 + share < items ? v0 + share : items;
   long long mine = 0;
   int mine_tiles = 0;
   for (int v = v0; v < v1; ++v) {
     const Item x = item_of(a, v);
-    mine += x.cost(x.tiles);
-    mine_tiles += (int)x.tiles;
+    mine += x.cost(a, x.tiles);
+    mine_tiles += x.tiles;
+    if (share == 1) known[v] = make_int3(x.t0, x.end, x.keys);
   }
   long long upto = mine;
   int tiles_upto = mine_tiles;
@@ -638,147 +738,166 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     if (blockIdx.x == 0 && tid == 0) a.first_tile[0] = 0;
     return;
   }
-  const long long from = piece_at(total, k, n), to = piece_at(total, k + 1, n);
+  const double each = (double)total / (double)n;
+  const long long from = piece_at(total, each, k, n), to = piece_at(total, each, k + 1, n);
   for (int v = v0; v < v1; ++v) {
-    const Item x = item_of(a, v);
-    const long long next = before + x.cost(x.tiles);
-    if (before <= from && from < next) {
-      found[0] = v;
-      found[1] = before;
-      found[2] = tiles_before;
+    long long next = before + mine;
+    int tiles_next = tiles_before + mine_tiles;
+    if (share > 1) {
+      const Item x = item_of(a, v);
+      next = before + x.cost(a, x.tiles);
+      tiles_next = tiles_before + x.tiles;
     }
-    if (v == a.pre.S) found[3] = tiles_before;           // tiles of prefixes
+    if (before <= from && from < next) {
+      found_start = before;
+      found[0] = v;
+      found[1] = tiles_before;
+    }
+    if (v == a.pre.S) found[2] = tiles_before;           // tiles of prefixes
     if (blockIdx.x == 0 && v < a.pre.S) a.first_tile[v + 2] = tiles_before;
     before = next;
-    tiles_before += (int)x.tiles;
+    tiles_before = tiles_next;
   }
   __syncthreads();
 
-  int v = __builtin_amdgcn_readfirstlane((int)found[0]);
-  long long start = found[1];
-  int tile0 = __builtin_amdgcn_readfirstlane((int)found[2]);
-  const int pre_tiles = __builtin_amdgcn_readfirstlane((int)found[3]);
+  auto item = [&](int v) {
+    if (share > 1) return item_of(a, v);
+    const int3 x = known[v];
+    return item_from(a, v < a.pre.S, x.x, x.y, x.z);
+  };
+  int v = __builtin_amdgcn_readfirstlane(found[0]), tile0 = __builtin_amdgcn_readfirstlane(found[1]);
+  long long start = found_start;
+  const int pre_tiles = __builtin_amdgcn_readfirstlane(found[2]);
   if (blockIdx.x == 0 && tid == 0) {
     a.first_tile[0] = all_tiles - pre_tiles;
     a.first_tile[1] = pre_tiles;
   }
-  Item x = item_of(a, v);
-  long long r = 0;
-  for (long long count = x.tiles; count > 1;) {          // the last tile that begins no later than the piece
-    const long long half = count / 2;
-    if (start + x.cost(r + half) <= from) {
+  Item x = item(v);
+  int r = 0;
+  for (int count = x.tiles; count > 1;) {                // the last tile that begins no later than the piece
+    const int half = count / 2;
+    if (start + x.cost(a, r + half) <= from) {
       r += half;
       count -= half;
     } else {
       count = half;
     }
   }
+  r = __builtin_amdgcn_readfirstlane(r);
   for (;;) {
-    const Stretch s = stretch_of(x, start, r);
+    const Stretch s = stretch_of(a, x, start, r);
     if (s.begin >= to) break;
     const int lo = __builtin_amdgcn_readfirstlane(s.at(from)), hi = __builtin_amdgcn_readfirstlane(s.at(to));
+    const unsigned r0 = (unsigned)r * kManyRows;
+    const int rows = __builtin_amdgcn_readfirstlane((int)(x.rows - r0 < kManyRows ? x.rows - r0 : kManyRows));
     if (lo < hi) {
       const bool prefix = v < a.pre.S;
-      const Sequences& q = prefix ? a.pre : a.own;
       const int line = prefix ? v : v - a.pre.S;
-      const long long r0 = r * kManyRows;
-      const int rows = __builtin_amdgcn_readfirstlane((int)(x.rows - r0 < kManyRows ? x.rows - r0 : kManyRows));
-      const int token0 = __builtin_amdgcn_readfirstlane((int)(r0 / a.group));
-      const int first = __builtin_amdgcn_readfirstlane((int)(r0 - (long long)token0 * a.group));
+      const int token0 = __builtin_amdgcn_readfirstlane((int)(((double)r0 + 0.5) * a.per_group));
+      const int first = __builtin_amdgcn_readfirstlane((int)(r0 - (unsigned)token0 * (unsigned)a.group));
       const int t0 = __builtin_amdgcn_readfirstlane(x.t0) + token0;
       const int keys = __builtin_amdgcn_readfirstlane(x.keys);
       const int ahead = __builtin_amdgcn_readfirstlane(x.ahead) + token0 + 1;   // of row r of the tile: + (first + r) / group
+      const float per_group = (float)a.per_group;
       auto sees = [&](int row) {
-        const int e = (first + row) / a.group + ahead;
+        const int e = quotient(first + row, per_group) + ahead;
         return e < 0 ? 0 : e < keys ? e : keys;
       };
-      Line where = {q.table + line * q.ld, q.shift, q.n_pages, keys, true};
-      where.look_over(lo * (kTileKeys / kGranule), hi * (kTileKeys / kGranule));
-      const long long tile = prefix ? a.own_tiles + tile0 + r : tile0 - pre_tiles + r;
-      if (lo == 0 && tid == 0 && tile < (prefix ? a.own_tiles + a.pre_tiles : a.own_tiles)) {
-        // the last piece that the tile lies in: of those that begin in front of its end
-        int last = (int)((s.end - 1) * n / total);
-        while (last > k && piece_at(total, last, n) >= s.end) --last;
-        while (last + 1 < n && piece_at(total, last + 1, n) < s.end) ++last;
-        a.tiles[tile * a.Hk + hk] = TileParts{k, last - k + 1, line, 0};
-      }
-      if (lo == 0 && hk == 0 && !prefix) {
-        // (tokens whose first row lies in the tile)
-        const int row = tid * a.group - first;
-        if (row >= 0 && row < rows) a.place[t0 + tid] = make_int2(tile0 - pre_tiles + (int)r, row);
-      }
-      const Store<T, DP> store(a.K, a.V, hk, q.shift, a.D);
-      Target<T> target;
-      target.O = static_cast<T*>(a.O) + t0 * a.o_token + (long long)hk * a.group * a.o_head;
-      target.lse = a.lse ? a.lse + (long long)t0 * a.Hq + hk * a.group : nullptr;
-      target.o_token = a.o_token;
-      target.o_head = a.o_head;
-      target.Hq = a.Hq;
-      target.group = a.group;
-      target.first = first;
-      target.scale_log2 = a.scale_log2;
-      target.D = a.D;
-      target.po = target.pml = nullptr;
-      if (lo > 0 || hi < s.tiles) {
-        const long long slot = 2 * ((long long)k * a.Hk + hk) + (lo > 0 ? 0 : 1);
-        target.po = a.part_o + slot * a.cap * a.D;
-        target.pml = a.part_ml + slot * a.cap * 2;
-      } else if (a.pre.S > 0) {
-        // (rows of a key head one after the other)
-        const long long at = ((prefix ? 0 : a.Hk) + hk) * a.Tq * a.group + (long long)t0 * a.group + first;
-        target.po = a.whole_o + at * a.D;
-        target.pml = a.whole_ml + at * 2;
-      }
+      const Line where = {prefix ? a.pre.table + line * a.pre.ld : a.own.table + line * a.own.ld, a.own.shift, a.own.n_pages,
+                          keys, true};
+      const Store<PagedArgs, T, DP> store(a, hk, a.own.shift, keys);
+      const int tiles = s.tiles;
+      auto target = [&]() {
+        const auto b = arguments<PagedArgs>();
+        Target<T> to;
+        to.O = static_cast<T*>(b->O) + t0 * b->o_token + (long long)hk * b->group * b->o_head;
+        to.lse = b->lse ? b->lse + (long long)t0 * b->Hq + hk * b->group : nullptr;
+        to.o_token = b->o_token;
+        to.o_head = b->o_head;
+        to.Hq = b->Hq;
+        to.group = b->group;
+        to.first = first;
+        to.D = b->D;
+        to.po = to.pml = nullptr;
+        if (lo > 0 || hi < tiles) {
+          const long long slot = 2 * ((long long)k * b->Hk + hk) + (lo > 0 ? 0 : 1);
+          to.po = b->part_o + slot * b->cap * b->D;
+          to.pml = b->part_ml + slot * b->cap * 2;
+        } else if (b->pre.S > 0) {
+          // (rows of a key head one after the other)
+          const long long at = ((prefix ? 0 : b->Hk) + hk) * b->Tq * b->group + (long long)t0 * b->group + first;
+          to.po = b->whole_o + at * b->D;
+          to.pml = b->whole_ml + at * 2;
+        }
+        return to;
+      };
       if (a.D < DC) clear<DP>(sh);
       else __syncthreads();
       const bool few = rows <= kFewRows;
       const int mine_row = few ? lane & 31 : wave * 32 + (lane & 31);
       const int row = mine_row < rows ? mine_row : rows - 1;
-      const int token = (first + row) / a.group, head = first + row - token * a.group;
+      const int token = quotient(first + row, per_group), head = first + row - token * a.group;
       const T* qp = static_cast<const T*>(a.Q) + (long long)(t0 + token) * a.q_token +
                     (long long)(hk * a.group + head) * a.q_head;
+      const int end = __builtin_amdgcn_readfirstlane(sees(rows - 1));
       if (few) {
-        const int end = __builtin_amdgcn_readfirstlane(sees(rows - 1)), all = __builtin_amdgcn_readfirstlane(sees(0));
+        const int all = __builtin_amdgcn_readfirstlane(sees(0));
         const int tiles = (end + kFewKeys - 1) / kFewKeys, stop = 2 * hi < tiles ? 2 * hi : tiles;
-        attend_few<T, DP, DC>(sh, store, where, qp, sees(row), all, keys, 2 * lo, stop, rows, true, a.flip,
-                              a.lift, target);
+        attend_few<PagedArgs, T, DP, DC>(sh, store, where, qp, a.D, sees(row), all, 2 * lo, stop, rows, true, a.flip,
+                                         a.scale_log2, a.lift, target);
       } else {
         const int from_row = wave * 32 < rows ? wave * 32 : rows - 1;
         const int last_row = wave * 32 + 31 < rows ? wave * 32 + 31 : rows - 1;
         const int last = wave * 32 < rows ? __builtin_amdgcn_readfirstlane(sees(last_row)) : 0;
         const int all = __builtin_amdgcn_readfirstlane(sees(from_row));
-        const int end = __builtin_amdgcn_readfirstlane(sees(rows - 1));
         const int tiles = (end + kTileKeys - 1) / kTileKeys, stop = hi < tiles ? hi : tiles;
-        attend_many<T, DP, DC>(sh, store, where, qp, sees(row), all, last, keys, lo, stop, rows, a.flip, a.lift, target);
+        attend_many<PagedArgs, T, DP, DC>(sh, store, where, qp, a.D, sees(row), all, last, lo, stop, rows, a.flip,
+                                          a.scale_log2, a.lift, target);
       }
-    }
-    if (lo >= hi && lo > 0 && lo < s.tiles && tid < kManyRows && tid < x.rows - r * kManyRows) {
+      // (for the second kernel)
+      const long long tile = prefix ? a.own_tiles + tile0 + r : tile0 - pre_tiles + r;
+      if (lo == 0 && tid == 0 && tile < (prefix ? a.own_tiles + a.pre_tiles : a.own_tiles)) {
+        // the last piece that the tile lies in: of those that begin in front of its end
+        int last = (int)((double)(s.end - 1) / each);
+        last = last < k ? k : last < n ? last : n - 1;
+        while (last > k && piece_at(total, each, last, n) >= s.end) --last;
+        while (last + 1 < n && piece_at(total, each, last + 1, n) < s.end) ++last;
+        a.tiles[tile * a.Hk + hk] = TileParts{k, last - k + 1, line, 0};
+      }
+      if (lo == 0 && hk == 0 && !prefix) {
+        // tokens whose first row lies in the tile
+        const int row = tid * a.group - first;
+        if (row >= 0 && row < rows) a.place[t0 + tid] = make_int2(tile0 - pre_tiles + r, row);
+      }
+    } else if (lo > 0 && lo < s.tiles && tid < rows) {
       // (no keys of the tile for this piece, though some for those before and behind)
       const long long slot = 2 * ((long long)k * a.Hk + hk);
       *reinterpret_cast<f32x2*>(a.part_ml + (slot * a.cap + tid) * 2) = f32x2{-INFINITY, 0.f};
     }
     if (s.end >= to) break;
     if (++r >= x.tiles) {
-      start += x.cost(x.tiles);
-      tile0 += (int)x.tiles;
+      start += x.cost(a, x.tiles);
+      tile0 += x.tiles;
       r = 0;
       do {
         if (++v >= items) return;
-        x = item_of(a, v);
+        x = item(v);
       } while (x.tiles == 0);
     }
   }
 }
 
-// Joins the tiles that lie in several pieces, and prefixes with sequences: a wavefront a row.
+// Joins the tiles that lie in several pieces, and prefixes with sequences.  A wavefront has `heads` rows of
+// a token, as many at a time as 4 outputs a lane allow; rows of many parts take all of it one by one.
 template <typename T>
-__global__ __launch_bounds__(256, 4) void k_join_pages(PagedArgs a, int chunks) {
+__global__ __launch_bounds__(256, 4) void k_join_pages(PagedArgs a, int heads, int chunks) {
   __shared__ float weight[4][kMaxParts];
   const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
   const long long t = id / chunks;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = (int)(id % chunks) * 4 + wave;
-  if (t >= a.Tq || h >= a.Hq) return;
-  const int lane = threadIdx.x & 63, hk = h / a.group, e = h - hk * a.group;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h0 = ((int)(id % chunks) * 4 + wave) * heads, h1 = h0 + heads < a.Hq ? h0 + heads : a.Hq;
+  if (t >= a.Tq || h0 >= a.Hq) return;
+  const int lane = threadIdx.x & 63;
   // (all on their way at once; what lies there is looked at if the token is one of a sequence)
   const int begin = start_of(a.own.cu, 0, a.Tq), end = start_of(a.own.cu, a.own.S, a.Tq);
   const int tiles = a.first_tile[0], pre_tiles = a.first_tile[1];
@@ -790,43 +909,60 @@ __global__ __launch_bounds__(256, 4) void k_join_pages(PagedArgs a, int chunks) 
     to = start_of(a.pre.cu, lane + 1, a.own.S);
     first = a.first_tile[2 + lane];
   }
-  if (t < begin || t >= end) return;
-  const long long own_row = place.y + e, tile = place.x + own_row / kManyRows;
-  if (place.y < 0 || tile < 0 || tile >= tiles || tile >= a.own_tiles) return;
-  const TileParts own = a.tiles[tile * a.Hk + hk];
-  if (own.count == 1 && a.pre.S == 0) return;            // (its one piece has written the output)
-  TileParts pre = {0, 0, 0, 0};
-  int pre_row = 0;
-  if (a.pre.S > 0) {
-    const int t0 = few ? start_of(a.own.cu, from, a.Tq) : 0;
-    bool there;                                          // whether the sequence has a prefix,
-    int pre_t0, pre_first;                               // and that one's first token and tile
-    if (few) {
-      const unsigned long long mine = __ballot(own.line >= from && own.line < to);
-      const int p = mine ? __builtin_ctzll(mine) : 0;
-      there = mine != 0;
-      pre_t0 = __shfl(t0, p, 64);
-      pre_first = __shfl(first, p, 64);
-    } else {
-      const int p = last_at_most(a.pre.S, own.line, [&](int i) { return start_of(a.pre.cu, i, a.own.S); });
-      const int s = start_of(a.pre.cu, p, a.own.S);
-      there = own.line >= s && own.line < start_of(a.pre.cu, p + 1, a.own.S);
-      pre_t0 = start_of(a.own.cu, s, a.Tq);
-      pre_first = a.first_tile[2 + p];
+  if (t < begin || t >= end || place.y < 0 || place.x < 0) return;
+  const int t0 = a.pre.S > 0 && few ? start_of(a.own.cu, from, a.Tq) : 0;
+  const float per_group = (float)a.per_group;
+  const int quads = a.D <= 32 ? 8 : a.D <= 64 ? 16 : a.D <= 128 ? 32 : 64, c = 4 * (lane & (quads - 1));
+  for (int hb = h0; hb < h1; hb += 64 / quads) {
+    const int h = hb + lane / quads, hk = quotient(h < h1 ? h : h1 - 1, per_group), e = h - hk * a.group;
+    const long long own_row = (long long)place.y + e, tile = place.x + own_row / kManyRows;
+    const bool real = h < h1 && tile < tiles && tile < a.own_tiles;
+    TileParts own = {0, 1, 0, 0}, pre = {0, 0, 0, 0};
+    if (real) own = a.tiles[tile * a.Hk + hk];
+    int pre_row = 0;
+    if (a.pre.S > 0) {
+      const int line = __builtin_amdgcn_readfirstlane(own.line);   // (of the token: the same for all its heads)
+      bool there;                                        // whether the sequence has a prefix,
+      int pre_t0, pre_first;                             // and that one's first token and tile
+      if (few) {
+        const unsigned long long mine = __ballot(line >= from && line < to);
+        const int p = mine ? __builtin_ctzll(mine) : 0;
+        there = mine != 0;
+        pre_t0 = __shfl(t0, p, 64);
+        pre_first = __shfl(first, p, 64);
+      } else {
+        const int p = last_at_most(a.pre.S, line, [&](int i) { return start_of(a.pre.cu, i, a.own.S); });
+        const int s = start_of(a.pre.cu, p, a.own.S);
+        there = line >= s && line < start_of(a.pre.cu, p + 1, a.own.S);
+        pre_t0 = start_of(a.own.cu, s, a.Tq);
+        pre_first = a.first_tile[2 + p];
+      }
+      const long long row = (t - pre_t0) * a.group + e, of = pre_first + row / kManyRows;
+      pre_row = (int)(row % kManyRows);
+      if (real && there && row >= 0 && of < pre_tiles && of < a.pre_tiles) pre = a.tiles[(a.own_tiles + of) * a.Hk + hk];
     }
-    const long long row = (t - pre_t0) * a.group + e, of = pre_first + row / kManyRows;
-    pre_row = (int)(row % kManyRows);
-    if (there && row >= 0 && of < pre_tiles && of < a.pre_tiles) pre = a.tiles[(a.own_tiles + of) * a.Hk + hk];
+    const bool wanted = real && (own.count > 1 || a.pre.S > 0);   // (else its one piece has written the output)
+    if (__ballot(wanted) == 0) continue;
+    const long long step = 2ll * a.Hk * a.cap, whole = hk * a.Tq * a.group + t * a.group + e;
+    // (parts of a tile: the first ends behind its piece, the others begin in front of theirs)
+    auto run = [&](const TileParts& d, int row, long long whole) {
+      const long long at = ((2ll * d.piece * a.Hk + 2 * hk) + 1) * a.cap + row;
+      return d.count == 1 ? Run{a.whole_ml + 2 * whole, a.whole_o + whole * a.D, 0, 0, 1}
+                          : Run{a.part_ml + 2 * at, a.part_o + at * a.D, step, a.cap, d.count};
+    };
+    const Run x = run(pre, pre_row, whole), y = run(own, (int)(own_row % kManyRows), a.Tq * a.Hq + whole);
+    T* op = static_cast<T*>(a.O) + t * a.o_token;
+    float* lse = a.lse ? a.lse + t * a.Hq : nullptr;
+    if (__ballot(wanted && x.count + y.count > kFewParts) == 0) {
+      if (wanted) join_few<T>(x, y, c, a.D, a.scale_log2, op + h * a.o_head, lse ? lse + h : nullptr);
+      continue;
+    }
+    for (int i = 0; i < 64; i += quads) {
+      if (!__shfl((int)wanted, i, 64)) continue;
+      const int g = hb + i / quads;
+      join_row<T>(weight[wave], run_of(x, i), run_of(y, i), a.D, a.scale_log2, op + g * a.o_head, lse ? lse + g : nullptr);
+    }
   }
-  const long long step = 2ll * a.Hk * a.cap, whole = hk * a.Tq * a.group + t * a.group + e;
-  // (parts of a tile: the first ends behind its piece, the others begin in front of theirs)
-  auto run = [&](const TileParts& d, int row, long long whole) {
-    const long long at = ((2ll * d.piece * a.Hk + 2 * hk) + 1) * a.cap + row;
-    return d.count == 1 ? Run{a.whole_ml + 2 * whole, a.whole_o + whole * a.D, 0, 0, 1}
-                        : Run{a.part_ml + 2 * at, a.part_o + at * a.D, step, a.cap, d.count};
-  };
-  join_row<T>(weight[wave], run(pre, pre_row, whole), run(own, (int)(own_row % kManyRows), a.Tq * a.Hq + whole), a.D,
-              a.scale_log2, static_cast<T*>(a.O) + t * a.o_token + h * a.o_head, a.lse ? a.lse + t * a.Hq + h : nullptr);
 }
 
 // Pieces for each key head's line: a workgroup each, as many as run at a time.
@@ -908,6 +1044,8 @@ hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages*
   a.D = D;
   a.causal = causal;
   scale_of(scale, dt, &a.scale_log2, &a.lift, &a.flip);
+  a.per_group = 1.0 / a.group;
+  a.half_tile = kManyRows * 0.5 / a.group;
   const PagedLayout l = paged_layout(Tq, seq->S, a.pre.S, Hq, Hk, D);
   a.pieces = l.pieces;
   a.cap = l.cap;
@@ -926,10 +1064,12 @@ hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages*
   if (dt == TDQ_F16) TDQ_BY_HEAD(TDQ_PAGED, _Float16);
   else TDQ_BY_HEAD(TDQ_PAGED, __bf16);
 #undef TDQ_PAGED
-  const int chunks = (Hq + 3) / 4;
+  // (few tokens: many parts a row, and wavefronts enough)
+  const int heads = Tq * Hq > 16384 ? 8 : 1;
+  const int chunks = (Hq + 4 * heads - 1) / (4 * heads);
   const dim3 join = two_axes(Tq * chunks);
-  if (dt == TDQ_F16) hipLaunchKernelGGL((k_join_pages<_Float16>), join, dim3(256), 0, st, a, chunks);
-  else hipLaunchKernelGGL((k_join_pages<__bf16>), join, dim3(256), 0, st, a, chunks);
+  if (dt == TDQ_F16) hipLaunchKernelGGL((k_join_pages<_Float16>), join, dim3(256), 0, st, a, heads, chunks);
+  else hipLaunchKernelGGL((k_join_pages<__bf16>), join, dim3(256), 0, st, a, heads, chunks);
   return hipGetLastError();
 }
 
@@ -939,6 +1079,7 @@ hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages*
 // Every token and key head has a list of pages of its own, so a tile has the group's rows and no more;
 // its pages are shared out to `splits` workgroups, and in each to four wavefronts.
 struct ChosenArgs {
+  static constexpr bool kReadAgain = false;
   const void* Q;
   void* O;
   float* lse;
@@ -974,8 +1115,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   const int rows = a.group - tile * kFewRows < kFewRows ? a.group - tile * kFewRows : kFewRows;
   const int lane = threadIdx.x & 63, row = (lane & 31) < rows ? lane & 31 : rows - 1;
   const int h0 = hk * a.group + tile * kFewRows;
-  const Chosen where = {a.chosen + (t * a.Hk + hk) * a.count, q.table + s * q.ld, a.count, q.shift, q.n_pages, keys};
-  const Store<T, DP> store(a.K, a.V, hk, q.shift, a.D);
+  const int* list = a.chosen + (t * a.Hk + hk) * a.count;
+  const Store<ChosenArgs, T, DP> store(a, hk, q.shift, keys);
   Target<T> target;
   target.O = static_cast<T*>(a.O) + t * a.o_token + h0 * a.o_head;
   target.lse = a.lse ? a.lse + t * a.Hq + h0 : nullptr;
@@ -984,7 +1125,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   target.Hq = a.Hq;
   target.group = kFewRows;                               // (all rows are heads of one token)
   target.first = 0;
-  target.scale_log2 = a.scale_log2;
   target.D = a.D;
   target.po = target.pml = nullptr;
   if (a.splits > 1) {
@@ -994,16 +1134,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     target.pml = a.part_ml + 2 * at;
   }
   int used = 0;                                          // the list up to its last page that is named
-  for (int i = lane; i < a.count; i += 64) used = where.list[i] >= 0 ? i + 1 : used;
+  for (int i = lane; i < a.count; i += 64) used = list[i] >= 0 ? i + 1 : used;
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) used = max(used, __shfl_xor(used, d, 64));
   used = __builtin_amdgcn_readfirstlane(used);
   const int tiles = sees > 0 ? (int)((((long long)used << q.shift) + kFewKeys - 1) / kFewKeys) : 0;
   const int share = (tiles + a.splits - 1) / a.splits;
   const int lo = split * share < tiles ? split * share : tiles, hi = lo + share < tiles ? lo + share : tiles;
+  Chosen where = {list, q.table + s * q.ld, used, q.shift, q.n_pages, keys, 0, -1, kNowhere};
+  if (lo < hi) where.hold((2 * lo) >> (q.shift - kGranuleBits) & ~63);
   if (a.D < DC) clear<DP>(sh);
-  attend_few<T, DP, DC>(sh, store, where, static_cast<const T*>(a.Q) + t * a.q_token + (h0 + row) * a.q_head, sees, sees,
-                        keys, lo, hi, rows, to - from == 1, a.flip, a.lift, target);
+  attend_few<ChosenArgs, T, DP, DC>(sh, store, where,
+                                    static_cast<const T*>(a.Q) + t * a.q_token + (h0 + row) * a.q_head, a.D, sees, sees,
+                                    lo, hi, rows, to - from == 1, a.flip, a.scale_log2, a.lift, [&] { return target; });
 }
 
 template <typename T>
