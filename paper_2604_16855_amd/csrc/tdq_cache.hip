@@ -74,14 +74,12 @@ __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a, int tok
   if (wave < here) {
     const Sequences& q = a.seq;
     const long long t = t0 + wave;
-    const int s = last_at_most(q.S, t, [&](int i) { return start_of(q.cu, i, a.T); });
-    const int from = start_of(q.cu, s, a.T), to = start_of(q.cu, s + 1, a.T);
+    const Owner o = owner_of(q, t, a.T);
     int j = -1, p = -2;
-    if (t >= from && t < to) {
-      const int n = q.len[s];
-      j = (int)((long long)n - to + t);
+    if (t >= o.from && t < o.to) {
+      j = (int)((long long)o.len - o.to + t);
       p = -1;
-      if (n >= 0 && j >= 0 && j >> q.shift < q.columns) p = q.table[s * q.ld + (j >> q.shift)];
+      if (o.len >= 0 && j >= 0 && j >> q.shift < q.columns) p = q.table[o.seq * q.ld + (j >> q.shift)];
       p = p >= 0 && p < q.n_pages ? p : -1;
     }
     if ((threadIdx.x & 63) == 0) {
@@ -351,67 +349,140 @@ struct Seen {
   int seq, keys;
 };
 __device__ __forceinline__ Seen seen_by(const Sequences& q, long long t, long long T, int causal) {
-  const int s = last_at_most(q.S, t, [&](int i) { return start_of(q.cu, i, T); });
-  const int from = start_of(q.cu, s, T), to = start_of(q.cu, s + 1, T), n = keys_of(q, s);
-  if (t < from || t >= to) return {s, -1};
-  const long long e = causal ? n - to + t + 1 : n;
-  return {s, e < 0 ? 0 : (int)e};
+  const Owner o = owner_of(q, t, T);
+  const int n = keys_in(q, o.len);
+  if (t < o.from || t >= o.to) return {o.seq, -1};
+  const long long e = causal ? n - o.to + t + 1 : n;
+  return {o.seq, e < 0 ? 0 : (int)e};
+}
+
+// The value of lane ^ 1 or lane ^ 2.
+template <int D>
+__device__ __forceinline__ u32 neighbour(u32 x) {
+  return __builtin_amdgcn_mov_dpp(x, D == 1 ? 0xB1 : 0x4E, 0xF, 0xF, true);
+}
+template <int D>
+__device__ __forceinline__ double neighbour(double x) {
+  const u32x2 w = __builtin_bit_cast(u32x2, x);
+  return __builtin_bit_cast(double, u32x2{neighbour<D>(w[0]), neighbour<D>(w[1])});
+}
+template <int D>
+__device__ __forceinline__ float neighbour(float x) {
+  return __uint_as_float(neighbour<D>(__float_as_uint(x)));
+}
+
+// Sums over L lanes of each of N values (1, 2 or 4), and the largest of them, rounded: the first two
+// exchanges halve what a lane has to add.
+template <int L, int N>
+__device__ __forceinline__ float largest_sum(const double (&s)[N]) {
+  const bool one = threadIdx.x & 1, two = threadIdx.x & 2;
+  double x;
+  if constexpr (N == 4) {
+    const double a = (one ? s[2] : s[0]) + neighbour<1>(one ? s[0] : s[2]);
+    const double b = (one ? s[3] : s[1]) + neighbour<1>(one ? s[1] : s[3]);
+    x = (two ? b : a) + neighbour<2>(two ? a : b);
+  } else if constexpr (N == 2) {
+    x = (one ? s[1] : s[0]) + neighbour<1>(one ? s[0] : s[1]);
+    x += neighbour<2>(x);
+  } else {
+    x = s[0] + neighbour<1>(s[0]);
+    x += neighbour<2>(x);
+  }
+#pragma unroll
+  for (int d = 4; d < L; d <<= 1) x += __shfl_xor(x, d, L);
+  float y = (float)x;
+  if constexpr (N > 1) y = most(y, neighbour<1>(y));
+  if constexpr (N > 2) y = most(y, neighbour<2>(y));
+  return y;
 }
 
 constexpr int kScorePages = 128;       // pages of a workgroup
 
 template <typename T, int L, int HEADS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_score(ChoiceArgs a) {
+  constexpr int GROUPS = 256 / L, STEPS = kScorePages / GROUPS;   // pages at a time, and how often
+  constexpr int AHEAD = STEPS < 8 ? STEPS : 8;                    // steps whose bounds are on their way at once
   __shared__ float top[kScorePages];
   const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
   const int h = (int)(id % a.Hk), chunk = (int)(id / a.Hk % a.chunks);
   const long long t = id / a.Hk / a.chunks;
   if (t >= a.Tq) return;
   const Sequences& q = a.seq;
+  const int sub = threadIdx.x & (L - 1), group = threadIdx.x / L;
+  const bool mine = 8 * sub < a.D;
+  auto query = [&](int e) {
+    // (past the last head: the last again, which changes no maximum)
+    const int head = h * a.group + (e < a.group ? e : a.group - 1);
+    u32x4 x = {0, 0, 0, 0};
+    if (mine) x = *reinterpret_cast<const u32x4_any*>(static_cast<const T*>(a.Q) + t * a.q_token + head * a.q_head + 8 * sub);
+    return x;
+  };
+  u32x4 x[HEADS];                                        // (on their way while the sequence is looked for)
+#pragma unroll
+  for (int e = 0; e < HEADS; ++e) x[e] = query(e);
   const Seen me = seen_by(q, t, a.Tq, a.causal);
   const int pages = me.keys <= 0 ? 0 : ((me.keys - 1) >> q.shift) + 1, b0 = chunk * kScorePages;
   if (b0 >= pages) return;
   const int here = pages - b0 < kScorePages ? pages - b0 : kScorePages;
-  const int sub = threadIdx.x & (L - 1), group = threadIdx.x / L;
-  const bool mine = 8 * sub < a.D;
   const int* line = q.table + me.seq * q.ld + b0;
   float* out = a.score + (t * a.Hk + h) * q.columns + b0;
+  // step i has page group + GROUPS i: lane i of the group holds which that is (-1: none)
+  int ids = -1;
+  if (sub < STEPS && group + GROUPS * sub < here) ids = line[group + GROUPS * sub];
+  ids = ids < q.n_pages ? ids : -1;
   for (int e0 = 0; e0 < a.group; e0 += HEADS) {
-    double up[HEADS][8], down[HEADS][8];
+    if (e0 > 0) {
 #pragma unroll
-    for (int e = 0; e < HEADS; ++e) {
-      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      // (past the last head: the last again, which changes no maximum)
-      const int head = h * a.group + (e0 + e < a.group ? e0 + e : a.group - 1);
-      if (mine) load_floats<T, 8>(static_cast<const T*>(a.Q) + t * a.q_token + head * a.q_head + 8 * sub, x);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        up[e][j] = x[j] < 0.f ? 0.0 : (double)x[j];
-        down[e][j] = x[j] > 0.f ? 0.0 : (double)x[j];
-      }
+      for (int e = 0; e < HEADS; ++e) x[e] = query(e0 + e);
     }
-    for (int b = group; b < here; b += 256 / L) {
-      const int page = line[b];
-      if (page < 0 || page >= q.n_pages) continue;       // (the same in the L lanes)
-      float lo[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, hi[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (mine) {
-        load_floats<T, 8>(static_cast<const T*>(a.lo) + page * a.lo_page + h * a.lo_head + 8 * sub, lo);
-        load_floats<T, 8>(static_cast<const T*>(a.hi) + page * a.hi_page + h * a.hi_head + 8 * sub, hi);
+#pragma unroll 1
+    for (int first = 0; first < STEPS && GROUPS * first < here; first += AHEAD) {
+      u32x4 lo[AHEAD], hi[AHEAD];
+      int page[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        page[i] = __shfl(ids, first + i, L);
+        lo[i] = hi[i] = u32x4{0, 0, 0, 0};
+        if (page[i] >= 0 && mine) {
+          const long long p = page[i];
+          lo[i] = *reinterpret_cast<const u32x4_any*>(static_cast<const T*>(a.lo) + p * a.lo_page + h * a.lo_head + 8 * sub);
+          hi[i] = *reinterpret_cast<const u32x4_any*>(static_cast<const T*>(a.hi) + p * a.hi_page + h * a.hi_head + 8 * sub);
+        }
       }
-      float best = -INFINITY;
+      double up[HEADS][8], down[HEADS][8];
 #pragma unroll
-      for (int e = 0; e < HEADS; ++e) {
-        double sum = 0.0;
+      for (int e = 0; e < HEADS; ++e)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum = fma(up[e][j], (double)hi[j], fma(down[e][j], (double)lo[j], sum));
+        for (int j = 0; j < 4; ++j) {
+          const f32x2 v = two_floats<T>(x[e][j]);
 #pragma unroll
-        for (int d = L / 2; d >= 1; d >>= 1) sum += __shfl_xor(sum, d, L);
-        best = most(best, (float)sum);
-      }
-      if (sub == 0) {
-        if (e0 > 0) best = most(best, top[b]);
-        top[b] = best;                                   // (read by this lane alone)
-        if (e0 + HEADS >= a.group) out[b] = best;
+          for (int u = 0; u < 2; ++u) {
+            up[e][2 * j + u] = v[u] < 0.f ? 0.0 : (double)v[u];
+            down[e][2 * j + u] = v[u] > 0.f ? 0.0 : (double)v[u];
+          }
+        }
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        double sum[HEADS];
+#pragma unroll
+        for (int e = 0; e < HEADS; ++e) sum[e] = 0.0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x2 l = two_floats<T>(lo[i][j]), g = two_floats<T>(hi[i][j]);
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const double y = (double)g[u], z = (double)l[u];
+#pragma unroll
+            for (int e = 0; e < HEADS; ++e) sum[e] = fma(up[e][2 * j + u], y, fma(down[e][2 * j + u], z, sum[e]));
+          }
+        }
+        float best = largest_sum<L, HEADS>(sum);
+        const int b = group + GROUPS * (first + i);
+        if (sub == 0 && page[i] >= 0) {
+          if (e0 > 0) best = most(best, top[b]);
+          if (e0 + HEADS >= a.group) out[b] = best;
+          else top[b] = best;                            // (read by this lane alone)
+        }
       }
     }
   }
@@ -423,8 +494,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 __global__ __launch_bounds__(256) void k_choose(ChoiceArgs a) {
   constexpr int HELD = 8;
   __shared__ u32 bins[256];
-  __shared__ u32 found[2];                               // digit, how many of the larger ones
-  __shared__ int count[2][4];
+  __shared__ u32 found[4];                               // digit, keys of larger ones, keys of it
+  __shared__ u32 ends[2][4];
+  __shared__ int count[2][4 * HELD];                     // above the limit, and at it
   const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
   if (id >= a.Tq * a.Hk) return;
   const Sequences& q = a.seq;
@@ -455,13 +527,62 @@ __global__ __launch_bounds__(256) void k_choose(ChoiceArgs a) {
       if (256 * i < pages) f(256 * i + tid, held[i]);
     for (int b = 256 * HELD; b < pages; b += 256) f(b + tid, read(b + tid));
   };
-  u32 prefix = 0, want = (u32)a.count;                   // the want-th largest of the keys that begin with prefix
-  bool all = pages <= a.count;
-  for (int shift = 24; shift >= 0 && !all; shift -= 8) {
-    bins[tid] = 0;
-    __syncthreads();
+  // Keys begin with the bits that all of them share but those at the two ends; the digits follow.
+  u32 both = 0xFFFFFFFFu, any = 0;
+  each([&](int, u32 k) {
+    if (k != 0 && k < 0xFFFFFFFEu) {
+      both &= k;
+      any |= k;
+    }
+  });
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) {
+    both &= __shfl_xor(both, d, 64);
+    any |= __shfl_xor(any, d, 64);
+  }
+  if (lane == 0) {
+    ends[0][wave] = both;
+    ends[1][wave] = any;
+  }
+  bins[tid] = 0;
+  __syncthreads();
+  u32 ands = 0xFFFFFFFFu, ors = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    ands &= ends[0][w];
+    ors |= ends[1][w];
+  }
+  const bool some = ors != 0;
+  u32 want = (u32)a.count, limit = 0;                    // taken: keys above limit, and the first `want` at it
+  bool all = pages <= a.count, done = false;
+  if (!all) {
+    // those that are always taken, or NaN, come first: the lowest places of them if they are too many
+    u32 c = 0;
+    u32 top_keys = 0xFFFFFFFFu;
+    for (int round = 0; round < 2 && !done; ++round, --top_keys) {
+      c = 0;
+      each([&](int, u32 k) { c += (u32)__popcll(__ballot(k == top_keys)); });
+      if (lane == 0) found[wave] = c;
+      __syncthreads();
+      c = found[0] + found[1] + found[2] + found[3];
+      __syncthreads();
+      if (c >= want) {
+        limit = top_keys;
+        done = true;
+      } else {
+        want -= c;
+      }
+    }
+    if (!done && !some) all = done = true;
+  }
+  const u32 differ = ands ^ ors;
+  int bits = differ ? 32 - __builtin_clz(differ) : 0;    // low bits that are not the same in all
+  u32 prefix = bits < 32 ? ands >> bits << bits : 0;
+  if (!all && !done && bits == 0) limit = prefix;        // (one key, however often; fewer than wanted: all of them)
+  while (!all && !done && bits > 0) {
+    const int shift = bits > 8 ? bits - 8 : 0;
     each([&](int, u32 k) {
-      if (k != 0 && (shift == 24 || k >> (shift + 8) == prefix >> (shift + 8))) atomicAdd(&bins[k >> shift & 255], 1u);
+      if (k != 0 && k < 0xFFFFFFFEu && (bits == 32 || k >> bits == prefix >> bits)) atomicAdd(&bins[k >> shift & ((1u << (bits - shift)) - 1)], 1u);
     });
     __syncthreads();
     if (wave == 0) {
@@ -484,44 +605,92 @@ __global__ __launch_bounds__(256) void k_choose(ChoiceArgs a) {
         if (above < want && above + c[i] >= want) {
           found[0] = 4 * lane + i;
           found[1] = above;
+          found[2] = c[i];
         }
         above += c[i];
       }
     }
     __syncthreads();
+    bins[tid] = 0;
     if (found[0] == 256) {
       all = true;
     } else {
       prefix |= found[0] << shift;
       want -= found[1];
+      limit = prefix;
+      if (found[2] == want && shift > 0) {               // every key of the bin: nothing to tell apart
+        limit = prefix - 1;
+        want = 0;
+        done = true;
+      }
     }
+    bits = shift;
     __syncthreads();
   }
-  // all: every key that is there; else those above prefix, and the first `want` of those that are equal
-  const u32 limit = all ? 0 : prefix;
-  int taken = 0, equal = 0;
-  each([&](int b, u32 k) {
-    const bool same = !all && k == limit;
-    const unsigned long long eq = __ballot(same);
-    if (lane == 0) count[0][wave] = __popcll(eq);
-    __syncthreads();
-    int before = equal;
-    for (int w = 0; w < 4; ++w) {
-      if (w < wave) before += count[0][w];
-      equal += count[0][w];
+  if (all) limit = 0;
+  auto takes = [&](u32 k, bool* same) {
+    *same = !all && k != 0 && k == limit && want > 0;
+    return k > limit;
+  };
+  const unsigned long long below = (1ull << lane) - 1;
+  // those in registers: counts of 256 at a time and wavefront, then a place for each
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    bool same;
+    const bool more = takes(held[i], &same);
+    const unsigned long long m = __ballot(more), e = __ballot(same);
+    if (lane == 0) {
+      count[0][4 * i + wave] = __popcll(m);
+      count[1][4 * i + wave] = __popcll(e);
     }
-    const unsigned long long below = (1ull << lane) - 1;
-    const bool take = k > limit || (same && before + __popcll(eq & below) < (int)want);
-    const unsigned long long tk = __ballot(take);
-    if (lane == 0) count[1][wave] = __popcll(tk);
-    __syncthreads();
-    int at = taken;
-    for (int w = 0; w < 4; ++w) {
-      if (w < wave) at += count[1][w];
-      taken += count[1][w];
+  }
+  __syncthreads();
+  // sums over what stands in front: lane 4 i + w
+  int mine_m = lane < 4 * HELD ? count[0][lane] : 0, mine_e = lane < 4 * HELD ? count[1][lane] : 0;
+  int upto_m = mine_m, upto_e = mine_e;
+#pragma unroll
+  for (int d = 1; d < 4 * HELD; d <<= 1) {
+    const int m = __shfl_up(upto_m, d, 64), e = __shfl_up(upto_e, d, 64);
+    if (lane >= d) {
+      upto_m += m;
+      upto_e += e;
     }
-    if (take) out[at + __popcll(tk & below)] = b;
-  });
+  }
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    bool same;
+    const bool more = takes(held[i], &same);
+    const unsigned long long m = __ballot(more), e = __ballot(same);
+    const int at_m = __shfl(upto_m - mine_m, 4 * i + wave, 64), at_e = __shfl(upto_e - mine_e, 4 * i + wave, 64);
+    const int rank = at_e + __popcll(e & below);         // among those at the limit
+    // (of those at the limit in front, the first `want` are taken)
+    const int before = at_m + __popcll(m & below) + (rank < (int)want ? rank : (int)want);
+    if (more || (same && rank < (int)want)) out[before] = 256 * i + tid;
+  }
+  int taken_m = __shfl(upto_m, 4 * HELD - 1, 64), taken_e = __shfl(upto_e, 4 * HELD - 1, 64);
+  for (int b = 256 * HELD; b < pages; b += 256) {
+    bool same;
+    const bool more = takes(read(b + tid), &same);
+    const unsigned long long m = __ballot(more), e = __ballot(same);
+    __syncthreads();
+    if (lane == 0) {
+      count[0][wave] = __popcll(m);
+      count[1][wave] = __popcll(e);
+    }
+    __syncthreads();
+    int at_m = taken_m, at_e = taken_e;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      at_m += w < wave ? count[0][w] : 0;
+      at_e += w < wave ? count[1][w] : 0;
+      taken_m += count[0][w];
+      taken_e += count[1][w];
+    }
+    const int rank = at_e + __popcll(e & below);
+    const int before = at_m + __popcll(m & below) + (rank < (int)want ? rank : (int)want);
+    if (more || (same && rank < (int)want)) out[before] = b + tid;
+  }
+  const int taken = taken_m + (taken_e < (int)want ? taken_e : (int)want);
   for (int i = taken + tid; i < a.count; i += 256) out[i] = -1;
 }
 

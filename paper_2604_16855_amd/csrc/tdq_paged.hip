@@ -1106,9 +1106,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   const long long t = rest / a.tiles;
   if (t >= a.Tq) return;
   const Sequences& q = a.seq;
-  const int s = last_at_most(q.S, t, [&](int i) { return start_of(q.cu, i, a.Tq); });
-  const int from = start_of(q.cu, s, a.Tq), to = start_of(q.cu, s + 1, a.Tq);
-  const int keys = __builtin_amdgcn_readfirstlane(keys_of(q, s));
+  const Owner o = owner_of(q, t, a.Tq);
+  const int s = o.seq, from = o.from, to = o.to, keys = __builtin_amdgcn_readfirstlane(keys_in(q, o.len));
   if (t < from || t >= to) return;
   const long long e = a.causal ? keys - to + t + 1 : keys;
   const int sees = __builtin_amdgcn_readfirstlane(e < 0 ? 0 : (int)e);

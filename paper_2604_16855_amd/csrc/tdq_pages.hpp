@@ -35,11 +35,12 @@ __device__ __forceinline__ int start_of(const int* cu, long long i, long long to
   const int c = cu[i];
   return c < 0 ? 0 : c < total ? c : (int)total;
 }
-// Keys of sequence s: no more than its line of the table has room for.
-__device__ __forceinline__ int keys_of(const Sequences& q, int s) {
-  const int n = q.len[s], room = q.columns << q.shift;
-  return n < 0 ? 0 : n < room ? n : room;
+// Keys of a sequence: no more than its line of the table has room for.
+__device__ __forceinline__ int keys_in(const Sequences& q, int len) {
+  const int room = q.columns << q.shift;
+  return len < 0 ? 0 : len < room ? len : room;
 }
+__device__ __forceinline__ int keys_of(const Sequences& q, int s) { return keys_in(q, q.len[s]); }
 
 // The last i < n with first(i) <= at, for an ascending `first` with first(0) <= at: 64 places at a
 // time, a lane each.  Every lane gets the answer.
@@ -59,6 +60,30 @@ __device__ __forceinline__ int last_at_most(int n, long long at, F first) {
     n = rest < step ? rest : step;
   }
   return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// The sequence of token t of T: which, its first token and the one behind its last (t is one of them, or
+// of no sequence), and what stands in len.
+struct Owner {
+  int seq, from, to, len;
+};
+__device__ __forceinline__ Owner owner_of(const Sequences& q, long long t, long long T) {
+  Owner o;
+  if (q.S <= 64) {                                       // all at once, a lane each
+    const int lane = threadIdx.x & 63, i = lane < q.S ? lane : q.S - 1;
+    const int from = start_of(q.cu, i, T), to = start_of(q.cu, i + 1, T), len = q.len[i];
+    const unsigned long long le = __ballot(lane < q.S && from <= t);
+    o.seq = le ? 63 - __builtin_clzll(le) : 0;
+    o.from = __builtin_amdgcn_readlane(from, o.seq);
+    o.to = __builtin_amdgcn_readlane(to, o.seq);
+    o.len = __builtin_amdgcn_readlane(len, o.seq);
+  } else {
+    o.seq = last_at_most(q.S, t, [&](int i) { return start_of(q.cu, i, T); });
+    o.from = start_of(q.cu, o.seq, T);
+    o.to = start_of(q.cu, o.seq + 1, T);
+    o.len = q.len[o.seq];
+  }
+  return o;
 }
 
 }  // namespace tdq
