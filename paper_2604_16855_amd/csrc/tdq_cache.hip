@@ -332,8 +332,9 @@ hipError_t launch_bounds(const tdq_pages* K, tdq_dtype dt, long long T, const td
 // with q = Q[t, e] and the bounds of page b: no product of q with a key of the page is larger.
 // The choice depends on which of two scores is larger, so they must not depend on the order of the sum:
 // products of two 16-bit types are added in binary64, which holds nearly all such sums without rounding,
-// and the result is rounded to binary32.  L lanes have a page's 16 bytes each of both bounds, HEADS heads
-// share them; the heads' parts stay in registers for all pages.
+// and the result is rounded to binary32.  The products are the 64-bit matrix instruction's: 16 pages x 4
+// heads x 4 channels at a time, four heads of a group and both of their signs in registers for all pages
+// of a workgroup.
 struct ChoiceArgs {
   const void *Q, *lo, *hi;
   long long q_token, q_head, lo_page, lo_head, hi_page, hi_head;
@@ -358,131 +359,109 @@ __device__ __forceinline__ Seen seen_by(const Sequences& q, long long t, long lo
 
 // The value of lane ^ 1 or lane ^ 2.
 template <int D>
-__device__ __forceinline__ u32 neighbour(u32 x) {
-  return __builtin_amdgcn_mov_dpp(x, D == 1 ? 0xB1 : 0x4E, 0xF, 0xF, true);
-}
-template <int D>
-__device__ __forceinline__ double neighbour(double x) {
-  const u32x2 w = __builtin_bit_cast(u32x2, x);
-  return __builtin_bit_cast(double, u32x2{neighbour<D>(w[0]), neighbour<D>(w[1])});
-}
-template <int D>
 __device__ __forceinline__ float neighbour(float x) {
-  return __uint_as_float(neighbour<D>(__float_as_uint(x)));
+  return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), D == 1 ? 0xB1 : 0x4E, 0xF, 0xF, true));
 }
 
-// Sums over L lanes of each of N values (1, 2 or 4), and the largest of them, rounded: the first two
-// exchanges halve what a lane has to add.
-template <int L, int N>
-__device__ __forceinline__ float largest_sum(const double (&s)[N]) {
-  const bool one = threadIdx.x & 1, two = threadIdx.x & 2;
-  double x;
-  if constexpr (N == 4) {
-    const double a = (one ? s[2] : s[0]) + neighbour<1>(one ? s[0] : s[2]);
-    const double b = (one ? s[3] : s[1]) + neighbour<1>(one ? s[1] : s[3]);
-    x = (two ? b : a) + neighbour<2>(two ? a : b);
-  } else if constexpr (N == 2) {
-    x = (one ? s[1] : s[0]) + neighbour<1>(one ? s[0] : s[1]);
-    x += neighbour<2>(x);
-  } else {
-    x = s[0] + neighbour<1>(s[0]);
-    x += neighbour<2>(x);
-  }
-#pragma unroll
-  for (int d = 4; d < L; d <<= 1) x += __shfl_xor(x, d, L);
-  float y = (float)x;
-  if constexpr (N > 1) y = most(y, neighbour<1>(y));
-  if constexpr (N > 2) y = most(y, neighbour<2>(y));
-  return y;
-}
+// Pages of a workgroup, 16 of a wavefront at a time.
+constexpr int score_pages(int W) { return W <= 16 ? 512 : 256; }
 
-constexpr int kScorePages = 128;       // pages of a workgroup
-
-template <typename T, int L, int HEADS>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_score(ChoiceArgs a) {
-  constexpr int GROUPS = 256 / L, STEPS = kScorePages / GROUPS;   // pages at a time, and how often
-  constexpr int AHEAD = STEPS < 8 ? STEPS : 8;                    // steps whose bounds are on their way at once
-  __shared__ float top[kScorePages];
+// W: channels of a lane.  Lane 16 k + p has of page p the 16-byte pieces k, k + 4, ..
+template <typename T, int W>
+__global__ __launch_bounds__(256, W == 16 ? 3 : 4) void k_score(ChoiceArgs a) {
+  constexpr int PIECES = W < 32 ? W / 8 : 4, PASSES = W / (8 * PIECES);   // pieces of a bound at a time
+  constexpr int PAGES = score_pages(W);
+  __shared__ float top[PAGES];
   const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
   const int h = (int)(id % a.Hk), chunk = (int)(id / a.Hk % a.chunks);
   const long long t = id / a.Hk / a.chunks;
   if (t >= a.Tq) return;
   const Sequences& q = a.seq;
-  const int sub = threadIdx.x & (L - 1), group = threadIdx.x / L;
-  const bool mine = 8 * sub < a.D;
-  auto query = [&](int e) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = lane >> 4;
+  auto at = [&](int pass, int i) { return 8 * (k + 4 * (pass * PIECES + i)); };   // first channel of a piece
+  // operand columns: head lane % 4, its positive and its negative channels
+  float up[8 * PIECES], down[8 * PIECES];
+  auto query = [&](int e0, int pass) {
     // (past the last head: the last again, which changes no maximum)
-    const int head = h * a.group + (e < a.group ? e : a.group - 1);
-    u32x4 x = {0, 0, 0, 0};
-    if (mine) x = *reinterpret_cast<const u32x4_any*>(static_cast<const T*>(a.Q) + t * a.q_token + head * a.q_head + 8 * sub);
-    return x;
-  };
-  u32x4 x[HEADS];                                        // (on their way while the sequence is looked for)
+    const int e = e0 + (lane & 3), head = h * a.group + (e < a.group ? e : a.group - 1);
+    const T* p = static_cast<const T*>(a.Q) + t * a.q_token + head * a.q_head;
+    u32x4 x[PIECES];
 #pragma unroll
-  for (int e = 0; e < HEADS; ++e) x[e] = query(e);
-  const Seen me = seen_by(q, t, a.Tq, a.causal);
-  const int pages = me.keys <= 0 ? 0 : ((me.keys - 1) >> q.shift) + 1, b0 = chunk * kScorePages;
-  if (b0 >= pages) return;
-  const int here = pages - b0 < kScorePages ? pages - b0 : kScorePages;
-  const int* line = q.table + me.seq * q.ld + b0;
-  float* out = a.score + (t * a.Hk + h) * q.columns + b0;
-  // step i has page group + GROUPS i: lane i of the group holds which that is (-1: none)
-  int ids = -1;
-  if (sub < STEPS && group + GROUPS * sub < here) ids = line[group + GROUPS * sub];
-  ids = ids < q.n_pages ? ids : -1;
-  for (int e0 = 0; e0 < a.group; e0 += HEADS) {
-    if (e0 > 0) {
-#pragma unroll
-      for (int e = 0; e < HEADS; ++e) x[e] = query(e0 + e);
+    for (int i = 0; i < PIECES; ++i) {
+      x[i] = u32x4{0, 0, 0, 0};
+      if (at(pass, i) < a.D) x[i] = *reinterpret_cast<const u32x4_any*>(p + at(pass, i));
     }
-#pragma unroll 1
-    for (int first = 0; first < STEPS && GROUPS * first < here; first += AHEAD) {
-      u32x4 lo[AHEAD], hi[AHEAD];
-      int page[AHEAD];
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        page[i] = __shfl(ids, first + i, L);
-        lo[i] = hi[i] = u32x4{0, 0, 0, 0};
-        if (page[i] >= 0 && mine) {
-          const long long p = page[i];
-          lo[i] = *reinterpret_cast<const u32x4_any*>(static_cast<const T*>(a.lo) + p * a.lo_page + h * a.lo_head + 8 * sub);
-          hi[i] = *reinterpret_cast<const u32x4_any*>(static_cast<const T*>(a.hi) + p * a.hi_page + h * a.hi_head + 8 * sub);
+    for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x2 v = two_floats<T>(x[i][j]);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          up[8 * i + 2 * j + u] = v[u] < 0.f ? 0.f : v[u];
+          down[8 * i + 2 * j + u] = v[u] > 0.f ? 0.f : v[u];
         }
       }
-      double up[HEADS][8], down[HEADS][8];
+  };
+  const Seen me = seen_by(q, t, a.Tq, a.causal);
+  const int pages = me.keys <= 0 ? 0 : ((me.keys - 1) >> q.shift) + 1, b0 = chunk * PAGES;
+  if (b0 + 16 * wave >= pages) return;
+  const int here = pages - b0 < PAGES ? pages - b0 : PAGES;
+  const int* line = q.table + me.seq * q.ld + b0;
+  float* out = a.score + (t * a.Hk + h) * q.columns + b0;
+  // pages b .. b + 15: -1: none, or not there
+  auto page_of = [&](int b) {
+    int p = -1;
+    if (b + (lane & 15) < here) p = line[b + (lane & 15)];
+    return p < q.n_pages ? p : -1;
+  };
+#pragma unroll 1
+  for (int e0 = 0; e0 < a.group; e0 += 4) {
+    int page = page_of(16 * wave);
+    if (PASSES == 1) query(e0, 0);
+#pragma unroll 1
+    for (int b = 16 * wave; b < here; b += 64) {
+      const T* lo = static_cast<const T*>(a.lo) + (long long)page * a.lo_page + h * a.lo_head;
+      const T* hi = static_cast<const T*>(a.hi) + (long long)page * a.hi_page + h * a.hi_head;
+      double part[4] = {0.0, 0.0, 0.0, 0.0};             // (a product waits for the last one of its sum)
+#pragma unroll 1
+      for (int pass = 0; pass < PASSES; ++pass) {
+        u32x4 los[PIECES], his[PIECES];
 #pragma unroll
-      for (int e = 0; e < HEADS; ++e)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const f32x2 v = two_floats<T>(x[e][j]);
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            up[e][2 * j + u] = v[u] < 0.f ? 0.0 : (double)v[u];
-            down[e][2 * j + u] = v[u] > 0.f ? 0.0 : (double)v[u];
+        for (int i = 0; i < PIECES; ++i) {
+          los[i] = his[i] = u32x4{0, 0, 0, 0};
+          if (page >= 0 && at(pass, i) < a.D) {
+            los[i] = *reinterpret_cast<const u32x4_any*>(lo + at(pass, i));
+            his[i] = *reinterpret_cast<const u32x4_any*>(hi + at(pass, i));
           }
         }
+        if (pass == PASSES - 1) page = page_of(b + 64);
+        if (PASSES > 1) query(e0, pass);
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        double sum[HEADS];
+        for (int i = 0; i < PIECES; ++i)
 #pragma unroll
-        for (int e = 0; e < HEADS; ++e) sum[e] = 0.0;
+          for (int j = 0; j < 4; ++j) {
+            const f32x2 l = two_floats<T>(los[i][j]), g = two_floats<T>(his[i][j]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const f32x2 l = two_floats<T>(lo[i][j]), g = two_floats<T>(hi[i][j]);
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const double y = (double)g[u], z = (double)l[u];
-#pragma unroll
-            for (int e = 0; e < HEADS; ++e) sum[e] = fma(up[e][2 * j + u], y, fma(down[e][2 * j + u], z, sum[e]));
+            for (int u = 0; u < 2; ++u) {
+              // (converted again for every 16 pages: as binary64 they would take the registers of half of
+              // the wavefronts that hide the bounds' way here)
+              float x = up[8 * i + 2 * j + u], y = down[8 * i + 2 * j + u];
+              if constexpr (W > 16) asm volatile("" : "+v"(x), "+v"(y));
+              part[u] = __builtin_amdgcn_mfma_f64_4x4x4f64((double)g[u], (double)x, part[u], 0, 0, 0);
+              part[2 + u] = __builtin_amdgcn_mfma_f64_4x4x4f64((double)l[u], (double)y, part[2 + u], 0, 0, 0);
+            }
           }
-        }
-        float best = largest_sum<L, HEADS>(sum);
-        const int b = group + GROUPS * (first + i);
-        if (sub == 0 && page[i] >= 0) {
-          if (e0 > 0) best = most(best, top[b]);
-          if (e0 + HEADS >= a.group) out[b] = best;
-          else top[b] = best;                            // (read by this lane alone)
-        }
+      }
+      // lane 16 i + 4 c + j has page 4 c + i and head j
+      float best = (float)((part[0] + part[1]) + (part[2] + part[3]));
+      best = most(best, neighbour<1>(best));
+      best = most(best, neighbour<2>(best));
+      const int mine = b + 4 * (lane >> 2 & 3) + (lane >> 4);
+      if ((lane & 3) == 0 && mine < here) {              // (of pages that are not there nobody asks)
+        if (e0 > 0) best = most(best, top[mine]);
+        if (e0 + 4 >= a.group) out[mine] = best;
+        else top[mine] = best;                           // (read by this lane alone)
       }
     }
   }
@@ -718,16 +697,21 @@ hipError_t launch_choice(const tdq_heads* Q, const tdq_heads* lo, const tdq_head
   a.first = first;
   a.last = last;
   a.count = count;
-  a.chunks = (seq->columns + kScorePages - 1) / kScorePages;
+  const int pages = score_pages(D <= 32 ? 8 : D <= 64 ? 16 : D <= 128 ? 32 : 64);
+  a.chunks = (seq->columns + pages - 1) / pages;
   a.score = static_cast<float*>(workspace);
   a.chosen = chosen;
   const dim3 grid = two_axes(Tq * Hk * a.chunks);
-#define TDQ_SCORE_L(T_, L)                                                                                      do {                                                                                                            if (a.group == 1) hipLaunchKernelGGL((k_score<T_, L, 1>), grid, dim3(256), 0, st, a);                         else if (a.group == 2) hipLaunchKernelGGL((k_score<T_, L, 2>), grid, dim3(256), 0, st, a);                    else hipLaunchKernelGGL((k_score<T_, L, 4>), grid, dim3(256), 0, st, a);                                    } while (0)
-#define TDQ_SCORE(T_)                          do {                                           if (D <= 32) TDQ_SCORE_L(T_, 4);             else if (D <= 64) TDQ_SCORE_L(T_, 8);        else if (D <= 128) TDQ_SCORE_L(T_, 16);      else TDQ_SCORE_L(T_, 32);                  } while (0)
+#define TDQ_SCORE(T_)                                                                        \
+  do {                                                                                       \
+    if (D <= 32) hipLaunchKernelGGL((k_score<T_, 8>), grid, dim3(256), 0, st, a);            \
+    else if (D <= 64) hipLaunchKernelGGL((k_score<T_, 16>), grid, dim3(256), 0, st, a);      \
+    else if (D <= 128) hipLaunchKernelGGL((k_score<T_, 32>), grid, dim3(256), 0, st, a);     \
+    else hipLaunchKernelGGL((k_score<T_, 64>), grid, dim3(256), 0, st, a);                   \
+  } while (0)
   if (dt == TDQ_F16) TDQ_SCORE(_Float16);
   else TDQ_SCORE(__bf16);
 #undef TDQ_SCORE
-#undef TDQ_SCORE_L
   hipLaunchKernelGGL(k_choose, two_axes(Tq * Hk), dim3(256), 0, st, a);
   return hipGetLastError();
 }
