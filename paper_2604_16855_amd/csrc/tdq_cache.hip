@@ -35,52 +35,66 @@ constexpr int kAppendTokens = 4;       // most tokens of a workgroup: one a wave
 
 template <typename T, int L, bool PAIRS>
 __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a, int tokens) {
+  constexpr int GROUPS = kAppendThreads / L;           // heads at a time
   __shared__ float turn[kAppendTokens][TDQ_MAX_HEAD];  // cosine and sine of each pair
   __shared__ int place[kAppendTokens], page[kAppendTokens];   // key of its sequence, page (negative: nowhere, -2: no sequence)
   const int P = a.R >> 1;
   const long long t0 = (blockIdx.x + (long long)blockIdx.y * gridDim.x) * tokens;
   if (t0 >= a.T) return;                               // (a last row of workgroups may be longer than needed)
   const int here = (int)(a.T - t0 < tokens ? a.T - t0 : tokens);
-  const int sub = threadIdx.x & (L - 1), heads = a.heads[2];
+  const int sub = threadIdx.x & (L - 1), first = threadIdx.x / L;
   const int D = a.D, R = a.R;
   const bool mine = 8 * sub < D, turned = 8 * sub < R;
   // 8 elements of a lane: neighbours, or 4 of the first half of the turned ones and their partners
   const int e0 = PAIRS || !turned ? 8 * sub : 4 * sub, e1 = PAIRS || !turned ? e0 + 4 : P + 4 * sub;
-  // token and head of an item: the quotient of small numbers by a reciprocal just above 1 / heads
-  const float per = 1.0f / (float)heads * 1.000001f;
   struct Item {
     u32x2 a, b;
   };
-  struct Head {
-    int t, which, h;
+  // Queries, keys or values of the workgroup's tokens: item i is head i % H of token i / H, the quotient
+  // of small numbers by a reciprocal just above 1 / H.
+  struct Kind {
+    const T* in;
+    T* out;
+    long long in_token, in_head, out_token, out_head, page;
+    const float* weight;
+    int H;
+    float per;
   };
-  auto head_of = [&](int i) {
-    const int t = (int)((float)i * per), hh = i - t * heads;
-    const int which = (hh >= a.heads[0]) + (hh >= a.heads[1]);
-    return Head{t, which, which ? hh - a.heads[which - 1] : hh};
+  auto kind = [&](int which) {
+    const int H = a.heads[which] - (which ? a.heads[which - 1] : 0);
+    return Kind{static_cast<const T*>(a.in[which]) + t0 * a.in_token[which],
+                static_cast<T*>(a.out[which]) + (which ? 0 : t0 * a.out_token[which]),
+                a.in_token[which], a.in_head[which], a.out_token[which], a.out_head[which], a.page[which],
+                which < 2 ? a.weight[which] : nullptr, H, 1.0f / (float)(H > 0 ? H : 1) * 1.000001f};
   };
-  auto load = [&](int i, Item& v) {
-    const Head x = head_of(i);
-    const T* src = static_cast<const T*>(a.in[x.which]) + (t0 + x.t) * a.in_token[x.which] + x.h * a.in_head[x.which];
+  const Kind Q = kind(0), K = kind(1), V = kind(2);
+  auto load = [&](const Kind& x, int i, Item& v) {
+    const int t = (int)((float)i * x.per);
+    const T* src = x.in + t * x.in_token + (i - t * x.H) * x.in_head;
     v.a = *reinterpret_cast<const u32x2_any*>(src + e0);
     v.b = *reinterpret_cast<const u32x2_any*>(src + e1);
   };
-  // The first items are on their way while the places are found and the angles computed, each next
-  // one while one is worked on.
-  const int first = threadIdx.x / L, items = here * heads;
-  Item next = {};
-  if (mine && first < items) load(first, next);
+  auto load_all = [&](const Kind& x, int i, auto& v) {
+#pragma unroll
+    for (int u = 0; u < (int)(sizeof(v) / sizeof(v[0])); ++u)
+      if (mine && i + u * GROUPS < here * x.H) load(x, i + u * GROUPS, v[u]);
+  };
+  // Many items are on their way while the places are found and the angles computed.
+  Item q[4] = {}, k[2] = {}, v[2] = {};                 // (zeros where a head has nothing)
+  load_all(Q, first, q);
+  load_all(K, first, k);
+  load_all(V, first, v);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (wave < here) {
-    const Sequences& q = a.seq;
+    const Sequences& s = a.seq;
     const long long t = t0 + wave;
-    const Owner o = owner_of(q, t, a.T);
+    const Owner o = owner_of(s, t, a.T);
     int j = -1, p = -2;
     if (t >= o.from && t < o.to) {
       j = (int)((long long)o.len - o.to + t);
       p = -1;
-      if (o.len >= 0 && j >= 0 && j >> q.shift < q.columns) p = q.table[o.seq * q.ld + (j >> q.shift)];
-      p = p >= 0 && p < q.n_pages ? p : -1;
+      if (o.len >= 0 && j >= 0 && j >> s.shift < s.columns) p = s.table[o.seq * s.ld + (j >> s.shift)];
+      p = p >= 0 && p < s.n_pages ? p : -1;
     }
     if ((threadIdx.x & 63) == 0) {
       place[wave] = j;
@@ -100,36 +114,55 @@ __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a, int tok
   }
   __syncthreads();
   const int slots = (1 << a.seq.shift) - 1;
-  for (int i = first; i < items; i += kAppendThreads / L) {
-    const Item v = next;
-    if (mine && i + kAppendThreads / L < items) load(i + kAppendThreads / L, next);
-    const Head at = head_of(i);
-    const int to = page[at.t];
-    if (to < (at.which ? 0 : -1)) continue;            // (the same in all lanes of a head)
-    const long long row = at.which ? to * a.page[at.which] + (place[at.t] & slots) * a.out_token[at.which]
-                                   : (t0 + at.t) * a.out_token[0];
-    T* dst = static_cast<T*>(a.out[at.which]) + row + at.h * a.out_head[at.which];
-    if (at.which == 2) {
-      if (mine) {
-        *reinterpret_cast<u32x2_any*>(dst + e0) = v.a;
-        *reinterpret_cast<u32x2_any*>(dst + e1) = v.b;
-      }
-      continue;
-    }
-    float x[4], y[4];
+  // Where item i goes; nullptr: nowhere.
+  auto place_of = [&](const Kind& x, bool cache, int i, int* token) -> T* {
+    const int t = (int)((float)i * x.per), to = page[t];
+    *token = t;
+    if (to < (cache ? 0 : -1)) return nullptr;
+    return x.out + (cache ? to * x.page + (place[t] & slots) * x.out_token : t * x.out_token) + (i - t * x.H) * x.out_head;
+  };
+  auto finish = [&](const Kind& x, bool cache, int i, const Item& v) {
+    if (i >= here * x.H) return;                       // (the same in all lanes of a head)
+    int t;
+    T* dst = place_of(x, cache, i, &t);
+    if (!dst) return;
+    float f[4], g[4];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const f32x2 f = two_floats<T>(v.a[j]), g = two_floats<T>(v.b[j]);
-      x[2 * j] = f[0];
-      x[2 * j + 1] = f[1];
-      y[2 * j] = g[0];
-      y[2 * j + 1] = g[1];
+      const f32x2 y = two_floats<T>(v.a[j]), z = two_floats<T>(v.b[j]);
+      f[2 * j] = y[0];
+      f[2 * j + 1] = y[1];
+      g[2 * j] = z[0];
+      g[2 * j + 1] = z[1];
     }
-    norm_and_turn<L, PAIRS>(x, y, a.weight[at.which], e0, e1, D, a.eps, mine, turned, &turn[at.t][8 * sub]);
+    norm_and_turn<L, PAIRS>(f, g, x.weight, e0, e1, D, a.eps, mine, turned, &turn[t][8 * sub]);
     if (mine) {
-      store_floats<T, 4>(dst + e0, x);
-      store_floats<T, 4>(dst + e1, y);
+      store_floats<T, 4>(dst + e0, f);
+      store_floats<T, 4>(dst + e1, g);
     }
+  };
+  auto copy = [&](int i, const Item& x) {
+    if (i >= here * V.H || !mine) return;
+    int t;
+    T* dst = place_of(V, true, i, &t);
+    if (!dst) return;
+    *reinterpret_cast<u32x2_any*>(dst + e0) = x.a;
+    *reinterpret_cast<u32x2_any*>(dst + e1) = x.b;
+  };
+  for (int i = first; i < here * V.H; i += 2 * GROUPS) {
+    if (i != first) load_all(V, i, v);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) copy(i + u * GROUPS, v[u]);
+  }
+  for (int i = first; i < here * K.H; i += 2 * GROUPS) {
+    if (i != first) load_all(K, i, k);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) finish(K, true, i + u * GROUPS, k[u]);
+  }
+  for (int i = first; i < here * Q.H; i += 4 * GROUPS) {
+    if (i != first) load_all(Q, i, q);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) finish(Q, false, i + u * GROUPS, q[u]);
   }
 }
 
