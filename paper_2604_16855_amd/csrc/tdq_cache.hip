@@ -31,10 +31,14 @@ struct AppendArgs {
 };
 
 constexpr int kAppendThreads = 256;
-constexpr int kAppendTokens = 4;       // most tokens of a workgroup: one a wavefront
+// Tokens of a workgroup in calls of many (one each in others); these leave rows behind each other that no
+// cache holds until they are read, so their stores pass the caches by.  13253 tokens of 32/8 heads of 128,
+// us: 1 token 121, 2 113, 4 117, 8-byte stores past the caches 108, with 2 tokens 105.
+constexpr int kAppendTokens = 2, kAppendMany = 4096;
 
-template <typename T, int L, bool PAIRS>
-__global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a, int tokens) {
+template <typename T, int L, bool PAIRS, bool MANY>
+__global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a) {
+  constexpr int tokens = MANY ? kAppendTokens : 1;
   constexpr int GROUPS = kAppendThreads / L;           // heads at a time
   __shared__ float turn[kAppendTokens][TDQ_MAX_HEAD];  // cosine and sine of each pair
   __shared__ int place[kAppendTokens], page[kAppendTokens];   // key of its sequence, page (negative: nowhere, -2: no sequence)
@@ -121,6 +125,10 @@ __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a, int tok
     if (to < (cache ? 0 : -1)) return nullptr;
     return x.out + (cache ? to * x.page + (place[t] & slots) * x.out_token : t * x.out_token) + (i - t * x.H) * x.out_head;
   };
+  auto put = [&](T* p, u32x2 x) {
+    if constexpr (MANY) __builtin_nontemporal_store(x, reinterpret_cast<u32x2_any*>(p));
+    else *reinterpret_cast<u32x2_any*>(p) = x;
+  };
   auto finish = [&](const Kind& x, bool cache, int i, const Item& v) {
     if (i >= here * x.H) return;                       // (the same in all lanes of a head)
     int t;
@@ -137,8 +145,8 @@ __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a, int tok
     }
     norm_and_turn<L, PAIRS>(f, g, x.weight, e0, e1, D, a.eps, mine, turned, &turn[t][8 * sub]);
     if (mine) {
-      store_floats<T, 4>(dst + e0, f);
-      store_floats<T, 4>(dst + e1, g);
+      put(dst + e0, u32x2{two_rounded<T>(f[0], f[1]), two_rounded<T>(f[2], f[3])});
+      put(dst + e1, u32x2{two_rounded<T>(g[0], g[1]), two_rounded<T>(g[2], g[3])});
     }
   };
   auto copy = [&](int i, const Item& x) {
@@ -146,8 +154,8 @@ __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a, int tok
     int t;
     T* dst = place_of(V, true, i, &t);
     if (!dst) return;
-    *reinterpret_cast<u32x2_any*>(dst + e0) = x.a;
-    *reinterpret_cast<u32x2_any*>(dst + e1) = x.b;
+    put(dst + e0, x.a);
+    put(dst + e1, x.b);
   };
   for (int i = first; i < here * V.H; i += 2 * GROUPS) {
     if (i != first) load_all(V, i, v);
@@ -206,10 +214,13 @@ hipError_t launch_append(const tdq_heads* Q, const tdq_heads* K, const tdq_heads
   a.ld_pos = ld_pos;
   a.axis = axis;
   a.freq = freq;
-  const int tokens = T >= 1024 * kAppendTokens ? kAppendTokens : 1;
+  const int tokens = T >= kAppendMany ? kAppendTokens : 1;
   const dim3 grid = two_axes((T + tokens - 1) / tokens);
-#define TDQ_APPEND_LP(T_, L, PAIRS) \
-  hipLaunchKernelGGL((k_append<T_, L, PAIRS>), grid, dim3(kAppendThreads), 0, st, a, tokens)
+#define TDQ_APPEND_LP(T_, L, PAIRS)                                                                                \
+  do {                                                                                                             \
+    if (tokens > 1) hipLaunchKernelGGL((k_append<T_, L, PAIRS, true>), grid, dim3(kAppendThreads), 0, st, a);      \
+    else hipLaunchKernelGGL((k_append<T_, L, PAIRS, false>), grid, dim3(kAppendThreads), 0, st, a);                \
+  } while (0)
 #define TDQ_APPEND_L(T_, L)                      \
   do {                                           \
     if (interleaved) TDQ_APPEND_LP(T_, L, true); \

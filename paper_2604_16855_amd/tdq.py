@@ -9,6 +9,8 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
+import threading
 from typing import Optional, Tuple
 
 import torch  # first: the library resolves libamdhip64 against the copy torch loaded
@@ -876,55 +878,77 @@ def tdq_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, cu_q: torch
 # --------------------------------------------------------------------------------------
 # a cache of keys and values in pages
 # --------------------------------------------------------------------------------------
-# The structures of a call one after the other: their places in an array of 64-bit numbers, in bytes.
+# The structures of a call one after the other: their places in a run of 64-bit numbers, in bytes.
 _HEADS, _PAGES, _SEQUENCES = 24, 32, 48
+_pack = {n: struct.Struct(f"{n}q").pack_into for n in (15, 16, 20, 26)}
 
 
-def _same_device(*tensors) -> None:
+class _Buffer(threading.local):
+    """Room for a call's structures, one for each thread: the library reads them before it returns."""
+
+    def __init__(self):
+        self.data = C.create_string_buffer(8 * 26)
+        self.at = C.addressof(self.data)
+
+
+_buffer = _Buffer()
+
+
+def _same_device(tensors) -> None:
     """The library runs on the current device: an address of another one would fault it."""
-    dev = None
-    for t in tensors:
-        if t is None:
-            continue
-        at = t.get_device()                  # (-1: the host)
-        if dev is None and at >= 0:
-            dev = _get_device() if _get_device is not None else torch.cuda.current_device()
-        if at < 0 or at != dev:
-            raise ValueError("all tensors must be on the current GPU")
+    at = {t.get_device() for t in tensors if t is not None}
+    dev = at.pop() if len(at) == 1 else -1           # (-1: the host)
+    if dev < 0 or dev != (torch.cuda.current_device() if _get_device is None else _get_device()):
+        raise ValueError("all tensors must be on the current GPU")
 
 
-def _ints(t: torch.Tensor, name: str, n: Optional[int] = None) -> torch.Tensor:
+def _ints(t: torch.Tensor, name: str, n: int) -> int:
+    """Address of contiguous int32 [n]."""
     if t.dtype is not torch.int32:
         raise _wrong_type(name, t, torch.int32)
-    if t.dim() != 1 or not t.is_contiguous() or (n is not None and t.shape[0] != n):
-        raise ValueError(f"{name} must be contiguous" + ("" if n is None else f" [{n}]"))
-    return t
+    if t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous [{n}]")
+    return t.data_ptr()
 
 
-def _cache(X: torch.Tensor, name: str, like=None) -> Tuple[int, int, int, int]:
+def _cache(X: torch.Tensor, shape, name: str) -> Tuple[int, int, int, int]:
     """(address, page, token and head strides) of [pages, page_size, heads, D]."""
-    shape, s = X.shape, X.stride()
-    if len(shape) != 4 or (s[3] != 1 and shape[3] > 1):
-        raise ValueError(f"{name} must be [pages, page_size, heads, D] with contiguous heads")
-    if like is not None and (shape != like.shape or X.dtype is not like.dtype):
+    p, t, h, d = X.stride()
+    if d != 1 and shape[3] > 1:
+        raise ValueError(f"{name} must have contiguous heads")
+    if (p | t | h) & 7:
+        # (the stride of an axis of extent 1 addresses nothing; torch may report any value for it)
+        p, t, h = (s if n > 1 else 0 for s, n in zip((p, t, h), shape))
+    return X.data_ptr(), p, t, h
+
+
+def _caches(cache_k: torch.Tensor, cache_v: torch.Tensor, dtype):
+    """Their shape; refused if they differ."""
+    shape = cache_k.shape
+    if len(shape) != 4 or cache_k.dtype is not dtype:
+        raise ValueError("the cache must be [pages, page_size, heads, D] of the other tensors' type")
+    if cache_v.shape != shape or cache_v.dtype is not dtype:
         raise ValueError("the caches of keys and values must have the same shape and type")
-    # (the stride of an axis of extent 1 addresses nothing; torch may report any value for it)
-    return (X.data_ptr(),) + tuple(s[i] if shape[i] > 1 else 0 for i in range(3))
+    return shape
 
 
-def _sequences(cu: Optional[torch.Tensor], table: torch.Tensor, len_k: torch.Tensor, cache_shape, what: str):
+def _sequences(cu: Optional[torch.Tensor], table: torch.Tensor, len_k: torch.Tensor, n_pages: int, page_size: int,
+               what: str = ""):
     """tdq_sequences as six 64-bit numbers."""
     if table.dtype is not torch.int32:
         raise _wrong_type(what + "table", table, torch.int32)
-    shape, at = table.shape, table.stride()
-    if len(shape) != 2 or (at[1] != 1 and shape[1] > 1):
+    shape = table.shape
+    if len(shape) != 2:
         raise ValueError(what + "table must be [sequences, pages] with contiguous rows")
     S, columns = shape
-    _ints(len_k, what + "len_k", S)
-    if cu is not None:
-        _ints(cu, what + "cu_q", S + 1)
-    return (0 if cu is None else cu.data_ptr(), len_k.data_ptr(), table.data_ptr(), at[0] if S > 1 else max(columns, 1),
-            S | columns << 32, cache_shape[0] | cache_shape[1] << 32)
+    ld, step = table.stride()
+    if step != 1 and columns > 1:
+        raise ValueError(what + "table must be [sequences, pages] with contiguous rows")
+    return (0 if cu is None else _ints(cu, what + "cu_q", S + 1), _ints(len_k, what + "len_k", S), table.data_ptr(),
+            ld if S > 1 else max(columns, 1), S | columns << 32, n_pages | page_size << 32)
+
+
+_NO_QUERIES = (0,) * 6
 
 
 def tdq_cache_append(Q: Optional[torch.Tensor], K: torch.Tensor, V: torch.Tensor, cache_k: torch.Tensor,
@@ -941,14 +965,15 @@ def tdq_cache_append(Q: Optional[torch.Tensor], K: torch.Tensor, V: torch.Tensor
     T, Hk, D = k_shape
     if V.shape != k_shape or V.dtype is not dtype:
         raise ValueError("K and V must have the same shape and type")
-    shape = cache_k.shape
-    if len(shape) != 4 or shape[2] != Hk or shape[3] != D or cache_k.dtype is not dtype:
-        raise ValueError("the cache must be [pages, page_size, heads, D] with K's heads, head size and type")
-    Hq, q = 0, (0,) * 6
+    shape = _caches(cache_k, cache_v, dtype)
+    pages, page_size, cache_heads, cache_d = shape
+    if cache_heads != Hk or cache_d != D:
+        raise ValueError("the cache must have K's heads and head size")
+    Hq, q = 0, _NO_QUERIES
     if Q is not None:
         q_shape = Q.shape
-        Hq = q_shape[1]
-        if q_shape[0] != T or q_shape[2] != D or Q.dtype is not dtype:
+        q_tokens, Hq, q_d = q_shape
+        if q_tokens != T or q_d != D or Q.dtype is not dtype:
             raise ValueError("Q must have K's tokens, head size and type")
         if out is None:
             out = torch.empty(q_shape, dtype=dtype, device=Q.device)
@@ -978,17 +1003,24 @@ def tdq_cache_append(Q: Optional[torch.Tensor], K: torch.Tensor, V: torch.Tensor
             if axis.numel() != P or not axis.is_contiguous():
                 raise ValueError("axis must be contiguous and name an axis for each of freq")
             p_axis = axis.data_ptr()
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None and (w.dtype is not torch.float32 or w.numel() != D or not w.is_contiguous()):
-            raise ValueError(name + " must be contiguous float32 [D]")
-    h = (C.c_int64 * 26)(*q, K.data_ptr(), *_strides(K, "K"), V.data_ptr(), *_strides(V, "V"),
-                         *_cache(cache_k, "cache_k"), *_cache(cache_v, "cache_v", cache_k),
-                         *_sequences(cu_q, table, len_k, shape, ""))
-    _same_device(Q, K, V, cache_k, cache_v, cu_q, table, len_k, freq, pos, q_weight, k_weight, axis, out)
-    at = C.addressof(h)
+    p_wq = p_wk = None
+    if q_weight is not None:
+        if q_weight.dtype is not torch.float32 or q_weight.shape != (D,) or not q_weight.is_contiguous():
+            raise ValueError("q_weight must be contiguous float32 [D]")
+        p_wq = q_weight.data_ptr()
+    if k_weight is not None:
+        if k_weight.dtype is not torch.float32 or k_weight.shape != (D,) or not k_weight.is_contiguous():
+            raise ValueError("k_weight must be contiguous float32 [D]")
+        p_wk = k_weight.data_ptr()
+    seq = _sequences(cu_q, table, len_k, pages, page_size)
+    _same_device((Q, K, V, cache_k, cache_v, cu_q, table, len_k, freq, pos, q_weight, k_weight, axis, out))
+    room = _buffer
+    _pack[26](room.data, 0, *q, K.data_ptr(), *_strides(K, "K"), V.data_ptr(), *_strides(V, "V"),
+              *_cache(cache_k, shape, "cache_k"), *_cache(cache_v, shape, "cache_v"), *seq)
+    at = room.at
     rc = (_lib or lib()).tdq_cache_append(
         at if Hq else None, at + 2 * _HEADS, at + 3 * _HEADS, _wdt(dtype), T, at + 4 * _HEADS + 2 * _PAGES, Hq, Hk, D,
-        _ptr(q_weight), _ptr(k_weight), eps, R, 1 if interleaved else 0, p_pos, ld_pos, axes, p_axis, p_freq,
+        p_wq, p_wk, eps, R, 1 if interleaved else 0, p_pos, ld_pos, axes, p_axis, p_freq,
         at + _HEADS if Hq else None, at + 4 * _HEADS, at + 4 * _HEADS + _PAGES, _stream())
     if rc:
         raise TdqError(rc, "tdq_cache_append")
@@ -1003,21 +1035,23 @@ def tdq_page_bounds(cache_k: torch.Tensor, table: torch.Tensor, len_k: torch.Ten
     sequence's last cu_q[s + 1] - cu_q[s] keys, Tq in all (or more).  The others are left as they are (zeros in a new
     `out`)."""
     shape, dtype = cache_k.shape, cache_k.dtype
-    c = _cache(cache_k, "cache_k")
-    pages, _, Hk, D = shape
+    if len(shape) != 4:
+        raise ValueError("cache_k must be [pages, page_size, heads, D]")
     if cu_q is not None and Tq is None:
         raise ValueError("cu_q needs Tq, the number of new tokens")
+    pages, page_size, Hk, D = shape
     if out is None:
         out = (torch.zeros((pages, Hk, D), dtype=dtype, device=cache_k.device),
                torch.zeros((pages, Hk, D), dtype=dtype, device=cache_k.device))
     lo, hi = out
-    for x in out:
-        if x.shape != (pages, Hk, D) or x.dtype is not dtype:
-            raise ValueError("out must be two of [pages, heads, D] of the cache's type")
-    h = (C.c_int64 * 16)(*c, lo.data_ptr(), *_strides(lo, "lo"), hi.data_ptr(), *_strides(hi, "hi"),
-                         *_sequences(cu_q, table, len_k, shape, ""))
-    _same_device(cache_k, lo, hi, cu_q, table, len_k)
-    at = C.addressof(h)
+    if lo.shape != (pages, Hk, D) or hi.shape != (pages, Hk, D) or lo.dtype is not dtype or hi.dtype is not dtype:
+        raise ValueError("out must be two of [pages, heads, D] of the cache's type")
+    seq = _sequences(cu_q, table, len_k, pages, page_size)
+    _same_device((cache_k, lo, hi, cu_q, table, len_k))
+    room = _buffer
+    _pack[16](room.data, 0, *_cache(cache_k, shape, "cache_k"), lo.data_ptr(), *_strides(lo, "lo"), hi.data_ptr(),
+              *_strides(hi, "hi"), *seq)
+    at = room.at
     rc = (_lib or lib()).tdq_page_bounds(at, _wdt(dtype), Tq or 0, at + _PAGES + 2 * _HEADS, Hk, D, at + _PAGES,
                                          at + _PAGES + _HEADS, _stream())
     if rc:
@@ -1055,12 +1089,14 @@ def tdq_select_pages(Q: torch.Tensor, lo: torch.Tensor, hi: torch.Tensor, cu_q: 
     elif out.dtype is not torch.int32 or out.shape != (Tq, Hk, count) or not out.is_contiguous():
         raise ValueError("out must be contiguous int32 [Tq, heads, count]")
     L = _lib or lib()
-    h = (C.c_int64 * 15)(Q.data_ptr(), *_strides(Q, "Q"), lo.data_ptr(), *_strides(lo, "lo"), hi.data_ptr(),
-                         *_strides(hi, "hi"), *_sequences(cu_q, table, len_k, (b_shape[0], page_size), ""))
+    seq = _sequences(cu_q, table, len_k, b_shape[0], page_size)
     n = L.tdq_select_pages_workspace_bytes(Tq, Hk, table.shape[1]) if workspace is None else 0
     workspace, p_work, n_work = _scratch(workspace, n, Q.device)
-    _same_device(Q, lo, hi, cu_q, table, len_k, out, workspace)
-    at = C.addressof(h)
+    _same_device((Q, lo, hi, cu_q, table, len_k, out, workspace))
+    room = _buffer
+    _pack[15](room.data, 0, Q.data_ptr(), *_strides(Q, "Q"), lo.data_ptr(), *_strides(lo, "lo"), hi.data_ptr(),
+              *_strides(hi, "hi"), *seq)
+    at = room.at
     rc = L.tdq_select_pages(at, at + _HEADS, at + 2 * _HEADS, _wdt(dtype), Tq, at + 3 * _HEADS, Hq, Hk, D,
                             1 if causal else 0, first, last, count, out.data_ptr(), p_work, n_work, _stream())
     if rc:
@@ -1068,12 +1104,14 @@ def tdq_select_pages(Q: torch.Tensor, lo: torch.Tensor, hi: torch.Tensor, cu_q: 
     return out
 
 
-def _paged_call(Q, cache_k, cache_v, cu_q, table, len_k, out, lse, want_lse, more=()):
-    """(structures Q, O, K, V, sequences and `more` one after the other, Tq, Hq, Hk, D, out, lse)."""
-    q_shape, dtype, shape = Q.shape, Q.dtype, cache_k.shape
+def _paged_call(Q, cache_k, cache_v, cu_q, table, len_k, out, lse, want_lse):
+    """(structures Q, O, K, V and sequences as 64-bit numbers, Tq, Hq, Hk, D, out, lse)."""
+    q_shape, dtype = Q.shape, Q.dtype
     Tq, Hq, D = q_shape
-    if len(shape) != 4 or shape[3] != D or cache_k.dtype is not dtype:
-        raise ValueError("the cache must be [pages, page_size, heads, D] with Q's head size and type")
+    shape = _caches(cache_k, cache_v, dtype)
+    pages, page_size, Hk, cache_d = shape
+    if cache_d != D:
+        raise ValueError("the cache must have Q's head size")
     if out is None:
         out = torch.empty(q_shape, dtype=dtype, device=Q.device)
     elif out.shape != q_shape or out.dtype is not dtype:
@@ -1083,10 +1121,9 @@ def _paged_call(Q, cache_k, cache_v, cu_q, table, len_k, out, lse, want_lse, mor
             lse = torch.empty((Tq, Hq), dtype=torch.float32, device=Q.device)
     elif lse.dtype is not torch.float32 or lse.shape != (Tq, Hq) or not lse.is_contiguous():
         raise ValueError("lse must be contiguous float32 [Tq, Hq]")
-    h = (C.c_int64 * (20 + len(more)))(
-        Q.data_ptr(), *_strides(Q, "Q"), out.data_ptr(), *_strides(out, "out"), *_cache(cache_k, "cache_k"),
-        *_cache(cache_v, "cache_v", cache_k), *_sequences(cu_q, table, len_k, shape, ""), *more)
-    return h, Tq, Hq, shape[2], D, out, lse
+    h = (Q.data_ptr(), *_strides(Q, "Q"), out.data_ptr(), *_strides(out, "out"), *_cache(cache_k, shape, "cache_k"),
+         *_cache(cache_v, shape, "cache_v"), *_sequences(cu_q, table, len_k, pages, page_size))
+    return h, Tq, Hq, Hk, D, out, lse
 
 
 _KC, _VC, _SEQ, _PRE = 2 * _HEADS, 2 * _HEADS + _PAGES, 2 * _HEADS + 2 * _PAGES, 2 * _HEADS + 2 * _PAGES + _SEQUENCES
@@ -1114,8 +1151,10 @@ def tdq_attention_selected(Q: torch.Tensor, cache_k: torch.Tensor, cache_v: torc
     if workspace is None:
         need = L.tdq_attention_selected_workspace_bytes(Tq, Hq, Hk, D, cache_k.shape[1], count)
     workspace, p_work, n_work = _scratch(workspace, need, Q.device)
-    _same_device(Q, cache_k, cache_v, chosen, cu_q, table, len_k, out, lse, workspace)
-    at = C.addressof(h)
+    _same_device((Q, cache_k, cache_v, chosen, cu_q, table, len_k, out, lse, workspace))
+    room = _buffer
+    _pack[20](room.data, 0, *h)
+    at = room.at
     rc = L.tdq_attention_selected(at, at + _KC, at + _VC, _wdt(Q.dtype), Tq, at + _SEQ, Hq, Hk, D,
                                   D ** -0.5 if scale is None else scale, 1 if causal else 0, chosen.data_ptr(), count,
                                   at + _HEADS, _ptr(lse), p_work, n_work, _stream())
@@ -1136,20 +1175,20 @@ def tdq_attention_paged(Q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.T
     cache_k and cache_v[pages, page_size, Hk, D] -> (O[Tq, Hq, D], lse[Tq, Hq] f32 or None).  prefix: None, or (first
     sequence of each prefix and the end [G + 1], its table [G, pages], its keys [G]), all int32: keys that stand in
     front of those of its sequences.  scale: 1 / sqrt(D) if None.  Rows of queries of no sequence are not written."""
-    more, tensors, G = (), (), 0
+    h, Tq, Hq, Hk, D, out, lse = _paged_call(Q, cache_k, cache_v, cu_q, table, len_k, out, lse, want_lse)
+    L, G = _lib or lib(), 0
     if prefix is not None:
-        tensors = tuple(prefix)
-        if len(tensors) != 3:
+        if len(prefix) != 3:
             raise ValueError("prefix must be (first sequences, table, keys)")
-        more = _sequences(*tensors, cache_k.shape, "prefix ")
-        G = tensors[1].shape[0]
-    h, Tq, Hq, Hk, D, out, lse = _paged_call(Q, cache_k, cache_v, cu_q, table, len_k, out, lse, want_lse, more)
-    L = _lib or lib()
+        h += _sequences(*prefix, cache_k.shape[0], cache_k.shape[1], "prefix ")
+        G = prefix[1].shape[0]
     need = L.tdq_attention_paged_workspace_bytes(Tq, table.shape[0], G, Hq, Hk, D) if workspace is None else 0
     workspace, p_work, n_work = _scratch(workspace, need, Q.device)
-    _same_device(Q, cache_k, cache_v, cu_q, table, len_k, out, lse, workspace, *tensors)
-    at = C.addressof(h)
-    rc = L.tdq_attention_paged(at, at + _KC, at + _VC, _wdt(Q.dtype), Tq, at + _SEQ, at + _PRE if more else None, Hq, Hk,
+    _same_device((Q, cache_k, cache_v, cu_q, table, len_k, out, lse, workspace, *(prefix or ())))
+    room = _buffer
+    _pack[len(h)](room.data, 0, *h)
+    at = room.at
+    rc = L.tdq_attention_paged(at, at + _KC, at + _VC, _wdt(Q.dtype), Tq, at + _SEQ, None if prefix is None else at + _PRE, Hq, Hk,
                                D, D ** -0.5 if scale is None else scale, 1 if causal else 0, at + _HEADS, _ptr(lse),
                                p_work, n_work, _stream())
     if rc:
