@@ -72,6 +72,12 @@ __device__ __forceinline__ int place_v(int r) {
   return DP >= 128 ? 4 * (r & 3) : DP == 64 ? 4 * ((r >> 1) & 1) : 0;
 }
 
+// The same for V read by Rows16: by 8 rows of 32 bytes.
+template <int DP>
+__device__ __forceinline__ int place_v16(int r) {
+  return place_v<DP>(r) ^ (2 * ((r >> 2) & 1));
+}
+
 // A wavefront's 32 rows: their queries, and the softmax and output so far.  Rows of LDS have DP
 // elements, a power of two, of which DC (a multiple of 32) are worked on.
 template <typename T, int DP, int DC = DP>
@@ -195,6 +201,117 @@ struct Rows {
         const u32x2 y = read_column(va[i] + (r + 16 * n + 8) * (2 * DP));
         o[i] = Mfma<T>::mul(u32x4{x[0], x[1], y[0], y[1]}, pb, o[i]);
       }
+    }
+  }
+};
+
+// A wavefront's 16 rows, for the 16 x 16 instructions: a row's keys are in four lanes, lane / 16 = 0 .. 3,
+// and half as many of them in each as of 32 rows, whose other half would be worked on for nothing.
+template <typename T>
+struct Mfma16;
+template <>
+struct Mfma16<_Float16> {
+  __device__ static __forceinline__ f32x4 mul(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, a), __builtin_bit_cast(h16x8, b), c, 0, 0, 0);
+  }
+};
+template <>
+struct Mfma16<__bf16> {
+  __device__ static __forceinline__ f32x4 mul(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, a), __builtin_bit_cast(b16x8, b), c, 0, 0, 0);
+  }
+};
+
+__device__ __forceinline__ float max_of_quarters(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return max_of_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+
+template <typename T, int DP, int DC = DP>
+struct Rows16 {
+  u32x4 q[DC / 32];                    // operand columns: row lane % 16, elements 32 i + 8 (lane / 16) ..
+  f32x4 o[DC / 16];                    // element j of o[i]: row lane % 16, output 16 i + 4 (lane / 16) + j
+  float m, l;                          // as in Rows
+  u32 ka[DC / 32], va[DC / 16];        // LDS addresses that this lane reads of a tile of 32 keys
+
+  __device__ __forceinline__ void start(const T* qp, int D, u32 flip) {
+    const int quarter = (threadIdx.x >> 4) & 3;
+#pragma unroll
+    for (int i = 0; i < DC / 32; ++i) {
+      const int c = 32 * i + 8 * quarter;
+      q[i] = u32x4{0, 0, 0, 0};
+      if (c < D) q[i] = *reinterpret_cast<const u32x4*>(qp + c) ^ flip;
+    }
+#pragma unroll
+    for (int i = 0; i < DC / 16; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY;
+    l = 0.f;
+  }
+  __device__ __forceinline__ void addresses(u32 lk, u32 lv) {
+    const int lane = threadIdx.x & 63, row = lane & 15, quarter = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < DC / 32; ++i) ka[i] = lk + row * (2 * DP) + 16 * ((4 * i + quarter) ^ place_k<DP>(row));
+    const int key = 4 * quarter + (row >> 2);
+#pragma unroll
+    for (int i = 0; i < DC / 16; ++i) {
+      const int c = 2 * i + ((row & 3) >> 1);
+      va[i] = lv + key * (2 * DP) + 16 * (c ^ place_v16<DP>(key)) + 8 * (row & 1);
+    }
+  }
+  // Products of 16 keys from row r (0 or 16) of a tile on: element j is key 4 (lane / 16) + j.
+  __device__ __forceinline__ f32x4 scores(int r) const {
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < DC / 32; ++i) s = Mfma16<T>::mul(read_lds16(ka[i] + r * (2 * DP)), q[i], s);
+    return s;
+  }
+  // Scores of 32 keys -> probabilities, as the next product's operand; the rest as in Rows.
+  template <typename F>
+  __device__ __forceinline__ u32x4 softmax(f32x4 (&s)[2], float c, float lift, bool masked, F seen) {
+    const int quarter = (threadIdx.x >> 4) & 3;
+    if (masked) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[n][j] = seen(16 * n + 4 * quarter + j) ? s[n][j] : -INFINITY;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) top = fmaxf(top, s[n][j]);
+    top = max_of_quarters(top);
+    if (__ballot((top - m) * c > 8.0f + kLift<T> || (m == -INFINITY && top > m))) {
+      const float m_new = fmaxf(m, kLift<T> == 0 ? top : top - lift);
+      // (rows that have seen no key yet keep their zeros)
+      const float keep = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - m_new) * c);
+      m = m_new;
+      l *= keep;
+#pragma unroll
+      for (int i = 0; i < DC / 16; ++i) o[i] *= keep;
+    }
+    const float base = m == -INFINITY ? 0.f : -m * c;
+    u32x4 p;
+    float sum = 0.f;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int j = 0; j < 4; j += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[n][j], c, base));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(s[n][j + 1], c, base));
+        sum += p0 + p1;
+        p[2 * n + j / 2] = two_rounded<T>(p0, p1);
+      }
+    l += sum;
+    return p;
+  }
+  // O^T += V^T P^T for the tile's 32 keys: a lane's 8 of an operand are 4 quarter .. + 3 and 16 behind
+  // those, as its probabilities lie.
+  __device__ __forceinline__ void values(u32x4 p) {
+#pragma unroll
+    for (int i = 0; i < DC / 16; ++i) {
+      const u32x2 x = read_column(va[i]), y = read_column(va[i] + 16 * (2 * DP));
+      o[i] = Mfma16<T>::mul(u32x4{x[0], x[1], y[0], y[1]}, p, o[i]);
     }
   }
 };

@@ -138,13 +138,13 @@ struct Spot {
   int rows, key;
 };
 
-// What copies the granules of key head h.
-template <typename A, typename T, int DP>
+// What copies the granules of key head h; V for 32 rows at a time, or for 16.
+template <typename A, typename T, int DP, int PLACE_V(int) = place_v<DP>>
 struct Store {
   int h, shift, keys;
   bool full;                           // D == DP
   GranuleCopy<T, DP, place_k<DP>> ko;
-  GranuleCopy<T, DP, place_v<DP>> vo;
+  GranuleCopy<T, DP, PLACE_V> vo;
   __device__ __forceinline__ Store(const A& a, int h, int shift, int keys)
       : h(h), shift(shift), keys(keys), full(a.D == DP), ko(a.K.token, a.D), vo(a.V.token, a.D) {}
   __device__ __forceinline__ Spot spot(const Granule& g) const {
@@ -187,7 +187,7 @@ struct Target {
   }
 };
 
-constexpr int kTileKeys = 64, kManyRows = 128, kFewRows = 32, kFewKeys = 32;
+constexpr int kTileKeys = 64, kManyRows = 128, kFewRows = 16, kFewKeys = 32;
 template <int DP>
 constexpr int kStages = DP <= 128 ? 2 : 1;
 template <int DP>
@@ -305,10 +305,42 @@ __device__ __forceinline__ void attend_many(Shared<DP>& sh, const Store<A, T, DP
   if (to.lse && half == 0) to.lse[(long long)token * to.Hq + head] = log_sum(w.m, l, c);
 }
 
-// Up to 32 rows: the wavefronts share out the tiles of 32 keys from lo to hi, each copying its own, K of
-// the next while it works on V of this and the other way round; their parts are joined in LDS.
-template <typename A, typename T, int DP, int DC, typename G, typename F>
-__device__ __forceinline__ void attend_few(Shared<DP>& sh, const Store<A, T, DP>& store, G where, const T* qp, int D,
+// 16 rows, for tiles of 32 keys.
+template <typename T, int DP, int DC>
+struct Few16 {
+  static constexpr int kRows = 16;
+  Rows16<T, DP, DC> w;
+  f32x4 s[2];
+  u32x4 p;
+  __device__ __forceinline__ void scores() {
+    s[0] = w.scores(0);
+    s[1] = w.scores(16);
+  }
+  template <typename F>
+  __device__ __forceinline__ void softmax(float c, float lift, bool masked, F seen) {
+    p = w.softmax(s, c, lift, masked, seen);
+  }
+  __device__ __forceinline__ void values() { w.values(p); }
+  __device__ __forceinline__ float sum() const {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(w.l), __float_as_uint(w.l), false, false);
+    const float x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    return x + other_half(x);
+  }
+  // This lane's outputs of its row times `keep`, zeros if there is none.
+  __device__ __forceinline__ void put(float* o, bool none, float keep) const {
+#pragma unroll
+    for (int i = 0; i < DC / 16; ++i) {
+      f32x4 y;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) y[u] = none ? 0.f : w.o[i][u] * keep;
+      *reinterpret_cast<f32x4*>(o + 16 * i + 4 * ((threadIdx.x >> 4) & 3)) = y;
+    }
+  }
+};
+// Up to R::kRows rows: the wavefronts share out the tiles of 32 keys from lo to hi, each copying its own, K
+// of the next while it works on V of this and the other way round; their parts are joined in LDS.
+template <typename R, typename T, int DP, int DC, typename S, typename G, typename F>
+__device__ __forceinline__ void attend_few(Shared<DP>& sh, const S& store, G where, const T* qp, int D,
                                            int sees, int all, int lo, int hi, int rows, bool once, u32 flip, float c,
                                            float lift, F target) {
   constexpr int BYTES = kGranule * 2 * DP, COPIES = 2 * GranuleCopy<T, DP, place_k<DP>>::N;
@@ -340,17 +372,15 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const Store<A, T, DP>
     key[1] = next.s[1].key;
     if (i + 4 < hi) next = look(i + 4);
   }
-  Rows<T, DP, DC> w;
-  w.start(qp, D, flip);
-  w.addresses(lk, lv);
+  R r;
+  r.w.start(qp, D, flip);
+  r.w.addresses(lk, lv);
   if constexpr (G::kInOrder) where.look_over(2 * lo, 2 * hi);
   for (; i < hi; i += 4) {
     const bool more = i + 4 < hi;
     // (copies arrive in order: all but the last COPIES, those of V, are there)
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
-    f32x16 s[1];
-    u32 p[1][8];
-    s[0] = w.scores(0);
+    r.scores();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // K has been read
     if (more) copy_k(next);
     bool masked = key[0] + kGranule > all || key[1] + kGranule > all;
@@ -361,10 +391,10 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const Store<A, T, DP>
         for (int g = 0; g < 2; ++g) key[g] = where.sure ? (2 * i + g) * kGranule : where(2 * i + g).key;
       }
     }
-    w.softmax(s, p, c, lift, masked, [&](int k) { return key[k / kGranule] + k % kGranule < sees; });
+    r.softmax(c, lift, masked, [&](int k) { return key[k / kGranule] + k % kGranule < sees; });
     if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
     else wait_copies();
-    w.values(0, p[0]);
+    r.values();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // V has been read
     if (more) {
       copy_v(next);
@@ -375,36 +405,26 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const Store<A, T, DP>
   }
 
   // join the wavefronts' parts: they refer to different maxima
-  const float l = w.l + other_half(w.l);
-  if (lane < 32) {
-    sh.ml[wave][lane][0] = w.m;
+  constexpr int ROWS = R::kRows;
+  const int mine = lane & (ROWS - 1);
+  const float m_own = r.w.m, l = r.sum();
+  if (lane < ROWS) {
+    sh.ml[wave][lane][0] = m_own;
     sh.ml[wave][lane][1] = l;
   }
   __syncthreads();                                       // (nobody reads K and V any more)
   float m = -INFINITY, sum = 0.f;
 #pragma unroll
-  for (int v = 0; v < 4; ++v) m = fmaxf(m, sh.ml[v][lane & 31][0]);
+  for (int v = 0; v < 4; ++v) m = fmaxf(m, sh.ml[v][mine][0]);
 #pragma unroll
   for (int v = 0; v < 4; ++v) {
-    const float mv = sh.ml[v][lane & 31][0], lv = sh.ml[v][lane & 31][1];
+    const float mv = sh.ml[v][mine][0], lv = sh.ml[v][mine][1];
     if (!no_weight(mv, lv)) sum += lv * __builtin_amdgcn_exp2f((mv - m) * c);
   }
   // (a part in which a row sees no key is 0: its sums may hold 0 * NaN from values that others see)
-  const bool none = no_weight(w.m, l);
-  const float keep = __builtin_amdgcn_exp2f((w.m - m) * c);
-  if ((lane & 31) < rows) {
-#pragma unroll
-    for (int d = 0; d < DC / 32; ++d)
-#pragma unroll
-      for (int j = 0; j < 16; j += 4) {
-        f32x4 y;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) y[u] = none ? 0.f : w.o[d][j + u] * keep;
-        *reinterpret_cast<f32x4*>(&sh.o[wave][lane & 31][32 * d + 2 * j + 4 * (lane >> 5)]) = y;
-      }
-  }
+  if (mine < rows) r.put(sh.o[wave][mine], no_weight(m_own, l), __builtin_amdgcn_exp2f((m_own - m) * c));
   __syncthreads();
-  if (wave == 0 && lane < 32) {                          // for the threads that store a row
+  if (wave == 0 && lane < ROWS) {                        // for the threads that store a row
     sh.ml[0][lane][0] = m;
     sh.ml[0][lane][1] = sum;
   }
@@ -690,8 +710,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   __shared__ long long wave_sum[4];
   __shared__ int wave_tiles[4];
   __shared__ int3 known[256];                            // first token, end and keys of items, if there are no more
-  __shared__ long long found_start;
-  __shared__ int found[3];                               // item, its first tile, tiles of prefixes
+  // Where the walk along the line is: in LDS, as the loops over keys leave no registers for it.
+  __shared__ struct {
+    long long start;                                     // where the item begins
+    long long from, to, total;                           // the piece, and the line
+    int item, tile0, r, pre_tiles;                       // item, its first tile, tile of it; tiles of prefixes
+  } walk;
   const int hk = (int)(blockIdx.x % (unsigned)a.Hk), k = (int)(blockIdx.x / (unsigned)a.Hk);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
@@ -749,14 +773,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
       tiles_next = tiles_before + x.tiles;
     }
     if (before <= from && from < next) {
-      found_start = before;
-      found[0] = v;
-      found[1] = tiles_before;
+      walk.start = before;
+      walk.item = v;
+      walk.tile0 = tiles_before;
+      walk.r = -1;
     }
-    if (v == a.pre.S) found[2] = tiles_before;           // tiles of prefixes
+    if (v == a.pre.S) walk.pre_tiles = tiles_before;
     if (blockIdx.x == 0 && v < a.pre.S) a.first_tile[v + 2] = tiles_before;
     before = next;
     tiles_before = tiles_next;
+  }
+  if (tid == 0) {
+    walk.from = from;
+    walk.to = to;
+    walk.total = total;
   }
   __syncthreads();
 
@@ -765,39 +795,85 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     const int3 x = known[v];
     return item_from(a, v < a.pre.S, x.x, x.y, x.z);
   };
-  int v = __builtin_amdgcn_readfirstlane(found[0]), tile0 = __builtin_amdgcn_readfirstlane(found[1]);
-  long long start = found_start;
-  const int pre_tiles = __builtin_amdgcn_readfirstlane(found[2]);
   if (blockIdx.x == 0 && tid == 0) {
-    a.first_tile[0] = all_tiles - pre_tiles;
-    a.first_tile[1] = pre_tiles;
+    a.first_tile[0] = all_tiles - walk.pre_tiles;
+    a.first_tile[1] = walk.pre_tiles;
   }
-  Item x = item(v);
-  int r = 0;
-  for (int count = x.tiles; count > 1;) {                // the last tile that begins no later than the piece
-    const int half = count / 2;
-    if (start + x.cost(a, r + half) <= from) {
-      r += half;
-      count -= half;
-    } else {
-      count = half;
+  for (bool more = true; more;) {
+    int v = __builtin_amdgcn_readfirstlane(walk.item), r = __builtin_amdgcn_readfirstlane(walk.r);
+    int tile0 = __builtin_amdgcn_readfirstlane(walk.tile0);
+    long long start = walk.start;
+    const long long from = walk.from, to = walk.to, total = walk.total;
+    const int n = pieces_of(a, total);
+    const double each = (double)total / (double)n;
+    const int pre_tiles = __builtin_amdgcn_readfirstlane(walk.pre_tiles);
+    Item x = item(v);
+    if (r < 0) {                                         // the last tile that begins no later than the piece
+      r = 0;
+      for (int count = x.tiles; count > 1;) {
+        const int half = count / 2;
+        if (start + x.cost(a, r + half) <= from) {
+          r += half;
+          count -= half;
+        } else {
+          count = half;
+        }
+      }
+      r = __builtin_amdgcn_readfirstlane(r);
     }
-  }
-  r = __builtin_amdgcn_readfirstlane(r);
-  for (;;) {
     const Stretch s = stretch_of(a, x, start, r);
     if (s.begin >= to) break;
     const int lo = __builtin_amdgcn_readfirstlane(s.at(from)), hi = __builtin_amdgcn_readfirstlane(s.at(to));
     const unsigned r0 = (unsigned)r * kManyRows;
     const int rows = __builtin_amdgcn_readfirstlane((int)(x.rows - r0 < kManyRows ? x.rows - r0 : kManyRows));
+    const bool prefix = v < a.pre.S;
+    const int line = prefix ? v : v - a.pre.S;
+    const int token0 = __builtin_amdgcn_readfirstlane((int)(((double)r0 + 0.5) * a.per_group));
+    const int first = __builtin_amdgcn_readfirstlane((int)(r0 - (unsigned)token0 * (unsigned)a.group));
+    const int t0 = __builtin_amdgcn_readfirstlane(x.t0) + token0;
+    const int keys = __builtin_amdgcn_readfirstlane(x.keys), tiles = __builtin_amdgcn_readfirstlane(s.tiles);
+    const int ahead = __builtin_amdgcn_readfirstlane(x.ahead) + token0 + 1;   // of row r of the tile: + (first + r) / group
+    // for the second kernel
+    if (lo == 0 && lo < hi) {
+      const long long tile = prefix ? a.own_tiles + tile0 + r : tile0 - pre_tiles + r;
+      if (tid == 0 && tile < (prefix ? a.own_tiles + a.pre_tiles : a.own_tiles)) {
+        // the last piece that the tile lies in: of those that begin in front of its end
+        int last = (int)((double)(s.end - 1) / each);
+        last = last < k ? k : last < n ? last : n - 1;
+        while (last > k && piece_at(total, each, last, n) >= s.end) --last;
+        while (last + 1 < n && piece_at(total, each, last + 1, n) < s.end) ++last;
+        a.tiles[tile * a.Hk + hk] = TileParts{k, last - k + 1, line, 0};
+      }
+      if (hk == 0 && !prefix) {
+        // tokens whose first row lies in the tile
+        const int row = tid * a.group - first;
+        if (row >= 0 && row < rows) a.place[t0 + tid] = make_int2(tile0 - pre_tiles + r, row);
+      }
+    }
+    if (lo >= hi && lo > 0 && lo < tiles && tid < rows) {
+      // (no keys of the tile for this piece, though some for those before and behind)
+      const long long slot = 2 * ((long long)k * a.Hk + hk);
+      *reinterpret_cast<f32x2*>(a.part_ml + (slot * a.cap + tid) * 2) = f32x2{-INFINITY, 0.f};
+    }
+    // the next tile
+    more = s.end < to;
+    if (++r >= x.tiles) {
+      start += x.cost(a, x.tiles);
+      tile0 += x.tiles;
+      r = 0;
+      while (more && ++v < items && item(v).tiles == 0) {
+      }
+      more = more && v < items;
+    }
+    __syncthreads();                                     // (this tile has been read)
+    if (tid == 0) {
+      walk.start = start;
+      walk.item = v;
+      walk.tile0 = tile0;
+      walk.r = r;
+    }
+    more = __builtin_amdgcn_readfirstlane((int)more) != 0;
     if (lo < hi) {
-      const bool prefix = v < a.pre.S;
-      const int line = prefix ? v : v - a.pre.S;
-      const int token0 = __builtin_amdgcn_readfirstlane((int)(((double)r0 + 0.5) * a.per_group));
-      const int first = __builtin_amdgcn_readfirstlane((int)(r0 - (unsigned)token0 * (unsigned)a.group));
-      const int t0 = __builtin_amdgcn_readfirstlane(x.t0) + token0;
-      const int keys = __builtin_amdgcn_readfirstlane(x.keys);
-      const int ahead = __builtin_amdgcn_readfirstlane(x.ahead) + token0 + 1;   // of row r of the tile: + (first + r) / group
       const float per_group = (float)a.per_group;
       auto sees = [&](int row) {
         const int e = quotient(first + row, per_group) + ahead;
@@ -805,8 +881,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
       };
       const Line where = {prefix ? a.pre.table + line * a.pre.ld : a.own.table + line * a.own.ld, a.own.shift, a.own.n_pages,
                           keys, true};
-      const Store<PagedArgs, T, DP> store(a, hk, a.own.shift, keys);
-      const int tiles = s.tiles;
       auto target = [&]() {
         const auto b = arguments<PagedArgs>();
         Target<T> to;
@@ -832,9 +906,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
         return to;
       };
       if (a.D < DC) clear<DP>(sh);
-      else __syncthreads();
       const bool few = rows <= kFewRows;
-      const int mine_row = few ? lane & 31 : wave * 32 + (lane & 31);
+      const int mine_row = few ? lane & 15 : wave * 32 + (lane & 31);
       const int row = mine_row < rows ? mine_row : rows - 1;
       const int token = quotient(first + row, per_group), head = first + row - token * a.group;
       const T* qp = static_cast<const T*>(a.Q) + (long long)(t0 + token) * a.q_token +
@@ -843,47 +916,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
       if (few) {
         const int all = __builtin_amdgcn_readfirstlane(sees(0));
         const int tiles = (end + kFewKeys - 1) / kFewKeys, stop = 2 * hi < tiles ? 2 * hi : tiles;
-        attend_few<PagedArgs, T, DP, DC>(sh, store, where, qp, a.D, sees(row), all, 2 * lo, stop, rows, true, a.flip,
-                                         a.scale_log2, a.lift, target);
+        const Store<PagedArgs, T, DP, place_v16<DP>> store(a, hk, a.own.shift, keys);
+        attend_few<Few16<T, DP, DC>, T, DP, DC>(sh, store, where, qp, a.D, sees(row), all, 2 * lo, stop, rows, true,
+                                                a.flip, a.scale_log2, a.lift, target);
       } else {
         const int from_row = wave * 32 < rows ? wave * 32 : rows - 1;
         const int last_row = wave * 32 + 31 < rows ? wave * 32 + 31 : rows - 1;
         const int last = wave * 32 < rows ? __builtin_amdgcn_readfirstlane(sees(last_row)) : 0;
         const int all = __builtin_amdgcn_readfirstlane(sees(from_row));
         const int tiles = (end + kTileKeys - 1) / kTileKeys, stop = hi < tiles ? hi : tiles;
+        const Store<PagedArgs, T, DP> store(a, hk, a.own.shift, keys);
         attend_many<PagedArgs, T, DP, DC>(sh, store, where, qp, a.D, sees(row), all, last, lo, stop, rows, a.flip,
                                           a.scale_log2, a.lift, target);
       }
-      // (for the second kernel)
-      const long long tile = prefix ? a.own_tiles + tile0 + r : tile0 - pre_tiles + r;
-      if (lo == 0 && tid == 0 && tile < (prefix ? a.own_tiles + a.pre_tiles : a.own_tiles)) {
-        // the last piece that the tile lies in: of those that begin in front of its end
-        int last = (int)((double)(s.end - 1) / each);
-        last = last < k ? k : last < n ? last : n - 1;
-        while (last > k && piece_at(total, each, last, n) >= s.end) --last;
-        while (last + 1 < n && piece_at(total, each, last + 1, n) < s.end) ++last;
-        a.tiles[tile * a.Hk + hk] = TileParts{k, last - k + 1, line, 0};
-      }
-      if (lo == 0 && hk == 0 && !prefix) {
-        // tokens whose first row lies in the tile
-        const int row = tid * a.group - first;
-        if (row >= 0 && row < rows) a.place[t0 + tid] = make_int2(tile0 - pre_tiles + r, row);
-      }
-    } else if (lo > 0 && lo < s.tiles && tid < rows) {
-      // (no keys of the tile for this piece, though some for those before and behind)
-      const long long slot = 2 * ((long long)k * a.Hk + hk);
-      *reinterpret_cast<f32x2*>(a.part_ml + (slot * a.cap + tid) * 2) = f32x2{-INFINITY, 0.f};
     }
-    if (s.end >= to) break;
-    if (++r >= x.tiles) {
-      start += x.cost(a, x.tiles);
-      tile0 += x.tiles;
-      r = 0;
-      do {
-        if (++v >= items) return;
-        x = item(v);
-      } while (x.tiles == 0);
-    }
+    if (more) __syncthreads();                           // (LDS is free, and the walk there)
   }
 }
 
@@ -1091,7 +1138,7 @@ struct ChosenArgs {
   int Hq, Hk, group, D, causal, count;
   float scale_log2, lift;
   u32 flip;
-  int splits, tiles;                   // tiles of 32 rows of a group
+  int splits, tiles;                   // tiles of 16 rows of a group
   float *part_o, *part_ml;             // [Tq Hq][splits]
 };
 
@@ -1111,18 +1158,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   if (t < from || t >= to) return;
   const long long e = a.causal ? keys - to + t + 1 : keys;
   const int sees = __builtin_amdgcn_readfirstlane(e < 0 ? 0 : (int)e);
-  const int rows = a.group - tile * kFewRows < kFewRows ? a.group - tile * kFewRows : kFewRows;
-  const int lane = threadIdx.x & 63, row = (lane & 31) < rows ? lane & 31 : rows - 1;
+  const int left = a.group - tile * kFewRows, rows = left < kFewRows ? left : kFewRows;
+  const int lane = threadIdx.x & 63, row = (lane & 15) < rows ? lane & 15 : rows - 1;
   const int h0 = hk * a.group + tile * kFewRows;
   const int* list = a.chosen + (t * a.Hk + hk) * a.count;
-  const Store<ChosenArgs, T, DP> store(a, hk, q.shift, keys);
+  const Store<ChosenArgs, T, DP, place_v16<DP>> store(a, hk, q.shift, keys);
   Target<T> target;
   target.O = static_cast<T*>(a.O) + t * a.o_token + h0 * a.o_head;
   target.lse = a.lse ? a.lse + t * a.Hq + h0 : nullptr;
   target.o_token = a.o_token;
   target.o_head = a.o_head;
   target.Hq = a.Hq;
-  target.group = kFewRows;                               // (all rows are heads of one token)
+  target.group = kFewRows;                            // (all rows are heads of one token)
   target.first = 0;
   target.D = a.D;
   target.po = target.pml = nullptr;
@@ -1143,9 +1190,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   Chosen where = {list, q.table + s * q.ld, used, q.shift, q.n_pages, keys, 0, -1, kNowhere};
   if (lo < hi) where.hold((2 * lo) >> (q.shift - kGranuleBits) & ~63);
   if (a.D < DC) clear<DP>(sh);
-  attend_few<ChosenArgs, T, DP, DC>(sh, store, where,
-                                    static_cast<const T*>(a.Q) + t * a.q_token + (h0 + row) * a.q_head, a.D, sees, sees,
-                                    lo, hi, rows, to - from == 1, a.flip, a.scale_log2, a.lift, [&] { return target; });
+  attend_few<Few16<T, DP, DC>, T, DP, DC>(sh, store, where,
+                                          static_cast<const T*>(a.Q) + t * a.q_token + (h0 + row) * a.q_head, a.D, sees,
+                                          sees, lo, hi, rows, to - from == 1, a.flip, a.scale_log2, a.lift,
+                                          [&] { return target; });
 }
 
 template <typename T>
