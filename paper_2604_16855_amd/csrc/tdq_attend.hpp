@@ -92,8 +92,7 @@ struct Rows {
 #pragma unroll
     for (int i = 0; i < DC / 16; ++i) {
       const int c = 16 * i + 8 * half;
-      q[i] = u32x4{0, 0, 0, 0};
-      if (c < D) q[i] = *reinterpret_cast<const u32x4*>(qp + c) ^ flip;
+      q[i] = *(c < D ? reinterpret_cast<const u32x4*>(qp + c) : reinterpret_cast<const u32x4*>(kZeros)) ^ flip;
     }
 #pragma unroll
     for (int i = 0; i < DC / 32; ++i)
@@ -239,8 +238,7 @@ struct Rows16 {
 #pragma unroll
     for (int i = 0; i < DC / 32; ++i) {
       const int c = 32 * i + 8 * quarter;
-      q[i] = u32x4{0, 0, 0, 0};
-      if (c < D) q[i] = *reinterpret_cast<const u32x4*>(qp + c) ^ flip;
+      q[i] = *(c < D ? reinterpret_cast<const u32x4*>(qp + c) : reinterpret_cast<const u32x4*>(kZeros)) ^ flip;
     }
 #pragma unroll
     for (int i = 0; i < DC / 16; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};

@@ -71,15 +71,14 @@ struct GranuleCopy {
   }
 };
 
-// The granules of a sequence, in order.
+// The granules of a sequence, in order.  (Any i, as long as there is a key.)
 struct Line {
-  static constexpr bool kInOrder = true;               // granule i is keys 16 i .. 16 i + 15
   const int* table;                    // the sequence's pages
   int shift, n_pages, keys;
   bool sure;                           // all pages of interest are there
-  __device__ __forceinline__ Granule operator()(int i) const {   // (any i, as long as there is a key)
+  __device__ __forceinline__ Granule operator()(int i) const {
     const int last = (keys - 1) >> kGranuleBits, at = i < last ? i : last;
-    const int page = load_scalar(table + (at >> (shift - kGranuleBits)));
+    const int page = table[at >> (shift - kGranuleBits)];
     const bool there = i <= last && page >= 0 && page < n_pages;
     return {there ? page : -1, there ? i << kGranuleBits : kNowhere};
   }
@@ -95,28 +94,16 @@ struct Line {
   }
 };
 
-// The granules of a list of pages of a sequence.  A lane holds a page of 64 of the list at a time.
+// The granules of a list of pages of a sequence.
 struct Chosen {
-  static constexpr bool kInOrder = false;
   const int *list, *table;
   int count, shift, n_pages, keys;
-  int base;                            // the 64 places of the list that the lanes hold
-  int page, key;                       // of place base + lane: page (negative: not there), its first key
-
-  __device__ __forceinline__ void hold(int from) {
-    base = from;
-    const int i = from + (threadIdx.x & 63), last = (keys - 1) >> shift;
-    const int b = i < count ? list[i] : -1;
-    page = table[b < 0 ? 0 : b < last ? b : last];
+  __device__ __forceinline__ Granule operator()(int i) const {
+    const int n = i >> (shift - kGranuleBits), last = (keys - 1) >> shift;
+    const int b = n < count ? list[n] : -1;
+    const int page = table[b < 0 ? 0 : b < last ? b : last];
     const bool there = b >= 0 && b <= last && page >= 0 && page < n_pages;
-    page = there ? page : -1;
-    key = there ? b << shift : kNowhere;
-  }
-  __device__ __forceinline__ Granule operator()(int i) {
-    const int n = i >> (shift - kGranuleBits);
-    if ((n & ~63) != base) hold(n & ~63);
-    const int page_of = __builtin_amdgcn_readlane(page, n & 63), first = __builtin_amdgcn_readlane(key, n & 63);
-    return {page_of, page_of < 0 ? kNowhere : first + ((i << kGranuleBits) & ((1 << shift) - 1))};
+    return {there ? page : -1, there ? (b << shift) + ((i << kGranuleBits) & ((1 << shift) - 1)) : kNowhere};
   }
 };
 
@@ -137,6 +124,17 @@ struct Spot {
   const void *k, *v;
   int rows, key;
 };
+struct __attribute__((aligned(16))) Place {
+  size_t k, v;                         // 0: not there
+};
+
+__device__ __forceinline__ size_t read_lane(size_t v, int lane) {
+  const u32 lo = __builtin_amdgcn_readlane((u32)v, lane), hi = __builtin_amdgcn_readlane((u32)(v >> 32), lane);
+  return (size_t)hi << 32 | lo;
+}
+__device__ __forceinline__ Place read_lane(const Place& p, int lane) {
+  return {read_lane(p.k, lane), read_lane(p.v, lane)};
+}
 
 // What copies the granules of key head h; V for 32 rows at a time, or for 16.
 template <typename A, typename T, int DP, int PLACE_V(int) = place_v<DP>>
@@ -147,16 +145,28 @@ struct Store {
   GranuleCopy<T, DP, PLACE_V> vo;
   __device__ __forceinline__ Store(const A& a, int h, int shift, int keys)
       : h(h), shift(shift), keys(keys), full(a.D == DP), ko(a.K.token, a.D), vo(a.V.token, a.D) {}
-  __device__ __forceinline__ Spot spot(const Granule& g) const {
+  // May differ from lane to lane.
+  __device__ __forceinline__ Place place(const Granule& g) const {
     const auto a = arguments<A>();
-    const long long page = g.page < 0 ? 0 : g.page, row = g.key & ((1 << shift) - 1);
+    const long long page = g.page, row = g.key & ((1 << shift) - 1);
+    Place p;
+    p.k = (size_t)(static_cast<const T*>(a->K.data) + page * a->K.page + row * a->K.token + h * a->K.head);
+    p.v = (size_t)(static_cast<const T*>(a->V.data) + page * a->V.page + row * a->V.token + h * a->V.head);
+    p.k = g.page < 0 ? 0 : p.k;
+    p.v = g.page < 0 ? 0 : p.v;
+    return p;
+  }
+  __device__ __forceinline__ bool quick() const {        // offsets of a granule's rows fit 32 bits
+    const auto a = arguments<A>();
+    return (unsigned long long)a->K.token < 1 << 24 && (unsigned long long)a->V.token < 1 << 24;
+  }
+  __device__ __forceinline__ Spot spot(const Place& p, int key, bool quick) const {
     Spot s;
-    s.k = static_cast<const T*>(a->K.data) + page * a->K.page + row * a->K.token + h * a->K.head;
-    s.v = static_cast<const T*>(a->V.data) + page * a->V.page + row * a->V.token + h * a->V.head;
-    const bool quick = (unsigned long long)a->K.token < 1 << 24 && (unsigned long long)a->V.token < 1 << 24;
-    const int left = keys - g.key;                       // (nothing of one that is not there)
+    s.k = (const void*)p.k;
+    s.v = (const void*)p.v;
+    const int left = s.k ? keys - key : 0;
     s.rows = left >= kGranule && quick ? kWhole : left;
-    s.key = g.key;
+    s.key = key;
     return s;
   }
   __device__ __forceinline__ void copy_k(const Spot& s, u32 lds, bool once) const {
@@ -195,9 +205,10 @@ struct Shared {
   union {
     uint8_t many[kStages<DP>][2][kTileKeys * 2 * DP];  // [stage][K, V]
     uint8_t few[4][2][kFewKeys * 2 * DP];              // [wavefront][K, V]
-    float o[4][32][DP + 4];                            // parts of the output, rows 16 bytes apart in the banks
+    float o[4][kFewRows][DP + 4];                      // parts of the output, rows 16 bytes apart in the banks
   };
-  float ml[4][32][2];
+  float ml[4][kFewRows][2];
+  Place place[4][64];                                  // [wavefront][tile] (many)
 };
 
 // Zeros where a whole granule's copies leave LDS alone and products of K read it.
@@ -218,13 +229,29 @@ __device__ __forceinline__ void attend_many(Shared<DP>& sh, const Store<A, T, DP
   constexpr int BYTES = kGranule * 2 * DP;             // of a granule in LDS
   constexpr int STAGES = kStages<DP>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-  auto look = [&](int i) { return store.spot(where(4 * i + wave)); };
+  const bool quick = store.quick();
+  // The places of the wave's granules of 64 tiles, in LDS: a look at the table in every step is three
+  // scalar loads in a row, which the matrix instructions behind them wait for (7 % of four times 1024 tokens
+  // over 8192 keys).
+  Place* const places = sh.place[wave];
+  int base = 0;
+  auto hold = [&](int i) {
+    base = i;
+    places[lane] = store.place(where(4 * (i + lane) + wave));
+  };
+  auto look = [&](int i) {
+    if (i - base == 64) hold(i);
+    return store.spot(read_lane(places[i - base], 0), (4 * i + wave) * kGranule, quick);
+  };
   auto copy = [&](const Spot& s, int stage) {
     store.copy_k(s, lds_address(sh.many[stage][0]) + wave * BYTES, false);
     store.copy_v(s, lds_address(sh.many[stage][1]) + wave * BYTES, false);
   };
   Spot next = {nullptr, nullptr, 0, 0};
-  if (lo < hi) next = look(lo);
+  if (lo < hi) {
+    hold(lo);
+    next = look(lo);
+  }
   if (STAGES == 2 && lo < hi) {
     copy(next, 0);
     if (lo + 1 < hi) next = look(lo + 1);
@@ -349,9 +376,21 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const S& store, G whe
   struct Two {
     Spot s[2];
   };
+  // (as above; lanes hold the places of the granules of 32 tiles)
+  const bool quick = store.quick();
+  Place held = {};
+  int held_key = 0, base = 0;
+  auto hold = [&](int i) {
+    base = i;
+    const Granule g = where(2 * (i + 4 * (lane >> 1)) + (lane & 1));
+    held = store.place(g);
+    held_key = g.key;
+  };
   auto look = [&](int i) {
-    const Granule a = where(2 * i), b = where(2 * i + 1);
-    return Two{{store.spot(a), store.spot(b)}};
+    if (i - base == 4 * 32) hold(i);
+    const int from = (i - base) >> 1;
+    return Two{{store.spot(read_lane(held, from), __builtin_amdgcn_readlane(held_key, from), quick),
+                store.spot(read_lane(held, from + 1), __builtin_amdgcn_readlane(held_key, from + 1), quick)}};
   };
   auto copy_k = [&](const Two& t) {
     store.copy_k(t.s[0], lk, once);
@@ -365,6 +404,7 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const S& store, G whe
   Two next = {};
   int key[2] = {0, 0};
   if (i < hi) {
+    hold(i);
     next = look(i);
     copy_k(next);
     copy_v(next);
@@ -375,7 +415,6 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const S& store, G whe
   R r;
   r.w.start(qp, D, flip);
   r.w.addresses(lk, lv);
-  if constexpr (G::kInOrder) where.look_over(2 * lo, 2 * hi);
   for (; i < hi; i += 4) {
     const bool more = i + 4 < hi;
     // (copies arrive in order: all but the last COPIES, those of V, are there)
@@ -383,14 +422,7 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const S& store, G whe
     r.scores();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // K has been read
     if (more) copy_k(next);
-    bool masked = key[0] + kGranule > all || key[1] + kGranule > all;
-    if constexpr (G::kInOrder) {
-      masked = !where.sure || (i + 1) * kFewKeys > all;
-      if (masked) {
-#pragma unroll
-        for (int g = 0; g < 2; ++g) key[g] = where.sure ? (2 * i + g) * kGranule : where(2 * i + g).key;
-      }
-    }
+    const bool masked = key[0] + kGranule > all || key[1] + kGranule > all;
     r.softmax(c, lift, masked, [&](int k) { return key[k / kGranule] + k % kGranule < sees; });
     if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
     else wait_copies();
@@ -464,7 +496,8 @@ struct Run {
 // Joins the parts of two runs for a row, by a wavefront.  A group of lanes has four outputs each of one
 // part, as many parts at a time as there are groups, the first ones on their way with the sums; weights are
 // found before, a lane a part.
-constexpr int kMaxParts = 512 + 4;
+constexpr int kMaxPieces = 512;        // of a line
+constexpr int kMaxParts = kMaxPieces + 4;
 template <typename T>
 __device__ __forceinline__ void join_row(float* weight, const Run& a, const Run& b, int D, float scale_log2, T* op,
                                          float* lse) {
@@ -698,10 +731,9 @@ __device__ __forceinline__ int pieces_of(const PagedArgs& a, long long total) {
   const long long n = total / kLeastPiece;
   return n < 1 ? 1 : n < a.pieces ? (int)n : a.pieces;
 }
-// Where piece k of n begins, `each` the length of one.
-__device__ __forceinline__ long long piece_at(long long total, double each, int k, int n) {
-  return k < n ? (long long)(each * k) : total;
-}
+// The tile of all that workgroup k of n takes in a round of whole tiles.
+__device__ __forceinline__ int tile_of_round(int round, int k, int n) { return round * n + (round & 1 ? n - 1 - k : k); }
+constexpr int kSpare = 5;              // whole tiles are no more than 1 + 1 / kSpare of a workgroup's share of the line
 
 template <typename T, int DP, int DC>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 2 : 1))) void k_attend_pages(
@@ -709,12 +741,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   __shared__ __attribute__((aligned(1024))) Shared<DP> sh;
   __shared__ long long wave_sum[4];
   __shared__ int wave_tiles[4];
-  __shared__ int3 known[256];                            // first token, end and keys of items, if there are no more
+  // Of items, if there are no more: first token, end and keys, where on the line, their first tile.
+  __shared__ int3 known[256];
+  __shared__ long long known_start[256];
+  __shared__ int known_tile[256];
+  __shared__ long long bounds[kMaxPieces + 1];           // where the pieces begin, and the last ends
+  __shared__ long long wave_most[4], wave_slack[4];
   // Where the walk along the line is: in LDS, as the loops over keys leave no registers for it.
   __shared__ struct {
     long long start;                                     // where the item begins
-    long long from, to, total;                           // the piece, and the line
     int item, tile0, r, pre_tiles;                       // item, its first tile, tile of it; tiles of prefixes
+    int n, rounds, round;                                // pieces; rounds of whole tiles, and how many are done
   } walk;
   const int hk = (int)(blockIdx.x % (unsigned)a.Hk), k = (int)(blockIdx.x / (unsigned)a.Hk);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -762,8 +799,104 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     if (blockIdx.x == 0 && tid == 0) a.first_tile[0] = 0;
     return;
   }
-  const double each = (double)total / (double)n;
-  const long long from = piece_at(total, each, k, n), to = piece_at(total, each, k + 1, n);
+  auto item = [&](int v) {
+    if (share > 1) return item_of(a, v);
+    const int3 x = known[v];
+    return item_from(a, v < a.pre.S, x.x, x.y, x.z);
+  };
+  if (share == 1 && tid < items) {
+    known_start[tid] = before;
+    known_tile[tid] = tiles_before;
+  }
+  // The item of a tile (of all): the last that begins no later and has one.
+  auto item_of_tile = [&](int j) {
+    int v = 0;
+    for (int count = items; count > 1;) {
+      const int half = count / 2;
+      if (known_tile[v + half] <= j) {
+        v += half;
+        count -= half;
+      } else {
+        count = half;
+      }
+    }
+    return v;
+  };
+  // Whole tiles first, as long as they leave no workgroup with much more than its share: in round i
+  // workgroup k takes tile i n + k, or in odd ones from the other end.
+  const long long each = total / n;
+  int rounds = 0;
+  long long load[2] = {0, 0};                            // of pieces 2 tid and 2 tid + 1
+  if (share == 1) {
+    __syncthreads();
+    for (int i = 0; (long long)(i + 1) * n <= all_tiles; ++i) {
+      long long with[2], top = 0;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int p = 2 * tid + u;
+        with[u] = load[u];
+        if (p < n) {
+          const int j = tile_of_round(i, p, n), w = item_of_tile(j), r = j - known_tile[w];
+          const Item x = item(w);
+          with[u] += x.cost(a, r + 1) - x.cost(a, r);
+        }
+        top = with[u] > top ? with[u] : top;
+      }
+#pragma unroll
+      for (int d = 32; d >= 1; d >>= 1) {
+        const long long o = __shfl_xor(top, d, 64);
+        top = o > top ? o : top;
+      }
+      if (lane == 0) wave_most[wave] = top;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < 4; ++w) top = wave_most[w] > top ? wave_most[w] : top;
+      __syncthreads();
+      if (top > each + each / kSpare) break;
+      rounds = i + 1;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) load[u] = with[u];
+    }
+  }
+  // The rest of the line is cut into pieces as long as what a workgroup's share is more than it has.
+  long long rest = 0;                                    // where it begins
+  if (rounds > 0) {
+    rest = total;
+    if (rounds * n < all_tiles) {
+      const int v = item_of_tile(rounds * n);
+      rest = known_start[v] + item(v).cost(a, rounds * n - known_tile[v]);
+    }
+  }
+  long long slack[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) slack[u] = 2 * tid + u < n && load[u] < each ? each - load[u] : 0;
+  long long sum = slack[0] + slack[1];
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const long long o = __shfl_up(sum, d, 64);
+    if (lane >= d) sum += o;
+  }
+  if (lane == 63) wave_slack[wave] = sum;
+  __syncthreads();
+  long long all_slack = 0;
+  sum -= slack[0] + slack[1];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) sum += wave_slack[w];
+    all_slack += wave_slack[w];
+  }
+  // (whole numbers times the same factor: the bounds ascend; where there is no slack, the last has it all)
+  const double stretch = all_slack > 0 ? (double)(total - rest) / (double)all_slack : 0.0;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const long long at = rest + (long long)((double)sum * stretch);
+    if (2 * tid + u < n) bounds[2 * tid + u] = at < total ? at : total;
+    sum += slack[u];
+  }
+  if (tid == 0) bounds[n] = total;
+  __syncthreads();
+
+  const long long from = bounds[k];
   for (int v = v0; v < v1; ++v) {
     long long next = before + mine;
     int tiles_next = tiles_before + mine_tiles;
@@ -784,29 +917,33 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     tiles_before = tiles_next;
   }
   if (tid == 0) {
-    walk.from = from;
-    walk.to = to;
-    walk.total = total;
+    walk.n = n;
+    walk.rounds = rounds;
+    walk.round = 0;
   }
   __syncthreads();
 
-  auto item = [&](int v) {
-    if (share > 1) return item_of(a, v);
-    const int3 x = known[v];
-    return item_from(a, v < a.pre.S, x.x, x.y, x.z);
-  };
   if (blockIdx.x == 0 && tid == 0) {
     a.first_tile[0] = all_tiles - walk.pre_tiles;
     a.first_tile[1] = walk.pre_tiles;
   }
+  // (a piece of no length may lie within a tile: then it says so)
+  if (rounds == 0 && from >= total) return;
   for (bool more = true; more;) {
     int v = __builtin_amdgcn_readfirstlane(walk.item), r = __builtin_amdgcn_readfirstlane(walk.r);
     int tile0 = __builtin_amdgcn_readfirstlane(walk.tile0);
     long long start = walk.start;
-    const long long from = walk.from, to = walk.to, total = walk.total;
-    const int n = pieces_of(a, total);
-    const double each = (double)total / (double)n;
+    const long long from = bounds[k], to = bounds[k + 1];
+    const int n = __builtin_amdgcn_readfirstlane(walk.n), round = __builtin_amdgcn_readfirstlane(walk.round);
     const int pre_tiles = __builtin_amdgcn_readfirstlane(walk.pre_tiles);
+    const bool whole = round < __builtin_amdgcn_readfirstlane(walk.rounds);
+    if (whole) {
+      const int j = tile_of_round(round, k, n);
+      v = __builtin_amdgcn_readfirstlane(item_of_tile(j));
+      tile0 = __builtin_amdgcn_readfirstlane(known_tile[v]);
+      start = known_start[v];
+      r = j - tile0;
+    }
     Item x = item(v);
     if (r < 0) {                                         // the last tile that begins no later than the piece
       r = 0;
@@ -822,8 +959,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
       r = __builtin_amdgcn_readfirstlane(r);
     }
     const Stretch s = stretch_of(a, x, start, r);
-    if (s.begin >= to) break;
-    const int lo = __builtin_amdgcn_readfirstlane(s.at(from)), hi = __builtin_amdgcn_readfirstlane(s.at(to));
+    if (!whole && s.begin >= to) break;                  // (from here on the next piece's)
+    const int lo = whole ? 0 : __builtin_amdgcn_readfirstlane(s.at(from));
+    const int hi = __builtin_amdgcn_readfirstlane(whole ? s.tiles : s.at(to));
     const unsigned r0 = (unsigned)r * kManyRows;
     const int rows = __builtin_amdgcn_readfirstlane((int)(x.rows - r0 < kManyRows ? x.rows - r0 : kManyRows));
     const bool prefix = v < a.pre.S;
@@ -837,11 +975,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     if (lo == 0 && lo < hi) {
       const long long tile = prefix ? a.own_tiles + tile0 + r : tile0 - pre_tiles + r;
       if (tid == 0 && tile < (prefix ? a.own_tiles + a.pre_tiles : a.own_tiles)) {
-        // the last piece that the tile lies in: of those that begin in front of its end
-        int last = (int)((double)(s.end - 1) / each);
-        last = last < k ? k : last < n ? last : n - 1;
-        while (last > k && piece_at(total, each, last, n) >= s.end) --last;
-        while (last + 1 < n && piece_at(total, each, last + 1, n) < s.end) ++last;
+        // the last piece that the tile lies in: of those that begin in front of its end, and have some of it
+        int last = k;
+        if (!whole) {
+          int beyond = n;
+          while (beyond - last > 1) {
+            const int half = (last + beyond) / 2;
+            if (bounds[half] < s.end) last = half;
+            else beyond = half;
+          }
+        }
         a.tiles[tile * a.Hk + hk] = TileParts{k, last - k + 1, line, 0};
       }
       if (hk == 0 && !prefix) {
@@ -856,21 +999,29 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
       *reinterpret_cast<f32x2*>(a.part_ml + (slot * a.cap + tid) * 2) = f32x2{-INFINITY, 0.f};
     }
     // the next tile
-    more = s.end < to;
-    if (++r >= x.tiles) {
-      start += x.cost(a, x.tiles);
-      tile0 += x.tiles;
-      r = 0;
-      while (more && ++v < items && item(v).tiles == 0) {
+    if (whole) {
+      more = round + 1 < __builtin_amdgcn_readfirstlane(walk.rounds) || from < bounds[n];
+    } else {
+      more = s.end < to;
+      if (++r >= x.tiles) {
+        start += x.cost(a, x.tiles);
+        tile0 += x.tiles;
+        r = 0;
+        while (more && ++v < items && item(v).tiles == 0) {
+        }
+        more = more && v < items;
       }
-      more = more && v < items;
     }
     __syncthreads();                                     // (this tile has been read)
     if (tid == 0) {
-      walk.start = start;
-      walk.item = v;
-      walk.tile0 = tile0;
-      walk.r = r;
+      if (whole) {
+        walk.round = round + 1;
+      } else {
+        walk.start = start;
+        walk.item = v;
+        walk.tile0 = tile0;
+        walk.r = r;
+      }
     }
     more = __builtin_amdgcn_readfirstlane((int)more) != 0;
     if (lo < hi) {
@@ -1187,8 +1338,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   const int tiles = sees > 0 ? (int)((((long long)used << q.shift) + kFewKeys - 1) / kFewKeys) : 0;
   const int share = (tiles + a.splits - 1) / a.splits;
   const int lo = split * share < tiles ? split * share : tiles, hi = lo + share < tiles ? lo + share : tiles;
-  Chosen where = {list, q.table + s * q.ld, used, q.shift, q.n_pages, keys, 0, -1, kNowhere};
-  if (lo < hi) where.hold((2 * lo) >> (q.shift - kGranuleBits) & ~63);
+  Chosen where = {list, q.table + s * q.ld, used, q.shift, q.n_pages, keys};
   if (a.D < DC) clear<DP>(sh);
   attend_few<Few16<T, DP, DC>, T, DP, DC>(sh, store, where,
                                           static_cast<const T*>(a.Q) + t * a.q_token + (h0 + row) * a.q_head, a.D, sees,
