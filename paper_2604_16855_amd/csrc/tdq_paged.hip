@@ -824,7 +824,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   };
   // Whole tiles first, as long as they leave no workgroup with much more than its share: in round i
   // workgroup k takes tile i n + k, or in odd ones from the other end.
-  const long long each = total / n;
+  const double per = (double)total / n;
+  const long long each = (long long)per;
   int rounds = 0;
   long long load[2] = {0, 0};                            // of pieces 2 tid and 2 tid + 1
   if (share == 1) {
@@ -858,40 +859,45 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
       for (int u = 0; u < 2; ++u) load[u] = with[u];
     }
   }
-  // The rest of the line is cut into pieces as long as what a workgroup's share is more than it has.
-  long long rest = 0;                                    // where it begins
-  if (rounds > 0) {
-    rest = total;
+  if (rounds == 0) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const long long at = (long long)((double)(2 * tid + u) * per);
+      if (2 * tid + u < n) bounds[2 * tid + u] = at < total ? at : total;
+    }
+  } else {
+    // The rest of the line is cut into pieces as long as what a workgroup's share is more than it has.
+    long long rest = total;                              // where it begins
     if (rounds * n < all_tiles) {
       const int v = item_of_tile(rounds * n);
       rest = known_start[v] + item(v).cost(a, rounds * n - known_tile[v]);
     }
-  }
-  long long slack[2];
+    long long slack[2];
 #pragma unroll
-  for (int u = 0; u < 2; ++u) slack[u] = 2 * tid + u < n && load[u] < each ? each - load[u] : 0;
-  long long sum = slack[0] + slack[1];
+    for (int u = 0; u < 2; ++u) slack[u] = 2 * tid + u < n && load[u] < each ? each - load[u] : 0;
+    long long sum = slack[0] + slack[1];
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const long long o = __shfl_up(sum, d, 64);
-    if (lane >= d) sum += o;
-  }
-  if (lane == 63) wave_slack[wave] = sum;
-  __syncthreads();
-  long long all_slack = 0;
-  sum -= slack[0] + slack[1];
+    for (int d = 1; d < 64; d <<= 1) {
+      const long long o = __shfl_up(sum, d, 64);
+      if (lane >= d) sum += o;
+    }
+    if (lane == 63) wave_slack[wave] = sum;
+    __syncthreads();
+    long long all_slack = 0;
+    sum -= slack[0] + slack[1];
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    if (w < wave) sum += wave_slack[w];
-    all_slack += wave_slack[w];
-  }
-  // (whole numbers times the same factor: the bounds ascend; where there is no slack, the last has it all)
-  const double stretch = all_slack > 0 ? (double)(total - rest) / (double)all_slack : 0.0;
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) sum += wave_slack[w];
+      all_slack += wave_slack[w];
+    }
+    // (whole numbers times the same factor: the bounds ascend; where there is no slack, the last has it all)
+    const double stretch = all_slack > 0 ? (double)(total - rest) / (double)all_slack : 0.0;
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const long long at = rest + (long long)((double)sum * stretch);
-    if (2 * tid + u < n) bounds[2 * tid + u] = at < total ? at : total;
-    sum += slack[u];
+    for (int u = 0; u < 2; ++u) {
+      const long long at = rest + (long long)((double)sum * stretch);
+      if (2 * tid + u < n) bounds[2 * tid + u] = at < total ? at : total;
+      sum += slack[u];
+    }
   }
   if (tid == 0) bounds[n] = total;
   __syncthreads();
