@@ -31,8 +31,7 @@ struct GranuleCopy {
   u32 off[N];                          // bytes from the granule's first row (whole granules)
   u32 mine;                            // bit i: whether the head has what this lane copies in copy i
 
-  __device__ __forceinline__ GranuleCopy(long long token, int D) {
-    const int lane = threadIdx.x & 63;
+  __device__ __forceinline__ GranuleCopy(long long token, int D, int lane) {
     mine = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -143,8 +142,8 @@ struct Store {
   bool full;                           // D == DP
   GranuleCopy<T, DP, place_k<DP>> ko;
   GranuleCopy<T, DP, PLACE_V> vo;
-  __device__ __forceinline__ Store(const A& a, int h, int shift, int keys)
-      : h(h), shift(shift), keys(keys), full(a.D == DP), ko(a.K.token, a.D), vo(a.V.token, a.D) {}
+  __device__ __forceinline__ Store(const A& a, int h, int shift, int keys, int lane)
+      : h(h), shift(shift), keys(keys), full(a.D == DP), ko(a.K.token, a.D, lane), vo(a.V.token, a.D, lane) {}
   // May differ from lane to lane.
   __device__ __forceinline__ Place place(const Granule& g) const {
     const auto a = arguments<A>();
@@ -1073,7 +1072,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
       if (few) {
         const int all = __builtin_amdgcn_readfirstlane(sees(0));
         const int tiles = (end + kFewKeys - 1) / kFewKeys, stop = 2 * hi < tiles ? 2 * hi : tiles;
-        const Store<PagedArgs, T, DP, place_v16<DP>> store(a, hk, a.own.shift, keys);
+        int here = lane;                                 // (offsets computed here: held over the other loop, they
+        if constexpr (DP <= 128) asm volatile("" : "+v"(here));   // are spilled there)
+        const Store<PagedArgs, T, DP, place_v16<DP>> store(a, hk, a.own.shift, keys, here);
         attend_few<Few16<T, DP, DC>, T, DP, DC>(sh, store, where, qp, a.D, sees(row), all, 2 * lo, stop, rows, true,
                                                 a.flip, a.scale_log2, a.lift, target);
       } else {
@@ -1082,7 +1083,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
         const int last = wave * 32 < rows ? __builtin_amdgcn_readfirstlane(sees(last_row)) : 0;
         const int all = __builtin_amdgcn_readfirstlane(sees(from_row));
         const int tiles = (end + kTileKeys - 1) / kTileKeys, stop = hi < tiles ? hi : tiles;
-        const Store<PagedArgs, T, DP> store(a, hk, a.own.shift, keys);
+        const Store<PagedArgs, T, DP> store(a, hk, a.own.shift, keys, lane);
         attend_many<PagedArgs, T, DP, DC>(sh, store, where, qp, a.D, sees(row), all, last, lo, stop, rows, a.flip,
                                           a.scale_log2, a.lift, target);
       }
@@ -1319,7 +1320,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   const int lane = threadIdx.x & 63, row = (lane & 15) < rows ? lane & 15 : rows - 1;
   const int h0 = hk * a.group + tile * kFewRows;
   const int* list = a.chosen + (t * a.Hk + hk) * a.count;
-  const Store<ChosenArgs, T, DP, place_v16<DP>> store(a, hk, q.shift, keys);
+  const Store<ChosenArgs, T, DP, place_v16<DP>> store(a, hk, q.shift, keys, lane);
   Target<T> target;
   target.O = static_cast<T*>(a.O) + t * a.o_token + h0 * a.o_head;
   target.lse = a.lse ? a.lse + t * a.Hq + h0 : nullptr;
