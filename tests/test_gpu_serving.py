@@ -1,0 +1,258 @@
+"""The operators on a cache in pages together, as a server would call them: prompts and then tokens one at a time, with
+chosen pages or over all of them, behind prefixes; captured into graphs, and on several streams at once."""
+import math
+
+import pytest
+import torch
+
+from paper_2604_16855_amd import tdq
+
+import layer_util as L
+import pages_util as U
+from test_gpu_pages import _choice
+
+pytestmark = pytest.mark.gpu
+
+
+def _i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+class Server:
+    """A cache for sequences of up to `room` tokens, with the bounds of its pages; a step writes new tokens and attends."""
+
+    def __init__(self, S, room, P, Hq, Hk, D, dtype, seed=0):
+        self.S, self.P, self.Hq, self.Hk, self.D, self.dtype = S, P, Hq, Hk, D, dtype
+        columns = -(-room // P)
+        n = S * columns + 2
+        ids = torch.randperm(n, generator=torch.Generator().manual_seed(seed))[:S * columns]
+        self.table = ids.view(S, columns).to(torch.int32).cuda()
+        self.k = torch.full((n, P, Hk, D), math.nan, dtype=dtype, device="cuda")
+        self.v = torch.full_like(self.k, math.nan)
+        self.bounds = tuple(torch.zeros((n, Hk, D), dtype=dtype, device="cuda") for _ in range(2))
+        self.len = torch.zeros(S, dtype=torch.int32, device="cuda")
+        self.freq = (10000.0 ** (-torch.arange(D // 2, device="cuda").double() / (D // 2))).float()
+        self.weight = 1 + 0.1 * L.randn(D, seed=seed + 1)
+
+    def projection(self, T, seed):
+        return L.randn(T, self.Hq + 2 * self.Hk, self.D, seed=seed, dtype=self.dtype)
+
+    def write(self, qkv, cu, counts, pos=None):
+        self.len += counts
+        Q = tdq.tdq_cache_append(qkv[:, :self.Hq], qkv[:, self.Hq:self.Hq + self.Hk], qkv[:, self.Hq + self.Hk:], self.k,
+                                 self.v, cu, self.table, self.len, self.freq, pos=pos, q_weight=self.weight,
+                                 k_weight=self.weight)
+        tdq.tdq_page_bounds(self.k, self.table, self.len, cu_q=cu, Tq=qkv.shape[0], out=self.bounds)
+        return Q
+
+    def choose(self, Q, cu, count):
+        return tdq.tdq_select_pages(Q, *self.bounds, cu, self.table, self.len, self.P, count)
+
+    def selected(self, Q, chosen, cu):
+        return tdq.tdq_attention_selected(Q, self.k, self.v, chosen, cu, self.table, self.len, want_lse=True)
+
+    def paged(self, Q, cu, **kw):
+        return tdq.tdq_attention_paged(Q, self.k, self.v, cu, self.table, self.len, want_lse=True, **kw)
+
+    def held(self, lengths):
+        """What the oracles take: the keys and values that the pages hold."""
+        c = U.Cache.__new__(U.Cache)
+        c.lengths = lengths
+        c.K, c.V = ([x[self.table[s].long()].flatten(0, 1)[:n].contiguous() for s, n in enumerate(lengths)] for x in (self.k, self.v))
+        return c
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("Hq,Hk,D,P", [(8, 2, 128, 64), (6, 6, 64, 16), (5, 1, 96, 32)])
+def test_prompts_then_tokens(Hq, Hk, D, P, dtype):
+    lengths, room, count = [70, 3, 333], 400, 4
+    s = Server(3, room, P, Hq, Hk, D, dtype)
+    given = [[] for _ in lengths]                            # (of each sequence: queries, keys, values as projected)
+    have = [0, 0, 0]
+    for step, ql in enumerate([lengths, [1, 1, 1], [1, 0, 2], [5, 1, 1]]):
+        print(f"[serving] {ql} {Hq}/{Hk} D={D} P={P} {dtype}", flush=True)
+        qkv, cu = s.projection(sum(ql), step), L.starts(ql)
+        Q = s.write(qkv, cu, _i32(ql))
+        have = [a + b for a, b in zip(have, ql)]
+        for g, part in zip(given, qkv.split(ql)):
+            g.append(part)
+        # the cache: every key normed and turned by its place, every value as it was
+        c = s.held(have)
+        for K, V, g in zip(c.K, c.V, given):
+            x = torch.cat(g)
+            k, pos = x[:, Hq:Hq + Hk], torch.arange(x.shape[0], device="cuda")[None]
+            want = L.norm_rotate(k, s.weight, 1e-6, pos, s.freq, None, False)
+            tol = 24 * 2.0 ** -24 * want.abs().amax(dim=-1, keepdim=True) + L.UNIT[dtype] * want.abs() + L.TINY[dtype]
+            assert bool(((K.double() - want).abs() <= tol).all()) and torch.equal(V, x[:, Hq + Hk:])
+        for n, K, line in zip(have, c.K, s.table.tolist()):
+            for b in range(-(-n // P)):
+                k = K[b * P:(b + 1) * P]
+                assert torch.equal(s.bounds[0][line[b]], k.amin(dim=0)) and torch.equal(s.bounds[1][line[b]], k.amax(dim=0))
+        L.check_attention(s.paged(Q, cu), U.sequences(Q, ql, c, 1 / math.sqrt(D)))
+        chosen = s.choose(Q, cu, count)
+        assert torch.equal(chosen, _choice(Q, *s.bounds, ql, have, s.table, P, count, 1, 1, True))
+        want, t = [], 0
+        for n, m, K, V in zip(ql, have, c.K, c.V):
+            seen = torch.zeros((n, Hk, room + P), dtype=torch.bool, device="cuda")
+            at = chosen[t:t + n].long()
+            for i in range(P):
+                seen.scatter_(2, torch.where(at >= 0, at * P + i, room + P - 1), True)
+            last = torch.arange(n, device="cuda") + (m - n)
+            seen &= torch.arange(room + P, device="cuda") <= last[:, None, None]
+            want.append(U.masked(Q[t:t + n], K, V, seen[..., :m], 1 / math.sqrt(D)))
+            t += n
+        L.check_attention(s.selected(Q, chosen, cu), tuple(torch.cat(x) for x in zip(*want)))
+    # with room for all pages, the choice is every page
+    every = s.choose(Q, cu, s.table.shape[1])
+    L.check_attention(s.selected(Q, every, cu), U.sequences(Q, ql, c, 1 / math.sqrt(D)))
+
+
+def test_tokens_behind_a_shared_prompt():
+    """A prompt written once, sequences behind it with keys of their own at positions behind its."""
+    Hq, Hk, D, P, dtype, long = 8, 2, 64, 16, torch.bfloat16, 130
+    s = Server(5, 150, P, Hq, Hk, D, dtype)
+    one = _i32([long, 0, 0, 0, 0])
+    s.write(s.projection(long, 0), L.starts([long, 0, 0, 0, 0]), one)
+    prefix = (_i32([0, 4]), s.table[:1], s.len[:1].clone())
+    own = Server.__new__(Server)
+    own.__dict__.update(s.__dict__)
+    own.table, own.len = s.table[1:], torch.zeros(4, dtype=torch.int32, device="cuda")
+    have = [0] * 4
+    for step, ql in enumerate([[3, 1, 20, 0], [1, 1, 1, 1], [1, 0, 1, 2]]):
+        cu = L.starts(ql)
+        pos = torch.cat([torch.arange(long + h, long + h + n, device="cuda") for h, n in zip(have, ql)]).to(torch.int32)
+        Q = own.write(s.projection(sum(ql), 5 + step), cu, _i32(ql), pos=pos)
+        have = [a + b for a, b in zip(have, ql)]
+        pre = s.held([long])
+        L.check_attention(own.paged(Q, cu, prefix=prefix), U.sequences(Q, ql, own.held(have), 0.125, True, pre, [0] * 4))
+
+
+# ---- graphs and streams --------------------------------------------------------------
+def _step(s, qkv, cu, counts, prefix):
+    Q = s.write(qkv, cu, counts)
+    chosen = s.choose(Q, cu, 3)
+    return [Q, chosen, *s.selected(Q, chosen, cu), *s.paged(Q, cu), *s.paged(Q, cu, prefix=prefix)]
+
+
+def _servers(n, ql, prompt):
+    """Servers with the same prompts."""
+    out = []
+    for _ in range(n):
+        s = Server(3, 700, 16, 8, 2, 64, torch.bfloat16)
+        s.write(s.projection(sum(prompt), 1), L.starts(prompt), _i32(prompt))
+        out.append(s)
+    return out
+
+
+@pytest.mark.parametrize("ql", [[1, 1, 1], [1, 40, 2]])
+def test_captured_steps_equal_eager_ones(ql):
+    """A step captured once and replayed with new tokens, eager work on the device between the replays; two graphs of
+    different caches one after the other, each with workspaces of its own."""
+    prompt = [300, 1, 77]
+    eager, first, second = _servers(3, ql, prompt)
+    T, cu, counts = sum(ql), L.starts(ql), _i32(ql)
+    prefix = (_i32([0, 2]), eager.table[2:], _i32([60]))
+    # (libraries and the allocator are warm before the capture)
+    warm, = _servers(1, ql, prompt)
+    _step(warm, warm.projection(T, 3), cu, counts, prefix)
+    torch.cuda.synchronize()
+    graphs = []
+    for s in (first, second):
+        token, before = s.projection(T, 3), s.len.clone()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = _step(s, token, cu, counts, prefix)
+        assert torch.equal(s.len, before)                    # (nothing has run)
+        graphs.append((g, s, token, out))
+    for step in range(4):
+        qkv = eager.projection(T, 10 + step)
+        want = _step(eager, qkv, cu, counts, prefix)
+        for g, s, token, out in graphs:
+            token.copy_(qkv)
+            g.replay()
+        torch.cuda.synchronize()
+        for g, s, token, out in graphs:
+            assert torch.equal(s.len, eager.len)
+            for i, (a, b) in enumerate(zip(out, want)):
+                assert torch.equal(a, b), (step, i)
+            for a, b in zip((s.k, s.v, *s.bounds), (eager.k, eager.v, *eager.bounds)):
+                assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+def test_steps_on_two_streams_at_once():
+    """Each with a cache and workspaces of its own, as many calls on their way as there are steps."""
+    ql, prompt = [1, 1, 30], [300, 1, 77]
+    eager, a, b = _servers(3, ql, prompt)
+    cu, counts, prefix = L.starts(ql), _i32(ql), (_i32([0, 2]), eager.table[2:], _i32([60]))
+    tokens = [eager.projection(sum(ql), 10 + i) for i in range(5)]
+    want = [_step(eager, x, cu, counts, prefix) for x in tokens]
+    torch.cuda.synchronize()
+    got = []
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for x in tokens:
+        for s, stream in zip((a, b), streams):
+            with torch.cuda.stream(stream):
+                got.append(_step(s, x, cu, counts, prefix))
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        assert all(torch.equal(x, y) for x, y in zip(g, want[i // 2])), i
+
+
+# ---- sizes where the plan changes ----------------------------------------------------
+def _check(ql, lens, P, Hq, Hk, D, dtype=torch.float16, causal=True, seed=0, pre=(), first=()):
+    """All rows, some heads."""
+    own = U.Cache(lens, P, Hk, D, dtype, seed=seed, rest=math.nan)
+    Q = L.randn(sum(ql), Hq, D, seed=seed + 100, dtype=dtype)
+    k, v, table, prefix, p, of = own.k, own.v, own.table, None, None, None
+    if pre:
+        p = U.Cache(pre, P, Hk, D, dtype, seed=seed + 50, rest=math.nan)
+        k, v, table, pre_table = U.merged(own, p)
+        prefix = (_i32(first), pre_table, p.len)
+        of = [next((g for g in range(len(pre)) if first[g] <= s < first[g + 1]), None) for s in range(len(ql))]
+    O, lse = tdq.tdq_attention_paged(Q, k, v, L.starts(ql), table, own.len, prefix=prefix, causal=causal, want_lse=True)
+    assert bool(torch.isfinite(O).all())
+    g = Hq // Hk
+    for h in sorted({0, Hk // 2, Hk - 1}):
+        cut = lambda x: [y[:, h:h + 1].contiguous() for y in x]  # noqa: E731
+        heads = slice(h * g, (h + 1) * g)
+        part = U.Cache.__new__(U.Cache)
+        part.lengths, part.K, part.V = lens, cut(own.K), cut(own.V)
+        behind = None
+        if p is not None:
+            behind = U.Cache.__new__(U.Cache)
+            behind.lengths, behind.K, behind.V = p.lengths, cut(p.K), cut(p.V)
+        want = U.sequences(Q[:, heads].contiguous(), ql, part, 1 / math.sqrt(D), causal, behind, of)
+        L.check_attention((O[:, heads], lse[:, heads]), want)
+
+
+@pytest.mark.parametrize("Hq,Hk,D", [(256, 256, 16), (512, 512, 8), (300, 150, 16)])
+def test_few_workgroups_to_a_head(Hq, Hk, D):
+    """Many keys to a workgroup, of a few rows and of many; tiles whole and cut."""
+    _check([1], [12000], 16, Hq, Hk, D)
+    _check([1, 40], [9000, 5000], 64, Hq, Hk, D, torch.bfloat16)
+    _check([300, 1, 129, 0, 40, 500], [300, 700, 800, 3, 40, 500], 16, Hq, Hk, D)
+    _check([128] * 5 + [1], [128, 90, 4000, 200, 130, 5000], 32, Hq, Hk, D, causal=False)
+
+
+@pytest.mark.parametrize("Hq,Hk,D", [(64, 64, 32), (96, 48, 64), (64, 32, 200)])
+def test_whole_tiles_and_the_rest(Hq, Hk, D):
+    _check([500, 900, 3, 64, 333], [500, 1200, 400, 64, 333], 16, Hq, Hk, D)
+    _check([256] * 9 + [1] * 20, [256] * 9 + [300] * 20, 32, Hq, Hk, D, torch.bfloat16)
+    _check([1] * 60, [7 * i for i in range(60)], 16, Hq, Hk, D)
+    _check([40] * 12, [100 + 90 * i for i in range(12)], 16, Hq, Hk, D, pre=[800, 64], first=[0, 8, 11])
+
+
+def test_one_head_and_many_tiles():
+    _check([3000, 1, 2000], [3000, 500, 2600], 64, 24, 1, 64)
+    _check([128] * 200, [128 + 3 * (i % 11) for i in range(200)], 16, 8, 1, 32)
+
+
+def test_many_items_and_prefixes():
+    """More sequences than threads, with prefixes; more prefixes than lanes."""
+    n = 300
+    ql, lens = [i % 3 for i in range(n)], [5 + (i * 5) % 39 for i in range(n)]
+    _check(ql, lens, 16, 4, 2, 32, pre=[100, 33, 0, 70], first=[3, 100, 200, 250, 299])
+    groups = 100
+    first = [3 * i for i in range(groups + 1)]
+    _check(ql, lens, 16, 4, 2, 32, torch.bfloat16, pre=[(17 * i) % 60 for i in range(groups)], first=first)
+    _check([2] * 150, [3] * 150, 16, 2, 1, 64, pre=[20 + i for i in range(70)], first=[2 * i for i in range(71)])
