@@ -407,143 +407,40 @@ __device__ __forceinline__ float neighbour(float x) {
   return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), D == 1 ? 0xB1 : 0x4E, 0xF, 0xF, true));
 }
 
-// Pages of a workgroup, 16 of a wavefront at a time.
-constexpr int score_pages(int W) { return W <= 16 ? 512 : 256; }
-
-// W: channels of a lane.  Lane 16 k + p has of page p the 16-byte pieces k, k + 4, ..
-template <typename T, int W>
-__global__ __launch_bounds__(256, W == 16 ? 3 : 4) void k_score(ChoiceArgs a) {
-  constexpr int PIECES = W < 32 ? W / 8 : 4, PASSES = W / (8 * PIECES);   // pieces of a bound at a time
-  constexpr int PAGES = score_pages(W);
-  __shared__ float top[PAGES];
-  const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
-  const int h = (int)(id % a.Hk), chunk = (int)(id / a.Hk % a.chunks);
-  const long long t = id / a.Hk / a.chunks;
-  if (t >= a.Tq) return;
-  const Sequences& q = a.seq;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = lane >> 4;
-  auto at = [&](int pass, int i) { return 8 * (k + 4 * (pass * PIECES + i)); };   // first channel of a piece
-  // operand columns: head lane % 4, its positive and its negative channels
-  float up[8 * PIECES], down[8 * PIECES];
-  auto query = [&](int e0, int pass) {
-    // (past the last head: the last again, which changes no maximum)
-    const int e = e0 + (lane & 3), head = h * a.group + (e < a.group ? e : a.group - 1);
-    const T* p = static_cast<const T*>(a.Q) + t * a.q_token + head * a.q_head;
-    u32x4 x[PIECES];
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      x[i] = u32x4{0, 0, 0, 0};
-      if (at(pass, i) < a.D) x[i] = *reinterpret_cast<const u32x4_any*>(p + at(pass, i));
-    }
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const f32x2 v = two_floats<T>(x[i][j]);
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          up[8 * i + 2 * j + u] = v[u] < 0.f ? 0.f : v[u];
-          down[8 * i + 2 * j + u] = v[u] > 0.f ? 0.f : v[u];
-        }
-      }
-  };
-  const Seen me = seen_by(q, t, a.Tq, a.causal);
-  const int pages = me.keys <= 0 ? 0 : ((me.keys - 1) >> q.shift) + 1, b0 = chunk * PAGES;
-  if (b0 + 16 * wave >= pages) return;
-  const int here = pages - b0 < PAGES ? pages - b0 : PAGES;
-  const int* line = q.table + me.seq * q.ld + b0;
-  float* out = a.score + (t * a.Hk + h) * q.columns + b0;
-  // pages b .. b + 15: -1: none, or not there
-  auto page_of = [&](int b) {
-    int p = -1;
-    if (b + (lane & 15) < here) p = line[b + (lane & 15)];
-    return p < q.n_pages ? p : -1;
-  };
-#pragma unroll 1
-  for (int e0 = 0; e0 < a.group; e0 += 4) {
-    int page = page_of(16 * wave);
-    if (PASSES == 1) query(e0, 0);
-#pragma unroll 1
-    for (int b = 16 * wave; b < here; b += 64) {
-      const T* lo = static_cast<const T*>(a.lo) + (long long)page * a.lo_page + h * a.lo_head;
-      const T* hi = static_cast<const T*>(a.hi) + (long long)page * a.hi_page + h * a.hi_head;
-      double part[4] = {0.0, 0.0, 0.0, 0.0};             // (a product waits for the last one of its sum)
-#pragma unroll 1
-      for (int pass = 0; pass < PASSES; ++pass) {
-        u32x4 los[PIECES], his[PIECES];
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-          los[i] = his[i] = u32x4{0, 0, 0, 0};
-          if (page >= 0 && at(pass, i) < a.D) {
-            los[i] = *reinterpret_cast<const u32x4_any*>(lo + at(pass, i));
-            his[i] = *reinterpret_cast<const u32x4_any*>(hi + at(pass, i));
-          }
-        }
-        if (pass == PASSES - 1) page = page_of(b + 64);
-        if (PASSES > 1) query(e0, pass);
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const f32x2 l = two_floats<T>(los[i][j]), g = two_floats<T>(his[i][j]);
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              // (converted again for every 16 pages: as binary64 they would take the registers of half of
-              // the wavefronts that hide the bounds' way here)
-              float x = up[8 * i + 2 * j + u], y = down[8 * i + 2 * j + u];
-              if constexpr (W > 16) asm volatile("" : "+v"(x), "+v"(y));
-              part[u] = __builtin_amdgcn_mfma_f64_4x4x4f64((double)g[u], (double)x, part[u], 0, 0, 0);
-              part[2 + u] = __builtin_amdgcn_mfma_f64_4x4x4f64((double)l[u], (double)y, part[2 + u], 0, 0, 0);
-            }
-          }
-      }
-      // lane 16 i + 4 c + j has page 4 c + i and head j
-      float best = (float)((part[0] + part[1]) + (part[2] + part[3]));
-      best = most(best, neighbour<1>(best));
-      best = most(best, neighbour<2>(best));
-      const int mine = b + 4 * (lane >> 2 & 3) + (lane >> 4);
-      if ((lane & 3) == 0 && mine < here) {              // (of pages that are not there nobody asks)
-        if (e0 > 0) best = most(best, top[mine]);
-        if (e0 + 4 >= a.group) out[mine] = best;
-        else top[mine] = best;                           // (read by this lane alone)
-      }
-    }
-  }
-}
-
 // The pages of a token and key head: a radix select of the count-th largest key among the scores'
-// bit patterns (8 bits a pass), then the pages above it and the first ones at it, ascending.  Keys of up
-// to 2048 pages stay in registers.
-__global__ __launch_bounds__(256) void k_choose(ChoiceArgs a) {
-  constexpr int HELD = 8;
-  __shared__ u32 bins[256];
-  __shared__ u32 found[4];                               // digit, keys of larger ones, keys of it
-  __shared__ u32 ends[2][4];
-  __shared__ int count[2][4 * HELD];                     // above the limit, and at it
-  const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
-  if (id >= a.Tq * a.Hk) return;
-  const Sequences& q = a.seq;
-  const Seen me = seen_by(q, id / a.Hk, a.Tq, a.causal);
-  if (me.keys < 0) return;                               // (no sequence: its pages are left as they are)
-  const int pages = me.keys == 0 ? 0 : ((me.keys - 1) >> q.shift) + 1;
-  const int* line = q.table + me.seq * q.ld;
-  const float* score = a.score + id * q.columns;
+// bit patterns (8 bits a pass), then the pages above it and the first ones at it, ascending.  Keys of
+// 256 HELD pages stay in registers, and `entry` is what the line of the table has of them.
+template <int HELD>
+struct ChoiceRoom {
+  u32 bins[256];
+  u32 found[4];                                          // digit, keys of larger ones, keys of it
+  u32 ends[2][4];
+  int count[2][4 * HELD];                                // above the limit, and at it
+};
+template <int HELD, typename F>
+__device__ __forceinline__ void choose(const ChoiceArgs& a, ChoiceRoom<HELD>& room, long long id, int pages, const int* line,
+                                       const int (&entry)[HELD], F score) {
+  auto &bins = room.bins;
+  auto &found = room.found;
+  auto &ends = room.ends;
+  auto &count = room.count;
   int* out = a.chosen + id * a.count;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   // larger for a larger score; 0: not there; the largest: always taken; NaN above all numbers
-  auto read = [&](int b) -> u32 {
-    if (b >= pages) return 0;
-    const int page = line[b];
-    if (page < 0 || page >= q.n_pages) return 0;
+  auto key = [&](int b, int page, float s) -> u32 {
+    if (b >= pages || page < 0 || page >= a.seq.n_pages) return 0;
     if (b < a.first || b >= pages - a.last) return 0xFFFFFFFFu;
-    const float s = score[b];
     if (s != s) return 0xFFFFFFFEu;
     const u32 u = __float_as_uint(s + 0.f);              // (-0 as 0)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
   };
+  auto read = [&](int b) { return b < pages ? key(b, line[b], score(b)) : 0; };
   u32 held[HELD];
 #pragma unroll
-  for (int i = 0; i < HELD; ++i) held[i] = read(256 * i + tid);
+  for (int i = 0; i < HELD; ++i) {
+    const int b = 256 * i + tid;
+    held[i] = key(b, entry[i], b < pages ? score(b) : 0.f);
+  }
   auto each = [&](auto f) {                              // all pages, 256 at a time
 #pragma unroll
     for (int i = 0; i < HELD; ++i)
@@ -717,6 +614,144 @@ __global__ __launch_bounds__(256) void k_choose(ChoiceArgs a) {
   for (int i = taken + tid; i < a.count; i += 256) out[i] = -1;
 }
 
+template <int HELD>
+__device__ __forceinline__ void entries(const int* line, int pages, int (&entry)[HELD]) {
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    const int b = 256 * i + threadIdx.x;
+    entry[i] = b < pages ? line[b] : -1;
+  }
+}
+
+// Pages of a workgroup, 16 of a wavefront at a time.
+constexpr int score_pages(int W) { return W <= 16 ? 512 : 256; }
+
+// W: channels of a lane.  Lane 16 k + p has of page p the 16-byte pieces k, k + 4, ..  WHOLE: a workgroup
+// has all pages of a line, and makes the choice as well.
+template <typename T, int W, bool WHOLE>
+__global__ __launch_bounds__(256, W == 16 ? 3 : 4) void k_score(ChoiceArgs a) {
+  constexpr int PIECES = W < 32 ? W / 8 : 4, PASSES = W / (8 * PIECES);   // pieces of a bound at a time
+  constexpr int PAGES = score_pages(W);
+  constexpr int HELD = PAGES / 256;
+  __shared__ float top[PAGES];
+  const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
+  const int h = (int)(id % a.Hk), chunk = (int)(id / a.Hk % a.chunks);
+  const long long t = id / a.Hk / a.chunks;
+  if (t >= a.Tq) return;
+  const Sequences& q = a.seq;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = lane >> 4;
+  auto at = [&](int pass, int i) { return 8 * (k + 4 * (pass * PIECES + i)); };   // first channel of a piece
+  // operand columns: head lane % 4, its positive and its negative channels
+  float up[8 * PIECES], down[8 * PIECES];
+  auto query = [&](int e0, int pass) {
+    // (past the last head: the last again, which changes no maximum)
+    const int e = e0 + (lane & 3), head = h * a.group + (e < a.group ? e : a.group - 1);
+    const T* p = static_cast<const T*>(a.Q) + t * a.q_token + head * a.q_head;
+    u32x4 x[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      x[i] = u32x4{0, 0, 0, 0};
+      if (at(pass, i) < a.D) x[i] = *reinterpret_cast<const u32x4_any*>(p + at(pass, i));
+    }
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x2 v = two_floats<T>(x[i][j]);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          up[8 * i + 2 * j + u] = v[u] < 0.f ? 0.f : v[u];
+          down[8 * i + 2 * j + u] = v[u] > 0.f ? 0.f : v[u];
+        }
+      }
+  };
+  const Seen me = seen_by(q, t, a.Tq, a.causal);
+  const int pages = me.keys <= 0 ? 0 : ((me.keys - 1) >> q.shift) + 1, b0 = chunk * PAGES;
+  if (WHOLE ? me.keys < 0 : b0 + 16 * wave >= pages) return;
+  const int here = pages - b0 < PAGES ? pages - b0 : PAGES;
+  const int* line = q.table + me.seq * q.ld + b0;
+  float* out = a.score + (t * a.Hk + h) * q.columns + b0;
+  int entry[HELD];
+  if constexpr (WHOLE) entries(line, pages, entry);
+  // pages b .. b + 15: -1: none, or not there
+  auto page_of = [&](int b) {
+    int p = -1;
+    if (b + (lane & 15) < here) p = line[b + (lane & 15)];
+    return p < q.n_pages ? p : -1;
+  };
+#pragma unroll 1
+  for (int e0 = 0; e0 < a.group; e0 += 4) {
+    int page = page_of(16 * wave);
+    if (PASSES == 1) query(e0, 0);
+#pragma unroll 1
+    for (int b = 16 * wave; b < here; b += 64) {
+      const T* lo = static_cast<const T*>(a.lo) + (long long)page * a.lo_page + h * a.lo_head;
+      const T* hi = static_cast<const T*>(a.hi) + (long long)page * a.hi_page + h * a.hi_head;
+      double part[4] = {0.0, 0.0, 0.0, 0.0};             // (a product waits for the last one of its sum)
+#pragma unroll 1
+      for (int pass = 0; pass < PASSES; ++pass) {
+        u32x4 los[PIECES], his[PIECES];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+          los[i] = his[i] = u32x4{0, 0, 0, 0};
+          if (page >= 0 && at(pass, i) < a.D) {
+            los[i] = *reinterpret_cast<const u32x4_any*>(lo + at(pass, i));
+            his[i] = *reinterpret_cast<const u32x4_any*>(hi + at(pass, i));
+          }
+        }
+        if (pass == PASSES - 1) page = page_of(b + 64);
+        if (PASSES > 1) query(e0, pass);
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const f32x2 l = two_floats<T>(los[i][j]), g = two_floats<T>(his[i][j]);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              // (converted again for every 16 pages: as binary64 they would take the registers of half of
+              // the wavefronts that hide the bounds' way here)
+              float x = up[8 * i + 2 * j + u], y = down[8 * i + 2 * j + u];
+              if constexpr (W > 16) asm volatile("" : "+v"(x), "+v"(y));
+              part[u] = __builtin_amdgcn_mfma_f64_4x4x4f64((double)g[u], (double)x, part[u], 0, 0, 0);
+              part[2 + u] = __builtin_amdgcn_mfma_f64_4x4x4f64((double)l[u], (double)y, part[2 + u], 0, 0, 0);
+            }
+          }
+      }
+      // lane 16 i + 4 c + j has page 4 c + i and head j
+      float best = (float)((part[0] + part[1]) + (part[2] + part[3]));
+      best = most(best, neighbour<1>(best));
+      best = most(best, neighbour<2>(best));
+      const int mine = b + 4 * (lane >> 2 & 3) + (lane >> 4);
+      if ((lane & 3) == 0 && mine < here) {              // (of pages that are not there nobody asks)
+        if (e0 > 0) best = most(best, top[mine]);
+        if (!WHOLE && e0 + 4 >= a.group) out[mine] = best;
+        else top[mine] = best;                           // (up to here read by this lane alone)
+      }
+    }
+  }
+  if constexpr (WHOLE) {
+    __shared__ ChoiceRoom<HELD> room;
+    __syncthreads();
+    choose(a, room, id, pages, line, entry, [&](int b) { return top[b]; });
+  }
+}
+
+__global__ __launch_bounds__(256) void k_choose(ChoiceArgs a) {
+  constexpr int HELD = 8;
+  __shared__ ChoiceRoom<HELD> room;
+  const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
+  if (id >= a.Tq * a.Hk) return;
+  const Sequences& q = a.seq;
+  const Seen me = seen_by(q, id / a.Hk, a.Tq, a.causal);
+  if (me.keys < 0) return;                               // (no sequence: its pages are left as they are)
+  const int pages = me.keys == 0 ? 0 : ((me.keys - 1) >> q.shift) + 1;
+  const int* line = q.table + me.seq * q.ld;
+  const float* score = a.score + id * q.columns;
+  int entry[HELD];
+  entries(line, pages, entry);
+  choose(a, room, id, pages, line, entry, [&](int b) { return score[b]; });
+}
+
 size_t choice_workspace(long long Tq, int Hk, int columns) { return (size_t)Tq * Hk * columns * sizeof(float); }
 
 hipError_t launch_choice(const tdq_heads* Q, const tdq_heads* lo, const tdq_heads* hi, tdq_dtype dt, long long Tq,
@@ -746,17 +781,23 @@ hipError_t launch_choice(const tdq_heads* Q, const tdq_heads* lo, const tdq_head
   a.score = static_cast<float*>(workspace);
   a.chosen = chosen;
   const dim3 grid = two_axes(Tq * Hk * a.chunks);
-#define TDQ_SCORE(T_)                                                                        \
-  do {                                                                                       \
-    if (D <= 32) hipLaunchKernelGGL((k_score<T_, 8>), grid, dim3(256), 0, st, a);            \
-    else if (D <= 64) hipLaunchKernelGGL((k_score<T_, 16>), grid, dim3(256), 0, st, a);      \
-    else if (D <= 128) hipLaunchKernelGGL((k_score<T_, 32>), grid, dim3(256), 0, st, a);     \
-    else hipLaunchKernelGGL((k_score<T_, 64>), grid, dim3(256), 0, st, a);                   \
+#define TDQ_SCORE(T_, W)                                                                              \
+  do {                                                                                                \
+    if (a.chunks == 1) hipLaunchKernelGGL((k_score<T_, W, true>), grid, dim3(256), 0, st, a);         \
+    else hipLaunchKernelGGL((k_score<T_, W, false>), grid, dim3(256), 0, st, a);                      \
   } while (0)
-  if (dt == TDQ_F16) TDQ_SCORE(_Float16);
-  else TDQ_SCORE(__bf16);
+#define TDQ_SCORES(T_)                    \
+  do {                                    \
+    if (D <= 32) TDQ_SCORE(T_, 8);        \
+    else if (D <= 64) TDQ_SCORE(T_, 16);  \
+    else if (D <= 128) TDQ_SCORE(T_, 32); \
+    else TDQ_SCORE(T_, 64);               \
+  } while (0)
+  if (dt == TDQ_F16) TDQ_SCORES(_Float16);
+  else TDQ_SCORES(__bf16);
+#undef TDQ_SCORES
 #undef TDQ_SCORE
-  hipLaunchKernelGGL(k_choose, two_axes(Tq * Hk), dim3(256), 0, st, a);
+  if (a.chunks > 1) hipLaunchKernelGGL(k_choose, two_axes(Tq * Hk), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
