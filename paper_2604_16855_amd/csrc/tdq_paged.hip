@@ -635,18 +635,12 @@ struct PagedArgs {
   double per_group, half_tile;         // 1 / group, and half of the tokens of a tile
   int pieces;                          // most pieces of a line
   int cap;                             // rows of a part: as many as a tile may have
-  int* first_tile;                     // [prefixes + 2]: tiles of the sequences, of the prefixes, and in front of each
-  struct TileParts* tiles;             // [own_tiles + pre_tiles][Hk]: where the parts of each are, sequences first
+  int2* first_tile;                    // [prefixes + 1]: tiles of sequences and prefixes; of each those in front, first token
+  int2* tiles;                         // [own_tiles + pre_tiles][Hk]: first piece of each, how many; sequences first
   long long own_tiles, pre_tiles;      // (room for so many)
-  int2* place;                         // [Tq]: tile and row of it of a token's first row
+  int4* place;                         // [Tq]: sequence, tile and row of it of a token's first row
   float *part_o, *part_ml;             // [pieces Hk][2][cap]: of tiles that begin before a piece, and that end behind it
   float *whole_o, *whole_ml;           // with prefixes: [2][Tq Hq], of tiles of one (prefixes, sequences) in one piece
-};
-
-// What the second kernel needs to know of a tile: its first piece, and how many it lies in, and the
-// sequence (or prefix).
-struct TileParts {
-  int piece, count, line, unused;
 };
 
 constexpr int kTileCost = 4;           // what a tile takes beside its keys, in tiles of 64 keys
@@ -795,7 +789,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   }
   const int n = pieces_of(a, total);
   if (total == 0 || k >= n) {
-    if (blockIdx.x == 0 && tid == 0) a.first_tile[0] = 0;
+    if (blockIdx.x == 0 && tid == 0) a.first_tile[0] = make_int2(0, 0);
     return;
   }
   auto item = [&](int v) {
@@ -917,7 +911,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
       walk.r = -1;
     }
     if (v == a.pre.S) walk.pre_tiles = tiles_before;
-    if (blockIdx.x == 0 && v < a.pre.S) a.first_tile[v + 2] = tiles_before;
+    if (blockIdx.x == 0 && v < a.pre.S) a.first_tile[v + 1] = make_int2(tiles_before, item(v).t0);
     before = next;
     tiles_before = tiles_next;
   }
@@ -928,10 +922,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   }
   __syncthreads();
 
-  if (blockIdx.x == 0 && tid == 0) {
-    a.first_tile[0] = all_tiles - walk.pre_tiles;
-    a.first_tile[1] = walk.pre_tiles;
-  }
+  if (blockIdx.x == 0 && tid == 0) a.first_tile[0] = make_int2(all_tiles - walk.pre_tiles, walk.pre_tiles);
   // (a piece of no length may lie within a tile: then it says so)
   if (rounds == 0 && from >= total) return;
   for (bool more = true; more;) {
@@ -990,12 +981,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
             else beyond = half;
           }
         }
-        a.tiles[tile * a.Hk + hk] = TileParts{k, last - k + 1, line, 0};
+        a.tiles[tile * a.Hk + hk] = make_int2(k, last - k + 1);
       }
       if (hk == 0 && !prefix) {
         // tokens whose first row lies in the tile
         const int row = tid * a.group - first;
-        if (row >= 0 && row < rows) a.place[t0 + tid] = make_int2(tile0 - pre_tiles + r, row);
+        if (row >= 0 && row < rows) a.place[t0 + tid] = make_int4(tile0 - pre_tiles + r, row, line, 0);
       }
     }
     if (lo >= hi && lo > 0 && lo < tiles && tid < rows) {
@@ -1105,57 +1096,53 @@ __global__ __launch_bounds__(256, 4) void k_join_pages(PagedArgs a, int heads, i
   const int lane = threadIdx.x & 63;
   // (all on their way at once; what lies there is looked at if the token is one of a sequence)
   const int begin = start_of(a.own.cu, 0, a.Tq), end = start_of(a.own.cu, a.own.S, a.Tq);
-  const int tiles = a.first_tile[0], pre_tiles = a.first_tile[1];
-  const int2 place = a.place[t];
-  int from = 0, to = 0, first = 0;                       // of prefix `lane`: its sequences, its first tile
+  const int2 tiles = a.first_tile[0];                    // of sequences, of prefixes
+  const int4 place = a.place[t];
+  int from = 0, to = 0;                                  // of prefix `lane`: its sequences, its first tile and token
+  int2 first = make_int2(0, 0);
   const bool few = a.pre.S <= 64;
   if (lane < a.pre.S && few) {
     from = start_of(a.pre.cu, lane, a.own.S);
     to = start_of(a.pre.cu, lane + 1, a.own.S);
-    first = a.first_tile[2 + lane];
+    first = a.first_tile[1 + lane];
   }
   if (t < begin || t >= end || place.y < 0 || place.x < 0) return;
-  const int t0 = a.pre.S > 0 && few ? start_of(a.own.cu, from, a.Tq) : 0;
+  bool behind = false;                                   // whether the token's sequence has a prefix
+  if (a.pre.S > 0) {
+    const int line = __builtin_amdgcn_readfirstlane(place.z);
+    int p;
+    if (few) {
+      const unsigned long long mine = __ballot(line >= from && line < to);
+      behind = mine != 0;
+      p = behind ? __builtin_ctzll(mine) : 0;
+      first.x = __builtin_amdgcn_readlane(first.x, p);
+      first.y = __builtin_amdgcn_readlane(first.y, p);
+    } else {
+      p = last_at_most(a.pre.S, line, [&](int i) { return start_of(a.pre.cu, i, a.own.S); });
+      behind = line >= start_of(a.pre.cu, p, a.own.S) && line < start_of(a.pre.cu, p + 1, a.own.S);
+      first = a.first_tile[1 + p];
+    }
+  }
   const float per_group = (float)a.per_group;
   const int quads = a.D <= 32 ? 8 : a.D <= 64 ? 16 : a.D <= 128 ? 32 : 64, c = 4 * (lane & (quads - 1));
   for (int hb = h0; hb < h1; hb += 64 / quads) {
     const int h = hb + lane / quads, hk = quotient(h < h1 ? h : h1 - 1, per_group), e = h - hk * a.group;
     const long long own_row = (long long)place.y + e, tile = place.x + own_row / kManyRows;
-    const bool real = h < h1 && tile < tiles && tile < a.own_tiles;
-    TileParts own = {0, 1, 0, 0}, pre = {0, 0, 0, 0};
+    const bool real = h < h1 && tile < tiles.x && tile < a.own_tiles;
+    const long long pre_at = (t - first.y) * a.group + e, of = first.x + pre_at / kManyRows;
+    int2 own = make_int2(0, 1), pre = make_int2(0, 0);   // first piece, how many
     if (real) own = a.tiles[tile * a.Hk + hk];
-    int pre_row = 0;
-    if (a.pre.S > 0) {
-      const int line = __builtin_amdgcn_readfirstlane(own.line);   // (of the token: the same for all its heads)
-      bool there;                                        // whether the sequence has a prefix,
-      int pre_t0, pre_first;                             // and that one's first token and tile
-      if (few) {
-        const unsigned long long mine = __ballot(line >= from && line < to);
-        const int p = mine ? __builtin_ctzll(mine) : 0;
-        there = mine != 0;
-        pre_t0 = __shfl(t0, p, 64);
-        pre_first = __shfl(first, p, 64);
-      } else {
-        const int p = last_at_most(a.pre.S, line, [&](int i) { return start_of(a.pre.cu, i, a.own.S); });
-        const int s = start_of(a.pre.cu, p, a.own.S);
-        there = line >= s && line < start_of(a.pre.cu, p + 1, a.own.S);
-        pre_t0 = start_of(a.own.cu, s, a.Tq);
-        pre_first = a.first_tile[2 + p];
-      }
-      const long long row = (t - pre_t0) * a.group + e, of = pre_first + row / kManyRows;
-      pre_row = (int)(row % kManyRows);
-      if (real && there && row >= 0 && of < pre_tiles && of < a.pre_tiles) pre = a.tiles[(a.own_tiles + of) * a.Hk + hk];
-    }
-    const bool wanted = real && (own.count > 1 || a.pre.S > 0);   // (else its one piece has written the output)
+    if (real && behind && pre_at >= 0 && of < tiles.y && of < a.pre_tiles) pre = a.tiles[(a.own_tiles + of) * a.Hk + hk];
+    const bool wanted = real && (own.y > 1 || a.pre.S > 0);   // (else its one piece has written the output)
     if (__ballot(wanted) == 0) continue;
     const long long step = 2ll * a.Hk * a.cap, whole = hk * a.Tq * a.group + t * a.group + e;
     // (parts of a tile: the first ends behind its piece, the others begin in front of theirs)
-    auto run = [&](const TileParts& d, int row, long long whole) {
-      const long long at = ((2ll * d.piece * a.Hk + 2 * hk) + 1) * a.cap + row;
-      return d.count == 1 ? Run{a.whole_ml + 2 * whole, a.whole_o + whole * a.D, 0, 0, 1}
-                          : Run{a.part_ml + 2 * at, a.part_o + at * a.D, step, a.cap, d.count};
+    auto run = [&](const int2& d, int row, long long whole) {
+      const long long at = ((2ll * d.x * a.Hk + 2 * hk) + 1) * a.cap + row;
+      return d.y == 1 ? Run{a.whole_ml + 2 * whole, a.whole_o + whole * a.D, 0, 0, 1}
+                      : Run{a.part_ml + 2 * at, a.part_o + at * a.D, step, a.cap, d.y};
     };
-    const Run x = run(pre, pre_row, whole), y = run(own, (int)(own_row % kManyRows), a.Tq * a.Hq + whole);
+    const Run x = run(pre, (int)(pre_at % kManyRows), whole), y = run(own, (int)(own_row % kManyRows), a.Tq * a.Hq + whole);
     T* op = static_cast<T*>(a.O) + t * a.o_token;
     float* lse = a.lse ? a.lse + t * a.Hq : nullptr;
     if (__ballot(wanted && x.count + y.count > kFewParts) == 0) {
@@ -1189,10 +1176,10 @@ static PagedLayout paged_layout(long long Tq, int S, int prefixes, int Hq, int H
   const size_t parts = 2ull * l.pieces * Hk * l.cap, whole = prefixes > 0 ? 2ull * Tq * Hq : 0;
   auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
   l.own_tiles = rows / kManyRows + S;
-  l.tiles = up((size_t)(prefixes + 2) * sizeof(int));
+  l.tiles = up((size_t)(prefixes + 1) * sizeof(int2));
   l.pre_tiles = prefixes > 0 ? rows / kManyRows + prefixes : 0;
-  l.place = l.tiles + up((size_t)(l.own_tiles + l.pre_tiles) * Hk * sizeof(TileParts));
-  l.ml = l.place + up((size_t)Tq * sizeof(int2));
+  l.place = l.tiles + up((size_t)(l.own_tiles + l.pre_tiles) * Hk * sizeof(int2));
+  l.ml = l.place + up((size_t)Tq * sizeof(int4));
   l.o = l.ml + up(parts * 2 * sizeof(float));
   l.whole_ml = l.o + up(parts * D * sizeof(float));
   l.whole_o = l.whole_ml + up(whole * 2 * sizeof(float));
@@ -1255,9 +1242,9 @@ hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages*
   a.pieces = l.pieces;
   a.cap = l.cap;
   char* w = static_cast<char*>(workspace);
-  a.first_tile = reinterpret_cast<int*>(w);
-  a.tiles = reinterpret_cast<TileParts*>(w + l.tiles);
-  a.place = reinterpret_cast<int2*>(w + l.place);
+  a.first_tile = reinterpret_cast<int2*>(w);
+  a.tiles = reinterpret_cast<int2*>(w + l.tiles);
+  a.place = reinterpret_cast<int4*>(w + l.place);
   a.own_tiles = l.own_tiles;
   a.pre_tiles = l.pre_tiles;
   a.part_ml = reinterpret_cast<float*>(w + l.ml);
