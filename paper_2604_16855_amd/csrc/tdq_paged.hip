@@ -726,7 +726,10 @@ __device__ __forceinline__ int pieces_of(const PagedArgs& a, long long total) {
 }
 // The tile of all that workgroup k of n takes in a round of whole tiles.
 __device__ __forceinline__ int tile_of_round(int round, int k, int n) { return round * n + (round & 1 ? n - 1 - k : k); }
-constexpr int kSpare = 5;              // whole tiles are no more than 1 + 1 / kSpare of a workgroup's share of the line
+// Whole tiles are no more than 1 + 1 / kSpare of a workgroup's share of the line.  us with none, 1 / 5, 1 / 3
+// and 1 / 2: 4 x 1024 tokens over 8192 keys 665, 610, 610, 613; 16 times 100 to 600 tokens 512, 481, 549, 549;
+// 40 times 1 to 500 733, 642, 643, 738; three long prompts of more tiles than workgroups 390, 399, 399, 400.
+constexpr int kSpare = 5;
 
 template <typename T, int DP, int DC>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 2 : 1))) void k_attend_pages(
@@ -816,12 +819,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     return v;
   };
   // Whole tiles first, as long as they leave no workgroup with much more than its share: in round i
-  // workgroup k takes tile i n + k, or in odd ones from the other end.
+  // workgroup k takes tile i n + k, or in odd ones from the other end.  A cut tile's parts are 512 bytes a
+  // row each way, so of tiles of few rows cuts cost little, and the plan more (256 single tokens 379 us,
+  // without 368).
   const double per = (double)total / n;
   const long long each = (long long)per;
   int rounds = 0;
   long long load[2] = {0, 0};                            // of pieces 2 tid and 2 tid + 1
-  if (share == 1) {
+  if (share == 1 && a.Tq * a.group > (long long)kFewRows * all_tiles) {
     __syncthreads();
     for (int i = 0; (long long)(i + 1) * n <= all_tiles; ++i) {
       long long with[2], top = 0;
