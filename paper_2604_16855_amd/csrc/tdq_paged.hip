@@ -227,7 +227,7 @@ __device__ __forceinline__ void attend_many(Shared<DP>& sh, const Store<A, T, DP
                                             float lift, F target) {
   constexpr int BYTES = kGranule * 2 * DP;             // of a granule in LDS
   constexpr int STAGES = kStages<DP>;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool quick = store.quick();
   // The places of the wave's granules of 64 tiles, in LDS: a look at the table in every step is three
   // scalar loads in a row, which the matrix instructions behind them wait for (7 % of four times 1024 tokens
@@ -290,6 +290,8 @@ __device__ __forceinline__ void attend_many(Shared<DP>& sh, const Store<A, T, DP
     }
   }
   const Target<T> to = target();
+  int half = lane >> 5;
+  if constexpr (DP > 128) asm volatile("" : "+v"(half)); // (or sums with it are held all the time, and spilled)
 
   const float l = w.l + other_half(w.l);
   const int r = wave * 32 + (lane & 31);
