@@ -32,7 +32,7 @@ struct AppendArgs {
 
 constexpr int kAppendThreads = 256;
 // Tokens of a workgroup in calls of many (one each in others); these leave rows behind each other that no
-// cache holds until they are read, so their stores pass the caches by.  13253 tokens of 32/8 heads of 128,
+// cache holds until they are read, so their stores pass the caches by.  23052 tokens of 32/8 heads of 128,
 // us: 1 token 121, 2 113, 4 117, 8-byte stores past the caches 108, with 2 tokens 105.
 constexpr int kAppendTokens = 2, kAppendMany = 4096;
 
@@ -246,7 +246,9 @@ hipError_t launch_append(const tdq_heads* Q, const tdq_heads* K, const tdq_heads
 // ---------------------------------------------------------------------------
 // Smallest and largest value of every channel over the keys of a page that are in use; NaN where one
 // is.  A workgroup has a page and a key head: a lane 8 channels of every 16th row or so (all of them on
-// their way at once), joined in the wavefront by exchanges and between wavefronts in LDS.
+// their way at once), joined in the wavefront by exchanges and between wavefronts in LDS.  Bound by memory where
+// there are many pages (48 MB in 11 us, 4.4 TB/s), and by three loads that wait for each other where there are
+// few: 64 pages 6 us.
 struct BoundsArgs {
   const void* K;
   void *lo, *hi;
@@ -378,7 +380,12 @@ hipError_t launch_bounds(const tdq_pages* K, tdq_dtype dt, long long T, const td
 // products of two 16-bit types are added in binary64, which holds nearly all such sums without rounding,
 // and the result is rounded to binary32.  The products are the 64-bit matrix instruction's: 16 pages x 4
 // heads x 4 channels at a time, four heads of a group and both of their signs in registers for all pages
-// of a workgroup.
+// of a workgroup.  What bounds it is the way to the first bounds (the token's sequence, its pages, the
+// bounds: 4 us), and beside the products the conversions of both operands: 32 tokens over 560 pages each, 8
+// heads of 128, 26 us (73 MB).  By products in binary32 with a bound of their error, and in binary64 only
+// where the order stays open, the scores took 21, but the choice 19 instead of 8.  16 columns of tokens and
+// heads by the 16 x 16 x 4 instruction, at two thirds of the rate, took 24 instead of 30 for 401 tokens over
+// 383 pages, as much as making the choice in the same kernel saves.
 struct ChoiceArgs {
   const void *Q, *lo, *hi;
   long long q_token, q_head, lo_page, lo_head, hi_page, hi_head;
@@ -409,7 +416,9 @@ __device__ __forceinline__ float neighbour(float x) {
 
 // The pages of a token and key head: a radix select of the count-th largest key among the scores'
 // bit patterns (8 bits a pass), then the pages above it and the first ones at it, ascending.  Keys of
-// 256 HELD pages stay in registers, and `entry` is what the line of the table has of them.
+// 256 HELD pages stay in registers, and `entry` is what the line of the table has of them.  Bound by the
+// passes' barriers, one after the other: 8 us for 256 lists of 560 pages on average; behind the scores in one
+// kernel, 401 tokens' calls are shorter by 5 (39.7 to 34.9).
 template <int HELD>
 struct ChoiceRoom {
   u32 bins[256];
@@ -623,7 +632,9 @@ __device__ __forceinline__ void entries(const int* line, int pages, int (&entry)
   }
 }
 
-// Pages of a workgroup, 16 of a wavefront at a time.
+// Pages of a workgroup, 16 of a wavefront at a time.  us of both kernels with 256 and 512: D = 64, 401 tokens
+// over 383 pages on average 47 and 35 (512 are all pages, and the choice is made here), 32 tokens over 469
+// 18.5 and 16.2, 4 over 938 16 and 20; D = 128, 32 over 560 34 and 38, 4 over 938 22 and 30.
 constexpr int score_pages(int W) { return W <= 16 ? 512 : 256; }
 
 // W: channels of a lane.  Lane 16 k + p has of page p the 16-byte pieces k, k + 4, ..  WHOLE: a workgroup

@@ -220,7 +220,10 @@ __device__ __forceinline__ void clear(Shared<DP>& sh) {
 }
 
 // Up to 128 rows by four wavefronts that share tiles of 64 keys, the next tile on its way while one is
-// worked on; key tiles from lo to hi.  A wavefront copies one granule of each tile.
+// worked on; key tiles from lo to hi.  A wavefront copies one granule of each tile.  Every key that is read
+// serves 128 rows, so what bounds it is what a wavefront issues, vector and matrix instructions hardly at the
+// same time, as in the packed attention: 0.98 PFLOP/s for 4 x 1024 tokens over 8192 keys, 32/8 heads of 128
+// (contiguous keys 0.98).
 template <typename A, typename T, int DP, int DC, typename F>
 __device__ __forceinline__ void attend_many(Shared<DP>& sh, const Store<A, T, DP>& store, Line where, const T* qp, int D,
                                             int sees, int all, int last, int lo, int hi, int rows, u32 flip, float c,
@@ -333,7 +336,9 @@ __device__ __forceinline__ void attend_many(Shared<DP>& sh, const Store<A, T, DP
   if (to.lse && half == 0) to.lse[(long long)token * to.Hq + head] = log_sum(w.m, l, c);
 }
 
-// 16 rows, for tiles of 32 keys.
+// 16 rows, for tiles of 32 keys: the heads of a single token's group.  Bound by memory, where tiles of 128
+// rows would be by the zeros that they multiply: 16 tokens of 4000 to 32000 keys 195 us, as tiles of 128 rows
+// 220; 256 tokens of 100 to 4000 366 and 406.
 template <typename T, int DP, int DC>
 struct Few16 {
   static constexpr int kRows = 16;
@@ -622,6 +627,9 @@ __device__ __forceinline__ Run run_of(const Run& r, int from) {
 // few long ones; a tile that lies in several pieces is joined by the second kernel.  Every workgroup finds
 // the line's length and its own place on it from the lengths (a sum over them by all threads), so that
 // nothing of the plan depends on the host, which does not know them.
+//
+// Keys and values that one tile reads stream past the caches (16 tokens of 4000 to 32000 keys 196 us, through
+// them 218; 256 of 100 to 4000 366 and 402): what bounds single tokens is memory, 6.3 TB/s in the kernel.
 struct PagedArgs {
   static constexpr bool kReadAgain = true;
   const void* Q;
@@ -645,8 +653,10 @@ struct PagedArgs {
   float *whole_o, *whole_ml;           // with prefixes: [2][Tq Hq], of tiles of one (prefixes, sequences) in one piece
 };
 
-constexpr int kTileCost = 4;           // what a tile takes beside its keys, in tiles of 64 keys
-constexpr int kLeastPiece = 4;
+// What a tile takes beside its keys (its place, its first keys on their way, its stores), in tiles of 64 keys.
+// us with 2, 4 and 8: 64 tokens behind a prefix 90, 87, 95; 16 questions behind three 32.6, 29.6, 31.5; others
+// the same.  A piece is no shorter.
+constexpr int kTileCost = 4, kLeastPiece = 4;
 
 // A prefix or a sequence: its rows, and its keys.
 struct Item {
@@ -1091,7 +1101,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
 }
 
 // Joins the tiles that lie in several pieces, and prefixes with sequences.  A wavefront has `heads` rows of
-// a token, as many at a time as 4 outputs a lane allow; rows of many parts take all of it one by one.
+// a token, as many at a time as 4 outputs a lane allow; rows of many parts take all of it one by one.  What
+// bounds it is a chain of four loads (the token's place, its tiles, their sums, their values), 5 us for single
+// tokens, and the parts of many rows, 67 MB of 2257 tokens 24 us.
 template <typename T>
 __global__ __launch_bounds__(256, 4) void k_join_pages(PagedArgs a, int heads, int chunks) {
   __shared__ float weight[4][kMaxParts];
@@ -1164,7 +1176,9 @@ __global__ __launch_bounds__(256, 4) void k_join_pages(PagedArgs a, int heads, i
   }
 }
 
-// Pieces for each key head's line: a workgroup each, as many as run at a time.
+// Pieces for each key head's line: a workgroup each, as many as run at a time.  us with half, as many and
+// twice: 16 tokens of 4000 to 32000 keys 194, 196, 201; 64 behind a prefix 119, 89, 105; 4 prompts' parts of
+// 300 to 1024 tokens 449, 302, 327.
 static int paged_pieces(int Hk, int D) {
   const int at_a_time = D <= 128 ? 512 : 256;
   return at_a_time / Hk > 0 ? at_a_time / Hk : 1;
@@ -1263,7 +1277,8 @@ hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages*
   if (dt == TDQ_F16) TDQ_BY_HEAD(TDQ_PAGED, _Float16);
   else TDQ_BY_HEAD(TDQ_PAGED, __bf16);
 #undef TDQ_PAGED
-  // (few tokens: many parts a row, and wavefronts enough)
+  // Few tokens: many parts a row, a wavefront each.  us with 1 and 8 rows a wavefront: 64 tokens behind a
+  // prefix 87 and 120; 4 prompts' parts of 300 to 1024 tokens 318 and 297; 8 x 2048 tokens 546 and 393.
   const int heads = Tq * Hq > 16384 ? 8 : 1;
   const int chunks = (Hq + 4 * heads - 1) / (4 * heads);
   const dim3 join = two_axes(Tq * chunks);
@@ -1276,7 +1291,9 @@ hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages*
 // chosen pages
 // ---------------------------------------------------------------------------
 // Every token and key head has a list of pages of its own, so a tile has the group's rows and no more;
-// its pages are shared out to `splits` workgroups, and in each to four wavefronts.
+// its pages are shared out to `splits` workgroups, and in each to four wavefronts.  Pages of single tokens are
+// read once, at 6.2 TB/s (32 tokens, 64 pages of 64 keys, 8 heads of 128: 87 us); those of a prompt's tokens
+// come from the caches, at 14 TB/s (401 tokens, 16 pages, 4 heads of 64: 29 us).
 struct ChosenArgs {
   static constexpr bool kReadAgain = false;
   const void* Q;
@@ -1362,10 +1379,12 @@ __global__ __launch_bounds__(256, 4) void k_join_chosen(ChosenArgs a) {
               static_cast<T*>(a.O) + t * a.o_token + h * a.o_head, a.lse ? a.lse + row : nullptr);
 }
 
-// Enough workgroups to fill the chip, as long as each has 256 keys.
+// Workgroups for the chip, as long as each has 256 keys.  us with 512, 1024 and 2048 of them: 32 tokens of 4096
+// keys 91, 92, 96; 128 tokens 330, 330, 344.  With 128, 256 and 512 keys at least: one token 14.8, 14.4, 15.8,
+// four 27, 22, 21.
 static int chosen_splits(long long Tq, int Hq, int Hk, int page_size, int count) {
   const long long base = Tq * Hk * ((Hq / Hk + kFewRows - 1) / kFewRows), most = (long long)count * page_size / 256;
-  long long n = 1024 / base;
+  long long n = 512 / base;
   if (n > most) n = most;
   if (n > 64) n = 64;
   return n > 1 ? (int)n : 1;
