@@ -530,7 +530,8 @@ typedef struct tdq_pages {
  *   table [S, ld_table]  key j of sequence s is row j % page_size of page table[s][j / page_size].  A page
  *                  outside 0 .. n_pages - 1 is not there: nobody sees its keys, nothing is written to it.
  * page_size a power of two from 16 to 1024, columns >= 1, columns * page_size <= 2^30, n_pages >= 1,
- * 1 <= S <= 2^20.  Entries of a line past its sequence's last key are not looked at. */
+ * 1 <= S <= 2^20.  Entries of a line past its sequence's last key are not looked at.
+ * Calls that may run at the same time need a workspace each; what it holds before a call does not matter. */
 typedef struct tdq_sequences {
   const int32_t *cu_q, *len_k, *table;
   int64_t ld_table;
@@ -583,8 +584,8 @@ int tdq_page_bounds(const tdq_pages* Kc, tdq_dtype dt, int64_t T, const tdq_sequ
  *
  * Q [Tq, Hq, D] of dt = TDQ_F16 or TDQ_BF16, lo and hi as tdq_page_bounds writes them.  0 <= first, last;
  * max(1, first + last) <= count <= 2^20.  D a multiple of 8 up to TDQ_MAX_HEAD, Hk divides Hq, Hq <= 4096,
- * 1 <= Tq <= 2^30.  workspace: device scratch of tdq_select_pages_workspace_bytes(Tq, Hk, columns), 256-byte
- * aligned.
+ * 1 <= Tq <= 2^30, Tq Hk columns <= 2^56.  workspace: device scratch of
+ * tdq_select_pages_workspace_bytes(Tq, Hk, columns), 256-byte aligned.
  */
 size_t tdq_select_pages_workspace_bytes(int64_t Tq, int32_t Hk, int32_t columns);
 int tdq_select_pages(const tdq_heads* Q, const tdq_heads* lo, const tdq_heads* hi, tdq_dtype dt, int64_t Tq,
@@ -597,6 +598,7 @@ int tdq_select_pages(const tdq_heads* Q, const tdq_heads* lo, const tdq_heads* h
  * the pages chosen[t, h, 0 .. count - 1] of their sequence's line, in any order.  Values outside the line's
  * pages in use (-1) name none; the keys of a page that is named twice count twice.  O, lse, scale, causal and
  * what is rounded as in tdq_attention; the same holds for keys that nobody sees and values that are not finite.
+ * O may be Q, but not overlap it in another way.
  *
  * Kc, Vc [n_pages, page_size, Hk, D], 16-byte aligned, strides multiples of 8; 1 <= count <= 2^20, count *
  * page_size <= 2^30; the other arguments as in tdq_attention.  workspace: device scratch of
@@ -617,7 +619,8 @@ int tdq_attention_selected(const tdq_heads* Q, const tdq_pages* Kc, const tdq_pa
  * keys are hidden from its earlier queries.  A prefix is read once for all of its sequences.
  * n_pages and page_size are the same for both.
  *
- * O, lse, scale, causal, rounding, keys that nobody sees and values that are not finite as in tdq_attention.
+ * O, lse, scale, causal, rounding, keys that nobody sees and values that are not finite as in tdq_attention; O
+ * may be Q, but not overlap it in another way.
  * Kc, Vc [n_pages, page_size, Hk, D], 16-byte aligned, strides multiples of 8; Tq * (Hq / Hk) <= 2^31;
  * the other arguments as in tdq_attention.  workspace: device scratch of
  * tdq_attention_paged_workspace_bytes(Tq, S, prefixes, Hq, Hk, D), 256-byte aligned.

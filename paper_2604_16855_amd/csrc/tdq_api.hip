@@ -1056,8 +1056,12 @@ static bool paged_shape(int64_t Tq, int32_t Hq, int32_t Hk, int32_t D) {
          D <= TDQ_MAX_HEAD && D % 8 == 0;
 }
 
+// (scores are counted in 64 bits)
+static bool choice_scores(int64_t Tq, int32_t Hk, int32_t columns) { return Tq * Hk <= ((int64_t)1 << 56) / columns; }
+
 size_t tdq_select_pages_workspace_bytes(int64_t Tq, int32_t Hk, int32_t columns) {
   if (Tq < 1 || Tq > (int64_t)1 << 30 || Hk < 1 || Hk > 4096 || columns < 1 || columns > 1 << 26) return 0;
+  if (!choice_scores(Tq, Hk, columns)) return 0;
   return choice_workspace(Tq, Hk, columns);
 }
 
@@ -1069,7 +1073,7 @@ int tdq_select_pages(const tdq_heads* Q, const tdq_heads* lo, const tdq_heads* h
   const int rc = check_sequences(seq, true);
   if (rc != TDQ_OK) return rc;
   if (!half_type(dt)) return TDQ_ERR_DTYPE;
-  if (!paged_shape(Tq, Hq, Hk, D)) return TDQ_ERR_SHAPE;
+  if (!paged_shape(Tq, Hq, Hk, D) || !choice_scores(Tq, Hk, seq->columns)) return TDQ_ERR_SHAPE;
   if (count < 1 || count > 1 << 20 || first < 0 || last < 0 || (int64_t)first + last > count) return TDQ_ERR_PARAM;
   if (misaligned(Q->data, 2) || misaligned(lo->data, 2) || misaligned(hi->data, 2) || misaligned(chosen, 4))
     return TDQ_ERR_ALIGN;

@@ -1147,11 +1147,13 @@ __global__ __launch_bounds__(256, 4) void k_join_pages(PagedArgs a, int heads, i
   for (int hb = h0; hb < h1; hb += 64 / quads) {
     const int h = hb + lane / quads, hk = quotient(h < h1 ? h : h1 - 1, per_group), e = h - hk * a.group;
     const long long own_row = (long long)place.y + e, tile = place.x + own_row / kManyRows;
-    const bool real = h < h1 && tile < tiles.x && tile < a.own_tiles;
+    const int row = (int)(own_row % kManyRows);
+    const bool real = h < h1 && tile < tiles.x && tile < a.own_tiles && row < a.cap;
     const long long pre_at = (t - first.y) * a.group + e, of = first.x + pre_at / kManyRows;
+    const int pre_row = (int)(pre_at % kManyRows);
     int2 own = make_int2(0, 1), pre = make_int2(0, 0);   // first piece, how many
     if (real) own = a.tiles[tile * a.Hk + hk];
-    if (real && behind && pre_at >= 0 && of < tiles.y && of < a.pre_tiles) pre = a.tiles[(a.own_tiles + of) * a.Hk + hk];
+    if (real && behind && pre_at >= 0 && of < tiles.y && of < a.pre_tiles && pre_row < a.cap) pre = a.tiles[(a.own_tiles + of) * a.Hk + hk];
     const bool wanted = real && (own.y > 1 || a.pre.S > 0);   // (else its one piece has written the output)
     if (__ballot(wanted) == 0) continue;
     const long long step = 2ll * a.Hk * a.cap, whole = hk * a.Tq * a.group + t * a.group + e;
@@ -1161,7 +1163,7 @@ __global__ __launch_bounds__(256, 4) void k_join_pages(PagedArgs a, int heads, i
       return d.y == 1 ? Run{a.whole_ml + 2 * whole, a.whole_o + whole * a.D, 0, 0, 1}
                       : Run{a.part_ml + 2 * at, a.part_o + at * a.D, step, a.cap, d.y};
     };
-    const Run x = run(pre, (int)(pre_at % kManyRows), whole), y = run(own, (int)(own_row % kManyRows), a.Tq * a.Hq + whole);
+    const Run x = run(pre, pre_row, whole), y = run(own, row, a.Tq * a.Hq + whole);
     T* op = static_cast<T*>(a.O) + t * a.o_token;
     float* lse = a.lse ? a.lse + t * a.Hq : nullptr;
     if (__ballot(wanted && x.count + y.count > kFewParts) == 0) {

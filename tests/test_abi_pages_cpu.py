@@ -104,11 +104,12 @@ def test_select():
         assert call(**kw) == tdq.ERR_PARAM, kw
     for kw in (dict(Q=_h(FAKE + 1)), dict(lo=_h(FAKE + 1)), dict(hi=_h(FAKE + 1)), dict(out=FAKE + 2)):
         assert call(**kw) == tdq.ERR_ALIGN, kw
+    assert call(Tq=1 << 30, Hq=4096, Hk=4096, seq=_s(columns=1 << 20, ld=1 << 20)) == tdq.ERR_SHAPE
     need = L.tdq_select_pages_workspace_bytes(10, 2, 10)
     assert need >= 10 * 2 * 10 * 4
     for kw in (dict(ws=None), dict(wsb=need - 1), dict(ws=FAKE + 128)):
         assert call(**kw) == tdq.ERR_WORKSPACE, kw
-    for a in ((0, 2, 10), (1 << 31, 2, 10), (10, 0, 10), (10, 5000, 10), (10, 2, 0), (10, 2, 1 << 27)):
+    for a in ((0, 2, 10), (1 << 31, 2, 10), (10, 0, 10), (10, 5000, 10), (10, 2, 0), (10, 2, 1 << 27), (1 << 30, 4096, 1 << 20)):
         assert L.tdq_select_pages_workspace_bytes(*a) == 0
 
 

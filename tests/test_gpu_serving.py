@@ -198,6 +198,59 @@ def test_steps_on_two_streams_at_once():
         assert all(torch.equal(x, y) for x, y in zip(g, want[i // 2])), i
 
 
+def test_what_a_workspace_holds_does_not_matter():
+    """One for calls of different sizes, full of what they and others left."""
+    s, = _servers(1, [1, 1, 30], [300, 1, 77])
+    work = torch.empty(tdq.tdq_attention_paged_workspace_bytes(200, 3, 1, 8, 2, 64), dtype=torch.uint8, device="cuda")
+    assert work.numel() >= tdq.tdq_attention_paged_workspace_bytes(6, 3, 1, 8, 2, 64)
+    prefix = (_i32([0, 2]), s.table[2:], _i32([60]))
+    for ql in ([1, 1, 30], [2, 1, 3], [100, 1, 70]):
+        T, cu = sum(ql), L.starts(ql)
+        Q = L.randn(T, 8, 64, seed=T, dtype=torch.bfloat16)
+        chosen = s.choose(Q, cu, 3)
+        calls = (lambda **kw: s.choose(Q, cu, 3) if not kw else tdq.tdq_select_pages(
+                     Q, *s.bounds, cu, s.table, s.len, s.P, 3, **kw),
+                 lambda **kw: tdq.tdq_attention_selected(Q, s.k, s.v, chosen, cu, s.table, s.len, want_lse=True, **kw),
+                 lambda **kw: s.paged(Q, cu, **kw), lambda **kw: s.paged(Q, cu, prefix=prefix, **kw))
+        for call in calls:
+            want = call()
+            for left in (0, 0x7F, 0xFF):
+                work.fill_(left)
+                for _ in range(2):
+                    got = call(workspace=work)
+                    for a, b in zip(got, want):
+                        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("ql", [[1, 1, 2], [1, 40, 2], [300, 77, 128]])
+def test_outputs_in_place_of_the_queries(ql):
+    s, = _servers(1, ql, [300, 100, 300])
+    T, cu = sum(ql), L.starts(ql)
+    Q = L.randn(T, 8, 64, seed=T, dtype=torch.bfloat16)
+    chosen, prefix = s.choose(Q, cu, 40), (_i32([0, 2]), s.table[2:], _i32([60]))
+    for call in (lambda q, **kw: tdq.tdq_attention_selected(q, s.k, s.v, chosen, cu, s.table, s.len, want_lse=True, **kw),
+                 lambda q, **kw: s.paged(q, cu, **kw), lambda q, **kw: s.paged(q, cu, prefix=prefix, **kw)):
+        want = call(Q)
+        for _ in range(3):
+            q = Q.clone()
+            got = call(q, out=q)
+            assert got[0] is q and torch.equal(q, want[0]) and torch.equal(got[1], want[1])
+
+
+def test_many_tokens_written_in_place():
+    Hq, Hk, D, P, n = 6, 2, 64, 16, 5000
+    s = Server(1, n, P, Hq, Hk, D, torch.float16)
+    other = Server(1, n, P, Hq, Hk, D, torch.float16)
+    qkv, cu = s.projection(n, 3), L.starts([n])
+    want = s.write(qkv, cu, _i32([n]))
+    Q, K, V = qkv[:, :Hq], qkv[:, Hq:Hq + Hk], qkv[:, Hq + Hk:]
+    other.len += n
+    got = tdq.tdq_cache_append(Q, K, V, other.k, other.v, cu, other.table, other.len, s.freq, q_weight=s.weight,
+                               k_weight=s.weight, out=Q)
+    assert got is Q and torch.equal(got, want)
+    assert torch.equal(other.k.view(torch.int16), s.k.view(torch.int16)) and torch.equal(other.v.view(torch.int16), s.v.view(torch.int16))
+
+
 # ---- sizes where the plan changes ----------------------------------------------------
 def _check(ql, lens, P, Hq, Hk, D, dtype=torch.float16, causal=True, seed=0, pre=(), first=()):
     """All rows, some heads."""
