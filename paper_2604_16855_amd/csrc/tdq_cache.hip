@@ -383,9 +383,7 @@ hipError_t launch_bounds(const tdq_pages* K, tdq_dtype dt, long long T, const td
 // of a workgroup.  What bounds it is the way to the first bounds (the token's sequence, its pages, the
 // bounds: 4 us), and beside the products the conversions of both operands: 32 tokens over 560 pages each, 8
 // heads of 128, 26 us (73 MB).  By products in binary32 with a bound of their error, and in binary64 only
-// where the order stays open, the scores took 21, but the choice 19 instead of 8.  16 columns of tokens and
-// heads by the 16 x 16 x 4 instruction, at two thirds of the rate, took 24 instead of 30 for 401 tokens over
-// 383 pages, as much as making the choice in the same kernel saves.
+// where the order stays open, the scores took 21, but the choice 19 instead of 8.
 struct ChoiceArgs {
   const void *Q, *lo, *hi;
   long long q_token, q_head, lo_page, lo_head, hi_page, hi_head;
@@ -414,6 +412,15 @@ __device__ __forceinline__ float neighbour(float x) {
   return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), D == 1 ? 0xB1 : 0x4E, 0xF, 0xF, true));
 }
 
+// Scores as they stand in an order of whole numbers: 0 is a page that is not there, the largest one that is
+// always taken, NaN above all numbers.
+constexpr u32 kAlways = 0xFFFFFFFFu, kNaN = 0xFFFFFFFEu;
+__device__ __forceinline__ u32 key_of(float s) {
+  if (s != s) return kNaN;
+  const u32 u = __float_as_uint(s + 0.f);                // (-0 as 0)
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
 // The pages of a token and key head: a radix select of the count-th largest key among the scores'
 // bit patterns (8 bits a pass), then the pages above it and the first ones at it, ascending.  Keys of
 // 256 HELD pages stay in registers, and `entry` is what the line of the table has of them.  Bound by the
@@ -435,13 +442,9 @@ __device__ __forceinline__ void choose(const ChoiceArgs& a, ChoiceRoom<HELD>& ro
   auto &count = room.count;
   int* out = a.chosen + id * a.count;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  // larger for a larger score; 0: not there; the largest: always taken; NaN above all numbers
   auto key = [&](int b, int page, float s) -> u32 {
     if (b >= pages || page < 0 || page >= a.seq.n_pages) return 0;
-    if (b < a.first || b >= pages - a.last) return 0xFFFFFFFFu;
-    if (s != s) return 0xFFFFFFFEu;
-    const u32 u = __float_as_uint(s + 0.f);              // (-0 as 0)
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    return b < a.first || b >= pages - a.last ? kAlways : key_of(s);
   };
   auto read = [&](int b) { return b < pages ? key(b, line[b], score(b)) : 0; };
   u32 held[HELD];
@@ -459,7 +462,7 @@ __device__ __forceinline__ void choose(const ChoiceArgs& a, ChoiceRoom<HELD>& ro
   // Keys begin with the bits that all of them share but those at the two ends; the digits follow.
   u32 both = 0xFFFFFFFFu, any = 0;
   each([&](int, u32 k) {
-    if (k != 0 && k < 0xFFFFFFFEu) {
+    if (k != 0 && k < kNaN) {
       both &= k;
       any |= k;
     }
@@ -487,7 +490,7 @@ __device__ __forceinline__ void choose(const ChoiceArgs& a, ChoiceRoom<HELD>& ro
   if (!all) {
     // those that are always taken, or NaN, come first: the lowest places of them if they are too many
     u32 c = 0;
-    u32 top_keys = 0xFFFFFFFFu;
+    u32 top_keys = kAlways;
     for (int round = 0; round < 2 && !done; ++round, --top_keys) {
       c = 0;
       each([&](int, u32 k) { c += (u32)__popcll(__ballot(k == top_keys)); });
@@ -511,7 +514,7 @@ __device__ __forceinline__ void choose(const ChoiceArgs& a, ChoiceRoom<HELD>& ro
   while (!all && !done && bits > 0) {
     const int shift = bits > 8 ? bits - 8 : 0;
     each([&](int, u32 k) {
-      if (k != 0 && k < 0xFFFFFFFEu && (bits == 32 || k >> bits == prefix >> bits)) atomicAdd(&bins[k >> shift & ((1u << (bits - shift)) - 1)], 1u);
+      if (k != 0 && k < kNaN && (bits == 32 || k >> bits == prefix >> bits)) atomicAdd(&bins[k >> shift & ((1u << (bits - shift)) - 1)], 1u);
     });
     __syncthreads();
     if (wave == 0) {
@@ -632,6 +635,20 @@ __device__ __forceinline__ void entries(const int* line, int pages, int (&entry)
   }
 }
 
+// The positive and the negative ones of 8 numbers, zeros in place of the others.
+template <typename T>
+__device__ __forceinline__ void signs_of(const u32x4& x, float* up, float* down) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const f32x2 v = two_floats<T>(x[j]);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      up[2 * j + u] = v[u] < 0.f ? 0.f : v[u];
+      down[2 * j + u] = v[u] > 0.f ? 0.f : v[u];
+    }
+  }
+}
+
 // Pages of a workgroup, 16 of a wavefront at a time.  us of both kernels with 256 and 512: D = 64, 401 tokens
 // over 383 pages on average 47 and 35 (512 are all pages, and the choice is made here), 32 tokens over 469
 // 18.5 and 16.2, 4 over 938 16 and 20; D = 128, 32 over 560 34 and 38, 4 over 938 22 and 30.
@@ -665,16 +682,7 @@ __global__ __launch_bounds__(256, W == 16 ? 3 : 4) void k_score(ChoiceArgs a) {
       if (at(pass, i) < a.D) x[i] = *reinterpret_cast<const u32x4_any*>(p + at(pass, i));
     }
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const f32x2 v = two_floats<T>(x[i][j]);
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          up[8 * i + 2 * j + u] = v[u] < 0.f ? 0.f : v[u];
-          down[8 * i + 2 * j + u] = v[u] > 0.f ? 0.f : v[u];
-        }
-      }
+    for (int i = 0; i < PIECES; ++i) signs_of<T>(x[i], up + 8 * i, down + 8 * i);
   };
   const Seen me = seen_by(q, t, a.Tq, a.causal);
   const int pages = me.keys <= 0 ? 0 : ((me.keys - 1) >> q.shift) + 1, b0 = chunk * PAGES;
@@ -763,6 +771,175 @@ __global__ __launch_bounds__(256) void k_choose(ChoiceArgs a) {
   choose(a, room, id, pages, line, entry, [&](int b) { return score[b]; });
 }
 
+// Many tokens of a sequence: 16 columns of tokens and 2^BITS heads at a time by the 16 x 16 x 4 instruction,
+// so that the bounds are read, and converted, once for all of them.  A workgroup has TOKENS tokens and, where
+// they are of several sequences, takes each run of them by itself; it keeps the keys of all their pages, and a
+// wavefront makes the choice of a token without any other: the count-th largest key bit by bit, by ballots.
+// Bound by that instruction (22 T products/s, two thirds of the small one's rate) and the ballots, about half
+// each: 8745 tokens of 4/2 heads of 32 over 355 pages 102 us.
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+constexpr int kRunPages = 1024;        // of a line, at most
+// Where it pays: two workgroups for every CU, and tokens of a sequence (on average, times the heads of a
+// column) so that few workgroups have two runs, one after the other.  us by tokens on their own and by runs:
+// 8745 tokens of 5 sequences, 4/2 heads of 32, over 355 pages 149 and 102; 2000 of 2, 32/8 of 128, over 142
+// 224 and 169; 256 of one over 473 (512 workgroups) 101 and 66.  200 of one, 32/8 of 64, over 253 (400) 27 and
+// 30; 128 of 4, 32/8 of 128, over 126 (256) 20 and 25.  30 times 30 tokens over 252 pages, 32/8 of 64 95 and
+// 102, 8/8 of 128 164 and 102; 200 times 3, 16/4 of 128 69 and 101, 8/8 of 128 123 and 227.
+constexpr long long kRunTokens = 16, kRunGroups = 512;
+template <typename T, int W, int BITS>
+__global__ __launch_bounds__(256, 2) void k_select_runs(ChoiceArgs a) {
+  constexpr int PIECES = W < 32 ? W / 8 : 4, PASSES = W / (8 * PIECES);
+  constexpr int TOKENS = 16 >> BITS, HEADS = 1 << BITS;
+  __shared__ u32 keys[TOKENS][kRunPages];
+  const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
+  const int h = (int)(id % a.Hk);
+  const long long t0 = id / a.Hk * TOKENS;
+  if (t0 >= a.Tq) return;
+  const Sequences& q = a.seq;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = lane >> 4;
+  const int token = (lane & 15) >> BITS, head = lane & (HEADS - 1);
+  const unsigned long long below = (1ull << lane) - 1;
+  auto at = [&](int pass, int i) { return 8 * (k + 4 * (pass * PIECES + i)); };   // first channel of a piece
+  for (int first = 0, n; first < TOKENS && t0 + first < a.Tq; first += n) {
+    const Owner o = owner_of(q, t0 + first, a.Tq);
+    n = 1;
+    if (t0 + first < o.from || t0 + first >= o.to) continue;
+    n = o.to - t0 < TOKENS ? (int)(o.to - t0) - first : TOKENS - first;
+    const int have = keys_in(q, o.len);
+    auto pages_of = [&](int i) {                         // that token first + i sees
+      const long long e = a.causal ? have - o.to + t0 + first + i + 1 : have;
+      return e <= 0 ? 0 : (int)((e - 1) >> q.shift) + 1;
+    };
+    const int pages = pages_of(n - 1);
+    const int* line = q.table + o.seq * q.ld;
+    const long long t = t0 + first + (token < n ? token : n - 1);   // of the lane's column
+    auto page_of = [&](int b) {
+      int p = -1;
+      if (b + (lane & 15) < pages) p = line[b + (lane & 15)];
+      return p < q.n_pages ? p : -1;
+    };
+#pragma unroll 1
+    for (int e0 = 0; e0 < a.group; e0 += HEADS) {
+      float up[8 * PIECES], down[8 * PIECES];
+      auto query = [&](int pass) {
+        // (past the last head: the last again, which changes no maximum)
+        const int row = h * a.group + (e0 + head < a.group ? e0 + head : a.group - 1);
+        const T* p = static_cast<const T*>(a.Q) + t * a.q_token + row * a.q_head;
+        u32x4 x[PIECES];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+          x[i] = u32x4{0, 0, 0, 0};
+          if (at(pass, i) < a.D) x[i] = *reinterpret_cast<const u32x4_any*>(p + at(pass, i));
+        }
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) signs_of<T>(x[i], up + 8 * i, down + 8 * i);
+      };
+      int page = page_of(16 * wave);
+      if (PASSES == 1) query(0);
+#pragma unroll 1
+      for (int b = 16 * wave; b < pages; b += 64) {
+        const T* lo = static_cast<const T*>(a.lo) + (long long)page * a.lo_page + h * a.lo_head;
+        const T* hi = static_cast<const T*>(a.hi) + (long long)page * a.hi_page + h * a.hi_head;
+        const unsigned there = (unsigned)__ballot(page >= 0);   // (of the first 16 lanes)
+        f64x4 part[2] = {{0.0, 0.0, 0.0, 0.0}, {0.0, 0.0, 0.0, 0.0}};
+#pragma unroll 1
+        for (int pass = 0; pass < PASSES; ++pass) {
+          u32x4 los[PIECES], his[PIECES];
+#pragma unroll
+          for (int i = 0; i < PIECES; ++i) {
+            los[i] = his[i] = u32x4{0, 0, 0, 0};
+            if (page >= 0 && at(pass, i) < a.D) {
+              los[i] = *reinterpret_cast<const u32x4_any*>(lo + at(pass, i));
+              his[i] = *reinterpret_cast<const u32x4_any*>(hi + at(pass, i));
+            }
+          }
+          if (PASSES > 1) query(pass);
+#pragma unroll
+          for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const f32x2 l = two_floats<T>(los[i][j]), g = two_floats<T>(his[i][j]);
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                float x = up[8 * i + 2 * j + u], y = down[8 * i + 2 * j + u];
+                if constexpr (W > 16) asm volatile("" : "+v"(x), "+v"(y));   // (as above)
+                part[0] = __builtin_amdgcn_mfma_f64_16x16x4f64((double)g[u], (double)x, part[0], 0, 0, 0);
+                part[1] = __builtin_amdgcn_mfma_f64_16x16x4f64((double)l[u], (double)y, part[1], 0, 0, 0);
+              }
+            }
+        }
+        page = page_of(b + 64);
+        // element r of lane 16 i + j: page 4 r + i, column j
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float best = (float)(part[0][r] + part[1][r]);
+          if (BITS > 0) best = most(best, neighbour<1>(best));
+          if (BITS > 1) best = most(best, neighbour<2>(best));
+          const int mine = 4 * r + k;
+          if (head == 0 && b + mine < pages) {
+            u32 x = there >> mine & 1 ? key_of(best) : 0;
+            if (e0 > 0) x = max(x, keys[token][b + mine]);   // (written by this lane)
+            keys[token][b + mine] = x;
+          }
+        }
+      }
+    }
+    __syncthreads();
+    for (int i = wave; i < n; i += 4) {
+      const int seen = pages_of(i);
+      int* out = a.chosen + ((t0 + first + i) * a.Hk + h) * a.count;
+      u32 held[kRunPages / 64];
+#pragma unroll
+      for (int j = 0; j < kRunPages / 64; ++j) {
+        const int b = 64 * j + lane;
+        held[j] = 0;
+        if (64 * j < seen) {
+          if (b < seen) held[j] = keys[i][b];
+          if (held[j] != 0 && (b < a.first || b >= seen - a.last)) held[j] = kAlways;
+        }
+      }
+      // limit: the count-th largest, or 0 if there are fewer; `want` of those at it are taken
+      u32 limit = 0;
+      int want = 0;
+      if (seen > a.count) {
+        for (u32 bit = 1u << 31; bit; bit >>= 1) {
+          const u32 at_least = limit | bit;
+          int c = 0;
+#pragma unroll
+          for (int j = 0; j < kRunPages / 64; ++j)
+            if (64 * j < seen) c += __popcll(__ballot(held[j] >= at_least));
+          if (c < a.count) continue;
+          limit = at_least;
+          if (c == a.count) {                            // those and no others
+            --limit;
+            break;
+          }
+        }
+        int above = 0;
+#pragma unroll
+        for (int j = 0; j < kRunPages / 64; ++j)
+          if (64 * j < seen) above += __popcll(__ballot(held[j] > limit));
+        want = limit > 0 ? a.count - above : 0;
+      }
+      int taken = 0, same = 0;                           // in front: above the limit, and at it
+#pragma unroll
+      for (int j = 0; j < kRunPages / 64; ++j)
+        if (64 * j < seen) {
+          const bool more = held[j] > limit, even = want > 0 && held[j] == limit;
+          const unsigned long long m = __ballot(more), e = __ballot(even);
+          const int rank = same + __popcll(e & below);
+          const int place = taken + __popcll(m & below) + (rank < want ? rank : want);
+          if (more || (even && rank < want)) out[place] = 64 * j + lane;
+          taken += __popcll(m);
+          same += __popcll(e);
+        }
+      taken += same < want ? same : want;
+      for (int j = taken + lane; j < a.count; j += 64) out[j] = -1;
+    }
+    __syncthreads();                                     // (the keys have been read)
+  }
+}
+
 size_t choice_workspace(long long Tq, int Hk, int columns) { return (size_t)Tq * Hk * columns * sizeof(float); }
 
 hipError_t launch_choice(const tdq_heads* Q, const tdq_heads* lo, const tdq_heads* hi, tdq_dtype dt, long long Tq,
@@ -787,10 +964,33 @@ hipError_t launch_choice(const tdq_heads* Q, const tdq_heads* lo, const tdq_head
   a.first = first;
   a.last = last;
   a.count = count;
-  const int pages = score_pages(D <= 32 ? 8 : D <= 64 ? 16 : D <= 128 ? 32 : 64);
-  a.chunks = (seq->columns + pages - 1) / pages;
   a.score = static_cast<float*>(workspace);
   a.chosen = chosen;
+  const int bits = a.group > 2 ? 2 : a.group - 1;
+  const long long run_groups = (Tq + (16 >> bits) - 1) / (16 >> bits) * Hk;
+  if (seq->columns <= kRunPages && Tq >= (kRunTokens << bits) * seq->S && run_groups >= kRunGroups) {
+    const dim3 grid = two_axes(run_groups);
+#define TDQ_RUN(T_, W)                                                                                    \
+  do {                                                                                                    \
+    if (bits == 2) hipLaunchKernelGGL((k_select_runs<T_, W, 2>), grid, dim3(256), 0, st, a);              \
+    else if (bits == 1) hipLaunchKernelGGL((k_select_runs<T_, W, 1>), grid, dim3(256), 0, st, a);         \
+    else hipLaunchKernelGGL((k_select_runs<T_, W, 0>), grid, dim3(256), 0, st, a);                        \
+  } while (0)
+#define TDQ_RUNS(T_)                    \
+  do {                                  \
+    if (D <= 32) TDQ_RUN(T_, 8);        \
+    else if (D <= 64) TDQ_RUN(T_, 16);  \
+    else if (D <= 128) TDQ_RUN(T_, 32); \
+    else TDQ_RUN(T_, 64);               \
+  } while (0)
+    if (dt == TDQ_F16) TDQ_RUNS(_Float16);
+    else TDQ_RUNS(__bf16);
+#undef TDQ_RUNS
+#undef TDQ_RUN
+    return hipGetLastError();
+  }
+  const int pages = score_pages(D <= 32 ? 8 : D <= 64 ? 16 : D <= 128 ? 32 : 64);
+  a.chunks = (seq->columns + pages - 1) / pages;
   const dim3 grid = two_axes(Tq * Hk * a.chunks);
 #define TDQ_SCORE(T_, W)                                                                              \
   do {                                                                                                \

@@ -265,6 +265,46 @@ def test_choice_of_many_pages():
     _check_choice([1], [16 * 4000 - 5], 16, 1, 1, 16, torch.bfloat16, 2700, 0, 0)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Hq,Hk,D,T", [(8, 2, 64, 1030), (4, 4, 32, 2050), (12, 4, 128, 520), (16, 8, 80, 530), (10, 1, 256, 2060),
+                                       (64, 64, 8, 260)])
+def test_choice_of_many_tokens(Hq, Hk, D, T, dtype):
+    """Tokens of a sequence together: runs that end inside a workgroup's tokens, queries that see few pages or none."""
+    for ql, lens, P, count, causal in (([T], [T], 32, 4, True), ([T - 203, 3, 200], [T + 300, 5, 150], 64, 6, True),
+                                       ([T - 77, 0, 77], [500, 100, 16 * 200], 16, 9, False)):
+        print(f"[choice] {ql} {lens} P={P} count={count} {Hq}/{Hk} D={D} {dtype}", flush=True)
+        _check_choice(ql, lens, P, Hq, Hk, D, dtype, count, causal=causal)
+
+
+def test_choice_of_many_tokens_and_pages():
+    """As many pages as fit, nearly all of them, one more than fit; scores that tie, strange ones, no sequence."""
+    def few(Q, lo, hi, table):
+        return Q.sign(), torch.full_like(lo, -1), (torch.arange(hi.shape[0], device="cuda") % 3)[:, None, None].to(hi.dtype).expand_as(hi).contiguous(), table
+
+    def strange(Q, lo, hi, table):
+        hi[table[0, 7], 0, 3], hi[table[0, 9], 0, 2], lo[table[0, 11]] = float("nan"), float("inf"), -float("inf")
+        table = table.clone()
+        table[0, 0], table[0, 5], table[0, 40] = -1, 1 << 30, -7
+        return Q, lo, hi, table
+
+    T = 260
+    for pages in (1024, 1025):
+        _check_choice([T], [16 * pages - 3], 16, 8, 8, 16, torch.float16, 40, 2, 3)
+    _check_choice([T], [16 * 1000], 16, 32, 8, 16, torch.bfloat16, 990)
+    _check_choice([T], [16 * 300], 16, 32, 8, 32, torch.float16, 50, change=few)
+    for count in (1, 3, 60, 200):
+        _check_choice([T], [16 * 100], 16, 32, 8, 32, torch.float16, count, min(1, count - 1), 0, change=strange)
+    _check_choice([T], [16 * 100], 16, 32, 8, 32, torch.bfloat16, 4, change=lambda Q, lo, hi, t: (Q, lo, hi, t * 0 - 1))
+    c = U.Cache([700], 16, 1, 8, torch.float16)
+    n = c.k.shape[0]
+    lo, hi = L.randn(n, 8, 32, seed=1, dtype=torch.float16), L.randn(n, 8, 32, seed=2, dtype=torch.float16)
+    Q = L.randn(300, 32, 32, dtype=torch.float16)
+    out = torch.full((300, 8, 5), 77, dtype=torch.int32, device="cuda")
+    tdq.tdq_select_pages(Q, lo, hi, _i32([6, 280]), c.table, c.len, 16, 5, out=out)
+    assert bool((out[:6] == 77).all()) and bool((out[280:] == 77).all())
+    assert torch.equal(out[6:280], _choice(Q[6:280], lo, hi, [274], [700], c.table, 16, 5, 1, 1, True))
+
+
 def test_choice_where_scores_tie():
     """Few different scores: the lower page is better.  All the same, and zeros of both signs."""
     def few(Q, lo, hi, table):
