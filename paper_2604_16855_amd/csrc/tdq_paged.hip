@@ -201,6 +201,7 @@ template <int DP>
 constexpr int kStages = DP <= 128 ? 2 : 1;
 template <int DP>
 struct Shared {
+  static constexpr int kWaves = 4;
   union {
     uint8_t many[kStages<DP>][2][kTileKeys * 2 * DP];  // [stage][K, V]
     uint8_t few[4][2][kFewKeys * 2 * DP];              // [wavefront][K, V]
@@ -209,13 +210,23 @@ struct Shared {
   float ml[4][kFewRows][2];
   Place place[4][64];                                  // [wavefront][tile] (many)
 };
+// The same for few rows and one wavefront or four.
+template <int DP, int WAVES>
+struct SharedFew {
+  static constexpr int kWaves = WAVES;
+  union {
+    uint8_t few[WAVES][2][kFewKeys * 2 * DP];
+    float o[WAVES][kFewRows][DP + 4];
+  };
+  float ml[WAVES][kFewRows][2];
+};
 
 // Zeros where a whole granule's copies leave LDS alone and products of K read it.
-template <int DP>
-__device__ __forceinline__ void clear(Shared<DP>& sh) {
+template <typename S>
+__device__ __forceinline__ void clear(S& sh) {
   __syncthreads();
   u32x4* p = reinterpret_cast<u32x4*>(&sh);
-  for (int i = threadIdx.x; i < (int)(sizeof(sh.few) / 16); i += 256) p[i] = u32x4{0, 0, 0, 0};
+  for (int i = threadIdx.x; i < (int)(sizeof(sh.few) / 16); i += 64 * S::kWaves) p[i] = u32x4{0, 0, 0, 0};
   __syncthreads();
 }
 
@@ -372,11 +383,11 @@ struct Few16 {
 };
 // Up to R::kRows rows: the wavefronts share out the tiles of 32 keys from lo to hi, each copying its own, K
 // of the next while it works on V of this and the other way round; their parts are joined in LDS.
-template <typename R, typename T, int DP, int DC, typename S, typename G, typename F>
-__device__ __forceinline__ void attend_few(Shared<DP>& sh, const S& store, G where, const T* qp, int D,
+template <typename R, typename T, int DP, int DC, typename S, typename G, typename F, typename SH>
+__device__ __forceinline__ void attend_few(SH& sh, const S& store, G where, const T* qp, int D,
                                            int sees, int all, int lo, int hi, int rows, bool once, u32 flip, float c,
                                            float lift, F target) {
-  constexpr int BYTES = kGranule * 2 * DP, COPIES = 2 * GranuleCopy<T, DP, place_k<DP>>::N;
+  constexpr int WAVES = SH::kWaves, BYTES = kGranule * 2 * DP, COPIES = 2 * GranuleCopy<T, DP, place_k<DP>>::N;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const u32 lk = lds_address(sh.few[wave][0]), lv = lds_address(sh.few[wave][1]);
   struct Two {
@@ -388,13 +399,13 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const S& store, G whe
   int held_key = 0, base = 0;
   auto hold = [&](int i) {
     base = i;
-    const Granule g = where(2 * (i + 4 * (lane >> 1)) + (lane & 1));
+    const Granule g = where(2 * (i + WAVES * (lane >> 1)) + (lane & 1));
     held = store.place(g);
     held_key = g.key;
   };
   auto look = [&](int i) {
-    if (i - base == 4 * 32) hold(i);
-    const int from = (i - base) >> 1;
+    if (i - base == 32 * WAVES) hold(i);
+    const int from = (i - base) / WAVES * 2;
     return Two{{store.spot(read_lane(held, from), __builtin_amdgcn_readlane(held_key, from), quick),
                 store.spot(read_lane(held, from + 1), __builtin_amdgcn_readlane(held_key, from + 1), quick)}};
   };
@@ -416,13 +427,13 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const S& store, G whe
     copy_v(next);
     key[0] = next.s[0].key;
     key[1] = next.s[1].key;
-    if (i + 4 < hi) next = look(i + 4);
+    if (i + WAVES < hi) next = look(i + WAVES);
   }
   R r;
   r.w.start(qp, D, flip);
   r.w.addresses(lk, lv);
-  for (; i < hi; i += 4) {
-    const bool more = i + 4 < hi;
+  for (; i < hi; i += WAVES) {
+    const bool more = i + WAVES < hi;
     // (copies arrive in order: all but the last COPIES, those of V, are there)
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
     r.scores();
@@ -438,7 +449,7 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const S& store, G whe
       copy_v(next);
       key[0] = next.s[0].key;
       key[1] = next.s[1].key;
-      if (i + 8 < hi) next = look(i + 8);
+      if (i + 2 * WAVES < hi) next = look(i + 2 * WAVES);
     }
   }
 
@@ -453,9 +464,9 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const S& store, G whe
   __syncthreads();                                       // (nobody reads K and V any more)
   float m = -INFINITY, sum = 0.f;
 #pragma unroll
-  for (int v = 0; v < 4; ++v) m = fmaxf(m, sh.ml[v][mine][0]);
+  for (int v = 0; v < WAVES; ++v) m = fmaxf(m, sh.ml[v][mine][0]);
 #pragma unroll
-  for (int v = 0; v < 4; ++v) {
+  for (int v = 0; v < WAVES; ++v) {
     const float mv = sh.ml[v][mine][0], lv = sh.ml[v][mine][1];
     if (!no_weight(mv, lv)) sum += lv * __builtin_amdgcn_exp2f((mv - m) * c);
   }
@@ -469,12 +480,12 @@ __device__ __forceinline__ void attend_few(Shared<DP>& sh, const S& store, G whe
   __syncthreads();
   const Target<T> to = target();
   constexpr int QUADS = DC / 4;
-  for (int e = threadIdx.x; e < rows * QUADS; e += 256) {
+  for (int e = threadIdx.x; e < rows * QUADS; e += 64 * WAVES) {
     const int r = e / QUADS, d = 4 * (e % QUADS);
     if (d >= to.D) continue;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int v = 0; v < 4; ++v) y += *reinterpret_cast<const f32x4*>(&sh.o[v][r][d]);
+    for (int v = 0; v < WAVES; ++v) y += *reinterpret_cast<const f32x4*>(&sh.o[v][r][d]);
     const float mr = sh.ml[0][r][0], lr = sh.ml[0][r][1];
     if (to.po) {
       *reinterpret_cast<f32x4*>(to.po + (long long)r * to.D + d) = y;
@@ -1071,7 +1082,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
         }
         return to;
       };
-      if (a.D < DC) clear<DP>(sh);
+      if (a.D < DC) clear(sh);
       const bool few = rows <= kFewRows;
       const int mine_row = few ? lane & 15 : wave * 32 + (lane & 31);
       const int row = mine_row < rows ? mine_row : rows - 1;
@@ -1295,7 +1306,7 @@ hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages*
 // chosen pages
 // ---------------------------------------------------------------------------
 // Every token and key head has a list of pages of its own, so a tile has the group's rows and no more;
-// its pages are shared out to `splits` workgroups, and in each to four wavefronts.  Pages of single tokens are
+// its pages are shared out to `splits` workgroups, and in each to four wavefronts, or, of many lists, one.  Pages of single tokens are
 // read once, at 6.2 TB/s (32 tokens, 64 pages of 64 keys, 8 heads of 128: 87 us); those of a prompt's tokens
 // come from the caches, at 14 TB/s (401 tokens, 16 pages, 4 heads of 64: 29 us).
 struct ChosenArgs {
@@ -1315,10 +1326,10 @@ struct ChosenArgs {
   float *part_o, *part_ml;             // [Tq Hq][splits]
 };
 
-template <typename T, int DP, int DC>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 2 : 1))) void k_attend_chosen(
+template <typename T, int DP, int DC, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 2 : 1))) void k_attend_chosen(
     ChosenArgs a) {
-  __shared__ __attribute__((aligned(1024))) Shared<DP> sh;
+  __shared__ __attribute__((aligned(1024))) SharedFew<DP, WAVES> sh;
   const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
   const int hk = (int)(id % a.Hk), split = (int)(id / a.Hk % a.splits);
   const long long rest = id / a.Hk / a.splits;
@@ -1361,7 +1372,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   const int share = (tiles + a.splits - 1) / a.splits;
   const int lo = split * share < tiles ? split * share : tiles, hi = lo + share < tiles ? lo + share : tiles;
   Chosen where = {list, q.table + s * q.ld, used, q.shift, q.n_pages, keys};
-  if (a.D < DC) clear<DP>(sh);
+  if (a.D < DC) clear(sh);
   attend_few<Few16<T, DP, DC>, T, DP, DC>(sh, store, where,
                                           static_cast<const T*>(a.Q) + t * a.q_token + (h0 + row) * a.q_head, a.D, sees,
                                           sees, lo, hi, rows, to - from == 1, a.flip, a.scale_log2, a.lift,
@@ -1392,6 +1403,15 @@ static int chosen_splits(long long Tq, int Hq, int Hk, int page_size, int count)
   if (n > most) n = most;
   if (n > 64) n = 64;
   return n > 1 ? (int)n : 1;
+}
+// Lists by a wavefront each, if there are three times as many as four wavefronts each have room for at a time
+// (LDS: 256 CUs, 256 / D workgroups on each): no keys too few for four, no parts to join, no waiting for the
+// slowest.  us by four and by one: 3200 tokens of 4 heads of 64, lists of 96 keys 64 and 29, of 1024 165 and 138,
+// 800 tokens of those 21 and 11, 48 and 45, 401 of 1024 keys 29 and 36; 800 tokens of 8 heads of 128 69 and 30,
+// 180 and 136, 128 tokens 15 and 11, 33 and 41; 128 tokens of 8 heads of 256 32 and 15, 85 and 68.
+static bool chosen_by_one(long long lists, int D) {
+  const int row = D <= 32 ? 32 : D <= 64 ? 64 : D <= 128 ? 128 : 256;
+  return lists * row >= 3ll * 256 * 256;
 }
 static size_t chosen_ml_bytes(long long Tq, int Hq, int splits) {
   return ((size_t)Tq * Hq * splits * 2 * sizeof(float) + 255) & ~(size_t)255;
@@ -1431,7 +1451,12 @@ hipError_t launch_chosen(const tdq_heads* Q, const tdq_pages* K, const tdq_pages
                  ? reinterpret_cast<float*>(static_cast<char*>(workspace) + chosen_ml_bytes(Tq, Hq, a.splits))
                  : nullptr;
   const dim3 grid = two_axes(Tq * a.tiles * a.splits * Hk);
-#define TDQ_CHOSEN(T, DP, DC) hipLaunchKernelGGL((k_attend_chosen<T, DP, DC>), grid, dim3(256), 0, st, a)
+  const bool one = chosen_by_one(Tq * a.tiles * a.splits * Hk, D);
+#define TDQ_CHOSEN(T, DP, DC)                                                                           \
+  do {                                                                                                  \
+    if (one) hipLaunchKernelGGL((k_attend_chosen<T, DP, DC, 1>), grid, dim3(64), 0, st, a);             \
+    else hipLaunchKernelGGL((k_attend_chosen<T, DP, DC, 4>), grid, dim3(256), 0, st, a);                \
+  } while (0)
   if (dt == TDQ_F16) TDQ_BY_HEAD(TDQ_CHOSEN, _Float16);
   else TDQ_BY_HEAD(TDQ_CHOSEN, __bf16);
 #undef TDQ_CHOSEN

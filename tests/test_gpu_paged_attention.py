@@ -229,6 +229,17 @@ def test_chosen(Hq, Hk, D, dtype):
             _chosen(ql, lens, P, Hq, Hk, D, dtype, count, causal)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Hq,Hk,D,T", [(32, 8, 128, 200), (16, 8, 64, 400), (12, 12, 32, 530), (16, 16, 8, 400), (8, 8, 256, 110),
+                                       (20, 10, 96, 160), (18, 1, 184, 400), (6, 6, 200, 140)])
+def test_lists_of_many_tokens(Hq, Hk, D, T, dtype):
+    for ql, lens, P, count in (([T], [T + 50], 16, 5), ([T - 40, 1, 39], [T - 40, 700, 0], 32, 9), ([T // 2, T - T // 2], [4, 1300], 64, 3)):
+        print(f"[chosen] {ql} {lens} P={P} count={count} {Hq}/{Hk} D={D} {dtype}", flush=True)
+        for causal in (True, False):
+            _chosen(ql, lens, P, Hq, Hk, D, dtype, count, causal)
+    _chosen([T], [400], 16, Hq, Hk, D, dtype, 6, pick=lambda n: [5, -1, 0, 99999, n - 1, 3])
+
+
 def test_chosen_in_any_order_and_none():
     _chosen([1, 4], [300, 100], 16, 4, 2, 64, torch.float16, 6, pick=lambda n: [5, -1, 0, 3])
     _chosen([1, 4], [300, 100], 16, 4, 2, 64, torch.float16, 6, pick=lambda n: [-1, -1, n - 1, 99999, -1, 2])
