@@ -510,18 +510,18 @@ struct Run {
   int count;
 };
 
-// Joins the parts of two runs for a row, by a wavefront.  A group of lanes has four outputs each of one
-// part, as many parts at a time as there are groups, the first ones on their way with the sums; weights are
-// found before, a lane a part.
+// Joins the parts of two runs for a row, by WAVES wavefronts that share them out.  A group of lanes has four
+// outputs each of one part, as many parts at a time as there are groups, four times as many on their way, the
+// first of them with the sums; weights are found before, a lane a part, by each wavefront for itself.
 constexpr int kMaxPieces = 512;        // of a line
 constexpr int kMaxParts = kMaxPieces + 4;
-template <typename T>
-__device__ __forceinline__ void join_row(float* weight, const Run& a, const Run& b, int D, float scale_log2, T* op,
-                                         float* lse) {
+template <typename T, int WAVES>
+__device__ __forceinline__ void join_row(float* weight, float (*sums)[TDQ_MAX_HEAD], const Run& a, const Run& b, int D,
+                                         float scale_log2, T* op, float* lse) {
   constexpr int AHEAD = 4;
-  const int lane = threadIdx.x & 63, n = a.count + b.count;
+  const int lane = threadIdx.x & 63, wave = WAVES > 1 ? threadIdx.x >> 6 : 0, n = a.count + b.count;
   const int quads = D <= 32 ? 8 : D <= 64 ? 16 : D <= 128 ? 32 : 64;
-  const int c = 4 * (lane & (quads - 1)), group = lane / quads, groups = 64 / quads;
+  const int c = 4 * (lane & (quads - 1)), groups = 64 / quads * WAVES, group = lane / quads * WAVES + wave;
   auto row = [&](int i) {                                // of its run
     const bool first = i < a.count;
     const int at = first ? i : i - a.count;
@@ -529,13 +529,16 @@ __device__ __forceinline__ void join_row(float* weight, const Run& a, const Run&
   };
   auto ml = [&](int i) { return *reinterpret_cast<const f32x2*>((i < a.count ? a.ml : b.ml) + 2 * row(i)); };
   auto value = [&](int i) { return *reinterpret_cast<const f32x4*>((i < a.count ? a.o : b.o) + row(i) * D + c); };
-  f32x4 early[AHEAD];
+  f32x4 ahead[AHEAD];
+  auto fetch = [&](int i0) {
 #pragma unroll
-  for (int j = 0; j < AHEAD; ++j) {
-    const int i = group + j * groups;
-    early[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (c < D && i < n) early[j] = value(i);
-  }
+    for (int j = 0; j < AHEAD; ++j) {
+      const int i = i0 + j * groups;
+      ahead[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (c < D && i < n) ahead[j] = value(i);
+    }
+  };
+  fetch(group);
   f32x2 own = {-INFINITY, 0.f};                          // of part `lane`
   if (lane < n) own = ml(lane);
   float m = own[0];
@@ -557,25 +560,27 @@ __device__ __forceinline__ void join_row(float* weight, const Run& a, const Run&
   for (int d = 32; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
   __builtin_amdgcn_wave_barrier();
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
-  if (c < D) {
+  for (int i0 = group; i0 < n; i0 += AHEAD * groups) {
+    if (i0 != group) fetch(i0);
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
-      const int i = group + j * groups;
+      const int i = i0 + j * groups;
       const float f = i < n ? weight[i] : -1.f;
-      if (!(f < 0.f)) y += early[j] * f;
-    }
-#pragma unroll 4
-    for (int i = group + AHEAD * groups; i < n; i += groups) {
-      const f32x4 x = value(i);
-      const float f = weight[i];
-      if (!(f < 0.f)) y += x * f;
+      if (!(f < 0.f)) y += ahead[j] * f;
     }
   }
   for (int d = 32; d >= quads; d >>= 1)
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] += __shfl_xor(y[i], d, 64);
+  if constexpr (WAVES > 1) {
+    if (lane < quads) *reinterpret_cast<f32x4*>(&sums[wave][c]) = y;
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) y += *reinterpret_cast<const f32x4*>(&sums[w][c]);
+  }
   const float inv = no_weight(m, l) ? 0.f : 1.0f / l;
-  if (group == 0 && c < D) {
+  if (lane < quads && c < D) {
     const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
     store_floats<T, 4>(op + c, z);
     if (lse && lane == 0) *lse = log_sum(m, l, scale_log2);
@@ -1113,17 +1118,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   }
 }
 
+// Rows of a call that four wavefronts each join: few rows have parts of up to 512 pieces, and wait for them.  us
+// by one and by four: 8 rows over 100000 keys 88 and 43, of a prefix of 21354 35 and 25, 64 rows over 10947 26 and
+// 21, 512 over 4000 to 32000 196 both; 1824 rows behind 11399 31 and 35, 2048 over 100 to 1000 38 and 41.
+constexpr int kWholeRows = 512;
+
 // Joins the tiles that lie in several pieces, and prefixes with sequences.  A wavefront has `heads` rows of
 // a token, as many at a time as 4 outputs a lane allow; rows of many parts take all of it one by one.  What
 // bounds it is a chain of four loads (the token's place, its tiles, their sums, their values), 5 us for single
 // tokens, and the parts of many rows, 67 MB of 2257 tokens 24 us.
-template <typename T>
+template <typename T, int WAVES>
 __global__ __launch_bounds__(256, 4) void k_join_pages(PagedArgs a, int heads, int chunks) {
   __shared__ float weight[4][kMaxParts];
+  __shared__ __attribute__((aligned(16))) float sums[WAVES][TDQ_MAX_HEAD];
   const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
   const long long t = id / chunks;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h0 = ((int)(id % chunks) * 4 + wave) * heads, h1 = h0 + heads < a.Hq ? h0 + heads : a.Hq;
+  const int h0 = WAVES > 1 ? (int)(id % chunks) : ((int)(id % chunks) * 4 + wave) * heads, h1 = h0 + heads < a.Hq ? h0 + heads : a.Hq;
   if (t >= a.Tq || h0 >= a.Hq) return;
   const int lane = threadIdx.x & 63;
   // (all on their way at once; what lies there is looked at if the token is one of a sequence)
@@ -1180,13 +1191,14 @@ __global__ __launch_bounds__(256, 4) void k_join_pages(PagedArgs a, int heads, i
     T* op = static_cast<T*>(a.O) + t * a.o_token;
     float* lse = a.lse ? a.lse + t * a.Hq : nullptr;
     if (__ballot(wanted && x.count + y.count > kFewParts) == 0) {
-      if (wanted) join_few<T>(x, y, c, a.D, a.scale_log2, op + h * a.o_head, lse ? lse + h : nullptr);
+      if (wanted && (WAVES == 1 || wave == 0)) join_few<T>(x, y, c, a.D, a.scale_log2, op + h * a.o_head, lse ? lse + h : nullptr);
       continue;
     }
     for (int i = 0; i < 64; i += quads) {
       if (!__shfl((int)wanted, i, 64)) continue;
       const int g = hb + i / quads;
-      join_row<T>(weight[wave], run_of(x, i), run_of(y, i), a.D, a.scale_log2, op + g * a.o_head, lse ? lse + g : nullptr);
+      join_row<T, WAVES>(weight[wave], sums, run_of(x, i), run_of(y, i), a.D, a.scale_log2, op + g * a.o_head,
+                         lse ? lse + g : nullptr);
     }
   }
 }
@@ -1292,13 +1304,20 @@ hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages*
   if (dt == TDQ_F16) TDQ_BY_HEAD(TDQ_PAGED, _Float16);
   else TDQ_BY_HEAD(TDQ_PAGED, __bf16);
 #undef TDQ_PAGED
-  // Few tokens: many parts a row, a wavefront each.  us with 1 and 8 rows a wavefront: 64 tokens behind a
+  // Few tokens: many parts a row, a wavefront each, or four.  us with 1 and 8 rows a wavefront: 64 tokens behind a
   // prefix 87 and 120; 4 prompts' parts of 300 to 1024 tokens 318 and 297; 8 x 2048 tokens 546 and 393.
   const int heads = Tq * Hq > 16384 ? 8 : 1;
-  const int chunks = (Hq + 4 * heads - 1) / (4 * heads);
+  const bool whole = Tq * Hq <= kWholeRows;
+  const int chunks = whole ? Hq : (Hq + 4 * heads - 1) / (4 * heads);
   const dim3 join = two_axes(Tq * chunks);
-  if (dt == TDQ_F16) hipLaunchKernelGGL((k_join_pages<_Float16>), join, dim3(256), 0, st, a, heads, chunks);
-  else hipLaunchKernelGGL((k_join_pages<__bf16>), join, dim3(256), 0, st, a, heads, chunks);
+#define TDQ_JOIN(T)                                                                                                 \
+  do {                                                                                                              \
+    if (whole) hipLaunchKernelGGL((k_join_pages<T, 4>), join, dim3(256), 0, st, a, 1, chunks);                      \
+    else hipLaunchKernelGGL((k_join_pages<T, 1>), join, dim3(256), 0, st, a, heads, chunks);                        \
+  } while (0)
+  if (dt == TDQ_F16) TDQ_JOIN(_Float16);
+  else TDQ_JOIN(__bf16);
+#undef TDQ_JOIN
   return hipGetLastError();
 }
 
@@ -1389,7 +1408,7 @@ __global__ __launch_bounds__(256, 4) void k_join_chosen(ChosenArgs a) {
   const Sequences& q = a.seq;
   const int s = last_at_most(q.S, t, [&](int i) { return start_of(q.cu, i, a.Tq); });
   if (t < start_of(q.cu, s, a.Tq) || t >= start_of(q.cu, s + 1, a.Tq)) return;
-  join_row<T>(weight[threadIdx.x >> 6], Run{}, Run{a.part_ml + 2 * row, a.part_o + row * a.D, a.Tq * a.Hq, 0, a.splits},
+  join_row<T, 1>(weight[threadIdx.x >> 6], nullptr, Run{}, Run{a.part_ml + 2 * row, a.part_o + row * a.D, a.Tq * a.Hq, 0, a.splits},
               a.D, a.scale_log2,
               static_cast<T*>(a.O) + t * a.o_token + h * a.o_head, a.lse ? a.lse + row : nullptr);
 }

@@ -300,6 +300,15 @@ def test_one_head_and_many_tiles():
     _check([128] * 200, [128 + 3 * (i % 11) for i in range(200)], 16, 8, 1, 32)
 
 
+def test_rows_of_many_parts():
+    """Few rows over so many keys that every workgroup has a part of them."""
+    _check([1], [100000], 64, 8, 1, 64, torch.bfloat16)
+    _check([2], [70001], 16, 3, 1, 200)
+    _check([1, 1], [60000, 4], 128, 2, 2, 8)
+    _check([1, 1, 2], [5, 900, 30], 16, 4, 1, 128, pre=[50000], first=[0, 3])
+    _check([100], [40000], 64, 6, 1, 32, torch.bfloat16)
+
+
 def test_many_items_and_prefixes():
     """More sequences than threads, with prefixes; more prefixes than lanes."""
     n = 300
