@@ -664,7 +664,8 @@ struct PagedArgs {
   int2* first_tile;                    // [prefixes + 1]: tiles of sequences and prefixes; of each those in front, first token
   int2* tiles;                         // [own_tiles + pre_tiles][Hk]: first piece of each, how many; sequences first
   long long own_tiles, pre_tiles;      // (room for so many)
-  int4* place;                         // [Tq]: sequence, tile and row of it of a token's first row
+  int4* place;                         // [Tq]: tile, row of it and sequence of a token's first row; or, of
+  bool by_tile;                        // [own_tiles]: first token, rows of it in front, rows, sequence of a tile
   float *part_o, *part_ml;             // [pieces Hk][2][cap]: of tiles that begin before a piece, and that end behind it
   float *whole_o, *whole_ml;           // with prefixes: [2][Tq Hq], of tiles of one (prefixes, sequences) in one piece
 };
@@ -1018,7 +1019,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
         }
         a.tiles[tile * a.Hk + hk] = make_int2(k, last - k + 1);
       }
-      if (hk == 0 && !prefix) {
+      if (hk == 0 && !prefix && a.by_tile) {
+        if (tid == 0 && tile < a.own_tiles) a.place[tile] = make_int4(t0, first, rows, line);
+      } else if (hk == 0 && !prefix) {
         // tokens whose first row lies in the tile
         const int row = tid * a.group - first;
         if (row >= 0 && row < rows) a.place[t0 + tid] = make_int4(tile0 - pre_tiles + r, row, line, 0);
@@ -1118,88 +1121,139 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   }
 }
 
-// Rows of a call that four wavefronts each join: few rows have parts of up to 512 pieces, and wait for them.  us
-// by one and by four: 8 rows over 100000 keys 88 and 43, of a prefix of 21354 35 and 25, 64 rows over 10947 26 and
-// 21, 512 over 4000 to 32000 196 both; 1824 rows behind 11399 31 and 35, 2048 over 100 to 1000 38 and 41.
-constexpr int kWholeRows = 512;
+// Whether a sequence has a prefix, and that one's first tile and token.
+struct Before {
+  bool there;
+  int2 first;
+};
+__device__ __forceinline__ Before prefix_of(const PagedArgs& a, int line) {
+  const int lane = threadIdx.x & 63;
+  Before b = {false, make_int2(0, 0)};
+  if (a.pre.S <= 64) {                                   // all at once, a lane each
+    int from = 0, to = 0;
+    if (lane < a.pre.S) {
+      from = start_of(a.pre.cu, lane, a.own.S);
+      to = start_of(a.pre.cu, lane + 1, a.own.S);
+      b.first = a.first_tile[1 + lane];
+    }
+    const unsigned long long mine = __ballot(line >= from && line < to);
+    b.there = mine != 0;
+    const int p = b.there ? __builtin_ctzll(mine) : 0;
+    b.first.x = __builtin_amdgcn_readlane(b.first.x, p);
+    b.first.y = __builtin_amdgcn_readlane(b.first.y, p);
+  } else {
+    const int p = last_at_most(a.pre.S, line, [&](int i) { return start_of(a.pre.cu, i, a.own.S); });
+    b.there = line >= start_of(a.pre.cu, p, a.own.S) && line < start_of(a.pre.cu, p + 1, a.own.S);
+    b.first = a.first_tile[1 + p];
+  }
+  return b;
+}
 
-// Joins the tiles that lie in several pieces, and prefixes with sequences.  A wavefront has `heads` rows of
-// a token, as many at a time as 4 outputs a lane allow; rows of many parts take all of it one by one.  What
-// bounds it is a chain of four loads (the token's place, its tiles, their sums, their values), 5 us for single
-// tokens, and the parts of many rows, 67 MB of 2257 tokens 24 us.
+// A row as its lanes have it: token and head, of key head hk and in its group, and its row of a tile in the
+// pieces from own.x on, own.y of them.
+struct RowOf {
+  bool real;
+  long long t;
+  int h, hk, e, row;
+  int2 own;
+};
+// Joins 64 / quads rows at a time, the lanes of each with four outputs; those of many parts one by one.
 template <typename T, int WAVES>
-__global__ __launch_bounds__(256, 4) void k_join_pages(PagedArgs a, int heads, int chunks) {
+__device__ __forceinline__ void join_rows(const PagedArgs& a, float* weight, float (*sums)[TDQ_MAX_HEAD], const RowOf& x,
+                                          const Before& before, const int2& tiles, int quads) {
+  const int lane = threadIdx.x & 63, c = 4 * (lane & (quads - 1));
+  const long long pre_at = (x.t - before.first.y) * a.group + x.e, of = before.first.x + pre_at / kManyRows;
+  const int pre_row = (int)(pre_at % kManyRows);
+  int2 pre = make_int2(0, 0);
+  if (x.real && before.there && pre_at >= 0 && of < tiles.y && of < a.pre_tiles && pre_row < a.cap)
+    pre = a.tiles[(a.own_tiles + of) * a.Hk + x.hk];
+  const bool wanted = x.real && (x.own.y > 1 || a.pre.S > 0);   // (else its one piece has written the output)
+  if (__ballot(wanted) == 0) return;
+  const long long step = 2ll * a.Hk * a.cap, whole = x.hk * a.Tq * a.group + x.t * a.group + x.e;
+  // (parts of a tile: the first ends behind its piece, the others begin in front of theirs)
+  auto run = [&](const int2& d, int row, long long whole) {
+    const long long at = ((2ll * d.x * a.Hk + 2 * x.hk) + 1) * a.cap + row;
+    return d.y == 1 ? Run{a.whole_ml + 2 * whole, a.whole_o + whole * a.D, 0, 0, 1}
+                    : Run{a.part_ml + 2 * at, a.part_o + at * a.D, step, a.cap, d.y};
+  };
+  const Run p = run(pre, pre_row, whole), y = run(x.own, x.row, a.Tq * a.Hq + whole);
+  T* op = static_cast<T*>(a.O) + x.t * a.o_token + x.h * a.o_head;
+  float* lse = a.lse ? a.lse + x.t * a.Hq + x.h : nullptr;
+  if (__ballot(wanted && p.count + y.count > kFewParts) == 0) {
+    if (wanted && (WAVES == 1 || threadIdx.x < 64)) join_few<T>(p, y, c, a.D, a.scale_log2, op, lse);
+    return;
+  }
+  for (int i = 0; i < 64; i += quads) {
+    if (!__shfl((int)wanted, i, 64)) continue;
+    join_row<T, WAVES>(weight, sums, run_of(p, i), run_of(y, i), a.D, a.scale_log2,
+                       (T*)__shfl((unsigned long long)op, i, 64), (float*)__shfl((unsigned long long)lse, i, 64));
+  }
+}
+__device__ __forceinline__ int quads_of(int D) { return D <= 32 ? 8 : D <= 64 ? 16 : D <= 128 ? 32 : 64; }
+
+// Joins the tiles that lie in several pieces, and prefixes with sequences: calls of few rows, a wavefront or a
+// workgroup a row.  What bounds it is a chain of four loads (the token's place, its tile, the sums, the values),
+// 5 us for single tokens.
+template <typename T, int WAVES>
+__global__ __launch_bounds__(256, 4) void k_join_pages(PagedArgs a, int chunks) {
   __shared__ float weight[4][kMaxParts];
   __shared__ __attribute__((aligned(16))) float sums[WAVES][TDQ_MAX_HEAD];
   const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
   const long long t = id / chunks;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h0 = WAVES > 1 ? (int)(id % chunks) : ((int)(id % chunks) * 4 + wave) * heads, h1 = h0 + heads < a.Hq ? h0 + heads : a.Hq;
-  if (t >= a.Tq || h0 >= a.Hq) return;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = (int)(id % chunks) * (4 / WAVES) + (WAVES > 1 ? 0 : wave);
+  if (t >= a.Tq || h >= a.Hq) return;
   // (all on their way at once; what lies there is looked at if the token is one of a sequence)
   const int begin = start_of(a.own.cu, 0, a.Tq), end = start_of(a.own.cu, a.own.S, a.Tq);
   const int2 tiles = a.first_tile[0];                    // of sequences, of prefixes
   const int4 place = a.place[t];
-  int from = 0, to = 0;                                  // of prefix `lane`: its sequences, its first tile and token
-  int2 first = make_int2(0, 0);
-  const bool few = a.pre.S <= 64;
-  if (lane < a.pre.S && few) {
-    from = start_of(a.pre.cu, lane, a.own.S);
-    to = start_of(a.pre.cu, lane + 1, a.own.S);
-    first = a.first_tile[1 + lane];
-  }
+  Before before = {false, make_int2(0, 0)};
+  if (a.pre.S > 0) before = prefix_of(a, __builtin_amdgcn_readfirstlane(place.z));
   if (t < begin || t >= end || place.y < 0 || place.x < 0) return;
-  bool behind = false;                                   // whether the token's sequence has a prefix
-  if (a.pre.S > 0) {
-    const int line = __builtin_amdgcn_readfirstlane(place.z);
-    int p;
-    if (few) {
-      const unsigned long long mine = __ballot(line >= from && line < to);
-      behind = mine != 0;
-      p = behind ? __builtin_ctzll(mine) : 0;
-      first.x = __builtin_amdgcn_readlane(first.x, p);
-      first.y = __builtin_amdgcn_readlane(first.y, p);
-    } else {
-      p = last_at_most(a.pre.S, line, [&](int i) { return start_of(a.pre.cu, i, a.own.S); });
-      behind = line >= start_of(a.pre.cu, p, a.own.S) && line < start_of(a.pre.cu, p + 1, a.own.S);
-      first = a.first_tile[1 + p];
-    }
-  }
-  const float per_group = (float)a.per_group;
-  const int quads = a.D <= 32 ? 8 : a.D <= 64 ? 16 : a.D <= 128 ? 32 : 64, c = 4 * (lane & (quads - 1));
-  for (int hb = h0; hb < h1; hb += 64 / quads) {
-    const int h = hb + lane / quads, hk = quotient(h < h1 ? h : h1 - 1, per_group), e = h - hk * a.group;
-    const long long own_row = (long long)place.y + e, tile = place.x + own_row / kManyRows;
-    const int row = (int)(own_row % kManyRows);
-    const bool real = h < h1 && tile < tiles.x && tile < a.own_tiles && row < a.cap;
-    const long long pre_at = (t - first.y) * a.group + e, of = first.x + pre_at / kManyRows;
-    const int pre_row = (int)(pre_at % kManyRows);
-    int2 own = make_int2(0, 1), pre = make_int2(0, 0);   // first piece, how many
-    if (real) own = a.tiles[tile * a.Hk + hk];
-    if (real && behind && pre_at >= 0 && of < tiles.y && of < a.pre_tiles && pre_row < a.cap) pre = a.tiles[(a.own_tiles + of) * a.Hk + hk];
-    const bool wanted = real && (own.y > 1 || a.pre.S > 0);   // (else its one piece has written the output)
-    if (__ballot(wanted) == 0) continue;
-    const long long step = 2ll * a.Hk * a.cap, whole = hk * a.Tq * a.group + t * a.group + e;
-    // (parts of a tile: the first ends behind its piece, the others begin in front of theirs)
-    auto run = [&](const int2& d, int row, long long whole) {
-      const long long at = ((2ll * d.x * a.Hk + 2 * hk) + 1) * a.cap + row;
-      return d.y == 1 ? Run{a.whole_ml + 2 * whole, a.whole_o + whole * a.D, 0, 0, 1}
-                      : Run{a.part_ml + 2 * at, a.part_o + at * a.D, step, a.cap, d.y};
-    };
-    const Run x = run(pre, pre_row, whole), y = run(own, row, a.Tq * a.Hq + whole);
-    T* op = static_cast<T*>(a.O) + t * a.o_token;
-    float* lse = a.lse ? a.lse + t * a.Hq : nullptr;
-    if (__ballot(wanted && x.count + y.count > kFewParts) == 0) {
-      if (wanted && (WAVES == 1 || wave == 0)) join_few<T>(x, y, c, a.D, a.scale_log2, op + h * a.o_head, lse ? lse + h : nullptr);
-      continue;
-    }
-    for (int i = 0; i < 64; i += quads) {
-      if (!__shfl((int)wanted, i, 64)) continue;
-      const int g = hb + i / quads;
-      join_row<T, WAVES>(weight[wave], sums, run_of(x, i), run_of(y, i), a.D, a.scale_log2, op + g * a.o_head,
-                         lse ? lse + g : nullptr);
-    }
+  const int quads = quads_of(a.D);
+  RowOf x;
+  x.t = t;
+  x.h = h;
+  x.hk = quotient(h, (float)a.per_group);
+  x.e = h - x.hk * a.group;
+  const long long own_row = (long long)place.y + x.e, tile = place.x + own_row / kManyRows;
+  x.row = (int)(own_row % kManyRows);
+  x.real = lane < quads && tile < tiles.x && tile < a.own_tiles && x.row < a.cap;
+  x.own = make_int2(0, 1);
+  if (x.real) x.own = a.tiles[tile * a.Hk + x.hk];
+  join_rows<T, WAVES>(a, weight[wave], sums, x, before, tiles, quads);
+}
+
+// The same for calls of many rows: a quarter of a tile a workgroup, which ends at once where the tile lies in
+// one piece.  Bound by the parts, 67 MB of 2257 tokens.
+constexpr int kQuarters = 4;
+template <typename T>
+__global__ __launch_bounds__(256, 4) void k_join_tiles(PagedArgs a) {
+  __shared__ float weight[4][kMaxParts];
+  const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
+  const int hk = (int)(id % a.Hk), quarter = (int)(id / a.Hk % kQuarters);
+  const long long tile = id / a.Hk / kQuarters;
+  if (tile >= a.own_tiles) return;
+  const int2 tiles = a.first_tile[0];
+  const int2 own = a.tiles[tile * a.Hk + hk];
+  if (tile >= tiles.x || (own.y <= 1 && a.pre.S == 0)) return;
+  const int4 span = a.place[tile];                       // first token, its row in front, rows, sequence
+  Before before = {false, make_int2(0, 0)};
+  if (a.pre.S > 0) before = prefix_of(a, __builtin_amdgcn_readfirstlane(span.w));
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int quads = quads_of(a.D), share = kManyRows / kQuarters / 4, r0 = (quarter * 4 + wave) * share;
+  for (int i = 0; i < share && r0 + i < span.z; i += 64 / quads) {
+    const int row = r0 + i + lane / quads;
+    RowOf x;
+    x.real = i + lane / quads < share && row < span.z;
+    const int at = span.y + (x.real ? row : 0), token = quotient(at, (float)a.per_group);
+    x.t = span.x + token;
+    x.hk = hk;
+    x.e = at - token * a.group;
+    x.h = hk * a.group + x.e;
+    x.row = row;
+    x.own = own;
+    join_rows<T, 1>(a, weight[wave], nullptr, x, before, tiles, quads);
   }
 }
 
@@ -1210,6 +1264,16 @@ static int paged_pieces(int Hk, int D) {
   const int at_a_time = D <= 128 ? 512 : 256;
   return at_a_time / Hk > 0 ? at_a_time / Hk : 1;
 }
+
+// Rows of a call that four wavefronts each join: few rows have parts of up to 512 pieces, and wait for them.  us
+// by one and by four: 8 rows over 100000 keys 88 and 43, of a prefix of 21354 35 and 25, 64 rows over 10947 26 and
+// 21, 512 over 4000 to 32000 196 both; 1824 rows behind 11399 31 and 35, 2048 over 100 to 1000 38 and 41.
+constexpr int kWholeRows = 512;
+
+// More rows than this are joined by tiles, others one by one.  us by rows and by tiles: 8 x 2048 tokens of 32 heads
+// 499 and 366, 4 x 1024 620 and 587, four prompts' parts of 355 to 1024 301 and 289; 512 tokens of 301 keys 131
+// and 135, 64 times 5 244 and 249, one prompt of 256 23.2 and 24.5.
+static bool by_tile(long long Tq, int Hq) { return Tq * Hq > 16384; }
 
 struct PagedLayout {
   size_t tiles, place, ml, o, whole_ml, whole_o, total;  // (the first tiles at 0)
@@ -1227,7 +1291,7 @@ static PagedLayout paged_layout(long long Tq, int S, int prefixes, int Hq, int H
   l.tiles = up((size_t)(prefixes + 1) * sizeof(int2));
   l.pre_tiles = prefixes > 0 ? rows / kManyRows + prefixes : 0;
   l.place = l.tiles + up((size_t)(l.own_tiles + l.pre_tiles) * Hk * sizeof(int2));
-  l.ml = l.place + up((size_t)Tq * sizeof(int4));
+  l.ml = l.place + up((size_t)(by_tile(Tq, Hq) ? l.own_tiles : Tq) * sizeof(int4));
   l.o = l.ml + up(parts * 2 * sizeof(float));
   l.whole_ml = l.o + up(parts * D * sizeof(float));
   l.whole_o = l.whole_ml + up(whole * 2 * sizeof(float));
@@ -1293,6 +1357,7 @@ hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages*
   a.first_tile = reinterpret_cast<int2*>(w);
   a.tiles = reinterpret_cast<int2*>(w + l.tiles);
   a.place = reinterpret_cast<int4*>(w + l.place);
+  a.by_tile = by_tile(Tq, Hq);
   a.own_tiles = l.own_tiles;
   a.pre_tiles = l.pre_tiles;
   a.part_ml = reinterpret_cast<float*>(w + l.ml);
@@ -1304,16 +1369,14 @@ hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages*
   if (dt == TDQ_F16) TDQ_BY_HEAD(TDQ_PAGED, _Float16);
   else TDQ_BY_HEAD(TDQ_PAGED, __bf16);
 #undef TDQ_PAGED
-  // Few tokens: many parts a row, a wavefront each, or four.  us with 1 and 8 rows a wavefront: 64 tokens behind a
-  // prefix 87 and 120; 4 prompts' parts of 300 to 1024 tokens 318 and 297; 8 x 2048 tokens 546 and 393.
-  const int heads = Tq * Hq > 16384 ? 8 : 1;
-  const bool whole = Tq * Hq <= kWholeRows;
-  const int chunks = whole ? Hq : (Hq + 4 * heads - 1) / (4 * heads);
-  const dim3 join = two_axes(Tq * chunks);
 #define TDQ_JOIN(T)                                                                                                 \
   do {                                                                                                              \
-    if (whole) hipLaunchKernelGGL((k_join_pages<T, 4>), join, dim3(256), 0, st, a, 1, chunks);                      \
-    else hipLaunchKernelGGL((k_join_pages<T, 1>), join, dim3(256), 0, st, a, heads, chunks);                        \
+    if (a.by_tile)                                                                                                  \
+      hipLaunchKernelGGL((k_join_tiles<T>), two_axes(l.own_tiles * Hk * kQuarters), dim3(256), 0, st, a);           \
+    else if (Tq * Hq <= kWholeRows)                                                                                 \
+      hipLaunchKernelGGL((k_join_pages<T, 4>), two_axes(Tq * Hq), dim3(256), 0, st, a, Hq);                         \
+    else                                                                                                            \
+      hipLaunchKernelGGL((k_join_pages<T, 1>), two_axes(Tq * ((Hq + 3) / 4)), dim3(256), 0, st, a, (Hq + 3) / 4);   \
   } while (0)
   if (dt == TDQ_F16) TDQ_JOIN(_Float16);
   else TDQ_JOIN(__bf16);

@@ -317,4 +317,6 @@ def test_many_items_and_prefixes():
     groups = 100
     first = [3 * i for i in range(groups + 1)]
     _check(ql, lens, 16, 4, 2, 32, torch.bfloat16, pre=[(17 * i) % 60 for i in range(groups)], first=first)
-    _check([2] * 150, [3] * 150, 16, 2, 1, 64, pre=[20 + i for i in range(70)], first=[2 * i for i in range(71)])
+    for Hq, Hk, D in ((2, 1, 64), (128, 32, 32)):
+        _check([2] * 150, [3] * 150, 16, Hq, Hk, D, pre=[20 + i for i in range(70)], first=[2 * i for i in range(71)])
+    _check([70, 1, 300, 2], [70, 90, 350, 1], 32, 64, 16, 40, pre=[200, 77], first=[0, 1, 3])
