@@ -1224,15 +1224,14 @@ __global__ __launch_bounds__(256, 4) void k_join_pages(PagedArgs a, int chunks) 
   join_rows<T, WAVES>(a, weight[wave], sums, x, before, tiles, quads);
 }
 
-// The same for calls of many rows: a quarter of a tile a workgroup, which ends at once where the tile lies in
-// one piece.  Bound by the parts, 67 MB of 2257 tokens.
-constexpr int kQuarters = 4;
+// The same for calls of many rows: a workgroup one of the shares of a tile, which ends at once where the tile
+// lies in one piece.  Bound by the parts, 67 MB of 2257 tokens.
 template <typename T>
-__global__ __launch_bounds__(256, 4) void k_join_tiles(PagedArgs a) {
+__global__ __launch_bounds__(256, 4) void k_join_tiles(PagedArgs a, int shares) {
   __shared__ float weight[4][kMaxParts];
   const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
-  const int hk = (int)(id % a.Hk), quarter = (int)(id / a.Hk % kQuarters);
-  const long long tile = id / a.Hk / kQuarters;
+  const int hk = (int)(id % a.Hk), part = (int)(id / a.Hk % shares);
+  const long long tile = id / a.Hk / shares;
   if (tile >= a.own_tiles) return;
   const int2 tiles = a.first_tile[0];
   const int2 own = a.tiles[tile * a.Hk + hk];
@@ -1241,7 +1240,7 @@ __global__ __launch_bounds__(256, 4) void k_join_tiles(PagedArgs a) {
   Before before = {false, make_int2(0, 0)};
   if (a.pre.S > 0) before = prefix_of(a, __builtin_amdgcn_readfirstlane(span.w));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int quads = quads_of(a.D), share = kManyRows / kQuarters / 4, r0 = (quarter * 4 + wave) * share;
+  const int quads = quads_of(a.D), share = kManyRows / 4 / shares, r0 = (part * 4 + wave) * share;
   for (int i = 0; i < share && r0 + i < span.z; i += 64 / quads) {
     const int row = r0 + i + lane / quads;
     RowOf x;
@@ -1369,10 +1368,13 @@ hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages*
   if (dt == TDQ_F16) TDQ_BY_HEAD(TDQ_PAGED, _Float16);
   else TDQ_BY_HEAD(TDQ_PAGED, __bf16);
 #undef TDQ_PAGED
+  // (of tiles with few rows one.  us with one and four: 4096 tokens over 301 keys 1010 and 1067, 600 times 4
+  // behind a prefix 315 and 384; 16 times 100 to 600 tokens 489 and 470)
+  const int shares = Tq * a.group >= 64ll * seq->S ? 4 : 1;
 #define TDQ_JOIN(T)                                                                                                 \
   do {                                                                                                              \
     if (a.by_tile)                                                                                                  \
-      hipLaunchKernelGGL((k_join_tiles<T>), two_axes(l.own_tiles * Hk * kQuarters), dim3(256), 0, st, a);           \
+      hipLaunchKernelGGL((k_join_tiles<T>), two_axes(l.own_tiles * Hk * shares), dim3(256), 0, st, a, shares);      \
     else if (Tq * Hq <= kWholeRows)                                                                                 \
       hipLaunchKernelGGL((k_join_pages<T, 4>), two_axes(Tq * Hq), dim3(256), 0, st, a, Hq);                         \
     else                                                                                                            \

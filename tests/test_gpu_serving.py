@@ -319,4 +319,5 @@ def test_many_items_and_prefixes():
     _check(ql, lens, 16, 4, 2, 32, torch.bfloat16, pre=[(17 * i) % 60 for i in range(groups)], first=first)
     for Hq, Hk, D in ((2, 1, 64), (128, 32, 32)):
         _check([2] * 150, [3] * 150, 16, Hq, Hk, D, pre=[20 + i for i in range(70)], first=[2 * i for i in range(71)])
+    _check([1, 2, 0, 1] * 130, [40, 2, 7, 90] * 130, 16, 64, 16, 16, pre=[50], first=[3, 515])
     _check([70, 1, 300, 2], [70, 90, 350, 1], 32, 64, 16, 40, pre=[200, 77], first=[0, 1, 3])
