@@ -87,12 +87,21 @@ struct Rows {
   f32x16 o[DC / 32];
   float m, l;                          // reference of the exponents (of the row), sum (of this lane's keys)
 
+  // TOGETHER: all on their way at once, from where there are zeros past D; else each under a condition.  us so
+  // and so: 4 prompts' parts in pages 282 and 319 (registers), windows 25.9 and 26.6; packed single tokens,
+  // whose first keys are on their way by then, 232 and 229.
+  template <bool TOGETHER = true>
   __device__ __forceinline__ void start(const T* qp, int D, u32 flip) {
     const int half = (threadIdx.x >> 5) & 1;
 #pragma unroll
     for (int i = 0; i < DC / 16; ++i) {
       const int c = 16 * i + 8 * half;
-      q[i] = *(c < D ? reinterpret_cast<const u32x4*>(qp + c) : reinterpret_cast<const u32x4*>(kZeros)) ^ flip;
+      if (TOGETHER) {
+        q[i] = *(c < D ? reinterpret_cast<const u32x4*>(qp + c) : reinterpret_cast<const u32x4*>(kZeros)) ^ flip;
+      } else {
+        q[i] = u32x4{0, 0, 0, 0};
+        if (c < D) q[i] = *reinterpret_cast<const u32x4*>(qp + c) ^ flip;
+      }
     }
 #pragma unroll
     for (int i = 0; i < DC / 32; ++i)

@@ -431,7 +431,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   const int stop = (split + 1) * share < tiles ? (split + 1) * share : tiles;
 
   Rows<T, DP> w;
-  w.start(static_cast<const T*>(a.Q) + (t.q0 + token) * a.q_token + head * a.q_head, D, a.flip);
+  w.template start<false>(static_cast<const T*>(a.Q) + (t.q0 + token) * a.q_token + head * a.q_head, D, a.flip);
   const T* kp = static_cast<const T*>(a.K) + t.k0 * a.k_token + hk * a.k_head;
   const T* vp = static_cast<const T*>(a.V) + t.k0 * a.v_token + hk * a.v_head;
   const u32 lk = lds_address(sh.kv[wave][0]), lv = lds_address(sh.kv[wave][1]);
