@@ -25,11 +25,6 @@ inline Sequences sequences_of(const tdq_sequences* q) {
   return s;
 }
 
-// A value that no kernel of this call writes, from an address that is the same in every lane.
-__device__ __forceinline__ int load_scalar(const int* p) {
-  return *(const __attribute__((address_space(4))) int*)(uintptr_t)p;
-}
-
 // cu[i] within 0 .. total.
 __device__ __forceinline__ int start_of(const int* cu, long long i, long long total) {
   const int c = cu[i];
