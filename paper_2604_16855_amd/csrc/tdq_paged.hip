@@ -210,7 +210,7 @@ struct Shared {
   float ml[4][kFewRows][2];
   Place place[4][64];                                  // [wavefront][tile] (many)
 };
-// The same for few rows and one wavefront or four.
+// The same for few rows and one, two or four wavefronts.
 template <int DP, int WAVES>
 struct SharedFew {
   static constexpr int kWaves = WAVES;
@@ -1390,7 +1390,7 @@ hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages*
 // chosen pages
 // ---------------------------------------------------------------------------
 // Every token and key head has a list of pages of its own, so a tile has the group's rows and no more;
-// its pages are shared out to `splits` workgroups, and in each to four wavefronts, or, of many lists, one.  Pages of single tokens are
+// its pages are shared out to `splits` workgroups, and in each to four wavefronts, or, of many lists, two or one.  Pages of single tokens are
 // read once, at 6.2 TB/s (32 tokens, 64 pages of 64 keys, 8 heads of 128: 87 us); those of a prompt's tokens
 // come from the caches, at 14 TB/s (401 tokens, 16 pages, 4 heads of 64: 29 us).
 struct ChosenArgs {
@@ -1488,14 +1488,17 @@ static int chosen_splits(long long Tq, int Hq, int Hk, int page_size, int count)
   if (n > 64) n = 64;
   return n > 1 ? (int)n : 1;
 }
-// Lists by a wavefront each, if there are three times as many as four wavefronts each have room for at a time
-// (LDS: 256 CUs, 256 / D workgroups on each): no keys too few for four, no parts to join, no waiting for the
-// slowest.  us by four and by one: 3200 tokens of 4 heads of 64, lists of 96 keys 64 and 29, of 1024 165 and 138,
-// 800 tokens of those 21 and 11, 48 and 45, 401 of 1024 keys 29 and 36; 800 tokens of 8 heads of 128 69 and 30,
-// 180 and 136, 128 tokens 15 and 11, 33 and 41; 128 tokens of 8 heads of 256 32 and 15, 85 and 68.
-static bool chosen_by_one(long long lists, int D) {
+// Wavefronts of a list: four, as long as there is room for all lists at a time (LDS: 256 CUs, 256 / D workgroups on
+// each); up to three times as many two; of more one: no keys too few for four, no parts to join, no waiting for
+// the slowest.  us by four / two / one wavefronts, lists of 96 and of 1024 keys:
+//   heads of 64   512 lists  11 /  - / 10 and  14 / 21 / 31   1604 lists 12 / 11 /  - and 28 / 27 / 36
+//                3200 lists  21 /  - / 11 and  48 /  - / 45  12800 lists 64 /  - / 29 and 165 / - / 138
+//   heads of 128  512 lists  11 / 11 /  - and  19 / 25 /  -   1024 lists 15 / 11 / 11 and 33 / 27 / 41
+//                1440 lists  20 / 16 /  - and  46 / 47 /  -   6400 lists 69 /  - / 30 and 180 / - / 136
+//   heads of 256  256 lists  11 / 11 /  - and  34 / 28 /  -   1024 lists 32 /  - / 15 and 85 / -  / 68
+static int chosen_waves(long long lists, int D) {
   const int row = D <= 32 ? 32 : D <= 64 ? 64 : D <= 128 ? 128 : 256;
-  return lists * row >= 3ll * 256 * 256;
+  return lists * row <= 256 * 256 ? 4 : lists * row < 3 * 256 * 256 ? 2 : 1;
 }
 static size_t chosen_ml_bytes(long long Tq, int Hq, int splits) {
   return ((size_t)Tq * Hq * splits * 2 * sizeof(float) + 255) & ~(size_t)255;
@@ -1535,11 +1538,12 @@ hipError_t launch_chosen(const tdq_heads* Q, const tdq_pages* K, const tdq_pages
                  ? reinterpret_cast<float*>(static_cast<char*>(workspace) + chosen_ml_bytes(Tq, Hq, a.splits))
                  : nullptr;
   const dim3 grid = two_axes(Tq * a.tiles * a.splits * Hk);
-  const bool one = chosen_by_one(Tq * a.tiles * a.splits * Hk, D);
-#define TDQ_CHOSEN(T, DP, DC)                                                                           \
-  do {                                                                                                  \
-    if (one) hipLaunchKernelGGL((k_attend_chosen<T, DP, DC, 1>), grid, dim3(64), 0, st, a);             \
-    else hipLaunchKernelGGL((k_attend_chosen<T, DP, DC, 4>), grid, dim3(256), 0, st, a);                \
+  const int waves = chosen_waves(Tq * a.tiles * a.splits * Hk, D);
+#define TDQ_CHOSEN(T, DP, DC)                                                                             \
+  do {                                                                                                    \
+    if (waves == 1) hipLaunchKernelGGL((k_attend_chosen<T, DP, DC, 1>), grid, dim3(64), 0, st, a);        \
+    else if (waves == 2) hipLaunchKernelGGL((k_attend_chosen<T, DP, DC, 2>), grid, dim3(128), 0, st, a);  \
+    else hipLaunchKernelGGL((k_attend_chosen<T, DP, DC, 4>), grid, dim3(256), 0, st, a);                  \
   } while (0)
   if (dt == TDQ_F16) TDQ_BY_HEAD(TDQ_CHOSEN, _Float16);
   else TDQ_BY_HEAD(TDQ_CHOSEN, __bf16);

@@ -231,7 +231,8 @@ def test_chosen(Hq, Hk, D, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("Hq,Hk,D,T", [(32, 8, 128, 200), (16, 8, 64, 400), (12, 12, 32, 530), (16, 16, 8, 400), (8, 8, 256, 110),
-                                       (20, 10, 96, 160), (18, 1, 184, 400), (6, 6, 200, 140)])
+                                       (20, 10, 96, 160), (18, 1, 184, 400), (6, 6, 200, 140), (16, 4, 64, 400), (32, 8, 128, 100),
+                                       (8, 8, 256, 45), (8, 4, 32, 600), (16, 8, 72, 90)])
 def test_lists_of_many_tokens(Hq, Hk, D, T, dtype):
     for ql, lens, P, count in (([T], [T + 50], 16, 5), ([T - 40, 1, 39], [T - 40, 700, 0], 32, 9), ([T // 2, T - T // 2], [4, 1300], 64, 3)):
         print(f"[chosen] {ql} {lens} P={P} count={count} {Hq}/{Hk} D={D} {dtype}", flush=True)
