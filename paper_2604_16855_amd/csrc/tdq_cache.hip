@@ -551,6 +551,7 @@ __device__ __forceinline__ void choose(const ChoiceArgs& a, ChoiceRoom<HELD>& ro
       want -= found[1];
       limit = prefix;
       if (found[2] == want && shift > 0) {               // every key of the bin: nothing to tell apart
+        all = prefix == 0;                               // (the lowest bin: every page that is there)
         limit = prefix - 1;
         want = 0;
         done = true;
