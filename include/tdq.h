@@ -525,8 +525,9 @@ typedef struct tdq_pages {
 /* S sequences whose keys lie in the pages of a cache (all arrays on the device):
  *   cu_q  [S + 1]  the queries (new tokens) of sequence s are cu_q[s] .. cu_q[s + 1] - 1: ascending, what
  *                  lies outside 0 .. Tq is cut off; queries of no sequence are left alone everywhere
- *   len_k [S]      its keys, those of its queries with them (the last ones); no more are used than its
- *                  line of the table has room for, columns * page_size
+ *   len_k [S]      its keys, those of its queries with them: query i of n is its key len_k - n + i.  Keys that
+ *                  its line of the table has no room for, from columns * page_size on, are not written and
+ *                  nobody sees them; a query among them sees, if causal, all that have room
  *   table [S, ld_table]  key j of sequence s is row j % page_size of page table[s][j / page_size].  A page
  *                  outside 0 .. n_pages - 1 is not there: nobody sees its keys, nothing is written to it.
  * page_size a power of two from 16 to 1024, columns >= 1, columns * page_size <= 2^30, n_pages >= 1,
@@ -561,8 +562,7 @@ int tdq_cache_append(const tdq_heads* Q, const tdq_heads* K, const tdq_heads* V,
 /*
  * Bounds of pages, for tdq_select_pages: lo[p, h, d] and hi[p, h, d] the smallest and largest value of
  * channel d over the keys in use (j < len) of page p, NaN where one of them is.  seq->cu_q NULL: all pages
- * of all sequences; else the pages that hold a sequence's last n keys, n its queries (T: all of them, an
- * upper bound).  Other pages' bounds are left alone.  A page that two sequences share has to hold the same
+ * of all sequences; else the pages that hold the keys of a sequence's queries (T: all of them, an upper bound).  Other pages' bounds are left alone.  A page that two sequences share has to hold the same
  * number of keys for both.
  *
  * Kc as in tdq_cache_append, data and strides aligned to 2 bytes; lo, hi: tdq_heads with a page for a token,
@@ -573,7 +573,7 @@ int tdq_page_bounds(const tdq_pages* Kc, tdq_dtype dt, int64_t T, const tdq_sequ
 
 /*
  * The pages that a token attends to, for each of its key heads: of the pages b that hold a key it sees
- * (causal: the last query of a sequence sees all keys, the one before it all but the last, and so on),
+ * (causal: up to its own, the last query of a sequence all of them, the one before it all but the last, and so on),
  * the first `first`, the last `last`, and the best of the others up to `count` in all, by
  *   score[t, h, b] = max over the query heads e of h of sum_d max(Q[t, e, d], 0) hi[p, h, d] + min(Q[t, e, d], 0) lo[p, h, d]
  * with p = table[s][b]: no key of the page has a larger product with one of the queries (for a positive

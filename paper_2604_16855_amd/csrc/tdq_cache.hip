@@ -276,7 +276,7 @@ __global__ __launch_bounds__(256) void k_bounds(BoundsArgs a) {
     // n new tokens lie in no more than n / P + 2 pages: sequence s has the slots from
     // floor(first token / P) + 2 s on
     s = last_at_most(q.S, slot, [&](int i) { return (long long)(start_of(q.cu, i, a.T) >> q.shift) + 2ll * i; });
-    const int from = start_of(q.cu, s, a.T), n = start_of(q.cu, s + 1, a.T) - from, len = keys_of(q, s);
+    const int from = start_of(q.cu, s, a.T), n = start_of(q.cu, s + 1, a.T) - from, len = q.len[s];
     if (n <= 0) return;
     const long long i = slot - ((from >> q.shift) + 2ll * s);
     if (i < 0 || i >= q.columns) return;
@@ -400,10 +400,8 @@ struct Seen {
 };
 __device__ __forceinline__ Seen seen_by(const Sequences& q, long long t, long long T, int causal) {
   const Owner o = owner_of(q, t, T);
-  const int n = keys_in(q, o.len);
   if (t < o.from || t >= o.to) return {o.seq, -1};
-  const long long e = causal ? n - o.to + t + 1 : n;
-  return {o.seq, e < 0 ? 0 : (int)e};
+  return {o.seq, keys_seen(q, o.len, o.to, t, causal)};
 }
 
 // The value of lane ^ 1 or lane ^ 2.
@@ -806,10 +804,9 @@ __global__ __launch_bounds__(256, 2) void k_select_runs(ChoiceArgs a) {
     n = 1;
     if (t0 + first < o.from || t0 + first >= o.to) continue;
     n = o.to - t0 < TOKENS ? (int)(o.to - t0) - first : TOKENS - first;
-    const int have = keys_in(q, o.len);
     auto pages_of = [&](int i) {                         // that token first + i sees
-      const long long e = a.causal ? have - o.to + t0 + first + i + 1 : have;
-      return e <= 0 ? 0 : (int)((e - 1) >> q.shift) + 1;
+      const int keys = keys_seen(q, o.len, o.to, t0 + first + i, a.causal);
+      return keys == 0 ? 0 : ((keys - 1) >> q.shift) + 1;
     };
     const int pages = pages_of(n - 1);
     const int* line = q.table + o.seq * q.ld;

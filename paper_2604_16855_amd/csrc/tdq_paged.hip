@@ -679,7 +679,8 @@ constexpr int kTileCost = 4, kLeastPiece = 3;
 
 // A prefix or a sequence: its rows, and its keys.
 struct Item {
-  int t0, end, keys;                   // first token and the one behind the last
+  int t0, end;                         // first token and the one behind the last
+  int len, keys;                       // as given, and those that are within the line's room
   int ahead;                           // token i sees the keys up to i + ahead
   unsigned rows;
   int tiles, skip;                     // tiles, and how many of them see no key
@@ -700,17 +701,20 @@ struct Item {
     return e < 0 ? 0 : e < keys ? e : keys;
   }
 };
-__device__ __forceinline__ Item item_from(const PagedArgs& a, bool prefix, int t0, int end, int keys) {
+__device__ __forceinline__ Item item_from(const PagedArgs& a, bool prefix, int t0, int end, int len) {
+  const int room = (prefix ? a.pre.columns : a.own.columns) << a.own.shift, have = len < 0 ? 0 : len;
   Item x;
   x.t0 = t0;
   x.end = end;
-  x.keys = keys;
+  x.len = len;
+  x.keys = have < room ? have : room;
   const int tokens = end > t0 ? end - t0 : 0;
   x.rows = (unsigned)tokens * (unsigned)a.group;
   x.tiles = (int)((x.rows + (unsigned)(kManyRows - 1)) / kManyRows);
-  // (what sees everything: as if all its tokens stood at the end)
+  // (what sees everything: as if all its tokens stood at the end.  Token i is key have - tokens + i, also where
+  // that is past the room; from the room's last key on a token sees all of them)
   x.causal = a.causal && !prefix;
-  x.ahead = x.causal ? keys - tokens : keys;
+  x.ahead = !x.causal ? x.keys : have - tokens < x.keys ? have - tokens : x.keys - 1;
   x.skip = 0;
   if (x.ahead < 0) {
     const long long none = (long long)-x.ahead * a.group / kManyRows;
@@ -726,7 +730,7 @@ __device__ __forceinline__ Item item_of(const PagedArgs& a, int v) {
     next = start_of(a.pre.cu, v + 1, a.own.S);
   }
   return item_from(a, prefix, start_of(a.own.cu, s, a.Tq), start_of(a.own.cu, next, a.Tq),
-                   prefix ? keys_of(a.pre, v) : keys_of(a.own, v - a.pre.S));
+                   prefix ? a.pre.len[v] : a.own.len[v - a.pre.S]);
 }
 
 // The tile of an item, and the place of it on the line.
@@ -768,7 +772,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
   __shared__ __attribute__((aligned(1024))) Shared<DP> sh;
   __shared__ long long wave_sum[4];
   __shared__ int wave_tiles[4];
-  // Of items, if there are no more: first token, end and keys, where on the line, their first tile.
+  // Of items, if there are no more: first token, end and length, where on the line, their first tile.
   __shared__ int3 known[256];
   __shared__ long long known_start[256];
   __shared__ int known_tile[256];
@@ -792,7 +796,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     const Item x = item_of(a, v);
     mine += x.cost(a, x.tiles);
     mine_tiles += x.tiles;
-    if (share == 1) known[v] = make_int3(x.t0, x.end, x.keys);
+    if (share == 1) known[v] = make_int3(x.t0, x.end, x.len);
   }
   long long upto = mine;
   int tiles_upto = mine_tiles;
@@ -1424,8 +1428,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(DP <
   const Owner o = owner_of(q, t, a.Tq);
   const int s = o.seq, from = o.from, to = o.to, keys = __builtin_amdgcn_readfirstlane(keys_in(q, o.len));
   if (t < from || t >= to) return;
-  const long long e = a.causal ? keys - to + t + 1 : keys;
-  const int sees = __builtin_amdgcn_readfirstlane(e < 0 ? 0 : (int)e);
+  const int sees = __builtin_amdgcn_readfirstlane(keys_seen(q, o.len, to, t, a.causal));
   const int left = a.group - tile * kFewRows, rows = left < kFewRows ? left : kFewRows;
   const int lane = threadIdx.x & 63, row = (lane & 15) < rows ? lane & 15 : rows - 1;
   const int h0 = hk * a.group + tile * kFewRows;

@@ -36,6 +36,13 @@ __device__ __forceinline__ int keys_in(const Sequences& q, int len) {
   return len < 0 ? 0 : len < room ? len : room;
 }
 __device__ __forceinline__ int keys_of(const Sequences& q, int s) { return keys_in(q, q.len[s]); }
+// Keys that token t sees of a sequence whose tokens end at `to`: it is key len - (to - t), also where that is
+// past the room, and sees no key behind itself if causal.
+__device__ __forceinline__ int keys_seen(const Sequences& q, int len, int to, long long t, bool causal) {
+  const int n = keys_in(q, len);
+  const long long e = (long long)len - to + t + 1;
+  return !causal || e >= n ? n : e < 0 ? 0 : (int)e;
+}
 
 // The last i < n with first(i) <= at, for an ascending `first` with first(0) <= at: 64 places at a
 // time, a lane each.  Every lane gets the answer.
