@@ -585,7 +585,8 @@ int tdq_page_bounds(const tdq_pages* Kc, tdq_dtype dt, int64_t T, const tdq_sequ
  * Q [Tq, Hq, D] of dt = TDQ_F16 or TDQ_BF16, lo and hi as tdq_page_bounds writes them.  0 <= first, last;
  * max(1, first + last) <= count <= 2^20.  D a multiple of 8 up to TDQ_MAX_HEAD, Hk divides Hq, Hq <= 4096,
  * 1 <= Tq <= 2^30, Tq Hk columns <= 2^56.  workspace: device scratch of
- * tdq_select_pages_workspace_bytes(Tq, Hk, columns), 256-byte aligned.
+ * tdq_select_pages_workspace_bytes(Tq, Hk, columns), 256-byte aligned: room for every score, asked for always
+ * though calls whose lines are short, or whose tokens are many, leave it untouched.
  */
 size_t tdq_select_pages_workspace_bytes(int64_t Tq, int32_t Hk, int32_t columns);
 int tdq_select_pages(const tdq_heads* Q, const tdq_heads* lo, const tdq_heads* hi, tdq_dtype dt, int64_t Tq,
@@ -616,7 +617,8 @@ int tdq_attention_selected(const tdq_heads* Q, const tdq_pages* Kc, const tdq_pa
  * keys of a prefix stand in front of them: prefix->cu_q [prefix->S + 1] counts sequences, prefix g belongs to
  * the sequences cu_q[g] .. cu_q[g + 1] - 1 (of none: no prefix), has prefix->len_k[g] keys in the pages of
  * prefix->table, and every query of its sequences sees all of them, causal or not: only a sequence's own
- * keys are hidden from its earlier queries.  A prefix is read once for all of its sequences.
+ * keys are hidden from its earlier queries.  A prefix is read once for every 128 rows (queries of its sequences
+ * times query heads of a key head), not once for each sequence.
  * n_pages and page_size are the same for both.
  *
  * O, lse, scale, causal, rounding, keys that nobody sees and values that are not finite as in tdq_attention; O

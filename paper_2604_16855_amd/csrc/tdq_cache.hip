@@ -384,6 +384,10 @@ hipError_t launch_bounds(const tdq_pages* K, tdq_dtype dt, long long T, const td
 // bounds: 4 us), and beside the products the conversions of both operands: 32 tokens over 560 pages each, 8
 // heads of 128, 26 us (73 MB).  By products in binary32 with a bound of their error, and in binary64 only
 // where the order stays open, the scores took 21, but the choice 19 instead of 8.
+// Which kernels run, and on how many workgroups, follows the width of the table, as the host does not know the
+// lengths.  us with tables of no more columns than pages, of 1025 and of 8192: 32 tokens over 134 to 1001 pages:
+// 34, 34 and 48; 401 over up to 508: 34, 45 and 213; 2000 over 141: 168, 339 and 1240; 8745 over up to 423: 108, 241
+// and 2088.
 struct ChoiceArgs {
   const void *Q, *lo, *hi;
   long long q_token, q_head, lo_page, lo_head, hi_page, hi_head;

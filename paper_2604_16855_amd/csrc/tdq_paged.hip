@@ -664,11 +664,16 @@ struct PagedArgs {
   int2* first_tile;                    // [prefixes + 1]: tiles of sequences and prefixes; of each those in front, first token
   int2* tiles;                         // [own_tiles + pre_tiles][Hk]: first piece of each, how many; sequences first
   long long own_tiles, pre_tiles;      // (room for so many)
-  int4* place;                         // [Tq]: tile, row of it and sequence of a token's first row; or, of
-  bool by_tile;                        // [own_tiles]: first token, rows of it in front, rows, sequence of a tile
+  int4* place;                         // [Tq]: tile, row of it and sequence of a token's first row; or, if by_tile,
+                                       // [own_tiles]: first token of a tile, rows of it in front, rows, sequence
+  bool by_tile;                        // the second kernel joins by tiles
   float *part_o, *part_ml;             // [pieces Hk][2][cap]: of tiles that begin before a piece, and that end behind it
   float *whole_o, *whole_ml;           // with prefixes: [2][Tq Hq], of tiles of one (prefixes, sequences) in one piece
 };
+
+// With prefixes in the call every row of both kinds of items goes through the workspace in binary32 and is joined by
+// the second kernel, those of sequences without a prefix too: 4 x 1024 tokens over 9024 keys of their own 595 us,
+// with a prefix that belongs to nobody in the call 626, over 1024 of their own behind 8000 shared 642.
 
 // What a tile takes beside its keys (its place, its first keys on their way, its stores), in tiles of 64 keys.
 // us with 2, 4 and 8: 64 tokens behind a prefix 90, 87, 95; 16 questions behind three 32.6, 29.6, 31.5; others
@@ -764,6 +769,8 @@ __device__ __forceinline__ int tile_of_round(int round, int k, int n) { return r
 // Whole tiles are no more than 1 + 1 / kSpare of a workgroup's share of the line.  us with none, 1 / 5, 1 / 3
 // and 1 / 2: 4 x 1024 tokens over 8192 keys 665, 610, 610, 613; 16 times 100 to 600 tokens 512, 481, 549, 549;
 // 40 times 1 to 500 733, 642, 643, 738; three long prompts of more tiles than workgroups 390, 399, 399, 400.
+// Only up to 256 sequences and prefixes, which LDS has room for: 8 x 2048 tokens in a call of 256 sequences 414 us, of
+// 257 436.
 constexpr int kSpare = 5;
 
 template <typename T, int DP, int DC>
@@ -1394,9 +1401,9 @@ hipError_t launch_paged(const tdq_heads* Q, const tdq_pages* K, const tdq_pages*
 // chosen pages
 // ---------------------------------------------------------------------------
 // Every token and key head has a list of pages of its own, so a tile has the group's rows and no more;
-// its pages are shared out to `splits` workgroups, and in each to four wavefronts, or, of many lists, two or one.  Pages of single tokens are
-// read once, at 6.2 TB/s (32 tokens, 64 pages of 64 keys, 8 heads of 128: 87 us); those of a prompt's tokens
-// come from the caches, at 14 TB/s (401 tokens, 16 pages, 4 heads of 64: 29 us).
+// its pages are shared out to `splits` workgroups, and in each to four wavefronts, or, of many lists, two or one.
+// Pages of single tokens are read once, at 6.2 TB/s (32 tokens, 64 pages of 64 keys, 8 heads of 128: 87 us); those
+// of a prompt's tokens come from the caches, at 14 TB/s (401 tokens, 16 pages, 4 heads of 64: 28 us).
 struct ChosenArgs {
   static constexpr bool kReadAgain = false;
   const void* Q;
@@ -1411,7 +1418,7 @@ struct ChosenArgs {
   float scale_log2, lift;
   u32 flip;
   int splits, tiles;                   // tiles of 16 rows of a group
-  float *part_o, *part_ml;             // [Tq Hq][splits]
+  float *part_o, *part_ml;             // [splits][Tq Hq]
 };
 
 template <typename T, int DP, int DC, int WAVES>
